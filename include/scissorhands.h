@@ -359,6 +359,101 @@ long long sh_launch_count(sh_handle h);
  * 128, SH_OPT_DECODE_KERNEL = 1 keeps the CUDA-core kernel).  For reports and profiles. */
 int sh_decode_kernel_choice(sh_handle h);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Query/key preparation and the window cache.
+ *
+ * These calls use no handle: all state is the caller's tensors and every call is a pure function of its arguments
+ * (safe in a CUDA graph; two calls may run at once unless they write the same rows).  They launch on the current
+ * device, which must be the one that holds the tensors.  Strides count elements.  Rows of head_dim elements are
+ * contiguous; every base address and every stride in bytes must be a multiple of 16 (else SH_EINVAL).
+ *
+ * The window cache is the fixed-policy sibling of the budgeted cache: instead of the importance record it keeps the
+ * first `sinks` tokens and the `window` most recent ones.  A token at position p (0-based) sees the positions j <= p
+ * with j < sinks or j > p - window.  The cache has sinks + window slots per (sequence, key head): position j lives in
+ * slot j when j < sinks, else in slot sinks + (j - sinks) % window.  Slots that hold no token are never used,
+ * whatever they contain, and neither are keys and values outside of a query's sight (infinities and NaN included).
+ */
+
+/* [tokens][heads][head_dim] rows: element (t, h, i) is data[t * token_stride + h * head_stride + i]. */
+typedef struct {
+    void *data;
+    long long token_stride, head_stride;
+} sh_rows;
+
+/* K and V slots: element (sequence, head, slot, i) of either is at the sum of index * stride, + i. */
+typedef struct {
+    void *k, *v;
+    long long sequence_stride, head_stride, slot_stride;
+} sh_window_cache;
+
+/* Shape of the attention.  q_heads must be a multiple of kv_heads: query head h reads key head h / (q_heads / kv_heads). */
+typedef struct {
+    int dtype;            /* SH_F32, SH_F16 or SH_BF16: q, k, v, caches and outputs alike */
+    int head_dim;         /* 64 or 128 */
+    int q_heads, kv_heads;
+    int window, sinks;    /* window >= 1, sinks >= 0, together below 2^30 */
+    double scale;         /* of the logits; 0: 1/sqrt(head_dim) */
+} sh_window;
+
+/* Normalisation and rotation of query and key rows:
+ *   y = x * w / sqrt(mean(x^2) + eps)             per row, when a weight is given;
+ *   (a, b) -> (a cos - b sin, a sin + b cos)      for the rot_dim / 2 pairs of the leading rot_dim elements,
+ * with the angle position[axis of the pair] * inv_freq[pair], taken in 64 bits before it is reduced, so that far positions
+ * keep their phase.  Pair i is (i, i + rot_dim/2), or (2i, 2i+1) with adjacent_pairs.  Several axes (time, height, width):
+ * sections[a] pairs belong to axis a, in consecutive blocks, or (spread, three axes) dealt out in turn: pair i turns with
+ * axis i % 3 while i < 3 * sections[i % 3], else with axis 0.  Computed in fp32, rounded once. */
+typedef struct {
+    int dtype, head_dim;  /* as in sh_window */
+    int rot_dim;          /* 0 .. head_dim, a multiple of 16 */
+    int axes;             /* 1 to 3 */
+    int sections[3];      /* sum over the axes: rot_dim / 2 */
+    int spread;           /* 0 or 1 */
+    int adjacent_pairs;   /* 0 or 1 */
+    float eps;            /* >= 0 */
+    const float *inv_freq_dev;                     /* [rot_dim / 2] */
+    const void *q_weight_dev, *k_weight_dev;       /* [head_dim] in dtype, 16-byte aligned; NULL: these rows are not normalised */
+} sh_rope;
+
+/*
+ * Normalise and rotate the query and key rows of `tokens` tokens, in one pass (the rows sh_decode_step, sh_prefill and
+ * the calls below take).  positions_dev: [axes] rows of `tokens` int32, axis_stride apart.  An output may be its own
+ * input (same address and strides) and must not overlap anything else.  k (with k_out) may be NULL: queries only.
+ * Errors: SH_EINVAL, SH_ECUDA.
+ */
+int sh_qk_norm_rope(const sh_rope *rope, int tokens, int q_heads, int k_heads, const sh_rows *q, const sh_rows *k, const int32_t *positions_dev,
+                    long long axis_stride, const sh_rows *q_out, const sh_rows *k_out, void *stream);
+
+/*
+ * Prompt chunks: the tokens starts[i] .. starts[i+1] - 1 of q, k, v continue sequence i, whose cache holds lengths[i]
+ * tokens; each attends over the cache and the chunk.  starts_dev [sequences + 1], lengths_dev [sequences]: int32 on the
+ * device.  cache and lengths_dev may both be NULL: nothing was cached.  A sequence may have no tokens; one with a negative
+ * length is idle and is skipped.  Rows of `out` that belong to no sequence (before starts[0], from starts[sequences] on) are
+ * left as they were.  The cache is only read: sh_window_append stores the chunk afterwards.
+ * starts that decrease or leave 0 .. tokens are clamped, so no access leaves the tensors; outputs are then meaningless.
+ * lengths[i] plus the chunk's tokens must stay below 2^30.  Errors: SH_EINVAL, SH_ECUDA.
+ */
+int sh_window_prefill(const sh_window *w, int tokens, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v,
+                      const int32_t *starts_dev, const int32_t *lengths_dev, const sh_window_cache *cache, const sh_rows *out, void *stream);
+
+/*
+ * Store the chunks' keys and values in the caches (arguments as above, lengths_dev as before the chunk; the caller advances
+ * them): of each sequence the rows that a later token can see.  Slots that get no row are left as they were.
+ */
+int sh_window_append(const sh_window *w, int tokens, int sequences, const sh_rows *k, const sh_rows *v, const int32_t *starts_dev,
+                     const int32_t *lengths_dev, const sh_window_cache *cache, void *stream);
+
+/*
+ * One token per sequence: token i of q, k, v is at position lengths[i] of sequence i; its key and value are stored in the
+ * cache and it attends over what it sees, itself included.  With `rope` (NULL: none; dtype and head_dim as in w) q and k are
+ * first normalised and rotated, by positions_dev as in sh_qk_norm_rope, or by lengths where that is NULL (one axis); the
+ * rotated key is what the cache gets.  lengths_dev: tokens before the step (the caller advances them), below 2^30; negative: an
+ * idle slot of the batch, for which nothing is read or written.
+ * Errors: SH_EINVAL, SH_ECUDA.
+ */
+int sh_window_decode(const sh_window *w, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *lengths_dev,
+                     const sh_window_cache *cache, const sh_rope *rope, const int32_t *positions_dev, long long axis_stride,
+                     const sh_rows *out, void *stream);
+
 /* Text for a status code; never NULL. */
 const char *sh_strerror(int status);
 

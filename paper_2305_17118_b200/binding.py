@@ -33,7 +33,28 @@ EXPORTS = ["sh_create", "sh_destroy", "sh_workspace_bytes", "sh_bind", "sh_set_o
            "sh_sequence_state",
            "sh_compress", "sh_compress_static", "sh_scores", "sh_select", "sh_state", "sh_export_unit",
            "sh_restore", "sh_launch_count", "sh_decode_kernel_choice", "sh_import_compressed", "sh_prefill_bulk",
-           "sh_prefill_bulk_scratch_bytes", "sh_strerror", "sh_last_cuda_error"]
+           "sh_prefill_bulk_scratch_bytes", "sh_strerror", "sh_last_cuda_error",
+           "sh_qk_norm_rope", "sh_window_prefill", "sh_window_append", "sh_window_decode"]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_longlong), ("head_stride", C.c_longlong)]
+
+
+class _WindowCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("sequence_stride", C.c_longlong), ("head_stride", C.c_longlong),
+                ("slot_stride", C.c_longlong)]
+
+
+class _Window(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("head_dim", C.c_int), ("q_heads", C.c_int), ("kv_heads", C.c_int), ("window", C.c_int),
+                ("sinks", C.c_int), ("scale", C.c_double)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("head_dim", C.c_int), ("rot_dim", C.c_int), ("axes", C.c_int), ("sections", C.c_int * 3),
+                ("spread", C.c_int), ("adjacent_pairs", C.c_int), ("eps", C.c_float), ("inv_freq_dev", C.c_void_p),
+                ("q_weight_dev", C.c_void_p), ("k_weight_dev", C.c_void_p)]
 
 
 def _load() -> C.CDLL:
@@ -84,6 +105,11 @@ def declare(lib: C.CDLL) -> C.CDLL:
     lib.sh_strerror.restype = C.c_char_p
     lib.sh_last_cuda_error.argtypes = [vp]
     lib.sh_last_cuda_error.restype = C.c_char_p
+    rows, cache, window, rope = C.POINTER(_Rows), C.POINTER(_WindowCache), C.POINTER(_Window), C.POINTER(_Rope)
+    lib.sh_qk_norm_rope.argtypes = [rope, C.c_int, C.c_int, C.c_int, rows, rows, vp, C.c_longlong, rows, rows, vp]
+    lib.sh_window_prefill.argtypes = [window, C.c_int, C.c_int, rows, rows, rows, vp, vp, cache, rows, vp]
+    lib.sh_window_append.argtypes = [window, C.c_int, C.c_int, rows, rows, vp, vp, cache, vp]
+    lib.sh_window_decode.argtypes = [window, C.c_int, rows, rows, rows, vp, cache, rope, vp, C.c_longlong, rows, vp]
     return lib
 
 
@@ -365,3 +391,270 @@ def select(counters: torch.Tensor, r: int, m: int, stream=None) -> torch.Tensor:
     if rc:
         raise ShError(rc)
     return out
+
+
+# -- query/key preparation and the window cache (no handle: tensors in, tensors out) ---------------------------------
+_CODE_OF = {torch.float32: SH_F32, torch.float16: SH_F16, torch.bfloat16: SH_BF16}
+
+
+def _fail(what: str, need: str, t) -> None:
+    got = f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}" if isinstance(t, torch.Tensor) else repr(t)
+    raise ValueError(f"{what}: need {need}, got {got}")
+
+
+def _check_rows(t, what: str, like: Optional[torch.Tensor] = None, shape=None) -> None:
+    """``t`` holds rows [tokens, heads, head_dim] of a supported type, on the device and of the type of ``like``."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in _CODE_OF and t.shape[2] in (64, 128)
+            and (t.stride(2) == 1 or t.numel() == 0)):
+        _fail(what, "a CUDA tensor [tokens, heads, 64 or 128] of f32, f16 or bf16 with contiguous rows", t)
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        _fail(what, f"{like.dtype} on {like.device}", t)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        _fail(what, f"shape {tuple(shape)}", t)
+
+
+def _check_ints(t, what: str, shape, device) -> None:
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype == torch.int32 and tuple(t.shape) == tuple(shape)
+            and (t.numel() <= 1 or t.stride(-1) == 1)):
+        _fail(what, f"an int32 tensor {tuple(shape)} on {device}, contiguous along its last dimension", t)
+
+
+def _rows(t: torch.Tensor) -> _Rows:
+    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _check_status(rc: int, what: str) -> None:
+    if rc:
+        raise ShError(rc, f"{what}: strides and addresses must be multiples of 16 bytes, outputs must not overlap themselves, "
+                          f"and sizes must lie in the ranges the header states" if rc == SH_EINVAL else what)
+
+
+class Rope:
+    """Norm and rotation of query and key rows (``sh_rope``): what a model keeps for ``qk_norm_rope`` and ``window_decode``.
+
+    ``inv_freq``: fp32 CUDA tensor of rot_dim / 2 frequencies (rot_dim a multiple of 16, at most head_dim; empty: no rotation).
+    ``q_weight`` / ``k_weight``: [head_dim] in the rows' type, or None (those rows are not normalised).
+    ``sections``: pairs per position axis, one to three of them (default: one axis); ``spread``: the pairs of three axes are
+    dealt out in turn instead of in blocks.  ``adjacent``: pairs (2i, 2i+1) instead of (i, i + rot_dim/2)."""
+
+    def __init__(self, inv_freq: torch.Tensor, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                 eps: float = 1e-6, sections=None, spread: bool = False, adjacent: bool = False):
+        if not (isinstance(inv_freq, torch.Tensor) and inv_freq.is_cuda and inv_freq.dim() == 1 and inv_freq.dtype == torch.float32
+                and (inv_freq.numel() <= 1 or inv_freq.stride(0) == 1)):
+            _fail("inv_freq", "a contiguous fp32 CUDA vector", inv_freq)
+        pairs = inv_freq.numel()
+        sections = (pairs,) if sections is None else tuple(int(x) for x in sections)
+        if pairs % 8 or not 1 <= len(sections) <= 3 or min(sections) < 0 or sum(sections) != pairs:
+            raise ValueError(f"sections {sections}: need one to three sizes that add up to the {pairs} pairs, a multiple of 8")
+        if spread and len(sections) != 3:
+            raise ValueError("spread needs three sections")
+        for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if w is not None and not (isinstance(w, torch.Tensor) and w.dim() == 1 and w.device == inv_freq.device and w.dtype in _CODE_OF
+                                      and w.numel() in (64, 128) and w.stride(0) == 1 and 2 * pairs <= w.numel()):
+                _fail(what, f"a contiguous [head_dim] vector on {inv_freq.device}", w)
+        self.inv_freq, self.q_weight, self.k_weight = inv_freq, q_weight, k_weight
+        self.eps, self.sections, self.spread, self.adjacent = float(eps), sections, bool(spread), bool(adjacent)
+
+    @property
+    def axes(self) -> int:
+        return len(self.sections)
+
+    def _struct(self, like: torch.Tensor) -> _Rope:
+        if like.device != self.inv_freq.device:
+            _fail("rope", f"tensors on {like.device}", self.inv_freq)
+        for w, what in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
+            if w is not None and (w.dtype != like.dtype or w.numel() != like.shape[2]):
+                _fail(what, f"[{like.shape[2]}] {like.dtype}", w)
+        sec = (C.c_int * 3)(*(self.sections + (0, 0))[:3])
+        ptr = lambda w: None if w is None else w.data_ptr()
+        return _Rope(_CODE_OF[like.dtype], like.shape[2], 2 * self.inv_freq.numel(), self.axes, sec, int(self.spread), int(self.adjacent),
+                     self.eps, self.inv_freq.data_ptr(), ptr(self.q_weight), ptr(self.k_weight))
+
+
+def _positions(positions: torch.Tensor, axes: int, tokens: int, device):
+    """(pointer, stride between axes) of [tokens] or [axes, tokens] positions."""
+    one = axes == 1 and isinstance(positions, torch.Tensor) and positions.dim() == 1
+    _check_ints(positions, "positions", (tokens,) if one else (axes, tokens), device)
+    return positions.data_ptr(), 0 if one else positions.stride(0)
+
+
+def _on(stream: Optional[torch.cuda.Stream], device) -> int:
+    return (stream or torch.cuda.current_stream(device)).cuda_stream
+
+
+def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, rope: Rope, q_out: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None, stream=None):
+    """``sh_qk_norm_rope``: rows ``q`` [tokens, q_heads, head_dim] and ``k`` [tokens, k_heads, head_dim] (or None), views of a packed
+    projection included, normalised and rotated in one pass.  ``positions``: int32 [tokens], or [axes, tokens].
+    Outputs default to new contiguous tensors; ``q_out=q`` works in place.  Returns (q_out, k_out)."""
+    _check_rows(q, "q")
+    tokens = q.shape[0]
+    if k is not None:
+        _check_rows(k, "k", q, (tokens, k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0, q.shape[2]))
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    ro = rope._struct(q)
+    pos, axis_stride = _positions(positions, rope.axes, tokens, q.device)
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    _check_rows(q_out, "q_out", q, q.shape)
+    if k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+        _check_rows(k_out, "k_out", q, k.shape)
+    with torch.cuda.device(q.device):
+        _check_status(lib.sh_qk_norm_rope(C.byref(ro), tokens, q.shape[1], 0 if k is None else k.shape[1], _rows(q),
+                                          None if k is None else _rows(k), pos, axis_stride, _rows(q_out),
+                                          None if k is None else _rows(k_out), _on(stream, q.device)), "qk_norm_rope")
+    return q_out, k_out
+
+
+def _window_struct(t: torch.Tensor, q_heads: int, kv_heads: int, window: int, sinks: int, scale: Optional[float]) -> _Window:
+    if window < 1 or sinks < 0 or window + sinks >= 1 << 30:
+        raise ValueError(f"window {window}, sinks {sinks}: need window >= 1, sinks >= 0, together below 2^30")
+    if kv_heads < 1 or q_heads < 1 or q_heads % kv_heads:
+        raise ValueError(f"{q_heads} query heads, {kv_heads} key heads: the first must be a multiple of the second")
+    if scale is not None and not (0.0 < scale < float("inf")):
+        raise ValueError(f"scale {scale}: need a positive number")
+    return _Window(_CODE_OF[t.dtype], t.shape[2], q_heads, kv_heads, window, sinks, 0.0 if scale is None else float(scale))
+
+
+def _cache_struct(k_cache, v_cache, like: torch.Tensor, sequences: int, kv_heads: int, slots: int) -> _WindowCache:
+    shape = (sequences, kv_heads, slots, like.shape[2])
+    for t, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if not (isinstance(t, torch.Tensor) and tuple(t.shape) == shape and t.dtype == like.dtype and t.device == like.device
+                and (t.numel() == 0 or t.stride(3) == 1)):
+            _fail(what, f"[sequences, key heads, sinks + window, head_dim] = {shape} of {like.dtype} on {like.device}", t)
+    walked = [i for i in range(3) if shape[i] > 1]
+    if any(k_cache.stride(i) != v_cache.stride(i) for i in walked):
+        _fail("v_cache", f"the strides of k_cache, {k_cache.stride()}", v_cache)
+    return _WindowCache(k_cache.data_ptr(), v_cache.data_ptr(), k_cache.stride(0), k_cache.stride(1), k_cache.stride(2))
+
+
+def window_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, *, window: int, sinks: int = 0,
+                   lengths: Optional[torch.Tensor] = None, k_cache: Optional[torch.Tensor] = None, v_cache: Optional[torch.Tensor] = None,
+                   scale: Optional[float] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``sh_window_prefill``: attention of prompt chunks with a sliding window and sink tokens.
+
+    ``q`` [tokens, q_heads, head_dim], ``k``/``v`` [tokens, kv_heads, head_dim]; the tokens ``starts[i] .. starts[i+1] - 1`` (int32, on the
+    device) continue sequence i, which holds ``lengths[i]`` tokens in ``k_cache``/``v_cache`` [sequences, kv_heads, sinks + window, head_dim]
+    (all three None: fresh prompts).  A token sees those before it among the first ``sinks`` positions and the last ``window``, itself
+    included.  Rows of ``out`` that belong to no sequence are left as they were (a new ``out`` is zeroed)."""
+    _check_rows(q, "q")
+    _check_rows(k, "k", q)
+    _check_rows(k, "k", q, (q.shape[0], k.shape[1], q.shape[2]))
+    _check_rows(v, "v", q, k.shape)
+    win = _window_struct(q, q.shape[1], k.shape[1], window, sinks, scale)
+    if not (isinstance(starts, torch.Tensor) and starts.dim() == 1 and starts.numel() >= 1):
+        _fail("starts", "an int32 vector of sequences + 1 entries", starts)
+    n = starts.numel() - 1
+    _check_ints(starts, "starts", (n + 1,), q.device)
+    cache = None
+    if lengths is not None or k_cache is not None or v_cache is not None:
+        _check_ints(lengths, "lengths", (n,), q.device)
+        cache = C.byref(_cache_struct(k_cache, v_cache, q, n, k.shape[1], window + sinks))
+    out = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    _check_rows(out, "out", q, q.shape)
+    with torch.cuda.device(q.device):
+        _check_status(lib.sh_window_prefill(C.byref(win), q.shape[0], n, _rows(q), _rows(k), _rows(v), starts.data_ptr(),
+                                            None if cache is None else lengths.data_ptr(), cache, _rows(out), _on(stream, q.device)),
+                      "window_prefill")
+    return out
+
+
+def window_append(k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, k_cache: torch.Tensor,
+                  v_cache: torch.Tensor, *, window: int, sinks: int = 0, stream=None) -> None:
+    """``sh_window_append``: store the chunks' keys and values (arguments as ``window_prefill``; ``lengths`` as before the chunk, the
+    caller advances them)."""
+    _check_rows(k, "k")
+    _check_rows(v, "v", k, k.shape)
+    win = _window_struct(k, k.shape[1], k.shape[1], window, sinks, None)
+    if not (isinstance(starts, torch.Tensor) and starts.dim() == 1 and starts.numel() >= 1):
+        _fail("starts", "an int32 vector of sequences + 1 entries", starts)
+    n = starts.numel() - 1
+    _check_ints(starts, "starts", (n + 1,), k.device)
+    _check_ints(lengths, "lengths", (n,), k.device)
+    cache = _cache_struct(k_cache, v_cache, k, n, k.shape[1], window + sinks)
+    with torch.cuda.device(k.device):
+        _check_status(lib.sh_window_append(C.byref(win), k.shape[0], n, _rows(k), _rows(v), starts.data_ptr(), lengths.data_ptr(),
+                                           C.byref(cache), _on(stream, k.device)), "window_append")
+
+
+def window_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                  *, window: int, sinks: int = 0, rope: Optional[Rope] = None, positions: Optional[torch.Tensor] = None,
+                  scale: Optional[float] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``sh_window_decode``: one token per sequence, in one launch: its ``q`` and ``k`` are prepared by ``rope`` (if given), its key and
+    value stored, and it attends over what it sees, itself included.
+
+    ``q`` [sequences, q_heads, head_dim], ``k``/``v`` [sequences, kv_heads, head_dim], ``lengths`` int32 [sequences]: tokens held before the
+    step (the caller advances them); negative: an idle slot of the batch, whose ``out`` row and cache are left as they were (a new ``out``
+    is zeroed).  ``positions`` as in ``qk_norm_rope``; default: ``lengths``."""
+    _check_rows(q, "q")
+    _check_rows(k, "k", q)
+    n = q.shape[0]
+    _check_rows(k, "k", q, (n, k.shape[1], q.shape[2]))
+    _check_rows(v, "v", q, k.shape)
+    win = _window_struct(q, q.shape[1], k.shape[1], window, sinks, scale)
+    _check_ints(lengths, "lengths", (n,), q.device)
+    cache = _cache_struct(k_cache, v_cache, q, n, k.shape[1], window + sinks)
+    ro, pos, axis_stride = None, None, 0
+    if rope is not None:
+        ro = C.byref(rope._struct(q))
+        if positions is not None:
+            pos, axis_stride = _positions(positions, rope.axes, n, q.device)
+        elif rope.axes != 1:
+            raise ValueError("a rope of several axes needs positions")
+    elif positions is not None:
+        raise ValueError("positions without rope")
+    out = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    _check_rows(out, "out", q, q.shape)
+    with torch.cuda.device(q.device):
+        _check_status(lib.sh_window_decode(C.byref(win), n, _rows(q), _rows(k), _rows(v), lengths.data_ptr(), C.byref(cache), ro, pos,
+                                           axis_stride, _rows(out), _on(stream, q.device)), "window_decode")
+    return out
+
+
+class WindowCache:
+    """Key/value cache of a batch under the fixed policy "first ``sinks`` tokens and last ``window`` ones": the sibling of ``Handle``
+    for attention with a sliding window.  Owns ``k``, ``v`` [sequences, kv_heads, sinks + window, head_dim] and ``lengths`` (int32, on the
+    device; -1 marks an idle slot of the batch).  ``rope``: prepares the queries and keys of every call (positions default to the
+    tokens' places in their sequences)."""
+
+    def __init__(self, sequences: int, q_heads: int, kv_heads: int, head_dim: int, window: int, sinks: int = 0, dtype="bf16", device="cuda:0",
+                 rope: Optional[Rope] = None, scale: Optional[float] = None):
+        dt = INPUT_TORCH_DTYPE[DTYPE_CODE[dtype]] if isinstance(dtype, str) else dtype
+        if dt not in _CODE_OF or dtype == "int4" or head_dim not in (64, 128):
+            raise ValueError(f"dtype {dtype}, head_dim {head_dim}: need f32, f16 or bf16 and 64 or 128")
+        self.window, self.sinks, self.rope, self.scale, self.q_heads = window, sinks, rope, scale, q_heads
+        shape = (sequences, kv_heads, sinks + window, head_dim)
+        self.k = torch.zeros(shape, dtype=dt, device=device)
+        self.v = torch.zeros(shape, dtype=dt, device=device)
+        self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
+        _window_struct(self.k[0], q_heads, kv_heads, window, sinks, scale)
+
+    def _prompt_positions(self, starts: torch.Tensor, tokens: int) -> torch.Tensor:
+        """Position of each row of a chunk tensor: its sequence's length plus its place in the chunk."""
+        row = torch.arange(tokens, dtype=torch.int32, device=self.k.device)
+        seq = (torch.searchsorted(starts, row, right=True) - 1).clamp(0, starts.numel() - 2)
+        return (self.lengths[seq] + row - starts[seq]).clamp(min=0)
+
+    def prefill(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Chunks of prompts (``window_prefill``), stored and counted.  On the current stream."""
+        if self.rope is not None:
+            if positions is None:
+                if self.rope.axes != 1:
+                    raise ValueError("a rope of several axes needs positions")
+                positions = self._prompt_positions(starts, q.shape[0])
+            q, k = qk_norm_rope(q, k, positions, self.rope)
+        win = dict(window=self.window, sinks=self.sinks)
+        out = window_prefill(q, k, v, starts, lengths=self.lengths, k_cache=self.k, v_cache=self.v, scale=self.scale, out=out, **win)
+        window_append(k, v, starts, self.lengths, self.k, self.v, **win)
+        self.lengths += torch.where(self.lengths < 0, 0, starts[1:] - starts[:-1])
+        return out
+
+    def decode(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """One token per sequence (``window_decode``), stored and counted.  On the current stream."""
+        out = window_decode(q, k, v, self.lengths, self.k, self.v, window=self.window, sinks=self.sinks, rope=self.rope, positions=positions,
+                            scale=self.scale, out=out)
+        self.lengths += (self.lengths >= 0).to(torch.int32)
+        return out

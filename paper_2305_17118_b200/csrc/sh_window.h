@@ -1,0 +1,43 @@
+// Internal declarations of the query/key preparation and the window cache kernels.
+#pragma once
+#include <stdint.h>
+
+#include "sh_internal.h"
+
+// Kernel-side forms of the public structs: byte strides, resolved options.
+struct WinRows {
+    char *p;
+    long long ts, hs;             // bytes between tokens, between heads
+};
+
+struct RopeParams {
+    WinRows q, k, qo, ko;
+    const int32_t *positions;     // [axes] rows, axis_stride apart
+    long long axis_stride;
+    const float *inv_freq;
+    const void *qw, *kw;
+    int tokens, q_heads, k_heads;
+    int rot, axes, sec0, sec01;   // pairs [0, sec0) turn with axis 0, [sec0, sec01) with axis 1, the rest with axis 2
+    int spread_h, spread_w;       // spread: 3 * sections[1], 3 * sections[2] (else 0 and `spread` false)
+    int spread, adjacent;
+    float eps;
+    int hpw;                      // set by the launcher: head groups a warp walks through
+};
+
+struct WindowParams {
+    WinRows q, k, v, out;
+    char *kc, *vc;                // caches, or NULL
+    long long css, chs, cls;      // bytes between sequences, heads, slots
+    const int32_t *starts, *lengths;
+    int tokens, sequences;
+    int hq, hk, g;                // query heads, key heads, query heads per key head
+    int window, sinks;
+    float scale_log2e;
+    RopeParams rope;              // decode only: how the step's q and k are prepared
+    bool with_rope;
+};
+
+cudaError_t sh_launch_qk_norm_rope(RopeParams p, int dtype, int D, cudaStream_t s);
+cudaError_t sh_launch_window_prefill_simt(const WindowParams &p, int dtype, int D, cudaStream_t s);
+cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, cudaStream_t s);
+cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, cudaStream_t s);
