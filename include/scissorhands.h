@@ -392,7 +392,7 @@ typedef struct {
     int head_dim;         /* 64 or 128 */
     int q_heads, kv_heads;
     int window, sinks;    /* window >= 1, sinks >= 0, together below 2^30 */
-    double scale;         /* of the logits; 0: 1/sqrt(head_dim) */
+    double scale;         /* of the logits, 1e-30 to 1e30; 0: 1/sqrt(head_dim) */
 } sh_window;
 
 /* Normalisation and rotation of query and key rows:
@@ -453,6 +453,12 @@ int sh_window_append(const sh_window *w, int tokens, int sequences, const sh_row
 int sh_window_decode(const sh_window *w, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *lengths_dev,
                      const sh_window_cache *cache, const sh_rope *rope, const int32_t *positions_dev, long long axis_stride,
                      const sh_rows *out, void *stream);
+
+/*
+ * Did a kernel of the window cache give up one of its bounded waits on the current device since the last call?  Its outputs are
+ * then incomplete.  Synchronises `stream`.  SH_OK, SH_EDEVICE or SH_ECUDA.
+ */
+int sh_window_status(void *stream);
 
 /* Text for a status code; never NULL. */
 const char *sh_strerror(int status);

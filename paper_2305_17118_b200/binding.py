@@ -34,7 +34,7 @@ EXPORTS = ["sh_create", "sh_destroy", "sh_workspace_bytes", "sh_bind", "sh_set_o
            "sh_compress", "sh_compress_static", "sh_scores", "sh_select", "sh_state", "sh_export_unit",
            "sh_restore", "sh_launch_count", "sh_decode_kernel_choice", "sh_import_compressed", "sh_prefill_bulk",
            "sh_prefill_bulk_scratch_bytes", "sh_strerror", "sh_last_cuda_error",
-           "sh_qk_norm_rope", "sh_window_prefill", "sh_window_append", "sh_window_decode"]
+           "sh_qk_norm_rope", "sh_window_prefill", "sh_window_append", "sh_window_decode", "sh_window_status"]
 
 
 class _Rows(C.Structure):
@@ -109,6 +109,7 @@ def declare(lib: C.CDLL) -> C.CDLL:
     lib.sh_qk_norm_rope.argtypes = [rope, C.c_int, C.c_int, C.c_int, rows, rows, vp, C.c_longlong, rows, rows, vp]
     lib.sh_window_prefill.argtypes = [window, C.c_int, C.c_int, rows, rows, rows, vp, vp, cache, rows, vp]
     lib.sh_window_append.argtypes = [window, C.c_int, C.c_int, rows, rows, vp, vp, cache, vp]
+    lib.sh_window_status.argtypes = [vp]
     lib.sh_window_decode.argtypes = [window, C.c_int, rows, rows, rows, vp, cache, rope, vp, C.c_longlong, rows, vp]
     return lib
 
@@ -512,8 +513,8 @@ def _window_struct(t: torch.Tensor, q_heads: int, kv_heads: int, window: int, si
         raise ValueError(f"window {window}, sinks {sinks}: need window >= 1, sinks >= 0, together below 2^30")
     if kv_heads < 1 or q_heads < 1 or q_heads % kv_heads:
         raise ValueError(f"{q_heads} query heads, {kv_heads} key heads: the first must be a multiple of the second")
-    if scale is not None and not (0.0 < scale < float("inf")):
-        raise ValueError(f"scale {scale}: need a positive number")
+    if scale is not None and not (1e-30 < scale < 1e30):
+        raise ValueError(f"scale {scale}: need a number between 1e-30 and 1e30")
     return _Window(_CODE_OF[t.dtype], t.shape[2], q_heads, kv_heads, window, sinks, 0.0 if scale is None else float(scale))
 
 
@@ -610,6 +611,13 @@ def window_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: to
         _check_status(lib.sh_window_decode(C.byref(win), n, _rows(q), _rows(k), _rows(v), lengths.data_ptr(), C.byref(cache), ro, pos,
                                            axis_stride, _rows(out), _on(stream, q.device)), "window_decode")
     return out
+
+
+def window_status(device="cuda:0", stream=None) -> None:
+    """``sh_window_status``: raise ShError(SH_EDEVICE) if a window kernel on ``device`` gave up one of its bounded waits since the last
+    call (its outputs are then incomplete).  Synchronises the stream."""
+    with torch.cuda.device(device):
+        _check_status(lib.sh_window_status(_on(stream, torch.device(device))), "window_status")
 
 
 class WindowCache:

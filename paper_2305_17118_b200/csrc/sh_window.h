@@ -39,5 +39,9 @@ struct WindowParams {
 
 cudaError_t sh_launch_qk_norm_rope(RopeParams p, int dtype, int D, cudaStream_t s);
 cudaError_t sh_launch_window_prefill_simt(const WindowParams &p, int dtype, int D, cudaStream_t s);
+// tensor cores: f16 and bf16
+cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int D, cudaStream_t s);
+// code of the first bounded wait that gave up in a window kernel of the current device since the last call (0: none); synchronises
+cudaError_t sh_window_error_take(int *code, cudaStream_t s);
 cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, cudaStream_t s);
 cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, cudaStream_t s);

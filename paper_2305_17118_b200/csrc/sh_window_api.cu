@@ -76,7 +76,7 @@ bool good_window(const sh_window *w) {
     if (!w || !good_type(w->dtype, w->head_dim) || w->kv_heads < 1 || w->q_heads < 1 || w->q_heads % w->kv_heads) return false;
     if (w->kv_heads > 65535) return false;
     if (w->window < 1 || w->sinks < 0 || (long long)w->window + w->sinks >= MAX_POS) return false;
-    return std::isfinite(w->scale) && w->scale >= 0.0;
+    return w->scale == 0.0 || (w->scale > 1e-30 && w->scale < 1e30);      // (NaN: no; fp32 has to hold it)
 }
 bool good_cache(const sh_window_cache *c, const sh_window *w, int sequences) {
     const int D = w->head_dim, es = elem_size(w->dtype);
@@ -145,7 +145,8 @@ int sh_window_prefill(const sh_window *w, int tokens, int sequences, const sh_ro
     p.v = rows(v, tokens, w->kv_heads, D, es);
     p.out = rows(out, tokens, w->q_heads, D, es);
     p.starts = starts_dev; p.lengths = lengths_dev;
-    return done(sh_launch_window_prefill_simt(p, w->dtype, D, (cudaStream_t)stream));
+    return done(w->dtype == SH_F32 ? sh_launch_window_prefill_simt(p, w->dtype, D, (cudaStream_t)stream)
+                                   : sh_launch_window_prefill_umma(p, w->dtype, D, (cudaStream_t)stream));
 }
 
 int sh_window_append(const sh_window *w, int tokens, int sequences, const sh_rows *k, const sh_rows *v, const int32_t *starts_dev,
@@ -188,6 +189,12 @@ int sh_window_decode(const sh_window *w, int sequences, const sh_rows *q, const 
     p.with_rope = rope != nullptr;
     if (rope) fill_rope(p.rope, rope, positions_dev ? positions_dev : lengths_dev, axis_stride);
     return done(sh_launch_window_decode(p, w->dtype, D, (cudaStream_t)stream));
+}
+
+int sh_window_status(void *stream) {
+    int code = 0;
+    if (sh_window_error_take(&code, (cudaStream_t)stream) != cudaSuccess) return SH_ECUDA;
+    return code ? SH_EDEVICE : SH_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,673 @@
+// sh_window_prefill on the 5th-generation tensor cores: 16-bit types, head_dim 64 or 128.
+//
+// out = softmax(scale Q.K^T + mask) V with the running maximum and sum of an online softmax.  A work item is one key head and
+// two query tiles; a tile is 128 rows = TPT tokens x GB query heads of the group (heads innermost), so the heads that share keys
+// share a tile and the tile spans few tokens.  The keys come in tiles of 128: first the slots of the cache, then the chunk's own
+// rows; tiles that none of the item's rows can see are never loaded, tiles that a query tile does not see are not multiplied for it.
+//
+//   warps 0-3, 4-7   softmax of query tile 0 and 1: thread = row.  S from tensor memory, mask, exponentials, P (16 bits) back into
+//                    the columns of S, the rare rescaling of O, and the division and store at the end
+//   warp 8           issues the MMAs: S = Q.K^T (both operands in shared memory, K-major), O += P.V (P in tensor memory, V MN-major)
+//   warp 9           requests query, key and value tiles (tiled TMA copies, 128-byte swizzle; rows outside a tensor are zeros)
+//
+// The tensor pipe takes the MMAs in the order PV0(n), S0(n+1), PV1(n), S1(n+1): one query tile's softmax runs while the other's
+// products do.  P overwrites S: S(n+1) of a query tile is issued behind PV(n) of the same tile, which reads P, and the pipe keeps
+// that order.  CTAs are persistent; the loads of the next item start while the present one drains.
+//
+// P is rounded to the storage type (the tensor cores take no other pair with 16-bit V); its row sum is taken before the rounding,
+// in fp32.  The subtracted maximum is only renewed when it has grown by more than 8 (log2), so weights stay below 2^8; fp16
+// weights carry a factor 2^7 (at most 2^15) that keeps small ones out of the subnormal numbers; it cancels in O / l.
+//
+// Weights of unseen keys are zero, but 0 * NaN is NaN: a value row that is not finite poisons rows that do not see it (a slot
+// that holds no token, a later token, another sequence's row).  That shows as an O that is not finite; such rows are computed
+// again at the end, one warp per row over the visible keys only.  Rows whose result is rightly not finite take that way too.
+//
+// Bound by the tensor pipe and the exponentials, which need the same time: 128 x 128 x D twice at 4096 multiply-adds per cycle
+// against 128 x 128 exponentials at 16 per cycle.
+#include <cuda.h>
+#include <math_constants.h>
+
+#include "sh_elem.cuh"
+#include "sh_umma.cuh"
+#include "sh_window.cuh"
+
+namespace {
+
+using namespace shasync;
+using namespace shumma;
+using namespace shwin;
+
+constexpr int TM = 128, TN = 128;          // rows of a query tile, keys of a key tile
+constexpr int HALF = 128 * 128;            // bytes of 128 rows x 64 elements
+constexpr int NTH = 320;
+constexpr float RENEW = 8.f;               // log2 growth of the maximum at which O is rescaled
+
+__device__ int g_window_error;             // code of the first bounded wait that gave up
+
+template <int D> struct Cfg {
+    static constexpr int TILE = D / 64 * HALF;         // bytes of a query, key or value tile
+    static constexpr int STAGES = D == 128 ? 5 : 8;    // key and value tiles in flight
+    static constexpr int OFF_KV = 2 * TILE;
+    static constexpr int OFF_BAR = OFF_KV + STAGES * TILE;
+    static constexpr int SMEM = OFF_BAR + 256;
+    static constexpr int O_COL = 2 * TN;               // tensor memory: S0, S1 (P inside), O0, O1
+    static_assert(SMEM <= 232448 && O_COL + 2 * D <= 512, "");
+};
+
+struct Bars {
+    uint64_t q_full[2], q_empty[2];        // a query tile landed / its last S has been computed
+    uint64_t full[8], empty[8];            // stages: landed / read by the MMAs
+    uint64_t s_full[2], p_ready[2], pv_done[2];
+    uint32_t tmem;
+    int abort_flag;
+};
+static_assert(sizeof(Bars) <= 256, "barrier block");
+
+struct UmmaParams {
+    WindowParams w;
+    int tpt, gb, hblocks;                  // tokens and heads of a tile, head blocks per key head
+};
+
+__device__ __forceinline__ uint64_t desc_sw128(uint32_t saddr, uint32_t lbo, uint32_t sbo) { return smem_desc(saddr, lbo, sbo) | (2ull << 61); }
+
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+        "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *map, int c0, int c1, int c2, uint64_t *bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                     smem_u32(dst)),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void tma_4d(void *dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar))
+        : "memory");
+}
+
+// One work item and the key tiles it has to walk over.  Tiles 0 .. ctiles - 1 are blocks of 128 cache slots, tile ctiles + j holds
+// the chunk's rows 128 j ...  In the cache, slots [sinks, head) hold the positions cached - (head - slot), and, once the ring has
+// wrapped, slots [head, sinks + window) the positions cached - window + (slot - head).
+struct Item {
+    int seq, first, count, cached;         // seq < 0: there is no such item
+    int kvh, hb;
+    int a;                                 // first token of query tile 0, counted in the chunk; tile t starts at a + t * tpt
+    int live, head, ctiles, jlo, jhi, tpt, sinks, window;
+    bool wrapped;
+
+    __device__ __forceinline__ int from(int t) const { return a + t * tpt; }
+    __device__ __forceinline__ bool has(int t) const { return from(t) < count; }
+    __device__ __forceinline__ int last(int t) const { return min(from(t) + tpt, count) - 1; }
+    // does query tile t see a key of tile i?
+    __device__ __forceinline__ bool need(int t, int i) const {
+        if (!has(t)) return false;
+        const int oldest = cached + from(t) - window + 1;      // position
+        if (i < ctiles) {
+            const int x = i * TN, y = min(x + TN, live);
+            if (x < min(sinks, cached)) return true;
+            if (wrapped && y > head) {
+                if (cached - window + (y - 1 - head) >= oldest) return true;
+            }
+            return x < head && y > sinks && cached - head + min(y, head) - 1 >= oldest;
+        }
+        const int j = (i - ctiles) * TN;
+        return j <= last(t) && (cached + j + TN - 1 >= oldest || cached + j < sinks);
+    }
+    __device__ __forceinline__ int next(int i) const {         // -1: no further tile
+        for (++i; i < ctiles; ++i)
+            if (need(0, i) || need(1, i)) return i;
+        if (i - ctiles < jlo && cached + (i - ctiles) * TN >= sinks) i = ctiles + jlo;      // what lies between the sinks and the window
+        return i <= ctiles + jhi ? i : -1;
+    }
+};
+
+__device__ __forceinline__ Item find_item(const UmmaParams &p, long long id) {
+    const int per = p.w.hk * p.hblocks, in = (int)(id % per);
+    // (rows = tokens here: a tile of find_tile is the 2 * tpt tokens of an item)
+    const int lane = threadIdx.x & 31, span = 2 * p.tpt;
+    const long long tile = id / per;
+    Item r;
+    r.seq = -1;
+    long long before = 0;
+    for (int base = 0; base < p.w.sequences; base += 32) {
+        int first = 0, count = 0, cached = 0;
+        if (base + lane < p.w.sequences) sequence_rows(p.w, base + lane, first, count, cached);
+        const int mine = (count + span - 1) / span;
+        long long upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, before + upto > tile);
+        if (hit) {
+            const int l = __ffs(hit) - 1;
+            r.seq = base + l;
+            r.first = __shfl_sync(0xffffffffu, first, l);
+            r.count = __shfl_sync(0xffffffffu, count, l);
+            r.cached = __shfl_sync(0xffffffffu, cached, l);
+            r.a = (int)(tile - before - __shfl_sync(0xffffffffu, upto - mine, l)) * span;
+            break;
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (r.seq < 0) return r;
+    r.kvh = in / p.hblocks; r.hb = in % p.hblocks;
+    r.tpt = p.tpt; r.sinks = p.w.sinks; r.window = p.w.window;
+    if (!p.w.kc) r.cached = 0;
+    r.live = min(r.cached, r.sinks + r.window);
+    r.wrapped = r.cached > r.sinks + r.window;
+    r.head = r.wrapped ? r.sinks + (r.cached - r.sinks) % r.window : r.cached;
+    r.ctiles = (r.live + TN - 1) / TN;
+    r.jlo = max(0, r.a - r.window + 1) / TN;
+    r.jhi = r.last(r.has(1) ? 1 : 0) / TN;
+    return r;
+}
+
+// Columns of tile i that the query at chunk index qi sees: up to three runs [lo, hi) counted from the tile's first key.
+struct Runs {
+    int lo[3], hi[3];
+};
+__device__ __forceinline__ Runs visible_runs(const Item &w, int i, int qi) {
+    Runs r;
+    if (i < w.ctiles) {
+        const int x = i * TN, d = w.head - w.cached;
+        r.lo[0] = -x; r.hi[0] = min(w.sinks, w.cached) - x;
+        r.lo[1] = max(w.sinks, w.cached + qi - w.window + d + 1) - x; r.hi[1] = w.head - x;
+        r.lo[2] = w.cached + qi + d + 1 - x; r.hi[2] = (w.wrapped ? w.sinks + w.window : 0) - x;
+    } else {
+        const int j = (i - w.ctiles) * TN;
+        r.lo[0] = -j; r.hi[0] = min(w.sinks - w.cached, qi + 1) - j;
+        r.lo[1] = max(0, qi - w.window + 1) - j; r.hi[1] = qi + 1 - j;
+        r.lo[2] = 0; r.hi[2] = 0;
+    }
+    return r;
+}
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u); }
+__device__ __forceinline__ uint32_t run_bits(const Runs &r, int base) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) m |= low_bits(r.hi[k] - base) & ~low_bits(r.lo[k] - base);
+    return m;
+}
+__device__ __forceinline__ bool covers(const Runs &r) {      // one run holds the whole tile
+    return (r.lo[0] <= 0 && r.hi[0] >= TN) || (r.lo[1] <= 0 && r.hi[1] >= TN) || (r.lo[2] <= 0 && r.hi[2] >= TN);
+}
+
+__device__ __forceinline__ uint64_t f2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void un2(uint64_t x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// One row by one warp, over its visible keys only, in fp32 on CUDA cores: for rows next to values that are not finite.
+template <typename T, int D>
+__device__ __noinline__ void slow_row(const UmmaParams &u, long long id, int qi, int h) {
+    constexpr int E = D / 32;
+    const WindowParams &p = u.w;
+    const Item w = find_item(u, id);
+    const int lane = threadIdx.x & 31;
+    float q[E], o[E], m = -CUDART_INF_F, l = 0.f;
+    const T *qr = reinterpret_cast<const T *>(p.q.p + (long long)(w.first + qi) * p.q.ts + h * p.q.hs) + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) { q[e] = (float)qr[e] * p.scale_log2e; o[e] = 0.f; }
+    for (int i = w.next(-1); i >= 0; i = w.next(i)) {
+        const Runs runs = visible_runs(w, i, qi);
+        const bool in_cache = i < w.ctiles;
+        const int base = (in_cache ? i : i - w.ctiles) * TN;
+        for (int c = 0; c < TN; ++c) {
+            if (!((run_bits(runs, c & ~31) >> (c & 31)) & 1u)) continue;
+            const long long ko = in_cache ? w.seq * p.css + w.kvh * p.chs + (long long)(base + c) * p.cls : (long long)(w.first + base + c) * p.k.ts + w.kvh * p.k.hs;
+            const long long vo = in_cache ? ko : (long long)(w.first + base + c) * p.v.ts + w.kvh * p.v.hs;
+            const T *kr = reinterpret_cast<const T *>((in_cache ? p.kc : p.k.p) + ko) + lane * E;
+            const T *vr = reinterpret_cast<const T *>((in_cache ? p.vc : p.v.p) + vo) + lane * E;
+            float s = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) s = fmaf(q[e], (float)kr[e], s);
+#pragma unroll
+            for (int x = 16; x; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
+            const float mn = fmaxf(m, s), b = mn == -CUDART_INF_F ? 0.f : mn, keep = ex2_approx(m - b), e1 = ex2_approx(s - b);
+            m = mn;
+            l = l * keep + e1;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = fmaf(e1, (float)vr[e], o[e] * keep);
+        }
+    }
+    T *dst = reinterpret_cast<T *>(p.out.p + (long long)(w.first + qi) * p.out.ts + h * p.out.hs) + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) dst[e] = (T)(o[e] / l);
+}
+
+template <typename T> struct Fmt;
+template <> struct Fmt<__half> { static constexpr int CODE = 0; static constexpr float LIFT = 7.f; };
+template <> struct Fmt<__nv_bfloat16> { static constexpr int CODE = 1; static constexpr float LIFT = 0.f; };
+
+template <typename T, int D>
+__global__ void __launch_bounds__(NTH, 1)
+sh_window_prefill_umma_kernel(const UmmaParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                              const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_kc,
+                              const __grid_constant__ CUtensorMap map_vc) {
+    using C = Cfg<D>;
+    extern __shared__ __align__(1024) unsigned char sm[];
+    unsigned char *kv = sm + C::OFF_KV;
+    Bars *bars = reinterpret_cast<Bars *>(sm + C::OFF_BAR);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    int *err = &g_window_error;
+    auto aborted = [&]() { return *(volatile int *)&bars->abort_flag != 0; };
+
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (tid == 0) {
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&bars->q_full[t], 1); mbar_init(&bars->q_empty[t], 1);
+            mbar_init(&bars->s_full[t], 1); mbar_init(&bars->p_ready[t], 128); mbar_init(&bars->pv_done[t], 1);
+        }
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
+        bars->abort_flag = 0;
+        if ((smem_u32(sm) & 1023u) != 0) {      // the swizzled tiles need the alignment the declaration asks for
+            atomicCAS(err, 0, 0x620);
+            bars->abort_flag = 1;
+        }
+        fence_barrier_init();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tbase = bars->tmem;
+    bool ok = !aborted();
+
+    if (warp == 8) {
+        // ------------------------------------------------------------------------------------------------ MMAs
+        // (the whole warp walks and waits, one lane issues)
+        const uint32_t idesc_s = instr_desc(Fmt<T>::CODE, 0, TM, TN), idesc_pv = instr_desc(Fmt<T>::CODE, 0, TM, D) | (1u << 16);
+        const uint32_t q_addr = smem_u32(sm), kv_addr = smem_u32(kv);
+        long long id = blockIdx.x;
+        Item cur = find_item(p, id), nxt = cur;       // items of the present step and of the step whose S comes next
+        int ci = -1, ni = cur.seq >= 0 ? cur.next(-1) : -1;
+        bool new_item = true;                         // the step (nxt, ni) is the first of its item
+        uint32_t n_items = 0, n_step = 0;             // items begun by S; steps begun by S
+        uint32_t cnt_p[2] = {0, 0};
+        bool started[2] = {false, false};
+        // S of tile t for the step (nxt, ni)
+        auto issue_s = [&](int t) {
+            if (!nxt.need(t, ni)) return;
+            tc_fence_after();
+            const uint32_t st = (2 * n_step) % C::STAGES, kb = kv_addr + st * C::TILE, qb = q_addr + t * C::TILE;
+            if (lane == 0) {
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+                    umma_f16(tbase + t * TN, desc_sw128(qb + (ks >> 2) * HALF + (ks & 3) * 32, 16, 1024),
+                             desc_sw128(kb + (ks >> 2) * HALF + (ks & 3) * 32, 16, 1024), idesc_s, ks > 0);
+                umma_commit(&bars->s_full[t]);
+            }
+        };
+        auto wait_s = [&]() {      // operands of the step (nxt, ni)
+            if (new_item) {
+                ok = ok && mbar_wait(&bars->q_full[0], n_items & 1, err, 0x601);
+                if (nxt.has(1)) ok = ok && mbar_wait(&bars->q_full[1], n_items & 1, err, 0x602);
+            }
+            const uint32_t u = 2 * n_step;
+            ok = ok && mbar_wait(&bars->full[u % C::STAGES], (u / C::STAGES) & 1, err, 0x603);
+            ok = ok && !aborted();
+        };
+        // after both tiles' S of a step: release the keys, and the queries behind the item's last step; move on
+        auto advance_s = [&]() {
+            const int after = nxt.next(ni);
+            if (lane == 0) {
+                umma_commit(&bars->empty[(2 * n_step) % C::STAGES]);
+                if (after < 0) { umma_commit(&bars->q_empty[0]); umma_commit(&bars->q_empty[1]); }
+            }
+            ++n_step;
+            new_item = after < 0;
+            if (after < 0) {
+                ++n_items;
+                id += gridDim.x;
+                nxt = find_item(p, id);
+                ni = nxt.seq >= 0 ? nxt.next(-1) : -1;
+            } else {
+                ni = after;
+            }
+        };
+        if (ni >= 0) {
+            wait_s();
+            if (ok) { issue_s(0); issue_s(1); }
+        }
+        while (ok && ni >= 0) {
+            cur = nxt; ci = ni;
+            const uint32_t n = n_step;
+            const bool fresh = new_item;
+            advance_s();                              // (nxt, ni): the step whose S comes next
+            const uint32_t u = 2 * n + 1, vs = u % C::STAGES, vb = kv_addr + vs * C::TILE;
+            const bool more = ni >= 0;
+            if (fresh) started[0] = started[1] = false;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if (cur.need(t, ci)) {
+                    ok = ok && mbar_wait(&bars->p_ready[t], cnt_p[t] & 1, err, 0x604);
+                    ++cnt_p[t];
+                    ok = ok && mbar_wait(&bars->full[vs], (u / C::STAGES) & 1, err, 0x605);
+                    ok = ok && !aborted();
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int ks = 0; ks < TN / 16; ++ks)
+                            umma_ts(tbase + C::O_COL + t * D, tbase + t * TN + ks * 8, desc_sw128(vb + ks * 2048, HALF, 1024), idesc_pv,
+                                    started[t] || ks > 0);      // (the first product of a query tile in its item overwrites O)
+                        umma_commit(&bars->pv_done[t]);
+                    }
+                    started[t] = true;
+                }
+                // within an item S of the next step follows at once; the next item's waits for its queries, behind both products
+                if (t == 1 && lane == 0) umma_commit(&bars->empty[vs]);
+                if (more && (!new_item || t == 1)) {
+                    if (t == 0 || new_item) wait_s();
+                    if (!ok) break;
+                    if (new_item) { issue_s(0); issue_s(1); } else issue_s(t);
+                }
+            }
+        }
+        if (!ok) *(volatile int *)&bars->abort_flag = 1;
+    } else if (warp == 9) {
+        // ------------------------------------------------------------------------------------------------ loads
+        uint32_t n = 0, items = 0;
+        const int rows = p.tpt * p.gb;
+        auto request = [&](bool value, const Item &w, int i) {
+            const uint32_t st = n % C::STAGES;
+            if (n >= C::STAGES) ok = ok && mbar_wait(&bars->empty[st], (n / C::STAGES - 1) & 1, err, 0x612);
+            ok = ok && !aborted();
+            if (!ok) return;
+            if (lane == 0) {
+                unsigned char *dst = kv + st * C::TILE;
+                mbar_arrive_expect_tx(&bars->full[st], C::TILE);
+#pragma unroll
+                for (int h = 0; h < D / 64; ++h) {
+                    if (i < w.ctiles) tma_4d(dst + h * HALF, value ? &map_vc : &map_kc, h * 64, i * TN, w.kvh, w.seq, &bars->full[st]);
+                    else tma_3d(dst + h * HALF, value ? &map_v : &map_k, h * 64, w.kvh, w.first + (i - w.ctiles) * TN, &bars->full[st]);
+                }
+            }
+            ++n;
+        };
+        for (long long id = blockIdx.x; ok; id += gridDim.x) {
+            const Item w = find_item(p, id);
+            if (w.seq < 0) break;
+            bool queries = false;
+            for (int i = w.next(-1); i >= 0 && ok; i = w.next(i)) {
+                if (!queries) {
+                    queries = true;
+                    for (int t = 0; t < 2; ++t) {
+                        if (items > 0) ok = ok && mbar_wait(&bars->q_empty[t], (items - 1) & 1, err, 0x611);
+                        ok = ok && !aborted();
+                        if (!ok) break;
+                        if (lane == 0) {
+                            if (w.has(t)) {
+                                mbar_arrive_expect_tx(&bars->q_full[t], D / 64 * rows * 128);
+#pragma unroll
+                                for (int h = 0; h < D / 64; ++h)
+                                    tma_3d(sm + t * C::TILE + h * HALF, &map_q, h * 64, w.kvh * p.w.g + w.hb * p.gb, w.first + w.from(t), &bars->q_full[t]);
+                            } else {
+                                mbar_arrive(&bars->q_full[t]);
+                            }
+                        }
+                        if (t == 0) request(false, w, i);
+                    }
+                    if (ok) request(true, w, i);
+                } else {
+                    request(false, w, i);
+                    if (ok) request(true, w, i);
+                }
+            }
+            ++items;
+        }
+        if (!ok) *(volatile int *)&bars->abort_flag = 1;
+        // let the copies requested last land before the CTA goes away (a phase that is past reads as complete)
+        if (lane == 0) {
+            if (items > 0)
+                for (int t = 0; t < 2; ++t) mbar_wait(&bars->q_full[t], (items - 1) & 1, nullptr, 0);
+            for (uint32_t k = 0; k < C::STAGES && k < n; ++k) mbar_wait(&bars->full[(n - 1 - k) % C::STAGES], ((n - 1 - k) / C::STAGES) & 1, nullptr, 0);
+        }
+        __syncwarp();
+    } else if (warp < 8) {
+        // ------------------------------------------------------------------------------------------------ softmax
+        const int t = warp >> 2, row = tid & 127;
+        const uint32_t lanes = tbase + ((uint32_t)((warp & 3) * 32) << 16), s_addr = lanes + t * TN, o_addr = lanes + C::O_COL + t * D;
+        const int tok = row / p.gb, hrow = row % p.gb;
+        const float c = p.w.scale_log2e;
+        uint32_t cnt = 0;
+        for (long long id = blockIdx.x; ok; id += gridDim.x) {
+            const Item w = find_item(p, id);
+            if (w.seq < 0) break;
+            if (!w.has(t)) continue;
+            const int qi = w.from(t) + tok, h = w.hb * p.gb + hrow;
+            const bool live = tok < p.tpt && qi < w.count && h < p.w.g;
+            float m = -CUDART_INF_F, l = 0.f;
+            bool begun = false;
+            for (int i = w.next(-1); i >= 0; i = w.next(i)) {
+                if (!w.need(t, i)) continue;
+                const Runs runs = visible_runs(w, i, qi);
+                const bool whole = __all_sync(0xffffffffu, !live || covers(runs));
+                ok = mbar_wait(&bars->s_full[t], cnt & 1, err, 0x621);
+                if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
+                tc_fence_after();
+                uint32_t s[TN];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) tmem_ld32_nowait(s_addr + b * 32, s + b * 32);
+                tmem_wait_ld();
+                if (!whole) {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const uint32_t bits = run_bits(runs, b * 32);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) s[b * 32 + k] = (bits >> k) & 1u ? s[b * 32 + k] : 0xff800000u;      // -inf
+                    }
+                }
+                float mx[4] = {m, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+                for (int k = 0; k < TN; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(s[k]));
+                const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                // renew the subtracted maximum when it has grown enough (or is the first): rescale O and l
+                const bool grown = live && (mn - m) * c > RENEW;      // (-inf - -inf: no)
+                if (__any_sync(0xffffffffu, grown)) {
+                    const float f = m == -CUDART_INF_F ? 0.f : ex2_approx((m - mn) * c);
+                    if (begun) {
+                        ok = mbar_wait(&bars->pv_done[t], (cnt - 1) & 1, err, 0x622);      // the product before this one is in O
+                        if (__any_sync(0xffffffffu, !ok)) { ok = false; break; }
+                        tc_fence_after();
+#pragma unroll
+                        for (int b = 0; b < D / 32; ++b) {
+                            uint32_t o[32];
+                            tmem_ld32_nowait(o_addr + b * 32, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_st32(o_addr + b * 32, o);
+                        }
+                    }
+                    l *= f;
+                    m = mn;
+                }
+                const float base = m == -CUDART_INF_F ? 0.f : m * c - Fmt<T>::LIFT;
+                const uint64_t c2 = f2(c, c), b2 = f2(-base, -base);
+                uint64_t sum0 = f2(0.f, 0.f), sum1 = sum0;
+                uint32_t pk[TN / 2];
+#pragma unroll
+                for (int k = 0; k < TN; k += 2) {
+                    float x, y;
+                    un2(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, b2), x, y);
+                    x = ex2_approx(x);
+                    y = ex2_approx(y);
+                    if (k & 2) sum1 = add2(sum1, f2(x, y)); else sum0 = add2(sum0, f2(x, y));
+                    pk[k / 2] = shelem::Vec<T>::pack2(x, y);
+                }
+                tmem_st32(s_addr, pk);
+                tmem_st32(s_addr + 32, pk + 32);
+                float x, y;
+                un2(add2(sum0, sum1), x, y);
+                l += x + y;
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(&bars->p_ready[t]);
+                ++cnt;
+                begun = true;
+            }
+            if (!ok) break;
+            ok = mbar_wait(&bars->pv_done[t], (cnt - 1) & 1, err, 0x623);
+            if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
+            tc_fence_after();
+            const float inv = 1.f / l;
+            char *dst = p.w.out.p + (long long)(w.first + qi) * p.w.out.ts + (long long)(w.kvh * p.w.g + h) * p.w.out.hs;
+            bool odd = false;
+#pragma unroll
+            for (int b = 0; b < D / 32; ++b) {
+                uint32_t o[32];
+                tmem_ld32_nowait(o_addr + b * 32, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 32; k += 8) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        x[e] = __uint_as_float(o[k + e]) * inv;
+                        odd |= !isfinite(x[e]);
+                    }
+                    if (live) *reinterpret_cast<uint4 *>(dst + (b * 32 + k) * 2) = shelem::Vec<T>::pack(x);
+                }
+            }
+            tc_fence_before();      // O has been read before the arrivals that let the next item overwrite it
+            __syncwarp();
+            unsigned again = __ballot_sync(0xffffffffu, live && odd);
+            while (again) {
+                const int l0 = __ffs(again) - 1;
+                again &= again - 1;
+                slow_row<T, D>(p, id, __shfl_sync(0xffffffffu, qi, l0), w.kvh * p.w.g + __shfl_sync(0xffffffffu, h, l0));
+            }
+        }
+        if (!ok) *(volatile int *)&bars->abort_flag = 1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512) : "memory");
+    }
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's tensor-map encoder, looked up through the runtime (the library does not link against the driver).
+EncodeTiled encoder() {
+    static EncodeTiled fn = [] {
+        void *sym = nullptr;
+        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
+            sym = nullptr;
+        return reinterpret_cast<EncodeTiled>(sym);
+    }();
+    return fn;
+}
+
+// Map over rows of D 16-bit elements, boxes of 64 elements x box[1] x box[2] (x 1), 128-byte swizzle, zeros outside the tensor.
+bool make_map(CUtensorMap *m, const void *base, int rank, int D, const uint64_t *dim, const uint64_t *stride, uint32_t box1, uint32_t box2) {
+    EncodeTiled enc = encoder();
+    if (!enc) return false;
+    const cuuint64_t gdim[4] = {(cuuint64_t)D, dim[0], dim[1], rank > 3 ? dim[2] : 1};
+    const cuuint64_t gstride[3] = {stride[0], stride[1], rank > 3 ? stride[2] : 16};
+    const cuuint32_t box[4] = {64u, box1, box2, 1u}, one[4] = {1u, 1u, 1u, 1u};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, rank, const_cast<void *>(base), gdim, gstride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool rows_map(CUtensorMap *m, const WinRows &r, int heads, int tokens, int D, uint32_t box_heads, uint32_t box_tokens) {
+    const uint64_t dim[2] = {(uint64_t)heads, (uint64_t)tokens}, st[2] = {(uint64_t)r.hs, (uint64_t)r.ts};
+    return make_map(m, r.p, 3, D, dim, st, box_heads, box_tokens);
+}
+
+template <typename T, int D>
+cudaError_t launch(const WindowParams &w, cudaStream_t s) {
+    UmmaParams p;
+    p.w = w;
+    p.gb = w.g < TM ? w.g : TM;
+    p.tpt = TM / p.gb;
+    p.hblocks = (w.g + p.gb - 1) / p.gb;
+    CUtensorMap mq, mk, mv, mkc, mvc;
+    if (!rows_map(&mq, w.q, w.hq, w.tokens, D, p.gb, p.tpt) || !rows_map(&mk, w.k, w.hk, w.tokens, D, 1, TN) || !rows_map(&mv, w.v, w.hk, w.tokens, D, 1, TN))
+        return cudaErrorNotSupported;
+    mkc = mk; mvc = mv;
+    if (w.kc) {
+        const uint64_t dim[3] = {(uint64_t)w.sinks + w.window, (uint64_t)w.hk, (uint64_t)w.sequences};
+        const uint64_t st[3] = {(uint64_t)w.cls, (uint64_t)w.chs, (uint64_t)w.css};
+        if (!make_map(&mkc, w.kc, 4, D, dim, st, TN, 1) || !make_map(&mvc, w.vc, 4, D, dim, st, TN, 1)) return cudaErrorNotSupported;
+    }
+    auto kern = sh_window_prefill_umma_kernel<T, D>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM);
+    int dev = 0, sms = 0;
+    if (e == cudaSuccess) e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    // each sequence adds at most one partly filled item
+    const long long items = ((long long)w.tokens / (2 * p.tpt) + w.sequences) * w.hk * p.hblocks;
+    kern<<<(unsigned)(items < sms ? items : sms), NTH, Cfg<D>::SMEM, s>>>(p, mq, mk, mv, mkc, mvc);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int D, cudaStream_t s) {
+    if (dtype == SH_F16) return D == 128 ? launch<__half, 128>(p, s) : launch<__half, 64>(p, s);
+    return D == 128 ? launch<__nv_bfloat16, 128>(p, s) : launch<__nv_bfloat16, 64>(p, s);
+}
+
+cudaError_t sh_window_error_take(int *code, cudaStream_t s) {
+    cudaError_t e = cudaMemcpyFromSymbolAsync(code, g_window_error, sizeof(int), 0, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e != cudaSuccess || *code == 0) return e;
+    static const int zero = 0;
+    e = cudaMemcpyToSymbolAsync(g_window_error, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, s);
+    return e == cudaSuccess ? cudaStreamSynchronize(s) : e;
+}

@@ -387,6 +387,12 @@ def test_prepared_rows_feed_the_budgeted_cache():
     ref.check(got1, want[n:], tol[n:])
 
 
+@pytest.fixture(autouse=True)
+def _no_wait_gave_up():
+    yield
+    _sh().window_status()
+
+
 def test_graphs_streams_and_calls_at_once():
     """Captured calls replay on new inputs; two graphs and an eager call run at once on three streams with the same results."""
     sh, gen, dt = _sh(), _gen(33), torch.bfloat16
