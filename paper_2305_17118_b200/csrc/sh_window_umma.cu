@@ -39,7 +39,8 @@ using namespace shwin;
 
 constexpr int TM = 128, TN = 128;          // rows of a query tile, keys of a key tile
 constexpr int HALF = 128 * 128;            // bytes of 128 rows x 64 elements
-constexpr int NTH = 320;
+constexpr int NTH = 384;                  // warps 10 and 11 only make the last warpgroup whole for setmaxnreg
+constexpr int REGS_SOFTMAX = 216, REGS_OTHER = 72;      // 256 * 216 + 128 * 72 = 384 * 168, what the CTA is launched with
 constexpr float RENEW = 8.f;               // log2 growth of the maximum at which O is rescaled
 
 __device__ int g_window_error;             // code of the first bounded wait that gave up
@@ -58,10 +59,12 @@ struct Bars {
     uint64_t q_full[2], q_empty[2];        // a query tile landed / its last S has been computed
     uint64_t full[8], empty[8];            // stages: landed / read by the MMAs
     uint64_t s_full[2], p_ready[2], pv_done[2];
+    uint32_t flags[8];                     // what the step whose keys lie in a stage asks for
     uint32_t tmem;
     int abort_flag;
 };
 static_assert(sizeof(Bars) <= 256, "barrier block");
+enum { STEP_NEED0 = 1, STEP_NEED1 = 2, STEP_FIRST = 4, STEP_LAST = 8, STEP_END = 16 };      // NEED: the query tile sees keys of this step
 
 struct UmmaParams {
     WindowParams w;
@@ -99,6 +102,14 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r) {
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
         "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
         "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
         : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -287,7 +298,7 @@ template <> struct Fmt<__nv_bfloat16> { static constexpr int CODE = 1; static co
 
 template <typename T, int D>
 __global__ void __launch_bounds__(NTH, 1)
-sh_window_prefill_umma_kernel(const UmmaParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                               const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_kc,
                               const __grid_constant__ CUtensorMap map_vc) {
     using C = Cfg<D>;
@@ -321,158 +332,144 @@ sh_window_prefill_umma_kernel(const UmmaParams p, const __grid_constant__ CUtens
     const uint32_t tbase = bars->tmem;
     bool ok = !aborted();
 
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
     if (warp == 8) {
         // ------------------------------------------------------------------------------------------------ MMAs
-        // (the whole warp walks and waits, one lane issues)
+        // Steps (key tiles of an item) come in the order of their loads; what they ask for stands in flags[stage of the keys].
+        // The whole warp waits, one lane issues.
         const uint32_t idesc_s = instr_desc(Fmt<T>::CODE, 0, TM, TN), idesc_pv = instr_desc(Fmt<T>::CODE, 0, TM, D) | (1u << 16);
-        const uint32_t q_addr = smem_u32(sm), kv_addr = smem_u32(kv);
-        long long id = blockIdx.x;
-        Item cur = find_item(p, id), nxt = cur;       // items of the present step and of the step whose S comes next
-        int ci = -1, ni = cur.seq >= 0 ? cur.next(-1) : -1;
-        bool new_item = true;                         // the step (nxt, ni) is the first of its item
-        uint32_t n_items = 0, n_step = 0;             // items begun by S; steps begun by S
-        uint32_t cnt_p[2] = {0, 0};
-        bool started[2] = {false, false};
-        // S of tile t for the step (nxt, ni)
-        auto issue_s = [&](int t) {
-            if (!nxt.need(t, ni)) return;
+        const uint64_t q_desc = desc_sw128(smem_u32(sm), 16, 1024), k_desc = desc_sw128(smem_u32(kv), 16, 1024),
+                       v_desc = desc_sw128(smem_u32(kv), HALF, 1024);
+        uint32_t ks = 0, kpar = 0;                    // stage and parity of the keys of the step whose S comes next; its values follow
+        uint32_t items = 0, cnt0 = 0, cnt1 = 0;
+        uint32_t now = 0, nxt = 0;                    // flags of the present step and of the one whose S comes next
+        bool begun0 = false, begun1 = false;          // O of a query tile holds products of this item
+        auto stage_after = [](uint32_t st) { return st + 1 == C::STAGES ? 0u : st + 1; };
+        auto operands = [&]() {                       // wait for the next step's keys, and for the queries if it is its item's first
+            ok = ok && mbar_wait(&bars->full[ks], kpar, err, 0x603);
+            nxt = ok ? *(volatile uint32_t *)&bars->flags[ks] : (uint32_t)STEP_END;
+            if (nxt & STEP_FIRST) {
+                ok = ok && mbar_wait(&bars->q_full[0], items & 1, err, 0x601) && mbar_wait(&bars->q_full[1], items & 1, err, 0x602);
+                ++items;
+            }
+            ok = ok && !aborted();
+            if (!ok) nxt = STEP_END;
             tc_fence_after();
-            const uint32_t st = (2 * n_step) % C::STAGES, kb = kv_addr + st * C::TILE, qb = q_addr + t * C::TILE;
-            if (lane == 0) {
+        };
+        auto issue_s = [&](int t) {
+            if (lane == 0 && (nxt & (STEP_NEED0 << t))) {
+                const uint64_t qd = q_desc + (uint64_t)(t * (C::TILE >> 4)), kd = k_desc + (uint64_t)(ks * (C::TILE >> 4));
 #pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks)
-                    umma_f16(tbase + t * TN, desc_sw128(qb + (ks >> 2) * HALF + (ks & 3) * 32, 16, 1024),
-                             desc_sw128(kb + (ks >> 2) * HALF + (ks & 3) * 32, 16, 1024), idesc_s, ks > 0);
+                for (int x = 0; x < D / 16; ++x)
+                    umma_f16(tbase + t * TN, qd + ((x >> 2) * HALF + (x & 3) * 32) / 16, kd + ((x >> 2) * HALF + (x & 3) * 32) / 16, idesc_s, x > 0);
                 umma_commit(&bars->s_full[t]);
             }
         };
-        auto wait_s = [&]() {      // operands of the step (nxt, ni)
-            if (new_item) {
-                ok = ok && mbar_wait(&bars->q_full[0], n_items & 1, err, 0x601);
-                if (nxt.has(1)) ok = ok && mbar_wait(&bars->q_full[1], n_items & 1, err, 0x602);
-            }
-            const uint32_t u = 2 * n_step;
-            ok = ok && mbar_wait(&bars->full[u % C::STAGES], (u / C::STAGES) & 1, err, 0x603);
-            ok = ok && !aborted();
-        };
-        // after both tiles' S of a step: release the keys, and the queries behind the item's last step; move on
-        auto advance_s = [&]() {
-            const int after = nxt.next(ni);
-            if (lane == 0) {
-                umma_commit(&bars->empty[(2 * n_step) % C::STAGES]);
-                if (after < 0) { umma_commit(&bars->q_empty[0]); umma_commit(&bars->q_empty[1]); }
-            }
-            ++n_step;
-            new_item = after < 0;
-            if (after < 0) {
-                ++n_items;
-                id += gridDim.x;
-                nxt = find_item(p, id);
-                ni = nxt.seq >= 0 ? nxt.next(-1) : -1;
-            } else {
-                ni = after;
-            }
-        };
-        if (ni >= 0) {
-            wait_s();
-            if (ok) { issue_s(0); issue_s(1); }
-        }
-        while (ok && ni >= 0) {
-            cur = nxt; ci = ni;
-            const uint32_t n = n_step;
-            const bool fresh = new_item;
-            advance_s();                              // (nxt, ni): the step whose S comes next
-            const uint32_t u = 2 * n + 1, vs = u % C::STAGES, vb = kv_addr + vs * C::TILE;
-            const bool more = ni >= 0;
-            if (fresh) started[0] = started[1] = false;
+        auto issue_pv = [&](int t, uint32_t &cnt, bool &begun, uint32_t vs, uint32_t vpar) {
+            if (!(now & (STEP_NEED0 << t))) return;
+            ok = ok && mbar_wait(&bars->p_ready[t], cnt & 1, err, 0x604) && mbar_wait(&bars->full[vs], vpar, err, 0x605) && !aborted();
+            ++cnt;
+            tc_fence_after();
+            if (ok && lane == 0) {
+                const uint64_t vd = v_desc + (uint64_t)(vs * (C::TILE >> 4));
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                if (cur.need(t, ci)) {
-                    ok = ok && mbar_wait(&bars->p_ready[t], cnt_p[t] & 1, err, 0x604);
-                    ++cnt_p[t];
-                    ok = ok && mbar_wait(&bars->full[vs], (u / C::STAGES) & 1, err, 0x605);
-                    ok = ok && !aborted();
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (lane == 0) {
-#pragma unroll
-                        for (int ks = 0; ks < TN / 16; ++ks)
-                            umma_ts(tbase + C::O_COL + t * D, tbase + t * TN + ks * 8, desc_sw128(vb + ks * 2048, HALF, 1024), idesc_pv,
-                                    started[t] || ks > 0);      // (the first product of a query tile in its item overwrites O)
-                        umma_commit(&bars->pv_done[t]);
-                    }
-                    started[t] = true;
-                }
-                // within an item S of the next step follows at once; the next item's waits for its queries, behind both products
-                if (t == 1 && lane == 0) umma_commit(&bars->empty[vs]);
-                if (more && (!new_item || t == 1)) {
-                    if (t == 0 || new_item) wait_s();
-                    if (!ok) break;
-                    if (new_item) { issue_s(0); issue_s(1); } else issue_s(t);
-                }
+                for (int x = 0; x < TN / 16; ++x)     // (the first product of a query tile in its item overwrites O)
+                    umma_ts(tbase + C::O_COL + t * D, tbase + t * TN + x * 8, vd + x * 128, idesc_pv, begun || x > 0);
+                umma_commit(&bars->pv_done[t]);
             }
+            begun = true;
+        };
+        if (ok) operands();
+        if (ok) { issue_s(0); issue_s(1); }
+        while (ok && !(nxt & STEP_END)) {
+            now = nxt;
+            if (now & STEP_FIRST) begun0 = begun1 = false;
+            const uint32_t vs = stage_after(ks), vpar = vs == 0 ? kpar ^ 1 : kpar;
+            if (lane == 0) {                          // both S of the step are issued: its keys go back, and the queries behind the last step
+                umma_commit(&bars->empty[ks]);
+                if (now & STEP_LAST) { umma_commit(&bars->q_empty[0]); umma_commit(&bars->q_empty[1]); }
+            }
+            ks = stage_after(vs);
+            kpar = ks == 0 ? vpar ^ 1 : vpar;
+            issue_pv(0, cnt0, begun0, vs, vpar);
+            // within an item S of the next step goes between the products; the next item's waits for its queries, behind both
+            if (!(now & STEP_LAST)) { operands(); issue_s(0); }
+            issue_pv(1, cnt1, begun1, vs, vpar);
+            if (lane == 0) umma_commit(&bars->empty[vs]);
+            if (now & STEP_LAST) { operands(); issue_s(0); }
+            issue_s(1);
         }
         if (!ok) *(volatile int *)&bars->abort_flag = 1;
     } else if (warp == 9) {
         // ------------------------------------------------------------------------------------------------ loads
-        uint32_t n = 0, items = 0;
-        const int rows = p.tpt * p.gb;
-        auto request = [&](bool value, const Item &w, int i) {
-            const uint32_t st = n % C::STAGES;
-            if (n >= C::STAGES) ok = ok && mbar_wait(&bars->empty[st], (n / C::STAGES - 1) & 1, err, 0x612);
+        uint32_t n = 0, items = 0;                    // loads requested, items begun
+        uint32_t st = 0, par = 1;                     // the next stage, and the parity of its last release (the first pass: none)
+        const int q_bytes = D / 64 * p.tpt * p.gb * 128;
+        auto room = [&]() {
+            ok = ok && (n < C::STAGES || mbar_wait(&bars->empty[st], par, err, 0x612));
             ok = ok && !aborted();
-            if (!ok) return;
-            if (lane == 0) {
-                unsigned char *dst = kv + st * C::TILE;
-                mbar_arrive_expect_tx(&bars->full[st], C::TILE);
-#pragma unroll
-                for (int h = 0; h < D / 64; ++h) {
-                    if (i < w.ctiles) tma_4d(dst + h * HALF, value ? &map_vc : &map_kc, h * 64, i * TN, w.kvh, w.seq, &bars->full[st]);
-                    else tma_3d(dst + h * HALF, value ? &map_v : &map_k, h * 64, w.kvh, w.first + (i - w.ctiles) * TN, &bars->full[st]);
-                }
-            }
+            return ok;
+        };
+        auto stage_done = [&]() {
             ++n;
+            if (++st == C::STAGES) { st = 0; par ^= 1; }
+        };
+        auto queries = [&](const Item &w, int t) {
+            ok = ok && (items == 0 || mbar_wait(&bars->q_empty[t], (items - 1) & 1, err, 0x611));
+            ok = ok && !aborted();
+            if (!ok || lane != 0) return;
+            if (!w.has(t)) { mbar_arrive(&bars->q_full[t]); return; }
+            mbar_arrive_expect_tx(&bars->q_full[t], q_bytes);
+#pragma unroll
+            for (int h = 0; h < D / 64; ++h)
+                tma_3d(sm + t * C::TILE + h * HALF, &map_q, h * 64, w.kvh * p.w.g + w.hb * p.gb, w.first + w.from(t), &bars->q_full[t]);
         };
         for (long long id = blockIdx.x; ok; id += gridDim.x) {
             const Item w = find_item(p, id);
             if (w.seq < 0) break;
-            bool queries = false;
-            for (int i = w.next(-1); i >= 0 && ok; i = w.next(i)) {
-                if (!queries) {
-                    queries = true;
-                    for (int t = 0; t < 2; ++t) {
-                        if (items > 0) ok = ok && mbar_wait(&bars->q_empty[t], (items - 1) & 1, err, 0x611);
-                        ok = ok && !aborted();
-                        if (!ok) break;
-                        if (lane == 0) {
-                            if (w.has(t)) {
-                                mbar_arrive_expect_tx(&bars->q_full[t], D / 64 * rows * 128);
+            uint32_t flags = STEP_FIRST;
+            for (int i = w.next(-1); i >= 0 && ok;) {
+                const int after = w.next(i);
+                flags |= (w.need(0, i) ? STEP_NEED0 : 0) | (w.need(1, i) ? STEP_NEED1 : 0) | (after < 0 ? STEP_LAST : 0);
+                if (flags & STEP_FIRST) queries(w, 0);
+#pragma unroll 1
+                for (int value = 0; value < 2; ++value) {
+                    if (!room()) break;
+                    if (lane == 0) {
+                        unsigned char *dst = kv + st * C::TILE;
+                        uint64_t *full = &bars->full[st];
+                        bars->flags[st] = flags;      // (of the key stage is read; published by the arrival)
+                        mbar_arrive_expect_tx(full, C::TILE);
 #pragma unroll
-                                for (int h = 0; h < D / 64; ++h)
-                                    tma_3d(sm + t * C::TILE + h * HALF, &map_q, h * 64, w.kvh * p.w.g + w.hb * p.gb, w.first + w.from(t), &bars->q_full[t]);
-                            } else {
-                                mbar_arrive(&bars->q_full[t]);
-                            }
+                        for (int h = 0; h < D / 64; ++h) {
+                            if (i < w.ctiles) tma_4d(dst + h * HALF, value ? &map_vc : &map_kc, h * 64, i * TN, w.kvh, w.seq, full);
+                            else tma_3d(dst + h * HALF, value ? &map_v : &map_k, h * 64, w.kvh, w.first + (i - w.ctiles) * TN, full);
                         }
-                        if (t == 0) request(false, w, i);
                     }
-                    if (ok) request(true, w, i);
-                } else {
-                    request(false, w, i);
-                    if (ok) request(true, w, i);
+                    stage_done();
+                    if ((flags & STEP_FIRST) && !value) { queries(w, 1); ++items; }
                 }
+                flags = 0;
+                i = after;
             }
-            ++items;
+        }
+        const uint32_t behind = room() ? C::STAGES - 1 : C::STAGES;      // loads that may not have been waited for
+        if (ok && lane == 0) {                        // the end: a stage without a load
+            bars->flags[st] = STEP_END;
+            mbar_arrive(&bars->full[st]);
         }
         if (!ok) *(volatile int *)&bars->abort_flag = 1;
         // let the copies requested last land before the CTA goes away (a phase that is past reads as complete)
         if (lane == 0) {
             if (items > 0)
                 for (int t = 0; t < 2; ++t) mbar_wait(&bars->q_full[t], (items - 1) & 1, nullptr, 0);
-            for (uint32_t k = 0; k < C::STAGES && k < n; ++k) mbar_wait(&bars->full[(n - 1 - k) % C::STAGES], ((n - 1 - k) / C::STAGES) & 1, nullptr, 0);
+            for (uint32_t k = 0; k < behind && k < n; ++k) mbar_wait(&bars->full[(n - 1 - k) % C::STAGES], ((n - 1 - k) / C::STAGES) & 1, nullptr, 0);
         }
         __syncwarp();
-    } else if (warp < 8) {
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
         // ------------------------------------------------------------------------------------------------ softmax
         const int t = warp >> 2, row = tid & 127;
         const uint32_t lanes = tbase + ((uint32_t)((warp & 3) * 32) << 16), s_addr = lanes + t * TN, o_addr = lanes + C::O_COL + t * D;
@@ -534,18 +531,20 @@ sh_window_prefill_umma_kernel(const UmmaParams p, const __grid_constant__ CUtens
                 const float base = m == -CUDART_INF_F ? 0.f : m * c - Fmt<T>::LIFT;
                 const uint64_t c2 = f2(c, c), b2 = f2(-base, -base);
                 uint64_t sum0 = f2(0.f, 0.f), sum1 = sum0;
-                uint32_t pk[TN / 2];
 #pragma unroll
-                for (int k = 0; k < TN; k += 2) {
-                    float x, y;
-                    un2(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, b2), x, y);
-                    x = ex2_approx(x);
-                    y = ex2_approx(y);
-                    if (k & 2) sum1 = add2(sum1, f2(x, y)); else sum0 = add2(sum0, f2(x, y));
-                    pk[k / 2] = shelem::Vec<T>::pack2(x, y);
+                for (int b = 0; b < 4; ++b) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int k = 0; k < 32; k += 2) {
+                        float x, y;
+                        un2(fma2(f2(__uint_as_float(s[b * 32 + k]), __uint_as_float(s[b * 32 + k + 1])), c2, b2), x, y);
+                        x = ex2_approx(x);
+                        y = ex2_approx(y);
+                        if (k & 2) sum1 = add2(sum1, f2(x, y)); else sum0 = add2(sum0, f2(x, y));
+                        pk[k / 2] = shelem::Vec<T>::pack2(x, y);
+                    }
+                    tmem_st16(s_addr + b * 16, pk);
                 }
-                tmem_st32(s_addr, pk);
-                tmem_st32(s_addr + 32, pk + 32);
                 float x, y;
                 un2(add2(sum0, sum1), x, y);
                 l += x + y;
