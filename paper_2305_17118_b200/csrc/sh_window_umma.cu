@@ -45,26 +45,42 @@ constexpr float RENEW = 8.f;               // log2 growth of the maximum at whic
 
 __device__ int g_window_error;             // code of the first bounded wait that gave up
 
+constexpr int STEPS = 8, BAR_BYTES = 768; // steps in flight between the load warp and the others; barriers and step ring
+
 template <int D> struct Cfg {
     static constexpr int TILE = D / 64 * HALF;         // bytes of a query, key or value tile
     static constexpr int STAGES = D == 128 ? 5 : 8;    // key and value tiles in flight
     static constexpr int OFF_KV = 2 * TILE;
     static constexpr int OFF_BAR = OFF_KV + STAGES * TILE;
-    static constexpr int SMEM = OFF_BAR + 256;
+    static constexpr int SMEM = OFF_BAR + BAR_BYTES;
     static constexpr int O_COL = 2 * TN;               // tensor memory: S0, S1 (P inside), O0, O1
     static_assert(SMEM <= 232448 && O_COL + 2 * D <= 512, "");
 };
 
+// A step is one key tile of one item.  The warp that requests the loads works out what it asks for and who sees what, and hands
+// that to the MMA warp and the softmax warps through a ring.
+enum {
+    STEP_NEED0 = 1, STEP_NEED1 = 2,        // the query tile sees keys of this step
+    STEP_WHOLE0 = 4, STEP_WHOLE1 = 8,      // every row of the query tile sees every key
+    STEP_CACHE = 16, STEP_FIRST = 32, STEP_LAST = 64, STEP_END = 128
+};
+struct __align__(16) Step {
+    int flags, x;                          // first slot of the tile, or its first row in the chunk
+    int first, count;                      // the sequence's rows of the chunk tensors
+    int cached, a, kvh, hb;                // as in Item
+    int head, ring2;                       // end of the slots [sinks, head), end of the slots [head, ring2)
+    int pad[2];
+};
 struct Bars {
     uint64_t q_full[2], q_empty[2];        // a query tile landed / its last S has been computed
     uint64_t full[8], empty[8];            // stages: landed / read by the MMAs
     uint64_t s_full[2], p_ready[2], pv_done[2];
-    uint32_t flags[8];                     // what the step whose keys lie in a stage asks for
+    uint64_t step_full[STEPS], step_empty[STEPS];
+    Step steps[STEPS];
     uint32_t tmem;
     int abort_flag;
 };
-static_assert(sizeof(Bars) <= 256, "barrier block");
-enum { STEP_NEED0 = 1, STEP_NEED1 = 2, STEP_FIRST = 4, STEP_LAST = 8, STEP_END = 16 };      // NEED: the query tile sees keys of this step
+static_assert(sizeof(Bars) <= BAR_BYTES, "barrier block");
 
 struct UmmaParams {
     WindowParams w;
@@ -138,6 +154,7 @@ struct Item {
     int live, head, ctiles, jlo, jhi, tpt, sinks, window;
     bool wrapped;
 
+    __device__ __forceinline__ int ring2() const { return wrapped ? sinks + window : 0; }
     __device__ __forceinline__ int from(int t) const { return a + t * tpt; }
     __device__ __forceinline__ bool has(int t) const { return from(t) < count; }
     __device__ __forceinline__ int last(int t) const { return min(from(t) + tpt, count) - 1; }
@@ -155,6 +172,18 @@ struct Item {
         }
         const int j = (i - ctiles) * TN;
         return j <= last(t) && (cached + j + TN - 1 >= oldest || cached + j < sinks);
+    }
+    // does every row of query tile t see every key of tile i?  (a tile over several runs of slots counts as no)
+    __device__ __forceinline__ bool whole(int t, int i) const {
+        const int newest = cached + last(t) - window + 1;      // the last row's window starts here
+        if (i < ctiles) {
+            const int x = i * TN, y = x + TN;
+            if (y <= min(sinks, cached)) return true;
+            if (x >= sinks && y <= head) return cached - head + x >= newest;
+            return wrapped && x >= head && y <= sinks + window && cached - window + x - head >= newest;
+        }
+        const int j = (i - ctiles) * TN;
+        return j + TN - 1 <= from(t) && (cached + j >= newest || cached + j + TN <= sinks);
     }
     __device__ __forceinline__ int next(int i) const {         // -1: no further tile
         for (++i; i < ctiles; ++i)
@@ -207,21 +236,19 @@ __device__ __forceinline__ Item find_item(const UmmaParams &p, long long id) {
     return r;
 }
 
-// Columns of tile i that the query at chunk index qi sees: up to three runs [lo, hi) counted from the tile's first key.
+// Keys of a tile that the query at chunk index qi sees: up to three runs [lo, hi) counted from the tile's first key.
 struct Runs {
     int lo[3], hi[3];
 };
-__device__ __forceinline__ Runs visible_runs(const Item &w, int i, int qi) {
+__device__ __forceinline__ Runs visible_runs(bool in_cache, int x, int cached, int head, int ring2, int sinks, int window, int qi) {
     Runs r;
-    if (i < w.ctiles) {
-        const int x = i * TN, d = w.head - w.cached;
-        r.lo[0] = -x; r.hi[0] = min(w.sinks, w.cached) - x;
-        r.lo[1] = max(w.sinks, w.cached + qi - w.window + d + 1) - x; r.hi[1] = w.head - x;
-        r.lo[2] = w.cached + qi + d + 1 - x; r.hi[2] = (w.wrapped ? w.sinks + w.window : 0) - x;
+    if (in_cache) {
+        r.lo[0] = 0; r.hi[0] = min(sinks, cached) - x;
+        r.lo[1] = max(sinks, head + qi - window + 1) - x; r.hi[1] = head - x;
+        r.lo[2] = head + qi + 1 - x; r.hi[2] = ring2 - x;
     } else {
-        const int j = (i - w.ctiles) * TN;
-        r.lo[0] = -j; r.hi[0] = min(w.sinks - w.cached, qi + 1) - j;
-        r.lo[1] = max(0, qi - w.window + 1) - j; r.hi[1] = qi + 1 - j;
+        r.lo[0] = 0; r.hi[0] = min(sinks - cached, qi + 1) - x;
+        r.lo[1] = max(0, qi - window + 1) - x; r.hi[1] = qi + 1 - x;
         r.lo[2] = 0; r.hi[2] = 0;
     }
     return r;
@@ -233,10 +260,6 @@ __device__ __forceinline__ uint32_t run_bits(const Runs &r, int base) {
     for (int k = 0; k < 3; ++k) m |= low_bits(r.hi[k] - base) & ~low_bits(r.lo[k] - base);
     return m;
 }
-__device__ __forceinline__ bool covers(const Runs &r) {      // one run holds the whole tile
-    return (r.lo[0] <= 0 && r.hi[0] >= TN) || (r.lo[1] <= 0 && r.hi[1] >= TN) || (r.lo[2] <= 0 && r.hi[2] >= TN);
-}
-
 __device__ __forceinline__ uint64_t f2(float a, float b) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
@@ -266,9 +289,9 @@ __device__ __noinline__ void slow_row(const UmmaParams &u, long long id, int qi,
 #pragma unroll
     for (int e = 0; e < E; ++e) { q[e] = (float)qr[e] * p.scale_log2e; o[e] = 0.f; }
     for (int i = w.next(-1); i >= 0; i = w.next(i)) {
-        const Runs runs = visible_runs(w, i, qi);
         const bool in_cache = i < w.ctiles;
         const int base = (in_cache ? i : i - w.ctiles) * TN;
+        const Runs runs = visible_runs(in_cache, base, w.cached, w.head, w.ring2(), w.sinks, w.window, qi);
         for (int c = 0; c < TN; ++c) {
             if (!((run_bits(runs, c & ~31) >> (c & 31)) & 1u)) continue;
             const long long ko = in_cache ? w.seq * p.css + w.kvh * p.chs + (long long)(base + c) * p.cls : (long long)(w.first + base + c) * p.k.ts + w.kvh * p.k.hs;
@@ -319,6 +342,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             mbar_init(&bars->s_full[t], 1); mbar_init(&bars->p_ready[t], 128); mbar_init(&bars->pv_done[t], 1);
         }
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
+        for (int s = 0; s < STEPS; ++s) { mbar_init(&bars->step_full[s], 1); mbar_init(&bars->step_empty[s], 8); }
         bars->abort_flag = 0;
         if ((smem_u32(sm) & 1023u) != 0) {      // the swizzled tiles need the alignment the declaration asks for
             atomicCAS(err, 0, 0x620);
@@ -336,19 +360,21 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
     if (warp == 8) {
         // ------------------------------------------------------------------------------------------------ MMAs
-        // Steps (key tiles of an item) come in the order of their loads; what they ask for stands in flags[stage of the keys].
-        // The whole warp waits, one lane issues.
+        // Steps come in the order of their loads (their entries of the ring are published with them, and not written again
+        // before this warp has released later stages).  The whole warp waits, one lane issues.
         const uint32_t idesc_s = instr_desc(Fmt<T>::CODE, 0, TM, TN), idesc_pv = instr_desc(Fmt<T>::CODE, 0, TM, D) | (1u << 16);
+        // descriptors: the high word is the same for all operands of a kind, the low word holds address / 16 in its low bits
         const uint64_t q_desc = desc_sw128(smem_u32(sm), 16, 1024), k_desc = desc_sw128(smem_u32(kv), 16, 1024),
                        v_desc = desc_sw128(smem_u32(kv), HALF, 1024);
+        auto plus = [](uint64_t d, uint32_t bytes) { return (d & 0xffffffff00000000ull) | (uint32_t)((uint32_t)d + (bytes >> 4)); };
         uint32_t ks = 0, kpar = 0;                    // stage and parity of the keys of the step whose S comes next; its values follow
-        uint32_t items = 0, cnt0 = 0, cnt1 = 0;
+        uint32_t items = 0, steps = 0, cnt0 = 0, cnt1 = 0;
         uint32_t now = 0, nxt = 0;                    // flags of the present step and of the one whose S comes next
         bool begun0 = false, begun1 = false;          // O of a query tile holds products of this item
         auto stage_after = [](uint32_t st) { return st + 1 == C::STAGES ? 0u : st + 1; };
         auto operands = [&]() {                       // wait for the next step's keys, and for the queries if it is its item's first
             ok = ok && mbar_wait(&bars->full[ks], kpar, err, 0x603);
-            nxt = ok ? *(volatile uint32_t *)&bars->flags[ks] : (uint32_t)STEP_END;
+            nxt = ok ? (uint32_t)*(volatile int *)&bars->steps[steps++ % STEPS].flags : (uint32_t)STEP_END;
             if (nxt & STEP_FIRST) {
                 ok = ok && mbar_wait(&bars->q_full[0], items & 1, err, 0x601) && mbar_wait(&bars->q_full[1], items & 1, err, 0x602);
                 ++items;
@@ -359,10 +385,10 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         };
         auto issue_s = [&](int t) {
             if (lane == 0 && (nxt & (STEP_NEED0 << t))) {
-                const uint64_t qd = q_desc + (uint64_t)(t * (C::TILE >> 4)), kd = k_desc + (uint64_t)(ks * (C::TILE >> 4));
+                const uint64_t qd = plus(q_desc, t * C::TILE), kd = plus(k_desc, ks * C::TILE);
 #pragma unroll
                 for (int x = 0; x < D / 16; ++x)
-                    umma_f16(tbase + t * TN, qd + ((x >> 2) * HALF + (x & 3) * 32) / 16, kd + ((x >> 2) * HALF + (x & 3) * 32) / 16, idesc_s, x > 0);
+                    umma_f16(tbase + t * TN, plus(qd, (x >> 2) * HALF + (x & 3) * 32), plus(kd, (x >> 2) * HALF + (x & 3) * 32), idesc_s, x > 0);
                 umma_commit(&bars->s_full[t]);
             }
         };
@@ -372,10 +398,10 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             ++cnt;
             tc_fence_after();
             if (ok && lane == 0) {
-                const uint64_t vd = v_desc + (uint64_t)(vs * (C::TILE >> 4));
+                const uint64_t vd = plus(v_desc, vs * C::TILE);
 #pragma unroll
                 for (int x = 0; x < TN / 16; ++x)     // (the first product of a query tile in its item overwrites O)
-                    umma_ts(tbase + C::O_COL + t * D, tbase + t * TN + x * 8, vd + x * 128, idesc_pv, begun || x > 0);
+                    umma_ts(tbase + C::O_COL + t * D, tbase + t * TN + x * 8, plus(vd, x * 2048), idesc_pv, begun || x > 0);
                 umma_commit(&bars->pv_done[t]);
             }
             begun = true;
@@ -403,7 +429,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         if (!ok) *(volatile int *)&bars->abort_flag = 1;
     } else if (warp == 9) {
         // ------------------------------------------------------------------------------------------------ loads
-        uint32_t n = 0, items = 0;                    // loads requested, items begun
+        uint32_t n = 0, items = 0, steps = 0;         // loads requested, items begun, steps published
         uint32_t st = 0, par = 1;                     // the next stage, and the parity of its last release (the first pass: none)
         const int q_bytes = D / 64 * p.tpt * p.gb * 128;
         auto room = [&]() {
@@ -414,6 +440,20 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         auto stage_done = [&]() {
             ++n;
             if (++st == C::STAGES) { st = 0; par ^= 1; }
+        };
+        auto publish = [&](const Item &w, int flags, int x) {
+            const uint32_t e = steps % STEPS;
+            ok = ok && (steps < STEPS || mbar_wait(&bars->step_empty[e], (steps / STEPS - 1) & 1, err, 0x613));
+            ok = ok && !aborted();
+            if (ok && lane == 0) {
+                Step &d = bars->steps[e];
+                d.flags = flags; d.x = x; d.first = w.first; d.count = w.count;
+                d.cached = w.cached; d.a = w.a; d.kvh = w.kvh; d.hb = w.hb;
+                d.head = w.head; d.ring2 = w.ring2();
+                mbar_arrive(&bars->step_full[e]);
+            }
+            ++steps;
+            return ok;
         };
         auto queries = [&](const Item &w, int t) {
             ok = ok && (items == 0 || mbar_wait(&bars->q_empty[t], (items - 1) & 1, err, 0x611));
@@ -428,35 +468,50 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         for (long long id = blockIdx.x; ok; id += gridDim.x) {
             const Item w = find_item(p, id);
             if (w.seq < 0) break;
-            uint32_t flags = STEP_FIRST;
-            for (int i = w.next(-1); i >= 0 && ok;) {
-                const int after = w.next(i);
-                flags |= (w.need(0, i) ? STEP_NEED0 : 0) | (w.need(1, i) ? STEP_NEED1 : 0) | (after < 0 ? STEP_LAST : 0);
-                if (flags & STEP_FIRST) queries(w, 0);
-#pragma unroll 1
-                for (int value = 0; value < 2; ++value) {
-                    if (!room()) break;
-                    if (lane == 0) {
-                        unsigned char *dst = kv + st * C::TILE;
-                        uint64_t *full = &bars->full[st];
-                        bars->flags[st] = flags;      // (of the key stage is read; published by the arrival)
-                        mbar_arrive_expect_tx(full, C::TILE);
+            bool first = true;
+            const int last_tile = w.ctiles + w.jhi;   // (the tile of the last row itself: always needed)
+            for (int base = 0; base <= last_tile && ok; base += 32) {
+                // 32 tiles at a time, a lane each; what lies between the sinks and the window is passed over
+                if (base >= w.ctiles && base - w.ctiles < w.jlo && w.cached + (base - w.ctiles) * TN >= w.sinks) base = w.ctiles + w.jlo;
+                const int i = base + lane;
+                const bool need0 = i <= last_tile && w.need(0, i), need1 = i <= last_tile && w.need(1, i);
+                const int mine = (need0 ? STEP_NEED0 : 0) | (need1 ? STEP_NEED1 : 0) | (need0 && w.whole(0, i) ? STEP_WHOLE0 : 0) |
+                                 (need1 && w.whole(1, i) ? STEP_WHOLE1 : 0) | (i < w.ctiles ? STEP_CACHE : 0) | (i == last_tile ? STEP_LAST : 0);
+                unsigned todo = __ballot_sync(0xffffffffu, need0 || need1);
+                while (todo && ok) {
+                    const int bit = __ffs(todo) - 1;
+                    todo &= todo - 1;
+                    const int flags = __shfl_sync(0xffffffffu, mine, bit) | (first ? STEP_FIRST : 0);
+                    const bool in_cache = flags & STEP_CACHE;
+                    const int x = (base + bit - (in_cache ? 0 : w.ctiles)) * TN;
+                    if (!publish(w, flags, x)) break;
+                    if (first) queries(w, 0);
 #pragma unroll
-                        for (int h = 0; h < D / 64; ++h) {
-                            if (i < w.ctiles) tma_4d(dst + h * HALF, value ? &map_vc : &map_kc, h * 64, i * TN, w.kvh, w.seq, full);
-                            else tma_3d(dst + h * HALF, value ? &map_v : &map_k, h * 64, w.kvh, w.first + (i - w.ctiles) * TN, full);
+                    for (int value = 0; value < 2; ++value) {
+                        if (!room()) break;
+                        if (lane == 0) {
+                            unsigned char *dst = kv + st * C::TILE;
+                            uint64_t *full = &bars->full[st];
+                            mbar_arrive_expect_tx(full, C::TILE);
+#pragma unroll
+                            for (int h = 0; h < D / 64; ++h) {
+                                if (in_cache) tma_4d(dst + h * HALF, value ? &map_vc : &map_kc, h * 64, x, w.kvh, w.seq, full);
+                                else tma_3d(dst + h * HALF, value ? &map_v : &map_k, h * 64, w.kvh, w.first + x, full);
+                            }
                         }
+                        stage_done();
+                        if (first && !value) { queries(w, 1); ++items; }
                     }
-                    stage_done();
-                    if ((flags & STEP_FIRST) && !value) { queries(w, 1); ++items; }
+                    first = false;
                 }
-                flags = 0;
-                i = after;
             }
         }
+        Item none;
+        none.first = none.count = none.cached = none.a = none.kvh = none.hb = none.head = 0;
+        none.wrapped = false;
+        if (ok) publish(none, STEP_END, 0);
         const uint32_t behind = room() ? C::STAGES - 1 : C::STAGES;      // loads that may not have been waited for
         if (ok && lane == 0) {                        // the end: a stage without a load
-            bars->flags[st] = STEP_END;
             mbar_arrive(&bars->full[st]);
         }
         if (!ok) *(volatile int *)&bars->abort_flag = 1;
@@ -475,19 +530,36 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         const uint32_t lanes = tbase + ((uint32_t)((warp & 3) * 32) << 16), s_addr = lanes + t * TN, o_addr = lanes + C::O_COL + t * D;
         const int tok = row / p.gb, hrow = row % p.gb;
         const float c = p.w.scale_log2e;
-        uint32_t cnt = 0;
-        for (long long id = blockIdx.x; ok; id += gridDim.x) {
-            const Item w = find_item(p, id);
-            if (w.seq < 0) break;
-            if (!w.has(t)) continue;
-            const int qi = w.from(t) + tok, h = w.hb * p.gb + hrow;
-            const bool live = tok < p.tpt && qi < w.count && h < p.w.g;
-            float m = -CUDART_INF_F, l = 0.f;
-            bool begun = false;
-            for (int i = w.next(-1); i >= 0; i = w.next(i)) {
-                if (!w.need(t, i)) continue;
-                const Runs runs = visible_runs(w, i, qi);
-                const bool whole = __all_sync(0xffffffffu, !live || covers(runs));
+        uint32_t cnt = 0, steps = 0;
+        long long id = (long long)blockIdx.x - gridDim.x;      // present item
+        int qi = 0, h = 0, kvh = 0, row0 = 0;
+        bool live = false, begun = false;
+        float m = -CUDART_INF_F, l = 0.f;
+        while (ok) {
+            const uint32_t e = steps % STEPS;
+            ok = mbar_wait(&bars->step_full[e], (steps / STEPS) & 1, err, 0x624);
+            if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
+            ++steps;
+            const Step &d = bars->steps[e];
+            const int flags = d.flags;
+            if (flags & STEP_END) break;
+            if (flags & STEP_FIRST) {
+                id += gridDim.x;
+                qi = d.a + t * p.tpt + tok;
+                h = d.hb * p.gb + hrow;
+                kvh = d.kvh;
+                row0 = d.first;
+                live = tok < p.tpt && qi < d.count && h < p.w.g;
+                begun = false;
+                m = -CUDART_INF_F;
+                l = 0.f;
+            }
+            const bool whole = flags & (STEP_WHOLE0 << t);
+            Runs runs;
+            if (!whole) runs = visible_runs(flags & STEP_CACHE, d.x, d.cached, d.head, d.ring2, p.w.sinks, p.w.window, qi);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->step_empty[e]);
+            if (flags & (STEP_NEED0 << t)) {
                 ok = mbar_wait(&bars->s_full[t], cnt & 1, err, 0x621);
                 if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
                 tc_fence_after();
@@ -503,10 +575,14 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                         for (int k = 0; k < 32; ++k) s[b * 32 + k] = (bits >> k) & 1u ? s[b * 32 + k] : 0xff800000u;      // -inf
                     }
                 }
-                float mx[4] = {m, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+                float mx[8];
 #pragma unroll
-                for (int k = 0; k < TN; ++k) mx[k & 3] = fmaxf(mx[k & 3], __uint_as_float(s[k]));
-                const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                for (int k = 0; k < 8; ++k) mx[k] = fmaxf(__uint_as_float(s[k]), __uint_as_float(s[k + 8]));
+#pragma unroll
+                for (int k = 16; k < TN; k += 16)
+#pragma unroll
+                    for (int c8 = 0; c8 < 8; ++c8) mx[c8] = fmaxf(fmaxf(mx[c8], __uint_as_float(s[k + c8])), __uint_as_float(s[k + 8 + c8]));
+                const float mn = fmaxf(fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))), m);
                 // renew the subtracted maximum when it has grown enough (or is the first): rescale O and l
                 const bool grown = live && (mn - m) * c > RENEW;      // (-inf - -inf: no)
                 if (__any_sync(0xffffffffu, grown)) {
@@ -554,12 +630,12 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 ++cnt;
                 begun = true;
             }
-            if (!ok) break;
+            if (!(flags & STEP_LAST) || !begun) continue;
             ok = mbar_wait(&bars->pv_done[t], (cnt - 1) & 1, err, 0x623);
             if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
             tc_fence_after();
             const float inv = 1.f / l;
-            char *dst = p.w.out.p + (long long)(w.first + qi) * p.w.out.ts + (long long)(w.kvh * p.w.g + h) * p.w.out.hs;
+            char *dst = p.w.out.p + (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs;
             bool odd = false;
 #pragma unroll
             for (int b = 0; b < D / 32; ++b) {
@@ -583,7 +659,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             while (again) {
                 const int l0 = __ffs(again) - 1;
                 again &= again - 1;
-                slow_row<T, D>(p, id, __shfl_sync(0xffffffffu, qi, l0), w.kvh * p.w.g + __shfl_sync(0xffffffffu, h, l0));
+                slow_row<T, D>(p, id, __shfl_sync(0xffffffffu, qi, l0), kvh * p.w.g + __shfl_sync(0xffffffffu, h, l0));
             }
         }
         if (!ok) *(volatile int *)&bars->abort_flag = 1;
