@@ -5,10 +5,10 @@
 // share a tile and the tile spans few tokens.  The keys come in tiles of 128: first the slots of the cache, then the chunk's own
 // rows; tiles that none of the item's rows can see are never loaded, tiles that a query tile does not see are not multiplied for it.
 //
-//   warps 0-3, 4-7   softmax of query tile 0 and 1: thread = row.  S from tensor memory, mask, exponentials, P (16 bits) back into
+//   warps 0-7, 8-15  softmax of query tile 0 and 1, two threads per row.  S from tensor memory, mask, exponentials, P (16 bits) back into
 //                    the columns of S, the rare rescaling of O, and the division and store at the end
-//   warp 8           issues the MMAs: S = Q.K^T (both operands in shared memory, K-major), O += P.V (P in tensor memory, V MN-major)
-//   warp 9           requests query, key and value tiles (tiled TMA copies, 128-byte swizzle; rows outside a tensor are zeros)
+//   warp 16          issues the MMAs: S = Q.K^T (both operands in shared memory, K-major), O += P.V (P in tensor memory, V MN-major)
+//   warp 17          requests query, key and value tiles (tiled TMA copies, 128-byte swizzle; rows outside a tensor are zeros)
 //
 // The tensor pipe takes the MMAs in the order PV0(n), S0(n+1), PV1(n), S1(n+1): one query tile's softmax runs while the other's
 // products do.  P overwrites S: S(n+1) of a query tile is issued behind PV(n) of the same tile, which reads P, and the pipe keeps
@@ -39,8 +39,13 @@ using namespace shwin;
 
 constexpr int TM = 128, TN = 128;          // rows of a query tile, keys of a key tile
 constexpr int HALF = 128 * 128;            // bytes of 128 rows x 64 elements
-constexpr int NTH = 384;                  // warps 10 and 11 only make the last warpgroup whole for setmaxnreg
-constexpr int REGS_SOFTMAX = 216, REGS_OTHER = 72;      // 256 * 216 + 128 * 72 = 384 * 168, what the CTA is launched with
+#ifndef SPLITS
+#define SPLITS 1
+#endif
+constexpr int SPLIT = SPLITS;              // threads that share a row
+constexpr int HN = TN / SPLIT;             // keys of a tile per softmax thread
+constexpr int SOFTMAX_WARPS = 8 * SPLIT, NTH = 32 * SOFTMAX_WARPS + 128;
+constexpr int REGS_SOFTMAX = SPLIT == 1 ? 216 : 104, REGS_OTHER = SPLIT == 1 ? 72 : 64;      // 512 * 104 + 128 * 64 = 640 * 96, what the CTA is launched with
 constexpr float RENEW = 8.f;               // log2 growth of the maximum at which O is rescaled
 
 __device__ int g_window_error;             // code of the first bounded wait that gave up
@@ -52,7 +57,8 @@ template <int D> struct Cfg {
     static constexpr int STAGES = D == 128 ? 5 : 8;    // key and value tiles in flight
     static constexpr int OFF_KV = 2 * TILE;
     static constexpr int OFF_BAR = OFF_KV + STAGES * TILE;
-    static constexpr int SMEM = OFF_BAR + BAR_BYTES;
+    static constexpr int OFF_STAT = OFF_BAR + BAR_BYTES;
+    static constexpr int SMEM = OFF_STAT + 2 * 2 * TM * 4;      // exchanged row values: [query tile][half][row]
     static constexpr int O_COL = 2 * TN;               // tensor memory: S0, S1 (P inside), O0, O1
     static_assert(SMEM <= 232448 && O_COL + 2 * D <= 512, "");
 };
@@ -108,17 +114,20 @@ __device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, uint32_t *r) {
           "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(taddr));
 }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r) {
+// Wait for this thread's tensor-memory loads; the values pass through the asm, so that no use of them moves before the wait.
+template <int N>
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[N]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+}
+__device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, uint32_t *r) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
-        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
-        "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
-        : "memory");
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
     asm volatile(
@@ -339,10 +348,10 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     if (tid == 0) {
         for (int t = 0; t < 2; ++t) {
             mbar_init(&bars->q_full[t], 1); mbar_init(&bars->q_empty[t], 1);
-            mbar_init(&bars->s_full[t], 1); mbar_init(&bars->p_ready[t], 128); mbar_init(&bars->pv_done[t], 1);
+            mbar_init(&bars->s_full[t], 1); mbar_init(&bars->p_ready[t], SPLIT * TM); mbar_init(&bars->pv_done[t], 1);
         }
-        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 1); }
-        for (int s = 0; s < STEPS; ++s) { mbar_init(&bars->step_full[s], 1); mbar_init(&bars->step_empty[s], 8); }
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 2); }
+        for (int s = 0; s < STEPS; ++s) { mbar_init(&bars->step_full[s], 1); mbar_init(&bars->step_empty[s], SOFTMAX_WARPS); }
         bars->abort_flag = 0;
         if ((smem_u32(sm) & 1023u) != 0) {      // the swizzled tiles need the alignment the declaration asks for
             atomicCAS(err, 0, 0x620);
@@ -356,78 +365,75 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     const uint32_t tbase = bars->tmem;
     bool ok = !aborted();
 
-    if (warp >= 8) {
+    if (warp >= SOFTMAX_WARPS) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
-    if (warp == 8) {
+    if (warp < SOFTMAX_WARPS + 2) {
         // ------------------------------------------------------------------------------------------------ MMAs
-        // Steps come in the order of their loads (their entries of the ring are published with them, and not written again
-        // before this warp has released later stages).  The whole warp waits, one lane issues.
+        // One warp per query tile.  Steps come in the order of their loads (their entries of the ring are published with them, and
+        // not written again before this warp has released later stages).  The whole warp waits, one lane issues.
+        const int t = warp - SOFTMAX_WARPS;
         const uint32_t idesc_s = instr_desc(Fmt<T>::CODE, 0, TM, TN), idesc_pv = instr_desc(Fmt<T>::CODE, 0, TM, D) | (1u << 16);
         // descriptors: the high word is the same for all operands of a kind, the low word holds address / 16 in its low bits
-        const uint64_t q_desc = desc_sw128(smem_u32(sm), 16, 1024), k_desc = desc_sw128(smem_u32(kv), 16, 1024),
+        const uint64_t q_desc = desc_sw128(smem_u32(sm) + t * C::TILE, 16, 1024), k_desc = desc_sw128(smem_u32(kv), 16, 1024),
                        v_desc = desc_sw128(smem_u32(kv), HALF, 1024);
         auto plus = [](uint64_t d, uint32_t bytes) { return (d & 0xffffffff00000000ull) | (uint32_t)((uint32_t)d + (bytes >> 4)); };
-        uint32_t ks = 0, kpar = 0;                    // stage and parity of the keys of the step whose S comes next; its values follow
-        uint32_t items = 0, steps = 0, cnt0 = 0, cnt1 = 0;
-        uint32_t now = 0, nxt = 0;                    // flags of the present step and of the one whose S comes next
-        bool begun0 = false, begun1 = false;          // O of a query tile holds products of this item
-        auto stage_after = [](uint32_t st) { return st + 1 == C::STAGES ? 0u : st + 1; };
-        auto operands = [&]() {                       // wait for the next step's keys, and for the queries if it is its item's first
-            ok = ok && mbar_wait(&bars->full[ks], kpar, err, 0x603);
-            nxt = ok ? (uint32_t)*(volatile int *)&bars->steps[steps++ % STEPS].flags : (uint32_t)STEP_END;
-            if (nxt & STEP_FIRST) {
-                ok = ok && mbar_wait(&bars->q_full[0], items & 1, err, 0x601) && mbar_wait(&bars->q_full[1], items & 1, err, 0x602);
-                ++items;
+        uint32_t st = 0, par = 0;                     // the next stage and its parity: keys and values of the steps in turn
+        uint32_t items = 0, steps = 0, cnt = 0;
+        int now = 0;                                  // what the present step asks for
+        bool begun = false;                           // O holds products of this item
+        auto stage_done = [&]() {
+            if (++st == C::STAGES) { st = 0; par ^= 1; }
+        };
+        // S of the next step, as soon as its keys (and, if it is the first of its item, the queries) are there
+        auto next_step = [&]() {
+            ok = ok && mbar_wait(&bars->full[st], par, err, 0x603);
+            now = ok ? *(volatile int *)&bars->steps[steps++ % STEPS].flags : (int)STEP_END;
+            if (now & STEP_END) return;
+            if (now & STEP_FIRST) {
+                ok = ok && mbar_wait(&bars->q_full[t], items++ & 1, err, 0x601);
+                begun = false;
             }
             ok = ok && !aborted();
-            if (!ok) nxt = STEP_END;
-            tc_fence_after();
-        };
-        auto issue_s = [&](int t) {
-            if (lane == 0 && (nxt & (STEP_NEED0 << t))) {
-                const uint64_t qd = plus(q_desc, t * C::TILE), kd = plus(k_desc, ks * C::TILE);
-#pragma unroll
-                for (int x = 0; x < D / 16; ++x)
-                    umma_f16(tbase + t * TN, plus(qd, (x >> 2) * HALF + (x & 3) * 32), plus(kd, (x >> 2) * HALF + (x & 3) * 32), idesc_s, x > 0);
-                umma_commit(&bars->s_full[t]);
-            }
-        };
-        auto issue_pv = [&](int t, uint32_t &cnt, bool &begun, uint32_t vs, uint32_t vpar) {
-            if (!(now & (STEP_NEED0 << t))) return;
-            ok = ok && mbar_wait(&bars->p_ready[t], cnt & 1, err, 0x604) && mbar_wait(&bars->full[vs], vpar, err, 0x605) && !aborted();
-            ++cnt;
             tc_fence_after();
             if (ok && lane == 0) {
-                const uint64_t vd = plus(v_desc, vs * C::TILE);
+                if (now & (STEP_NEED0 << t)) {
+                    const uint64_t kd = plus(k_desc, st * C::TILE);
 #pragma unroll
-                for (int x = 0; x < TN / 16; ++x)     // (the first product of a query tile in its item overwrites O)
-                    umma_ts(tbase + C::O_COL + t * D, tbase + t * TN + x * 8, plus(vd, x * 2048), idesc_pv, begun || x > 0);
-                umma_commit(&bars->pv_done[t]);
+                    for (int x = 0; x < D / 16; ++x)
+                        umma_f16(tbase + t * TN, plus(q_desc, (x >> 2) * HALF + (x & 3) * 32), plus(kd, (x >> 2) * HALF + (x & 3) * 32), idesc_s, x > 0);
+                    umma_commit(&bars->s_full[t]);
+                    umma_commit(&bars->empty[st]);
+                } else {
+                    mbar_arrive(&bars->empty[st]);
+                }
+                if (now & STEP_LAST) umma_commit(&bars->q_empty[t]);
             }
-            begun = true;
+            stage_done();
         };
-        if (ok) operands();
-        if (ok) { issue_s(0); issue_s(1); }
-        while (ok && !(nxt & STEP_END)) {
-            now = nxt;
-            if (now & STEP_FIRST) begun0 = begun1 = false;
-            const uint32_t vs = stage_after(ks), vpar = vs == 0 ? kpar ^ 1 : kpar;
-            if (lane == 0) {                          // both S of the step are issued: its keys go back, and the queries behind the last step
-                umma_commit(&bars->empty[ks]);
-                if (now & STEP_LAST) { umma_commit(&bars->q_empty[0]); umma_commit(&bars->q_empty[1]); }
+        next_step();
+        while (ok && !(now & STEP_END)) {
+            const bool need = now & (STEP_NEED0 << t);
+            if (need) ok = ok && mbar_wait(&bars->p_ready[t], cnt++ & 1, err, 0x604);
+            ok = ok && mbar_wait(&bars->full[st], par, err, 0x605) && !aborted();
+            tc_fence_after();
+            if (ok && lane == 0) {
+                if (need) {
+                    const uint64_t vd = plus(v_desc, st * C::TILE);
+#pragma unroll
+                    for (int x = 0; x < TN / 16; ++x)     // (the first product of an item overwrites O)
+                        umma_ts(tbase + C::O_COL + t * D, tbase + t * TN + x * 8, plus(vd, x * 2048), idesc_pv, begun || x > 0);
+                    umma_commit(&bars->pv_done[t]);
+                    umma_commit(&bars->empty[st]);
+                } else {
+                    mbar_arrive(&bars->empty[st]);
+                }
             }
-            ks = stage_after(vs);
-            kpar = ks == 0 ? vpar ^ 1 : vpar;
-            issue_pv(0, cnt0, begun0, vs, vpar);
-            // within an item S of the next step goes between the products; the next item's waits for its queries, behind both
-            if (!(now & STEP_LAST)) { operands(); issue_s(0); }
-            issue_pv(1, cnt1, begun1, vs, vpar);
-            if (lane == 0) umma_commit(&bars->empty[vs]);
-            if (now & STEP_LAST) { operands(); issue_s(0); }
-            issue_s(1);
+            begun = begun || need;
+            stage_done();
+            next_step();
         }
         if (!ok) *(volatile int *)&bars->abort_flag = 1;
-    } else if (warp == 9) {
+    } else if (warp == SOFTMAX_WARPS + 2) {
         // ------------------------------------------------------------------------------------------------ loads
         uint32_t n = 0, items = 0, steps = 0;         // loads requested, items begun, steps published
         uint32_t st = 0, par = 1;                     // the next stage, and the parity of its last release (the first pass: none)
@@ -526,11 +532,23 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
         // ------------------------------------------------------------------------------------------------ softmax
-        const int t = warp >> 2, row = tid & 127;
-        const uint32_t lanes = tbase + ((uint32_t)((warp & 3) * 32) << 16), s_addr = lanes + t * TN, o_addr = lanes + C::O_COL + t * D;
+        // two threads share a row: `half` 0 has keys 0 .. 63 of a tile and the first half of O's columns, 1 the others
+        const int t = warp / (4 * SPLIT), half = SPLIT == 2 ? (warp >> 2) & 1 : 0, row = tid & 127, pair = t * 4 + (warp & 3);
+        const uint32_t lanes = tbase + ((uint32_t)((warp & 3) * 32) << 16), s_addr = lanes + t * TN + half * HN,
+                       p_addr = lanes + t * TN + half * (HN / 2), o_addr = lanes + C::O_COL + t * D + half * (D / SPLIT);
         const int tok = row / p.gb, hrow = row % p.gb;
         const float c = p.w.scale_log2e;
+        float (*stat)[TM] = reinterpret_cast<float (*)[TM]>(sm + C::OFF_STAT) + t * 2;      // [half][row]
         uint32_t cnt = 0, steps = 0;
+        // this row's value from the thread with the other half.  One buffer is enough: between two exchanges of an item lies a
+        // wait that needs arrivals of all threads of the query tile, and behind the last one of an item a barrier.
+        auto other = [&](float mine) {
+            stat[half][row] = mine;
+            tc_fence_before();      // (also: the other half's columns of S have been read before P is written over them)
+            asm volatile("bar.sync %0, 64;" ::"r"(pair + 1) : "memory");
+            tc_fence_after();
+            return stat[half ^ 1][row];
+        };
         long long id = (long long)blockIdx.x - gridDim.x;      // present item
         int qi = 0, h = 0, kvh = 0, row0 = 0;
         bool live = false, begun = false;
@@ -561,16 +579,15 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             if (lane == 0) mbar_arrive(&bars->step_empty[e]);
             if (flags & (STEP_NEED0 << t)) {
                 ok = mbar_wait(&bars->s_full[t], cnt & 1, err, 0x621);
-                if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
                 tc_fence_after();
-                uint32_t s[TN];
+                uint32_t s[HN];
 #pragma unroll
-                for (int b = 0; b < 4; ++b) tmem_ld32_nowait(s_addr + b * 32, s + b * 32);
-                tmem_wait_ld();
+                for (int b = 0; b < HN / 32; ++b) tmem_ld32_nowait(s_addr + b * 32, s + b * 32);
+                tmem_wait_ld(s);
                 if (!whole) {
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const uint32_t bits = run_bits(runs, b * 32);
+                    for (int b = 0; b < HN / 32; ++b) {
+                        const uint32_t bits = run_bits(runs, half * HN + b * 32);
 #pragma unroll
                         for (int k = 0; k < 32; ++k) s[b * 32 + k] = (bits >> k) & 1u ? s[b * 32 + k] : 0xff800000u;      // -inf
                     }
@@ -579,11 +596,15 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
 #pragma unroll
                 for (int k = 0; k < 8; ++k) mx[k] = fmaxf(__uint_as_float(s[k]), __uint_as_float(s[k + 8]));
 #pragma unroll
-                for (int k = 16; k < TN; k += 16)
+                for (int k = 16; k < HN; k += 16)
 #pragma unroll
                     for (int c8 = 0; c8 < 8; ++c8) mx[c8] = fmaxf(fmaxf(mx[c8], __uint_as_float(s[k + c8])), __uint_as_float(s[k + 8 + c8]));
-                const float mn = fmaxf(fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))), m);
-                // renew the subtracted maximum when it has grown enough (or is the first): rescale O and l
+                float mn = fmaxf(fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))), m);
+                if constexpr (SPLIT == 2) mn = fmaxf(mn, other(mn));
+                // (a wait that gave up is acted on here, behind the exchange that both halves go through)
+                if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
+                // renew the subtracted maximum when it has grown enough (or is the first): rescale O and l.  Both halves of a row
+                // have the same m and mn, so they decide alike.
                 const bool grown = live && (mn - m) * c > RENEW;      // (-inf - -inf: no)
                 if (__any_sync(0xffffffffu, grown)) {
                     const float f = m == -CUDART_INF_F ? 0.f : ex2_approx((m - mn) * c);
@@ -592,13 +613,13 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                         if (__any_sync(0xffffffffu, !ok)) { ok = false; break; }
                         tc_fence_after();
 #pragma unroll
-                        for (int b = 0; b < D / 32; ++b) {
-                            uint32_t o[32];
-                            tmem_ld32_nowait(o_addr + b * 32, o);
-                            tmem_wait_ld();
+                        for (int b = 0; b < D / 16 / SPLIT; ++b) {      // (16 columns at a time: S is held meanwhile)
+                            uint32_t o[16];
+                            tmem_ld16_nowait(o_addr + b * 16, o);
+                            tmem_wait_ld(o);
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                            tmem_st32(o_addr + b * 32, o);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_st16(o_addr + b * 16, o);
                         }
                     }
                     l *= f;
@@ -608,7 +629,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 const uint64_t c2 = f2(c, c), b2 = f2(-base, -base);
                 uint64_t sum0 = f2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
+                for (int b = 0; b < HN / 32; ++b) {
                     uint32_t pk[16];
 #pragma unroll
                     for (int k = 0; k < 32; k += 2) {
@@ -619,7 +640,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                         if (k & 2) sum1 = add2(sum1, f2(x, y)); else sum0 = add2(sum0, f2(x, y));
                         pk[k / 2] = shelem::Vec<T>::pack2(x, y);
                     }
-                    tmem_st16(s_addr + b * 16, pk);
+                    tmem_st16(p_addr + b * 16, pk);
                 }
                 float x, y;
                 un2(add2(sum0, sum1), x, y);
@@ -632,16 +653,17 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             }
             if (!(flags & STEP_LAST) || !begun) continue;
             ok = mbar_wait(&bars->pv_done[t], (cnt - 1) & 1, err, 0x623);
-            if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
             tc_fence_after();
+            if constexpr (SPLIT == 2) l += other(l);
             const float inv = 1.f / l;
-            char *dst = p.w.out.p + (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs;
+            if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
+            char *dst = p.w.out.p + (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs + half * D;
             bool odd = false;
 #pragma unroll
-            for (int b = 0; b < D / 32; ++b) {
+            for (int b = 0; b < D / 32 / SPLIT; ++b) {
                 uint32_t o[32];
                 tmem_ld32_nowait(o_addr + b * 32, o);
-                tmem_wait_ld();
+                tmem_wait_ld(o);
 #pragma unroll
                 for (int k = 0; k < 32; k += 8) {
                     float x[8];
@@ -654,8 +676,22 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 }
             }
             tc_fence_before();      // O has been read before the arrivals that let the next item overwrite it
+            if constexpr (SPLIT == 2) {
+            int any;                // does either half of one of these 32 rows have a value that is not finite?
+            asm volatile(
+                "{\n\t.reg .pred p, q;\n\t"
+                "setp.ne.b32 q, %1, 0;\n\t"
+                "barrier.cta.red.or.pred p, %2, 64, q;\n\t"
+                "selp.b32 %0, 1, 0, p;\n\t}"
+                : "=r"(any)
+                : "r"((int)(live && odd)), "r"(pair + 1)
+                : "memory");
+            if (!any) continue;
+            odd = other(odd ? 1.f : 0.f) != 0.f || odd;
+            asm volatile("bar.sync %0, 64;" ::"r"(pair + 1) : "memory");
+            }
             __syncwarp();
-            unsigned again = __ballot_sync(0xffffffffu, live && odd);
+            unsigned again = half ? 0u : __ballot_sync(0xffffffffu, live && odd);
             while (again) {
                 const int l0 = __ffs(again) - 1;
                 again &= again - 1;
