@@ -30,7 +30,7 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t saddr, uint32_t lbo, uint
     return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) | (1ull << 46);
 }
 // Instruction descriptor of kind::f16: fp32 accumulator, 16-bit A and B of format fmt (0 f16, 1 bf16).
-__device__ __forceinline__ uint32_t instr_desc(int fmt, int a_mn_major, int M, int N) {
+__host__ __device__ constexpr __forceinline__ uint32_t instr_desc(int fmt, int a_mn_major, int M, int N) {
     return (1u << 4) | ((uint32_t)fmt << 7) | ((uint32_t)fmt << 10) | ((uint32_t)a_mn_major << 15) | ((uint32_t)(N >> 3) << 17) |
            ((uint32_t)(M >> 4) << 24);
 }

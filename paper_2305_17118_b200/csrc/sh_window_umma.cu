@@ -2,17 +2,21 @@
 //
 // out = softmax(scale Q.K^T + mask) V with the running maximum and sum of an online softmax.  A work item is one key head and
 // two query tiles; a tile is 128 rows = TPT tokens x GB query heads of the group (heads innermost), so the heads that share keys
-// share a tile and the tile spans few tokens.  The keys come in tiles of 128: first the slots of the cache, then the chunk's own
+// share a tile and the tile spans few tokens.  The keys come in tiles of 64: first the slots of the cache, then the chunk's own
 // rows; tiles that none of the item's rows can see are never loaded, tiles that a query tile does not see are not multiplied for it.
 //
-//   warps 0-7, 8-15  softmax of query tile 0 and 1, two threads per row.  S from tensor memory, mask, exponentials, P (16 bits) back into
+//   warps 0-3, 4-7   softmax of query tile 0 and 1: thread = row.  S from tensor memory, mask, exponentials, P (16 bits) back into
 //                    the columns of S, the rare rescaling of O, and the division and store at the end
-//   warp 16          issues the MMAs: S = Q.K^T (both operands in shared memory, K-major), O += P.V (P in tensor memory, V MN-major)
-//   warp 17          requests query, key and value tiles (tiled TMA copies, 128-byte swizzle; rows outside a tensor are zeros)
+//   warps 8, 9       issue the MMAs of query tile 0 and 1: S = Q.K^T (both operands in shared memory, K-major), O += P.V (P in
+//                    tensor memory, V MN-major)
+//   warp 10          works out the steps (key tiles of an item) and who sees what in them, publishes them in a ring, and requests
+//                    the tiles (tiled TMA copies, 128-byte swizzle; rows outside a tensor are zeros)
 //
-// The tensor pipe takes the MMAs in the order PV0(n), S0(n+1), PV1(n), S1(n+1): one query tile's softmax runs while the other's
-// products do.  P overwrites S: S(n+1) of a query tile is issued behind PV(n) of the same tile, which reads P, and the pipe keeps
-// that order.  CTAs are persistent; the loads of the next item start while the present one drains.
+// A query tile has two buffers of S: S(n+1) is made while the softmax of step n runs, and goes into the buffer whose P the product
+// P.V(n-1), issued before it, has read (the tensor pipe keeps the order of one warp's MMAs).  Tensor memory is full with that: two
+// query tiles x (2 x 64 columns of S + 128 of O).  With one buffer of 128 columns each step waited for softmax and both products in
+// turn: 2.3 instead of 2.0 ms for the 32768-token prompt below.  CTAs are persistent; the loads of the next item start while the
+// present one drains.
 //
 // P is rounded to the storage type (the tensor cores take no other pair with 16-bit V); its row sum is taken before the rounding,
 // in fp32.  The subtracted maximum is only renewed when it has grown by more than 8 (log2), so weights stay below 2^8; fp16
@@ -22,8 +26,10 @@
 // that holds no token, a later token, another sequence's row).  That shows as an O that is not finite; such rows are computed
 // again at the end, one warp per row over the visible keys only.  Rows whose result is rightly not finite take that way too.
 //
-// Bound by the tensor pipe and the exponentials, which need the same time: 128 x 128 x D twice at 4096 multiply-adds per cycle
-// against 128 x 128 exponentials at 16 per cycle.
+// 32768 tokens, window 4096, 16 sinks, 32 query and 8 key heads of 128, fp16: 2.03 ms, 1017 TFLOP/s.  Bound by shared-memory
+// reads of the operands (48 KB per S of 64 keys, 16 KB per P.V, 32 KB written: about 1250 cycles a step for both query tiles) and
+// by the softmax warps (1024 cycles of exponentials a step on each quarter of the SM), which do not overlap perfectly: a step
+// takes about 1950 cycles, 1600 with the exponentials left out.
 #include <cuda.h>
 #include <math_constants.h>
 
@@ -37,29 +43,23 @@ using namespace shasync;
 using namespace shumma;
 using namespace shwin;
 
-constexpr int TM = 128, TN = 128;          // rows of a query tile, keys of a key tile
-constexpr int HALF = 128 * 128;            // bytes of 128 rows x 64 elements
-#ifndef SPLITS
-#define SPLITS 1
-#endif
-constexpr int SPLIT = SPLITS;              // threads that share a row
-constexpr int HN = TN / SPLIT;             // keys of a tile per softmax thread
-constexpr int SOFTMAX_WARPS = 8 * SPLIT, NTH = 32 * SOFTMAX_WARPS + 128;
-constexpr int REGS_SOFTMAX = SPLIT == 1 ? 216 : 104, REGS_OTHER = SPLIT == 1 ? 72 : 64;      // 512 * 104 + 128 * 64 = 640 * 96, what the CTA is launched with
+constexpr int TM = 128, TN = 64;           // rows of a query tile, keys of a key tile
+constexpr int QHALF = TM * 128, HALF = TN * 128;      // bytes of a tile's rows x 64 elements
+constexpr int SOFTMAX_WARPS = 8, NTH = 384;      // 8 softmax warps, 2 that issue MMAs, 1 that loads; the last one only makes a whole warpgroup
+constexpr int REGS_SOFTMAX = 216, REGS_OTHER = 72;      // 256 * 216 + 128 * 72 = 384 * 168, what the CTA is launched with
 constexpr float RENEW = 8.f;               // log2 growth of the maximum at which O is rescaled
 
 __device__ int g_window_error;             // code of the first bounded wait that gave up
 
-constexpr int STEPS = 8, BAR_BYTES = 768; // steps in flight between the load warp and the others; barriers and step ring
+constexpr int STEPS = 8, BAR_BYTES = 896;  // steps in flight between the load warp and the others; barriers and step ring
 
 template <int D> struct Cfg {
-    static constexpr int TILE = D / 64 * HALF;         // bytes of a query, key or value tile
-    static constexpr int STAGES = D == 128 ? 5 : 8;    // key and value tiles in flight
-    static constexpr int OFF_KV = 2 * TILE;
-    static constexpr int OFF_BAR = OFF_KV + STAGES * TILE;
-    static constexpr int OFF_STAT = OFF_BAR + BAR_BYTES;
-    static constexpr int SMEM = OFF_STAT + 2 * 2 * TM * 4;      // exchanged row values: [query tile][half][row]
-    static constexpr int O_COL = 2 * TN;               // tensor memory: S0, S1 (P inside), O0, O1
+    static constexpr int QTILE = D / 64 * QHALF, TILE = D / 64 * HALF;      // bytes of a query tile, of a key or value tile
+    static constexpr int STAGES = 5;                   // steps in flight: a stage holds a key and a value tile
+    static constexpr int OFF_KV = 2 * QTILE;
+    static constexpr int OFF_BAR = OFF_KV + STAGES * 2 * TILE;
+    static constexpr int SMEM = OFF_BAR + BAR_BYTES;
+    static constexpr int O_COL = 4 * TN;               // tensor memory: per query tile two buffers of S (P inside), then O0, O1
     static_assert(SMEM <= 232448 && O_COL + 2 * D <= 512, "");
 };
 
@@ -79,14 +79,26 @@ struct __align__(16) Step {
 };
 struct Bars {
     uint64_t q_full[2], q_empty[2];        // a query tile landed / its last S has been computed
-    uint64_t full[8], empty[8];            // stages: landed / read by the MMAs
-    uint64_t s_full[2], p_ready[2], pv_done[2];
+    uint64_t full[5], empty[5];            // stages: landed / read by the MMAs
+    uint64_t s_full[2][2], p_ready[2][2];  // [query tile][buffer of S]
+    uint64_t pv_done[2];
     uint64_t step_full[STEPS], step_empty[STEPS];
     Step steps[STEPS];
     uint32_t tmem;
     int abort_flag;
 };
 static_assert(sizeof(Bars) <= BAR_BYTES, "barrier block");
+
+// Wait for a phase, bounded like mbar_wait, in few instructions: the code of a wait that gave up goes to the CTA's abort word, and
+// from there to g_window_error at the end.
+__device__ __forceinline__ bool wait_for(Bars *bars, uint64_t *bar, uint32_t parity, int code) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < WAIT_NS)
+        if (mbar_try_wait(bar, parity)) return true;
+    if (code) *(volatile int *)&bars->abort_flag = code;
+    return false;
+}
 
 struct UmmaParams {
     WindowParams w;
@@ -145,12 +157,30 @@ __device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *map, int c0
                  "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
                  : "memory");
 }
-__device__ __forceinline__ void tma_4d(void *dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, uint64_t *bar) {
+// Key and value tiles: the halves of a row are the outermost dimension of the map, so one copy brings both.
+__device__ __forceinline__ void tma_4d(void *dst, const CUtensorMap *map, int head, int token, uint64_t *bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
             smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar))
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(head), "r"(token), "r"(0), "r"(smem_u32(bar))
         : "memory");
+}
+__device__ __forceinline__ void tma_5d(void *dst, const CUtensorMap *map, int slot, int head, int sequence, uint64_t *bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(slot), "r"(head), "r"(sequence), "r"(0), "r"(smem_u32(bar))
+        : "memory");
+}
+// One lane of the warp, which must be converged.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(p));
+    return p != 0;
 }
 
 // One work item and the key tiles it has to walk over.  Tiles 0 .. ctiles - 1 are blocks of 128 cache slots, tile ctiles + j holds
@@ -286,6 +316,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // One row by one warp, over its visible keys only, in fp32 on CUDA cores: for rows next to values that are not finite.
 template <typename T, int D>
 __device__ __noinline__ void slow_row(const UmmaParams &u, long long id, int qi, int h) {
@@ -338,7 +373,6 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     unsigned char *kv = sm + C::OFF_KV;
     Bars *bars = reinterpret_cast<Bars *>(sm + C::OFF_BAR);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    int *err = &g_window_error;
     auto aborted = [&]() { return *(volatile int *)&bars->abort_flag != 0; };
 
     if (warp == 0) {
@@ -348,128 +382,128 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     if (tid == 0) {
         for (int t = 0; t < 2; ++t) {
             mbar_init(&bars->q_full[t], 1); mbar_init(&bars->q_empty[t], 1);
-            mbar_init(&bars->s_full[t], 1); mbar_init(&bars->p_ready[t], SPLIT * TM); mbar_init(&bars->pv_done[t], 1);
+            mbar_init(&bars->pv_done[t], 1);
+            for (int b = 0; b < 2; ++b) { mbar_init(&bars->s_full[t][b], 1); mbar_init(&bars->p_ready[t][b], 4); }
         }
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 2); }
         for (int s = 0; s < STEPS; ++s) { mbar_init(&bars->step_full[s], 1); mbar_init(&bars->step_empty[s], SOFTMAX_WARPS); }
         bars->abort_flag = 0;
         if ((smem_u32(sm) & 1023u) != 0) {      // the swizzled tiles need the alignment the declaration asks for
-            atomicCAS(err, 0, 0x620);
-            bars->abort_flag = 1;
+            bars->abort_flag = 0x620;
         }
         fence_barrier_init();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tbase = bars->tmem;
-    bool ok = !aborted();
+    const uint32_t tbase = bars->tmem;             // 0: all 512 columns are this CTA's
+    bool ok = __all_sync(0xffffffffu, !aborted() && tbase == 0);
+    if (tbase != 0) *(volatile int *)&bars->abort_flag = 0x621;
 
     if (warp >= SOFTMAX_WARPS) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
+    // What these warps issue takes its operands from uniform registers.  So their control flow and values are kept uniform in a
+    // way the compiler can see: outcomes of waits go through a vote, values from memory through a shuffle.
     if (warp < SOFTMAX_WARPS + 2) {
         // ------------------------------------------------------------------------------------------------ MMAs
-        // One warp per query tile.  Steps come in the order of their loads (their entries of the ring are published with them, and
-        // not written again before this warp has released later stages).  The whole warp waits, one lane issues.
-        const int t = warp - SOFTMAX_WARPS;
-        const uint32_t idesc_s = instr_desc(Fmt<T>::CODE, 0, TM, TN), idesc_pv = instr_desc(Fmt<T>::CODE, 0, TM, D) | (1u << 16);
+        // One warp per query tile.  A step's entry in the ring is published with its loads and not written again before this warp
+        // has released the stage of a later step.
+        const int t = __shfl_sync(0xffffffffu, warp, 0) - SOFTMAX_WARPS;
+        constexpr uint32_t idesc_s = instr_desc(Fmt<T>::CODE, 0, TM, TN), idesc_pv = instr_desc(Fmt<T>::CODE, 0, TM, D) | (1u << 16);
         // descriptors: the high word is the same for all operands of a kind, the low word holds address / 16 in its low bits
-        const uint64_t q_desc = desc_sw128(smem_u32(sm) + t * C::TILE, 16, 1024), k_desc = desc_sw128(smem_u32(kv), 16, 1024),
-                       v_desc = desc_sw128(smem_u32(kv), HALF, 1024);
+        const uint64_t q_desc = desc_sw128(smem_u32(sm) + t * C::QTILE, 16, 1024), k_desc = desc_sw128(smem_u32(kv), 16, 1024),
+                       v_desc = desc_sw128(smem_u32(kv) + C::TILE, HALF, 1024);
         auto plus = [](uint64_t d, uint32_t bytes) { return (d & 0xffffffff00000000ull) | (uint32_t)((uint32_t)d + (bytes >> 4)); };
-        uint32_t st = 0, par = 0;                     // the next stage and its parity: keys and values of the steps in turn
-        uint32_t items = 0, steps = 0, cnt = 0;
-        int now = 0;                                  // what the present step asks for
+        uint32_t st = 0, par = 0;                     // stage and parity of the next step
+        uint32_t items = 0, steps = 0, done_s = 0, done_pv = 0;      // products S and P.V issued
+        uint32_t due = C::STAGES;                     // stage of the step whose P.V is due (STAGES: none)
         bool begun = false;                           // O holds products of this item
-        auto stage_done = [&]() {
-            if (++st == C::STAGES) { st = 0; par ^= 1; }
+        auto issue_pv = [&]() {
+            const uint32_t b = done_pv & 1;
+            ok = __all_sync(0xffffffffu, wait_for(bars, &bars->p_ready[t][b], (done_pv >> 1) & 1, 0x604));
+            tc_fence_after();
+            if (ok && elect_one()) {
+                const uint64_t vd = plus(v_desc, due * 2 * C::TILE);
+#pragma unroll
+                for (int x = 0; x < TN / 16; ++x)     // (the first product of an item overwrites O)
+                    umma_ts(C::O_COL + t * D, (2 * t + b) * TN + x * 8, plus(vd, x * 2048), idesc_pv, begun || x > 0);
+                umma_commit(&bars->pv_done[t]);
+                umma_commit(&bars->empty[due]);
+            }
+            __syncwarp();
+            ++done_pv;
+            begun = true;
+            due = C::STAGES;
         };
-        // S of the next step, as soon as its keys (and, if it is the first of its item, the queries) are there
-        auto next_step = [&]() {
-            ok = ok && mbar_wait(&bars->full[st], par, err, 0x603);
-            now = ok ? *(volatile int *)&bars->steps[steps++ % STEPS].flags : (int)STEP_END;
-            if (now & STEP_END) return;
+        while (ok) {
+            ok = __all_sync(0xffffffffu, wait_for(bars, &bars->full[st], par, 0x603));
+            if (!ok) break;
+            const int now = __shfl_sync(0xffffffffu, *(volatile int *)&bars->steps[steps++ % STEPS].flags, 0);
+            if (now & STEP_END) break;
             if (now & STEP_FIRST) {
-                ok = ok && mbar_wait(&bars->q_full[t], items++ & 1, err, 0x601);
+                ok = __all_sync(0xffffffffu, wait_for(bars, &bars->q_full[t], items++ & 1, 0x601) && !aborted());
+                if (!ok) break;
                 begun = false;
             }
-            ok = ok && !aborted();
+            const bool need = now & (STEP_NEED0 << t);
             tc_fence_after();
-            if (ok && lane == 0) {
-                if (now & (STEP_NEED0 << t)) {
-                    const uint64_t kd = plus(k_desc, st * C::TILE);
+            if (elect_one()) {
+                if (need) {
+                    // S of this step goes into the buffer whose P the last but one P.V has read: the pipe keeps that order
+                    const uint64_t kd = plus(k_desc, st * 2 * C::TILE);
+                    const uint32_t b = done_s & 1;
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x)
-                        umma_f16(tbase + t * TN, plus(q_desc, (x >> 2) * HALF + (x & 3) * 32), plus(kd, (x >> 2) * HALF + (x & 3) * 32), idesc_s, x > 0);
-                    umma_commit(&bars->s_full[t]);
-                    umma_commit(&bars->empty[st]);
+                        umma_f16((2 * t + b) * TN, plus(q_desc, (x >> 2) * QHALF + (x & 3) * 32), plus(kd, (x >> 2) * HALF + (x & 3) * 32), idesc_s, x > 0);
+                    umma_commit(&bars->s_full[t][b]);
                 } else {
                     mbar_arrive(&bars->empty[st]);
                 }
                 if (now & STEP_LAST) umma_commit(&bars->q_empty[t]);
             }
-            stage_done();
-        };
-        next_step();
-        while (ok && !(now & STEP_END)) {
-            const bool need = now & (STEP_NEED0 << t);
-            if (need) ok = ok && mbar_wait(&bars->p_ready[t], cnt++ & 1, err, 0x604);
-            ok = ok && mbar_wait(&bars->full[st], par, err, 0x605) && !aborted();
-            tc_fence_after();
-            if (ok && lane == 0) {
-                if (need) {
-                    const uint64_t vd = plus(v_desc, st * C::TILE);
-#pragma unroll
-                    for (int x = 0; x < TN / 16; ++x)     // (the first product of an item overwrites O)
-                        umma_ts(tbase + C::O_COL + t * D, tbase + t * TN + x * 8, plus(vd, x * 2048), idesc_pv, begun || x > 0);
-                    umma_commit(&bars->pv_done[t]);
-                    umma_commit(&bars->empty[st]);
-                } else {
-                    mbar_arrive(&bars->empty[st]);
-                }
+            __syncwarp();
+            if (due < C::STAGES) issue_pv();          // of the step before: its softmax ran while this S was made
+            if (need) {
+                ++done_s;
+                due = st;
             }
-            begun = begun || need;
-            stage_done();
-            next_step();
+            if (++st == C::STAGES) { st = 0; par ^= 1; }
+            if ((now & STEP_LAST) && due < C::STAGES && ok) issue_pv();      // (the next item waits for its queries)
         }
-        if (!ok) *(volatile int *)&bars->abort_flag = 1;
     } else if (warp == SOFTMAX_WARPS + 2) {
         // ------------------------------------------------------------------------------------------------ loads
-        uint32_t n = 0, items = 0, steps = 0;         // loads requested, items begun, steps published
+        uint32_t items = 0, steps = 0;                // items begun, steps published
         uint32_t st = 0, par = 1;                     // the next stage, and the parity of its last release (the first pass: none)
         const int q_bytes = D / 64 * p.tpt * p.gb * 128;
-        auto room = [&]() {
-            ok = ok && (n < C::STAGES || mbar_wait(&bars->empty[st], par, err, 0x612));
-            ok = ok && !aborted();
-            return ok;
-        };
-        auto stage_done = [&]() {
-            ++n;
-            if (++st == C::STAGES) { st = 0; par ^= 1; }
-        };
+        // publish a step and take the stage for its tiles
         auto publish = [&](const Item &w, int flags, int x) {
             const uint32_t e = steps % STEPS;
-            ok = ok && (steps < STEPS || mbar_wait(&bars->step_empty[e], (steps / STEPS - 1) & 1, err, 0x613));
-            ok = ok && !aborted();
-            if (ok && lane == 0) {
+            bool go = steps < STEPS || wait_for(bars, &bars->step_empty[e], (steps / STEPS - 1) & 1, 0x613);
+            go = go && (steps < C::STAGES || wait_for(bars, &bars->empty[st], par, 0x612));
+            ok = __all_sync(0xffffffffu, go);
+            if (ok && elect_one()) {
                 Step &d = bars->steps[e];
-                d.flags = flags; d.x = x; d.first = w.first; d.count = w.count;
-                d.cached = w.cached; d.a = w.a; d.kvh = w.kvh; d.hb = w.hb;
-                d.head = w.head; d.ring2 = w.ring2();
+                *reinterpret_cast<int4 *>(&d) = make_int4(flags, x, w.first, w.count);
+                *reinterpret_cast<int4 *>(&d.cached) = make_int4(w.cached, w.a, w.kvh, w.hb);
+                *reinterpret_cast<int2 *>(&d.head) = make_int2(w.head, w.ring2());
                 mbar_arrive(&bars->step_full[e]);
             }
+            __syncwarp();
             ++steps;
-            return ok;
         };
         auto queries = [&](const Item &w, int t) {
-            ok = ok && (items == 0 || mbar_wait(&bars->q_empty[t], (items - 1) & 1, err, 0x611));
-            ok = ok && !aborted();
-            if (!ok || lane != 0) return;
-            if (!w.has(t)) { mbar_arrive(&bars->q_full[t]); return; }
-            mbar_arrive_expect_tx(&bars->q_full[t], q_bytes);
+            ok = __all_sync(0xffffffffu, (items == 0 || wait_for(bars, &bars->q_empty[t], (items - 1) & 1, 0x611)) && !aborted());
+            if (ok && elect_one()) {
+                if (w.has(t)) {
+                    mbar_arrive_expect_tx(&bars->q_full[t], q_bytes);
 #pragma unroll
-            for (int h = 0; h < D / 64; ++h)
-                tma_3d(sm + t * C::TILE + h * HALF, &map_q, h * 64, w.kvh * p.w.g + w.hb * p.gb, w.first + w.from(t), &bars->q_full[t]);
+                    for (int h = 0; h < D / 64; ++h)
+                        tma_3d(sm + t * C::QTILE + h * QHALF, &map_q, h * 64, w.kvh * p.w.g + w.hb * p.gb, w.first + w.from(t), &bars->q_full[t]);
+                } else {
+                    mbar_arrive(&bars->q_full[t]);
+                }
+            }
+            __syncwarp();
         };
         for (long long id = blockIdx.x; ok; id += gridDim.x) {
             const Item w = find_item(p, id);
@@ -488,106 +522,107 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                     const int bit = __ffs(todo) - 1;
                     todo &= todo - 1;
                     const int flags = __shfl_sync(0xffffffffu, mine, bit) | (first ? STEP_FIRST : 0);
-                    const bool in_cache = flags & STEP_CACHE;
-                    const int x = (base + bit - (in_cache ? 0 : w.ctiles)) * TN;
-                    if (!publish(w, flags, x)) break;
-                    if (first) queries(w, 0);
-#pragma unroll
-                    for (int value = 0; value < 2; ++value) {
-                        if (!room()) break;
-                        if (lane == 0) {
-                            unsigned char *dst = kv + st * C::TILE;
-                            uint64_t *full = &bars->full[st];
-                            mbar_arrive_expect_tx(full, C::TILE);
-#pragma unroll
-                            for (int h = 0; h < D / 64; ++h) {
-                                if (in_cache) tma_4d(dst + h * HALF, value ? &map_vc : &map_kc, h * 64, x, w.kvh, w.seq, full);
-                                else tma_3d(dst + h * HALF, value ? &map_v : &map_k, h * 64, w.kvh, w.first + x, full);
-                            }
+                    const int x = (base + bit - (flags & STEP_CACHE ? 0 : w.ctiles)) * TN;
+                    publish(w, flags, x);
+                    if (ok && first) queries(w, 0);
+                    if (ok && elect_one()) {
+                        unsigned char *dst = kv + st * 2 * C::TILE;
+                        uint64_t *full = &bars->full[st];
+                        mbar_arrive_expect_tx(full, 2 * C::TILE);
+                        if (flags & STEP_CACHE) {
+                            tma_5d(dst, &map_kc, x, w.kvh, w.seq, full);
+                            tma_5d(dst + C::TILE, &map_vc, x, w.kvh, w.seq, full);
+                        } else {
+                            tma_4d(dst, &map_k, w.kvh, w.first + x, full);
+                            tma_4d(dst + C::TILE, &map_v, w.kvh, w.first + x, full);
                         }
-                        stage_done();
-                        if (first && !value) { queries(w, 1); ++items; }
                     }
+                    __syncwarp();
+                    if (++st == C::STAGES) { st = 0; par ^= 1; }
+                    if (ok && first) queries(w, 1);
+                    items += first;
                     first = false;
                 }
             }
         }
-        Item none;
-        none.first = none.count = none.cached = none.a = none.kvh = none.hb = none.head = 0;
-        none.wrapped = false;
-        if (ok) publish(none, STEP_END, 0);
-        const uint32_t behind = room() ? C::STAGES - 1 : C::STAGES;      // loads that may not have been waited for
-        if (ok && lane == 0) {                        // the end: a stage without a load
-            mbar_arrive(&bars->full[st]);
+        const uint32_t loads = steps;                 // (a step that was published without a load only makes the drain below wait in vain)
+        if (ok) {                                     // the end: a step without a load
+            Item none;
+            none.first = none.count = none.cached = none.a = none.kvh = none.hb = none.head = 0;
+            none.wrapped = false;
+            publish(none, STEP_END, 0);
+            if (ok && elect_one()) mbar_arrive(&bars->full[st]);
+            __syncwarp();
         }
-        if (!ok) *(volatile int *)&bars->abort_flag = 1;
-        // let the copies requested last land before the CTA goes away (a phase that is past reads as complete)
+        // let the copies requested last land before the CTA goes away (a phase that is past reads as complete; with the last step
+        // published, its stage's earlier load has been waited for)
         if (lane == 0) {
             if (items > 0)
-                for (int t = 0; t < 2; ++t) mbar_wait(&bars->q_full[t], (items - 1) & 1, nullptr, 0);
-            for (uint32_t k = 0; k < behind && k < n; ++k) mbar_wait(&bars->full[(n - 1 - k) % C::STAGES], ((n - 1 - k) / C::STAGES) & 1, nullptr, 0);
+                for (int t = 0; t < 2; ++t) wait_for(bars, &bars->q_full[t], (items - 1) & 1, 0);
+            for (uint32_t k = 0; k < C::STAGES - (ok ? 1u : 0u) && k < loads; ++k)
+                wait_for(bars, &bars->full[(loads - 1 - k) % C::STAGES], ((loads - 1 - k) / C::STAGES) & 1, 0);
         }
         __syncwarp();
     }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
         // ------------------------------------------------------------------------------------------------ softmax
-        // two threads share a row: `half` 0 has keys 0 .. 63 of a tile and the first half of O's columns, 1 the others
-        const int t = warp / (4 * SPLIT), half = SPLIT == 2 ? (warp >> 2) & 1 : 0, row = tid & 127, pair = t * 4 + (warp & 3);
-        const uint32_t lanes = tbase + ((uint32_t)((warp & 3) * 32) << 16), s_addr = lanes + t * TN + half * HN,
-                       p_addr = lanes + t * TN + half * (HN / 2), o_addr = lanes + C::O_COL + t * D + half * (D / SPLIT);
+        const int t = warp >> 2, row = tid & 127;
+        const uint32_t lanes = tbase + ((uint32_t)((warp & 3) * 32) << 16), s_addr = lanes + 2 * t * TN, o_addr = lanes + C::O_COL + t * D;
         const int tok = row / p.gb, hrow = row % p.gb;
         const float c = p.w.scale_log2e;
-        float (*stat)[TM] = reinterpret_cast<float (*)[TM]>(sm + C::OFF_STAT) + t * 2;      // [half][row]
         uint32_t cnt = 0, steps = 0;
-        // this row's value from the thread with the other half.  One buffer is enough: between two exchanges of an item lies a
-        // wait that needs arrivals of all threads of the query tile, and behind the last one of an item a barrier.
-        auto other = [&](float mine) {
-            stat[half][row] = mine;
-            tc_fence_before();      // (also: the other half's columns of S have been read before P is written over them)
-            asm volatile("bar.sync %0, 64;" ::"r"(pair + 1) : "memory");
-            tc_fence_after();
-            return stat[half ^ 1][row];
-        };
         long long id = (long long)blockIdx.x - gridDim.x;      // present item
         int qi = 0, h = 0, kvh = 0, row0 = 0;
         bool live = false, begun = false;
         float m = -CUDART_INF_F, l = 0.f;
-        while (ok) {
+        // The entry of the next step is read while the present one is worked on.
+        int4 e0, e1;
+        int2 e2;
+        auto fetch = [&]() {
             const uint32_t e = steps % STEPS;
-            ok = mbar_wait(&bars->step_full[e], (steps / STEPS) & 1, err, 0x624);
-            if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
+            ok = wait_for(bars, &bars->step_full[e], (steps / STEPS) & 1, 0x624) && ok;
             ++steps;
             const Step &d = bars->steps[e];
-            const int flags = d.flags;
+            e0 = *reinterpret_cast<const int4 *>(&d);
+            e1 = *reinterpret_cast<const int4 *>(&d.cached);
+            e2 = *reinterpret_cast<const int2 *>(&d.head);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->step_empty[e]);
+        };
+        fetch();
+        while (true) {
+            if (__any_sync(0xffffffffu, !ok)) break;
+            const int flags = e0.x;
             if (flags & STEP_END) break;
             if (flags & STEP_FIRST) {
                 id += gridDim.x;
-                qi = d.a + t * p.tpt + tok;
-                h = d.hb * p.gb + hrow;
-                kvh = d.kvh;
-                row0 = d.first;
-                live = tok < p.tpt && qi < d.count && h < p.w.g;
+                qi = e1.y + t * p.tpt + tok;
+                h = e1.w * p.gb + hrow;
+                kvh = e1.z;
+                row0 = e0.z;
+                live = tok < p.tpt && qi < e0.w && h < p.w.g;
                 begun = false;
                 m = -CUDART_INF_F;
                 l = 0.f;
+                ok = !aborted();
             }
-            const bool whole = flags & (STEP_WHOLE0 << t);
-            Runs runs;
-            if (!whole) runs = visible_runs(flags & STEP_CACHE, d.x, d.cached, d.head, d.ring2, p.w.sinks, p.w.window, qi);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bars->step_empty[e]);
             if (flags & (STEP_NEED0 << t)) {
-                ok = mbar_wait(&bars->s_full[t], cnt & 1, err, 0x621);
+                const bool whole = flags & (STEP_WHOLE0 << t);
+                Runs runs;
+                if (!whole) runs = visible_runs(flags & STEP_CACHE, e0.y, e1.x, e2.x, e2.y, p.w.sinks, p.w.window, qi);
+                const uint32_t buf = cnt & 1;
+                ok = wait_for(bars, &bars->s_full[t][buf], (cnt >> 1) & 1, 0x621) && ok;
+                if (__any_sync(0xffffffffu, !ok)) break;
                 tc_fence_after();
-                uint32_t s[HN];
+                uint32_t s[TN];
 #pragma unroll
-                for (int b = 0; b < HN / 32; ++b) tmem_ld32_nowait(s_addr + b * 32, s + b * 32);
+                for (int x = 0; x < TN / 32; ++x) tmem_ld32_nowait(s_addr + buf * TN + x * 32, s + x * 32);
                 tmem_wait_ld(s);
                 if (!whole) {
 #pragma unroll
-                    for (int b = 0; b < HN / 32; ++b) {
-                        const uint32_t bits = run_bits(runs, half * HN + b * 32);
+                    for (int b = 0; b < TN / 32; ++b) {
+                        const uint32_t bits = run_bits(runs, b * 32);
 #pragma unroll
                         for (int k = 0; k < 32; ++k) s[b * 32 + k] = (bits >> k) & 1u ? s[b * 32 + k] : 0xff800000u;      // -inf
                     }
@@ -596,24 +631,20 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
 #pragma unroll
                 for (int k = 0; k < 8; ++k) mx[k] = fmaxf(__uint_as_float(s[k]), __uint_as_float(s[k + 8]));
 #pragma unroll
-                for (int k = 16; k < HN; k += 16)
+                for (int k = 16; k < TN; k += 16)
 #pragma unroll
-                    for (int c8 = 0; c8 < 8; ++c8) mx[c8] = fmaxf(fmaxf(mx[c8], __uint_as_float(s[k + c8])), __uint_as_float(s[k + 8 + c8]));
-                float mn = fmaxf(fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))), m);
-                if constexpr (SPLIT == 2) mn = fmaxf(mn, other(mn));
-                // (a wait that gave up is acted on here, behind the exchange that both halves go through)
-                if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
-                // renew the subtracted maximum when it has grown enough (or is the first): rescale O and l.  Both halves of a row
-                // have the same m and mn, so they decide alike.
+                    for (int c8 = 0; c8 < 8; ++c8) mx[c8] = max3(mx[c8], __uint_as_float(s[k + c8]), __uint_as_float(s[k + 8 + c8]));
+                const float mn = fmaxf(fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7]))), m);
+                // renew the subtracted maximum when it has grown enough (or is the first): rescale O and l.
                 const bool grown = live && (mn - m) * c > RENEW;      // (-inf - -inf: no)
                 if (__any_sync(0xffffffffu, grown)) {
                     const float f = m == -CUDART_INF_F ? 0.f : ex2_approx((m - mn) * c);
                     if (begun) {
-                        ok = mbar_wait(&bars->pv_done[t], (cnt - 1) & 1, err, 0x622);      // the product before this one is in O
-                        if (__any_sync(0xffffffffu, !ok)) { ok = false; break; }
+                        ok = wait_for(bars, &bars->pv_done[t], (cnt - 1) & 1, 0x622);      // the product before this one is in O
+                        if (__any_sync(0xffffffffu, !ok)) break;
                         tc_fence_after();
 #pragma unroll
-                        for (int b = 0; b < D / 16 / SPLIT; ++b) {      // (16 columns at a time: S is held meanwhile)
+                        for (int b = 0; b < D / 16; ++b) {      // (16 columns at a time: S is held meanwhile)
                             uint32_t o[16];
                             tmem_ld16_nowait(o_addr + b * 16, o);
                             tmem_wait_ld(o);
@@ -625,11 +656,12 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                     l *= f;
                     m = mn;
                 }
+                fetch();
                 const float base = m == -CUDART_INF_F ? 0.f : m * c - Fmt<T>::LIFT;
                 const uint64_t c2 = f2(c, c), b2 = f2(-base, -base);
                 uint64_t sum0 = f2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-                for (int b = 0; b < HN / 32; ++b) {
+                for (int b = 0; b < TN / 32; ++b) {
                     uint32_t pk[16];
 #pragma unroll
                     for (int k = 0; k < 32; k += 2) {
@@ -640,27 +672,29 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                         if (k & 2) sum1 = add2(sum1, f2(x, y)); else sum0 = add2(sum0, f2(x, y));
                         pk[k / 2] = shelem::Vec<T>::pack2(x, y);
                     }
-                    tmem_st16(p_addr + b * 16, pk);
+                    tmem_st16(s_addr + buf * TN + b * 16, pk);
                 }
                 float x, y;
                 un2(add2(sum0, sum1), x, y);
                 l += x + y;
                 tmem_wait_st();
                 tc_fence_before();
-                mbar_arrive(&bars->p_ready[t]);
+                __syncwarp();                  // (one arrival per warp: those of 32 lanes on one barrier are taken one by one)
+                if (lane == 0) mbar_arrive(&bars->p_ready[t][buf]);
                 ++cnt;
                 begun = true;
+            } else {
+                fetch();
             }
             if (!(flags & STEP_LAST) || !begun) continue;
-            ok = mbar_wait(&bars->pv_done[t], (cnt - 1) & 1, err, 0x623);
+            ok = wait_for(bars, &bars->pv_done[t], (cnt - 1) & 1, 0x623);
             tc_fence_after();
-            if constexpr (SPLIT == 2) l += other(l);
             const float inv = 1.f / l;
-            if (__any_sync(0xffffffffu, !ok || aborted())) { ok = false; break; }
-            char *dst = p.w.out.p + (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs + half * D;
+            if (__any_sync(0xffffffffu, !ok)) break;
+            char *dst = p.w.out.p + (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs;
             bool odd = false;
 #pragma unroll
-            for (int b = 0; b < D / 32 / SPLIT; ++b) {
+            for (int b = 0; b < D / 32; ++b) {
                 uint32_t o[32];
                 tmem_ld32_nowait(o_addr + b * 32, o);
                 tmem_wait_ld(o);
@@ -676,32 +710,18 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 }
             }
             tc_fence_before();      // O has been read before the arrivals that let the next item overwrite it
-            if constexpr (SPLIT == 2) {
-            int any;                // does either half of one of these 32 rows have a value that is not finite?
-            asm volatile(
-                "{\n\t.reg .pred p, q;\n\t"
-                "setp.ne.b32 q, %1, 0;\n\t"
-                "barrier.cta.red.or.pred p, %2, 64, q;\n\t"
-                "selp.b32 %0, 1, 0, p;\n\t}"
-                : "=r"(any)
-                : "r"((int)(live && odd)), "r"(pair + 1)
-                : "memory");
-            if (!any) continue;
-            odd = other(odd ? 1.f : 0.f) != 0.f || odd;
-            asm volatile("bar.sync %0, 64;" ::"r"(pair + 1) : "memory");
-            }
             __syncwarp();
-            unsigned again = half ? 0u : __ballot_sync(0xffffffffu, live && odd);
+            unsigned again = __ballot_sync(0xffffffffu, live && odd);
             while (again) {
                 const int l0 = __ffs(again) - 1;
                 again &= again - 1;
                 slow_row<T, D>(p, id, __shfl_sync(0xffffffffu, qi, l0), kvh * p.w.g + __shfl_sync(0xffffffffu, h, l0));
             }
         }
-        if (!ok) *(volatile int *)&bars->abort_flag = 1;
     }
     tc_fence_before();
     __syncthreads();
+    if (tid == 0 && bars->abort_flag) atomicCAS(&g_window_error, 0, bars->abort_flag);
     if (warp == 0) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512) : "memory");
@@ -724,19 +744,26 @@ EncodeTiled encoder() {
     return fn;
 }
 
-// Map over rows of D 16-bit elements, boxes of 64 elements x box[1] x box[2] (x 1), 128-byte swizzle, zeros outside the tensor.
-bool make_map(CUtensorMap *m, const void *base, int rank, int D, const uint64_t *dim, const uint64_t *stride, uint32_t box1, uint32_t box2) {
+// Map over rows of 16-bit elements, 64 of them innermost: dims and byte strides of what lies outside of them, the box's extents
+// there; 128-byte swizzle, zeros outside the tensor.
+bool make_map(CUtensorMap *m, const void *base, int outer, const uint64_t *dim, const uint64_t *stride, const uint32_t *extent, uint64_t inner = 64) {
     EncodeTiled enc = encoder();
     if (!enc) return false;
-    const cuuint64_t gdim[4] = {(cuuint64_t)D, dim[0], dim[1], rank > 3 ? dim[2] : 1};
-    const cuuint64_t gstride[3] = {stride[0], stride[1], rank > 3 ? stride[2] : 16};
-    const cuuint32_t box[4] = {64u, box1, box2, 1u}, one[4] = {1u, 1u, 1u, 1u};
-    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, rank, const_cast<void *>(base), gdim, gstride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    cuuint64_t gdim[5] = {inner}, gstride[4];
+    cuuint32_t box[5] = {64u}, one[5] = {1u, 1u, 1u, 1u, 1u};
+    for (int i = 0; i < outer; ++i) {
+        gdim[i + 1] = dim[i];
+        gstride[i] = stride[i];
+        box[i + 1] = extent[i];
+    }
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, outer + 1, const_cast<void *>(base), gdim, gstride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-bool rows_map(CUtensorMap *m, const WinRows &r, int heads, int tokens, int D, uint32_t box_heads, uint32_t box_tokens) {
-    const uint64_t dim[2] = {(uint64_t)heads, (uint64_t)tokens}, st[2] = {(uint64_t)r.hs, (uint64_t)r.ts};
-    return make_map(m, r.p, 3, D, dim, st, box_heads, box_tokens);
+// [half][token][head][64]: all halves of TN tokens of one head are one copy
+bool keys_map(CUtensorMap *m, const WinRows &r, int heads, int tokens, uint64_t halves) {
+    const uint64_t dim[3] = {(uint64_t)heads, (uint64_t)tokens, halves}, st[3] = {(uint64_t)r.hs, (uint64_t)r.ts, 128};
+    const uint32_t box[3] = {1, TN, (uint32_t)halves};
+    return make_map(m, r.p, 3, dim, st, box);
 }
 
 template <typename T, int D>
@@ -747,13 +774,16 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     p.tpt = TM / p.gb;
     p.hblocks = (w.g + p.gb - 1) / p.gb;
     CUtensorMap mq, mk, mv, mkc, mvc;
-    if (!rows_map(&mq, w.q, w.hq, w.tokens, D, p.gb, p.tpt) || !rows_map(&mk, w.k, w.hk, w.tokens, D, 1, TN) || !rows_map(&mv, w.v, w.hk, w.tokens, D, 1, TN))
+    const uint64_t qdim[2] = {(uint64_t)w.hq, (uint64_t)w.tokens}, qst[2] = {(uint64_t)w.q.hs, (uint64_t)w.q.ts};
+    const uint32_t qbox[2] = {(uint32_t)p.gb, (uint32_t)p.tpt};
+    if (!make_map(&mq, w.q.p, 2, qdim, qst, qbox, D) || !keys_map(&mk, w.k, w.hk, w.tokens, D / 64) || !keys_map(&mv, w.v, w.hk, w.tokens, D / 64))
         return cudaErrorNotSupported;
     mkc = mk; mvc = mv;
     if (w.kc) {
-        const uint64_t dim[3] = {(uint64_t)w.sinks + w.window, (uint64_t)w.hk, (uint64_t)w.sequences};
-        const uint64_t st[3] = {(uint64_t)w.cls, (uint64_t)w.chs, (uint64_t)w.css};
-        if (!make_map(&mkc, w.kc, 4, D, dim, st, TN, 1) || !make_map(&mvc, w.vc, 4, D, dim, st, TN, 1)) return cudaErrorNotSupported;
+        const uint64_t dim[4] = {(uint64_t)w.sinks + w.window, (uint64_t)w.hk, (uint64_t)w.sequences, D / 64};
+        const uint64_t st[4] = {(uint64_t)w.cls, (uint64_t)w.chs, (uint64_t)w.css, 128};
+        const uint32_t box[4] = {TN, 1, 1, D / 64};
+        if (!make_map(&mkc, w.kc, 4, dim, st, box) || !make_map(&mvc, w.vc, 4, dim, st, box)) return cudaErrorNotSupported;
     }
     auto kern = sh_window_prefill_umma_kernel<T, D>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM);
