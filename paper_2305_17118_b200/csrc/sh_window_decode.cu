@@ -11,6 +11,8 @@
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
+#include <type_traits>
+
 #include "sh_rope.cuh"
 #include "sh_umma.cuh"
 #include "sh_window.cuh"
@@ -28,8 +30,8 @@ constexpr int R = 2;                 // rows in flight per group of eight lanes
 constexpr int BLOCK = 4 * R;         // rows of a warp per pass
 
 // q rows (fp32) and the new token's key and value (as the cache holds them) into shared memory, prepared by `rope` if there is one.
-template <typename T, int D, int GQ>
-__device__ __forceinline__ void stage_token(const WindowParams &p, int seq, int kvh, int h0, int nq, float *qs, float *ks, float *vs) {
+template <typename T, int D, int WARPS>
+__device__ __forceinline__ void stage_token(const WindowParams &p, int seq, int kvh, int h0, int nq, float qscale, float *qs, float *ks, float *vs) {
     constexpr int LPR = D / 16, ROWS = 32 / LPR;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pl = lane % LPR, sub = lane / LPR;
     // rows: the nq queries, the key, the value
@@ -65,7 +67,7 @@ __device__ __forceinline__ void stage_token(const WindowParams &p, int seq, int 
 #pragma unroll
                 for (int i = 0; i < 16; i += Vec<T>::N) Vec<T>::unpack(Vec<T>::pack(x + i), x + i);
             }
-            const float f = is_q ? p.scale_log2e : 1.f;
+            const float f = is_q ? qscale : 1.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) { dst[e0 + i] = x[i] * f; dst[e1 + i] = x[8 + i] * f; }
         }
@@ -89,7 +91,7 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
     const int live = min(t, p.sinks + p.window), snew = slot_of(t, p.sinks, p.window);
     for (int i = tid; i < GQ * D; i += NT) qs[i] = 0.f;
     __syncthreads();
-    stage_token<T, D, GQ>(p, seq, kvh, h0, nq, qs, ks, vs);
+    stage_token<T, D, WARPS>(p, seq, kvh, h0, nq, p.scale_log2e, qs, ks, vs);
     __syncthreads();
 
     float m[GQ], l[GQ], o[GQ][EL];
@@ -240,42 +242,341 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
     cluster.sync();      // nobody's shared memory goes away while it is read
 }
 
-template <typename T, int D, int GQ>
-cudaError_t launch(const WindowParams &p, cudaStream_t s) {
-    const int qblocks = (p.g + GQ - 1) / GQ;
+// ---------------------------------------------------------------------------------------------------------------------
+// 16-bit types: the same on warp-level MMAs (m16n8k16, fp32 accumulation).
+//
+// A warp takes blocks of 16 rows: S[q][key] = Q.K^T with the queries as M, O^T[d][q] += V^T.P^T with d as M, so that the
+// accumulators of S are, lane by lane, the B operand of the second product.  Up to 8 query heads share a pass over the rows.  The
+// other 8 rows of M hold what rounding a prepared query to 16 bits leaves (zero for queries that come as they are), and P enters as
+// two 16-bit parts, so the step is as exact as fp32 arithmetic on the stored rows.  The arithmetic is a fifth of what the
+// tensor pipe can do; the kernel is bound by HBM.
+//
+// Each warp brings its rows in by cp.async, 16 bytes a lane, into a ring of its own (no barrier on the way; pieces permuted by
+// row so that ldmatrix reads without bank conflicts).  Rows that hold no token are filled with zeros and never read.
+constexpr int MW = 4;                // warps of a CTA
+constexpr int MB = 16;               // rows of a block
+constexpr int MQ = 8;                // query heads of a unit
+
+template <int D> struct Mma {
+    static constexpr int STAGES = D == 128 ? 3 : 6;
+    static constexpr int ROW = 2 * D, TILE = MB * ROW, STAGE = 2 * TILE;      // bytes: a row, 16 rows, key and value rows of a block
+    static constexpr int OFF_Q = MW * STAGES * STAGE;                         // [16][D]: high parts of the queries, low parts
+    static constexpr int OFF_NEW = OFF_Q + 16 * ROW;                          // the new token's key and value, 16 bits
+    static constexpr int OFF_F32 = OFF_NEW + 2 * ROW;                         // [MQ + 2][D] fp32: the same rows before the rounding
+    static constexpr int OFF_PART = OFF_F32;                                  // (later) this CTA's maximum, sum, output: [MQ][D + 2]
+    static constexpr int SMEM = OFF_F32 + (MQ + 2) * D * 4;
+    static_assert(MQ * (D + 2) <= (MQ + 2) * D, "");
+    static_assert(STAGES * STAGE >= MQ * (D + 2) * 4, "a warp's result takes the place of its ring");
+};
+
+__device__ __forceinline__ void cp16_or_zero(uint32_t dst, const void *src, bool take) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <typename T> __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <> __device__ __forceinline__ void mma16816<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// (x, y) as 16-bit pairs hi + lo
+template <typename T> __device__ __forceinline__ void split2(float x, float y, uint32_t &hi, uint32_t &lo) {
+    hi = Vec<T>::pack2(x, y);
+    float a, b;
+    if constexpr (std::is_same<T, __half>::value) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
+        a = f.x; b = f.y;
+    } else {
+        a = __uint_as_float(hi << 16); b = __uint_as_float(hi & 0xffff0000u);
+    }
+    lo = Vec<T>::pack2(x - a, y - b);
+}
+
+// One query by the D / 8 lanes that finish it: every live row once, in fp32.
+template <typename T, int D>
+__device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, int live, int snew, const unsigned char *qs, int q, const unsigned char *fresh,
+                                       char *dst) {
+    constexpr int CHUNKS = D / 8;
+    const int c = threadIdx.x % CHUNKS;
+    const unsigned group = ((1u << CHUNKS) - 1u) << ((threadIdx.x & 31) & ~(CHUNKS - 1));
+    float hi[8], lo[8], o[8], m = -CUDART_INF_F, l = 0.f;
+    Vec<T>::unpack(*reinterpret_cast<const uint4 *>(qs + q * 2 * D + ((c ^ (q & 7)) << 4)), hi);
+    Vec<T>::unpack(*reinterpret_cast<const uint4 *>(qs + (q + 8) * 2 * D + ((c ^ (q & 7)) << 4)), lo);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        hi[e] = (isfinite(hi[e]) ? hi[e] + lo[e] : hi[e]) * p.scale_log2e;
+        o[e] = 0.f;
+    }
+    for (int j = 0; j < live; ++j) {
+        const long long off = seq * p.css + kvh * p.chs + j * p.cls + c * 16;
+        float k[8], v[8];
+        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(j == snew ? reinterpret_cast<const char *>(fresh) + c * 16 : p.kc + off), k);
+        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(j == snew ? reinterpret_cast<const char *>(fresh) + 2 * D + c * 16 : p.vc + off), v);
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(hi[e], k[e], s);
+#pragma unroll
+        for (int x = CHUNKS / 2; x; x >>= 1) s += __shfl_xor_sync(group, s, x);
+        const float mn = fmaxf(m, s), b = mn == -CUDART_INF_F ? 0.f : mn, keep = ex2_approx(m - b), w = ex2_approx(s - b);
+        m = mn;
+        l = l * keep + w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = fmaf(w, v[e], o[e] * keep);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] /= l;
+    *reinterpret_cast<uint4 *>(dst + c * 16) = Vec<T>::pack(o);
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __grid_constant__ WindowParams p, int qblocks) {
+    using C = Mma<D>;
+    constexpr int CHUNKS = D / 8;                     // 16-byte pieces of a row
+    extern __shared__ __align__(128) unsigned char sm[];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int S = cluster.num_blocks(), rank = cluster.block_rank();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const long long unit = blockIdx.x / S;
+    const int qb = (int)(unit % qblocks), kvh = (int)(unit / qblocks % p.hk), seq = (int)(unit / qblocks / p.hk);
+    const int t = min(p.lengths[seq], MAX_POS);
+    if (t < 0) return;                                // idle: the whole cluster leaves
+    const int h0 = kvh * p.g + qb * MQ, nq = min(MQ, p.g - qb * MQ);
+    const int live = min(t + 1, p.sinks + p.window), snew = slot_of(t, p.sinks, p.window);      // rows after the append
+    const char *kc = p.kc + seq * p.css + kvh * p.chs, *vc = p.vc + seq * p.css + kvh * p.chs;
+    const uint32_t ring = shasync::smem_u32(sm) + warp * C::STAGES * C::STAGE;
+
+    // rows base .. base + 15 into a stage: a pass of the warp brings 32 / CHUNKS rows of keys and of values
+    const int crow = lane / CHUNKS, cchunk = lane % CHUNKS;
+    auto request = [&](int base, int st) {
+#pragma unroll
+        for (int i = 0; i < MB; i += 32 / CHUNKS) {
+            const int r = i + crow, j = base + r;
+            const bool take = j < live && j != snew;
+            const long long off = take ? j * p.cls + cchunk * 16 : 0;
+            const uint32_t dst = ring + st * C::STAGE + r * C::ROW + ((cchunk ^ (r & 7)) << 4);
+            cp16_or_zero(dst, kc + off, take);
+            cp16_or_zero(dst + C::TILE, vc + off, take);
+        }
+    };
+    const int first = (rank * MW + warp) * MB, stride = S * MW * MB;
+    int ahead = first;
+#pragma unroll
+    for (int st = 0; st < C::STAGES - 1; ++st, ahead += stride) {
+        if (ahead < live) request(ahead, st);
+        shumma::cp_async_commit();
+    }
+    // the token: prepared in fp32, then queries as two 16-bit parts, key and value as the cache holds them
+    float *rows = reinterpret_cast<float *>(sm + C::OFF_F32);
+    stage_token<T, D, MW>(p, seq, kvh, h0, nq, 1.f, rows, rows + MQ * D, rows + (MQ + 1) * D);
+    __syncthreads();
+    for (int i = tid; i < (MQ + 2) * CHUNKS; i += MW * 32) {
+        const int r = i / CHUNKS, c = i % CHUNKS;
+        uint32_t hi[4] = {}, lo[4] = {};
+        if (r < nq || r >= MQ) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split2<T>(rows[r * D + c * 8 + 2 * e], rows[r * D + c * 8 + 2 * e + 1], hi[e], lo[e]);
+        }
+        const uint4 h4 = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        if (r < MQ) {
+            *reinterpret_cast<uint4 *>(sm + C::OFF_Q + r * C::ROW + ((c ^ (r & 7)) << 4)) = h4;
+            *reinterpret_cast<uint4 *>(sm + C::OFF_Q + (r + 8) * C::ROW + ((c ^ (r & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        } else {
+            *reinterpret_cast<uint4 *>(sm + C::OFF_NEW + (r - MQ) * C::ROW + c * 16) = h4;
+        }
+    }
+    __syncthreads();
+    // Q fragments: for each 16 of d, rows 0-7 and 8-15 by d 0-7 and 8-15
+    uint32_t qf[D / 16][4];
+    const int mrow = (lane & 7) + ((lane >> 3) & 1) * 8, mcol = lane >> 4;      // ldmatrix: this lane's row and piece among four 8 x 8 blocks
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) ldsm4(shasync::smem_u32(sm) + C::OFF_Q + mrow * C::ROW + (((2 * k + mcol) ^ (mrow & 7)) << 4), qf[k]);
+
+    float o[D / 16][4];
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.f;
+    float m = -CUDART_INF_F, l = 0.f;                 // of query lane / 4; l: this lane's keys only
+    int st = 0;
+    for (int base = first; base < live; base += stride) {
+        cp_wait<C::STAGES - 2>();
+        __syncwarp();                                 // everyone's pieces of this block are there, everyone has left the block before
+        const int nst = st == 0 ? C::STAGES - 1 : st - 1;
+        if (ahead < live) request(ahead, nst);
+        shumma::cp_async_commit();
+        ahead += stride;
+        const uint32_t kt = ring + st * C::STAGE, vt = kt + C::TILE;
+        if (snew >= base && snew < base + MB) {       // the new token's rows
+            const int r = snew - base;
+            if (lane < CHUNKS) {
+                unsigned char *dst = sm + (kt - shasync::smem_u32(sm)) + r * C::ROW + ((lane ^ (r & 7)) << 4);
+                const uint4 kk = *reinterpret_cast<const uint4 *>(sm + C::OFF_NEW + lane * 16), vv = *reinterpret_cast<const uint4 *>(sm + C::OFF_NEW + C::ROW + lane * 16);
+                *reinterpret_cast<uint4 *>(dst) = kk;
+                *reinterpret_cast<uint4 *>(dst + C::TILE) = vv;
+                if (qb == 0) {                        // (one unit of the key head stores them)
+                    *reinterpret_cast<uint4 *>(p.kc + seq * p.css + kvh * p.chs + snew * p.cls + lane * 16) = kk;
+                    *reinterpret_cast<uint4 *>(p.vc + seq * p.css + kvh * p.chs + snew * p.cls + lane * 16) = vv;
+                }
+            }
+            __syncwarp();
+        }
+        float s[2][4] = {};                           // keys 0-7, 8-15 of the block; two chains each would not pay: the pipe is far from full
+        const int krow = lane & 7, kcol = lane >> 3;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                uint32_t b[4];
+                ldsm4(kt + (n * 8 + krow) * C::ROW + (((4 * k + kcol) ^ krow) << 4), b);
+                mma16816<T>(s[n], qf[2 * k], b[0], b[1]);
+                mma16816<T>(s[n], qf[2 * k + 1], b[2], b[3]);
+            }
+        float x[4];                                   // scores of query lane / 4 with keys 2 (lane % 4), + 1, + 8, + 9
+        const int j = base + 2 * (lane & 3);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) x[2 * n + e] = j + 8 * n + e < live ? (s[n][e] + s[n][2 + e]) * p.scale_log2e : -CUDART_INF_F;
+        float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        // the subtracted maximum is renewed when it has grown by more than 8 (log2): weights stay below 2^8
+        if (__any_sync(0xffffffffu, mx - m > 8.f)) {
+            const float mn = fmaxf(m, mx), f = mn == -CUDART_INF_F ? 1.f : ex2_approx(m - mn);
+            m = mn;
+            l *= f;
+            const float f0 = __shfl_sync(0xffffffffu, f, (lane & 3) * 8), f1 = __shfl_sync(0xffffffffu, f, (lane & 3) * 8 + 4);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) { o[k][0] *= f0; o[k][1] *= f1; o[k][2] *= f0; o[k][3] *= f1; }
+        }
+        const float mb = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = ex2_approx(x[e] - mb);
+        l += (x[0] + x[1]) + (x[2] + x[3]);
+        uint32_t h0p, l0p, h1p, l1p;
+        split2<T>(x[0], x[1], h0p, l0p);
+        split2<T>(x[2], x[3], h1p, l1p);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {            // 16 of d: blocks (keys 0-7, d 0-7), (keys 0-7, d 8-15), (keys 8-15, ..) transposed
+            uint32_t a[4];
+            const int vrow = (lane & 7) + (lane >> 4) * 8, vcol = 2 * k + ((lane >> 3) & 1);
+            ldsm4_t(vt + vrow * C::ROW + ((vcol ^ (vrow & 7)) << 4), a);
+            mma16816<T>(o[k], a, h0p, h1p);
+            mma16816<T>(o[k], a, l0p, l1p);
+        }
+        st = st == C::STAGES - 1 ? 0 : st + 1;
+    }
+    cp_wait<0>();
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    __syncwarp();
+    // this warp's result in place of its ring: [query][maximum, sum, output]
+    float *mine = reinterpret_cast<float *>(sm + warp * C::STAGES * C::STAGE);
+    if ((lane & 3) == 0) { mine[(lane >> 2) * (D + 2)] = m; mine[(lane >> 2) * (D + 2) + 1] = l; }
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine[(2 * (lane & 3) + (e & 1)) * (D + 2) + 2 + 16 * k + (lane >> 2) + (e >> 1) * 8] = o[k][e];
+    __syncthreads();
+    float *cta = reinterpret_cast<float *>(sm + C::OFF_PART);
+    auto warp_part = [&](int w) { return reinterpret_cast<const float *>(sm + w * C::STAGES * C::STAGE); };
+    for (int i = tid; i < nq * D; i += MW * 32) {
+        const int q = i / D, d = i % D;
+        float M = -CUDART_INF_F, L = 0.f, acc = 0.f;
+#pragma unroll
+        for (int w = 0; w < MW; ++w) M = fmaxf(M, warp_part(w)[q * (D + 2)]);
+        const float mb = M == -CUDART_INF_F ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < MW; ++w) {
+            const float *c = warp_part(w) + q * (D + 2);
+            const float f = ex2_approx(c[0] - mb);
+            L += c[1] * f;
+            acc += c[2 + d] * f;
+        }
+        cta[q * (D + 2) + 2 + d] = acc;
+        if (d == 0) { cta[q * (D + 2)] = M; cta[q * (D + 2) + 1] = L; }
+    }
+    cluster.sync();
+    if (rank == 0 && tid / CHUNKS < nq) {             // one CTA finishes: a thread per 8 elements
+        const int q = tid / CHUNKS, d = tid % CHUNKS * 8;
+        float M = -CUDART_INF_F, L = 0.f, acc[8] = {};
+        for (int r = 0; r < S; ++r) M = fmaxf(M, cluster.map_shared_rank(cta + q * (D + 2), r)[0]);
+        const float mb = M == -CUDART_INF_F ? 0.f : M;
+        for (int r = 0; r < S; ++r) {
+            const float *c = cluster.map_shared_rank(cta + q * (D + 2), r);
+            const float f = ex2_approx(c[0] - mb);
+            L += c[1] * f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = fmaf(c[2 + d + e], f, acc[e]);
+        }
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            acc[e] /= L;
+            odd |= !isfinite(acc[e]);
+        }
+        char *dst = p.out.p + seq * p.out.ts + (h0 + q) * p.out.hs;
+        // the low part of a weight or of a query may be zero and meet an infinity: such rows are computed again in plain fp32
+        const unsigned group = ((1u << CHUNKS) - 1u) << (lane & ~(CHUNKS - 1));
+        if (__any_sync(group, odd))
+            plain_row<T, D>(p, seq, kvh, live, snew, sm + C::OFF_Q, q, sm + C::OFF_NEW, dst);
+        else
+            *reinterpret_cast<uint4 *>(dst + d * 2) = Vec<T>::pack(acc);
+    }
+    cluster.sync();                                   // nobody's shared memory goes away while it is read
+}
+
+// Launch `kern` over units of S CTAs.  S: few units split the axis of keys while that fills SMs (ctas: what the device holds at once)
+// and leaves each CTA `least` rows.
+template <typename K>
+cudaError_t launch_units(K kern, const WindowParams &p, int qblocks, int threads, size_t smem, int per_sm, int least, cudaStream_t s) {
     const long long units = (long long)p.sequences * p.hk * qblocks;
     int sms = 0, dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && smem > 48 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    // few units: split the axis of keys while that fills SMs and leaves each CTA two passes of its warps at least
     int S = 1;
-    while (S < 8 && units * S * 2 <= 2 * sms && (p.window + p.sinks) >= 2 * S * 2 * WARPS * BLOCK) S *= 2;
+    while (S < 8 && units * S * 2 <= (long long)per_sm * sms && p.window + p.sinks >= 2 * S * least) S *= 2;
     if (units * S > 0x7fffffffll) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(units * S));
-    cfg.blockDim = dim3(NT);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = S; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, sh_window_decode_simt_kernel<T, D, GQ>, p, qblocks);
+    return cudaLaunchKernelEx(&cfg, kern, p, qblocks);
 }
 
-template <typename T, int D>
-cudaError_t launch_g(const WindowParams &p, cudaStream_t s) {
-    return p.g == 1 ? launch<T, D, 1>(p, s) : (p.g == 2 ? launch<T, D, 2>(p, s) : launch<T, D, 4>(p, s));
+template <int D, int GQ>
+cudaError_t launch_simt(const WindowParams &p, cudaStream_t s) {
+    return launch_units(sh_window_decode_simt_kernel<float, D, GQ>, p, (p.g + GQ - 1) / GQ, NT, 0, 2, 2 * WARPS * BLOCK, s);
 }
-template <typename T>
-cudaError_t launch_d(const WindowParams &p, int D, cudaStream_t s) {
-    return D == 128 ? launch_g<T, 128>(p, s) : launch_g<T, 64>(p, s);
+template <int D>
+cudaError_t launch_f32(const WindowParams &p, cudaStream_t s) {
+    return p.g == 1 ? launch_simt<D, 1>(p, s) : (p.g == 2 ? launch_simt<D, 2>(p, s) : launch_simt<D, 4>(p, s));
+}
+template <typename T, int D>
+cudaError_t launch_mma(const WindowParams &p, cudaStream_t s) {
+    return launch_units(sh_window_decode_mma_kernel<T, D>, p, (p.g + MQ - 1) / MQ, MW * 32, Mma<D>::SMEM, 2, 2 * MW * MB, s);
 }
 
 }  // namespace
 
 cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, cudaStream_t s) {
-    if (dtype == SH_F32) return launch_d<float>(p, D, s);
-    return dtype == SH_F16 ? launch_d<__half>(p, D, s) : launch_d<__nv_bfloat16>(p, D, s);
+    if (dtype == SH_F32) return D == 128 ? launch_f32<128>(p, s) : launch_f32<64>(p, s);
+    if (dtype == SH_F16) return D == 128 ? launch_mma<__half, 128>(p, s) : launch_mma<__half, 64>(p, s);
+    return D == 128 ? launch_mma<__nv_bfloat16, 128>(p, s) : launch_mma<__nv_bfloat16, 64>(p, s);
 }

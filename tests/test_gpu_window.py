@@ -325,6 +325,35 @@ def test_cache_offsets_pass_32_bits():
         assert ((out[0, h].double().cpu() - want).abs() <= 2.0 ** -25 + want * 2.0 ** -10).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_infinite_values_in_sight_come_out(dtype):
+    """An infinite value that a query sees makes that element of its output infinite, and no other element."""
+    sh, gen, dt = _sh(), _gen(26), DT[dtype]
+    n, d, g, inf = 200, 128, 3, float("inf")
+    q, k, v = _rnd(gen, n, g, d, dtype=dt), _rnd(gen, n, 1, d, dtype=dt), _rnd(gen, n, 1, d, dtype=dt)
+    v[120, 0, 17] = inf
+    v[130, 0, 40] = -inf
+    out = sh.window_prefill(q, k, v, _i32([0, n]), window=60, sinks=1)
+    kc, vc = torch.zeros(1, 1, 61, d, dtype=dt, device="cuda"), torch.zeros(1, 1, 61, d, dtype=dt, device="cuda")
+    sh.window_append(k[:-1], v[:-1], _i32([0, n - 1]), _i32([0]), kc, vc, window=60, sinks=1)
+    late = v.clone()
+    late[150, 0, 17], late[n - 1, 0, 99] = inf, inf
+    sh.window_append(k[:-1], late[:-1], _i32([0, n - 1]), _i32([0]), kc, vc, window=60, sinks=1)
+    step = sh.window_decode(q[-1:], k[-1:], late[-1:], _i32([n - 1]), kc, vc, window=60, sinks=1)
+    for i in range(n):
+        want = torch.zeros(d)
+        want[17] = inf if 120 <= i < 180 else 0
+        want[40] = -inf if 130 <= i < 190 else 0
+        for h in range(g):
+            got = out[i, h].float().cpu()
+            assert torch.equal(torch.where(torch.isinf(got), got, 0.0), want) and not torch.isnan(got).any(), i
+    want = torch.zeros(d)
+    want[17], want[99] = inf, inf
+    for h in range(g):
+        got = step[0, h].float().cpu()
+        assert torch.equal(torch.where(torch.isinf(got), got, 0.0), want) and not torch.isnan(got).any()
+
+
 # ------------------------------------------------------------------------------------------------ together
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_a_served_batch_from_prompts_to_tokens(dtype):
