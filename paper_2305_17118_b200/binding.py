@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Tuple
 
 import numpy as np
@@ -105,7 +106,7 @@ def declare(lib: C.CDLL) -> C.CDLL:
     lib.sh_strerror.restype = C.c_char_p
     lib.sh_last_cuda_error.argtypes = [vp]
     lib.sh_last_cuda_error.restype = C.c_char_p
-    rows, cache, window, rope = C.POINTER(_Rows), C.POINTER(_WindowCache), C.POINTER(_Window), C.POINTER(_Rope)
+    rows = cache = window = rope = vp      # (structs arrive as packed bytes or by reference)
     lib.sh_qk_norm_rope.argtypes = [rope, C.c_int, C.c_int, C.c_int, rows, rows, vp, C.c_longlong, rows, rows, vp]
     lib.sh_window_prefill.argtypes = [window, C.c_int, C.c_int, rows, rows, rows, vp, vp, cache, rows, vp]
     lib.sh_window_append.argtypes = [window, C.c_int, C.c_int, rows, rows, vp, vp, cache, vp]
@@ -395,7 +396,12 @@ def select(counters: torch.Tensor, r: int, m: int, stream=None) -> torch.Tensor:
 
 
 # -- query/key preparation and the window cache (no handle: tensors in, tensors out) ---------------------------------
+# The wrappers sit on the path of every decoded token, so they look at each tensor once and hand the structs over as bytes packed
+# in C layout (the layout of _Rows, _WindowCache, _Window and _Rope above).
 _CODE_OF = {torch.float32: SH_F32, torch.float16: SH_F16, torch.bfloat16: SH_BF16}
+_pack_rows, _pack_cache = struct.Struct("Pqq").pack, struct.Struct("PPqqq").pack
+_pack_window, _pack_rope = struct.Struct("iiiiiid").pack, struct.Struct("9ifPPP").pack
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
 
 
 def _fail(what: str, need: str, t) -> None:
@@ -403,28 +409,66 @@ def _fail(what: str, need: str, t) -> None:
     raise ValueError(f"{what}: need {need}, got {got}")
 
 
-def _check_rows(t, what: str, like: Optional[torch.Tensor] = None, shape=None) -> None:
-    """``t`` holds rows [tokens, heads, head_dim] of a supported type, on the device and of the type of ``like``."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in _CODE_OF and t.shape[2] in (64, 128)
-            and (t.stride(2) == 1 or t.numel() == 0)):
-        _fail(what, "a CUDA tensor [tokens, heads, 64 or 128] of f32, f16 or bf16 with contiguous rows", t)
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        _fail(what, f"{like.dtype} on {like.device}", t)
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        _fail(what, f"shape {tuple(shape)}", t)
+def _head_rows(t, what: str):
+    """Shape, type, device and packed sh_rows of rows [tokens, heads, head_dim]."""
+    if isinstance(t, torch.Tensor) and t.dim() == 3:
+        shape, dtype, device = t.shape, t.dtype, t.get_device()
+        ts, hs, es = t.stride()
+        if device >= 0 and dtype in _CODE_OF and (shape[2] == 64 or shape[2] == 128) and (es == 1 or t.numel() == 0):
+            return shape, dtype, device, _pack_rows(t.data_ptr(), ts, hs)
+    _fail(what, "a CUDA tensor [tokens, heads, 64 or 128] of f32, f16 or bf16 with contiguous rows", t)
 
 
-def _check_ints(t, what: str, shape, device) -> None:
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype == torch.int32 and tuple(t.shape) == tuple(shape)
-            and (t.numel() <= 1 or t.stride(-1) == 1)):
-        _fail(what, f"an int32 tensor {tuple(shape)} on {device}, contiguous along its last dimension", t)
+def _more_rows(t, what: str, shape, dtype, device):
+    """Packed sh_rows of a tensor that must look like the first one."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape):
+        _fail(what, f"{tuple(shape)} of {dtype} on cuda:{device}", t)
+    ts, hs, es = t.stride()
+    if es != 1 and t.numel():
+        _fail(what, "contiguous rows", t)
+    return _pack_rows(t.data_ptr(), ts, hs)
 
 
-def _rows(t: torch.Tensor) -> _Rows:
-    return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+def _key_rows(k, what: str, tokens: int, d: int, dtype, device):
+    """The same for keys, whose number of heads is free: (shape, packed sh_rows)."""
+    if not (isinstance(k, torch.Tensor) and k.dim() == 3):
+        _fail(what, "a tensor [tokens, heads, head_dim]", k)
+    shape = k.shape
+    if shape[0] != tokens or shape[2] != d:
+        _fail(what, f"[{tokens}, heads, {d}]", k)
+    return shape, _more_rows(k, what, shape, dtype, device)
 
 
-def _check_status(rc: int, what: str) -> None:
+def _ints(t, what: str, n: int, device: int) -> int:
+    """Address of an int32 vector of n entries."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.get_device() == device and t.shape == (n,) and (n <= 1 or t.stride(0) == 1)):
+        _fail(what, f"a contiguous int32 vector of {n} entries on cuda:{device}", t)
+    return t.data_ptr()
+
+
+def _sequences(starts) -> int:
+    if not (isinstance(starts, torch.Tensor) and starts.dim() == 1 and starts.numel() >= 1):
+        _fail("starts", "an int32 vector of sequences + 1 entries", starts)
+    return starts.numel() - 1
+
+
+def _positions(positions, axes: int, tokens: int, device: int):
+    """(address, stride between axes) of [tokens] or [axes, tokens] positions."""
+    if axes == 1 and isinstance(positions, torch.Tensor) and positions.dim() == 1:
+        return _ints(positions, "positions", tokens, device), 0
+    if not (isinstance(positions, torch.Tensor) and positions.dtype is torch.int32 and positions.get_device() == device
+            and positions.shape == (axes, tokens) and (tokens <= 1 or positions.stride(1) == 1)):
+        _fail("positions", f"an int32 tensor [{axes}, {tokens}] on cuda:{device}, contiguous along its last dimension", positions)
+    return positions.data_ptr(), positions.stride(0)
+
+
+def _launch(what: str, fn, device: int, stream, *args) -> None:
+    """Call a library entry on the tensors' device and the given (or that device's current) stream."""
+    if device == _current_device():
+        rc = fn(*args, _raw_stream(device) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _raw_stream(device) if stream is None else stream.cuda_stream)
     if rc:
         raise ShError(rc, f"{what}: strides and addresses must be multiples of 16 bytes, outputs must not overlap themselves, "
                           f"and sizes must lie in the ranges the header states" if rc == SH_EINVAL else what)
@@ -455,32 +499,18 @@ class Rope:
                 _fail(what, f"a contiguous [head_dim] vector on {inv_freq.device}", w)
         self.inv_freq, self.q_weight, self.k_weight = inv_freq, q_weight, k_weight
         self.eps, self.sections, self.spread, self.adjacent = float(eps), sections, bool(spread), bool(adjacent)
+        self.axes = len(sections)
+        # what does not change from call to call (addresses are looked up each time: parameters can be moved)
+        self._head = (2 * pairs, self.axes, *(sections + (0, 0))[:3], int(self.spread), int(self.adjacent), self.eps)
 
-    @property
-    def axes(self) -> int:
-        return len(self.sections)
-
-    def _struct(self, like: torch.Tensor) -> _Rope:
-        if like.device != self.inv_freq.device:
-            _fail("rope", f"tensors on {like.device}", self.inv_freq)
-        for w, what in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight")):
-            if w is not None and (w.dtype != like.dtype or w.numel() != like.shape[2]):
-                _fail(what, f"[{like.shape[2]}] {like.dtype}", w)
-        sec = (C.c_int * 3)(*(self.sections + (0, 0))[:3])
-        ptr = lambda w: None if w is None else w.data_ptr()
-        return _Rope(_CODE_OF[like.dtype], like.shape[2], 2 * self.inv_freq.numel(), self.axes, sec, int(self.spread), int(self.adjacent),
-                     self.eps, self.inv_freq.data_ptr(), ptr(self.q_weight), ptr(self.k_weight))
-
-
-def _positions(positions: torch.Tensor, axes: int, tokens: int, device):
-    """(pointer, stride between axes) of [tokens] or [axes, tokens] positions."""
-    one = axes == 1 and isinstance(positions, torch.Tensor) and positions.dim() == 1
-    _check_ints(positions, "positions", (tokens,) if one else (axes, tokens), device)
-    return positions.data_ptr(), 0 if one else positions.stride(0)
-
-
-def _on(stream: Optional[torch.cuda.Stream], device) -> int:
-    return (stream or torch.cuda.current_stream(device)).cuda_stream
+    def _packed(self, d: int, dtype, device: int) -> bytes:
+        f, qw, kw = self.inv_freq, self.q_weight, self.k_weight
+        if f.get_device() != device or 2 * f.numel() != self._head[0]:
+            _fail("rope", f"{self._head[0] // 2} frequencies on cuda:{device}", f)
+        for w in (qw, kw):
+            if w is not None and (w.dtype is not dtype or w.shape != (d,) or w.get_device() != device):
+                _fail("weight", f"[{d}] of {dtype} on cuda:{device}", w)
+        return _pack_rope(_CODE_OF[dtype], d, *self._head, f.data_ptr(), 0 if qw is None else qw.data_ptr(), 0 if kw is None else kw.data_ptr())
 
 
 def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, rope: Rope, q_out: Optional[torch.Tensor] = None,
@@ -488,46 +518,44 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Te
     """``sh_qk_norm_rope``: rows ``q`` [tokens, q_heads, head_dim] and ``k`` [tokens, k_heads, head_dim] (or None), views of a packed
     projection included, normalised and rotated in one pass.  ``positions``: int32 [tokens], or [axes, tokens].
     Outputs default to new contiguous tensors; ``q_out=q`` works in place.  Returns (q_out, k_out)."""
-    _check_rows(q, "q")
-    tokens = q.shape[0]
+    shape, dtype, device, qr = _head_rows(q, "q")
+    tokens, q_heads, d = shape
+    kshape, kr, kor = (0, 0), None, None
     if k is not None:
-        _check_rows(k, "k", q, (tokens, k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 3 else 0, q.shape[2]))
+        kshape, kr = _key_rows(k, "k", tokens, d, dtype, device)
     elif k_out is not None:
         raise ValueError("k_out without k")
-    ro = rope._struct(q)
-    pos, axis_stride = _positions(positions, rope.axes, tokens, q.device)
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    _check_rows(q_out, "q_out", q, q.shape)
+    ro = rope._packed(d, dtype, device)
+    pos, axis_stride = _positions(positions, rope.axes, tokens, device)
+    q_out = q.new_empty(shape) if q_out is None else q_out
+    qor = _more_rows(q_out, "q_out", shape, dtype, device)
     if k is not None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
-        _check_rows(k_out, "k_out", q, k.shape)
-    with torch.cuda.device(q.device):
-        _check_status(lib.sh_qk_norm_rope(C.byref(ro), tokens, q.shape[1], 0 if k is None else k.shape[1], _rows(q),
-                                          None if k is None else _rows(k), pos, axis_stride, _rows(q_out),
-                                          None if k is None else _rows(k_out), _on(stream, q.device)), "qk_norm_rope")
+        k_out = k.new_empty(kshape) if k_out is None else k_out
+        kor = _more_rows(k_out, "k_out", kshape, dtype, device)
+    _launch("qk_norm_rope", lib.sh_qk_norm_rope, device, stream, ro, tokens, q_heads, kshape[1], qr, kr, pos, axis_stride, qor, kor)
     return q_out, k_out
 
 
-def _window_struct(t: torch.Tensor, q_heads: int, kv_heads: int, window: int, sinks: int, scale: Optional[float]) -> _Window:
+def _window_packed(dtype, d: int, q_heads: int, kv_heads: int, window: int, sinks: int, scale: Optional[float]) -> bytes:
     if window < 1 or sinks < 0 or window + sinks >= 1 << 30:
         raise ValueError(f"window {window}, sinks {sinks}: need window >= 1, sinks >= 0, together below 2^30")
     if kv_heads < 1 or q_heads < 1 or q_heads % kv_heads:
         raise ValueError(f"{q_heads} query heads, {kv_heads} key heads: the first must be a multiple of the second")
     if scale is not None and not (1e-30 < scale < 1e30):
         raise ValueError(f"scale {scale}: need a number between 1e-30 and 1e30")
-    return _Window(_CODE_OF[t.dtype], t.shape[2], q_heads, kv_heads, window, sinks, 0.0 if scale is None else float(scale))
+    return _pack_window(_CODE_OF[dtype], d, q_heads, kv_heads, window, sinks, 0.0 if scale is None else scale)
 
 
-def _cache_struct(k_cache, v_cache, like: torch.Tensor, sequences: int, kv_heads: int, slots: int) -> _WindowCache:
-    shape = (sequences, kv_heads, slots, like.shape[2])
+def _cache_packed(k_cache, v_cache, shape, dtype, device: int) -> bytes:
     for t, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if not (isinstance(t, torch.Tensor) and tuple(t.shape) == shape and t.dtype == like.dtype and t.device == like.device
-                and (t.numel() == 0 or t.stride(3) == 1)):
-            _fail(what, f"[sequences, key heads, sinks + window, head_dim] = {shape} of {like.dtype} on {like.device}", t)
-    walked = [i for i in range(3) if shape[i] > 1]
-    if any(k_cache.stride(i) != v_cache.stride(i) for i in walked):
-        _fail("v_cache", f"the strides of k_cache, {k_cache.stride()}", v_cache)
-    return _WindowCache(k_cache.data_ptr(), v_cache.data_ptr(), k_cache.stride(0), k_cache.stride(1), k_cache.stride(2))
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape):
+            _fail(what, f"[sequences, key heads, sinks + window, head_dim] = {shape} of {dtype} on cuda:{device}", t)
+    ks, vs = k_cache.stride(), v_cache.stride()
+    if ks[3] != 1 and k_cache.numel():
+        _fail("k_cache", "contiguous rows", k_cache)
+    if ks != vs and any(ks[i] != vs[i] for i in range(4) if shape[i] > 1):
+        _fail("v_cache", f"the strides of k_cache, {ks}", v_cache)
+    return _pack_cache(k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2])
 
 
 def window_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, *, window: int, sinks: int = 0,
@@ -539,25 +567,20 @@ def window_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: to
     device) continue sequence i, which holds ``lengths[i]`` tokens in ``k_cache``/``v_cache`` [sequences, kv_heads, sinks + window, head_dim]
     (all three None: fresh prompts).  A token sees those before it among the first ``sinks`` positions and the last ``window``, itself
     included.  Rows of ``out`` that belong to no sequence are left as they were (a new ``out`` is zeroed)."""
-    _check_rows(q, "q")
-    _check_rows(k, "k", q)
-    _check_rows(k, "k", q, (q.shape[0], k.shape[1], q.shape[2]))
-    _check_rows(v, "v", q, k.shape)
-    win = _window_struct(q, q.shape[1], k.shape[1], window, sinks, scale)
-    if not (isinstance(starts, torch.Tensor) and starts.dim() == 1 and starts.numel() >= 1):
-        _fail("starts", "an int32 vector of sequences + 1 entries", starts)
-    n = starts.numel() - 1
-    _check_ints(starts, "starts", (n + 1,), q.device)
-    cache = None
+    shape, dtype, device, qr = _head_rows(q, "q")
+    tokens, q_heads, d = shape
+    kshape, kr = _key_rows(k, "k", tokens, d, dtype, device)
+    vr = _more_rows(v, "v", kshape, dtype, device)
+    win = _window_packed(dtype, d, q_heads, kshape[1], window, sinks, scale)
+    n = _sequences(starts)
+    sp = _ints(starts, "starts", n + 1, device)
+    cache, lp = None, None
     if lengths is not None or k_cache is not None or v_cache is not None:
-        _check_ints(lengths, "lengths", (n,), q.device)
-        cache = C.byref(_cache_struct(k_cache, v_cache, q, n, k.shape[1], window + sinks))
-    out = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-    _check_rows(out, "out", q, q.shape)
-    with torch.cuda.device(q.device):
-        _check_status(lib.sh_window_prefill(C.byref(win), q.shape[0], n, _rows(q), _rows(k), _rows(v), starts.data_ptr(),
-                                            None if cache is None else lengths.data_ptr(), cache, _rows(out), _on(stream, q.device)),
-                      "window_prefill")
+        lp = _ints(lengths, "lengths", n, device)
+        cache = _cache_packed(k_cache, v_cache, (n, kshape[1], window + sinks, d), dtype, device)
+    out = q.new_zeros(shape) if out is None else out
+    _launch("window_prefill", lib.sh_window_prefill, device, stream, win, tokens, n, qr, kr, vr, sp, lp, cache,
+            _more_rows(out, "out", shape, dtype, device))
     return out
 
 
@@ -565,18 +588,13 @@ def window_append(k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, length
                   v_cache: torch.Tensor, *, window: int, sinks: int = 0, stream=None) -> None:
     """``sh_window_append``: store the chunks' keys and values (arguments as ``window_prefill``; ``lengths`` as before the chunk, the
     caller advances them)."""
-    _check_rows(k, "k")
-    _check_rows(v, "v", k, k.shape)
-    win = _window_struct(k, k.shape[1], k.shape[1], window, sinks, None)
-    if not (isinstance(starts, torch.Tensor) and starts.dim() == 1 and starts.numel() >= 1):
-        _fail("starts", "an int32 vector of sequences + 1 entries", starts)
-    n = starts.numel() - 1
-    _check_ints(starts, "starts", (n + 1,), k.device)
-    _check_ints(lengths, "lengths", (n,), k.device)
-    cache = _cache_struct(k_cache, v_cache, k, n, k.shape[1], window + sinks)
-    with torch.cuda.device(k.device):
-        _check_status(lib.sh_window_append(C.byref(win), k.shape[0], n, _rows(k), _rows(v), starts.data_ptr(), lengths.data_ptr(),
-                                           C.byref(cache), _on(stream, k.device)), "window_append")
+    shape, dtype, device, kr = _head_rows(k, "k")
+    tokens, kv_heads, d = shape
+    vr = _more_rows(v, "v", shape, dtype, device)
+    win = _window_packed(dtype, d, kv_heads, kv_heads, window, sinks, None)
+    n = _sequences(starts)
+    _launch("window_append", lib.sh_window_append, device, stream, win, tokens, n, kr, vr, _ints(starts, "starts", n + 1, device),
+            _ints(lengths, "lengths", n, device), _cache_packed(k_cache, v_cache, (n, kv_heads, window + sinks, d), dtype, device))
 
 
 def window_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -588,36 +606,33 @@ def window_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: to
     ``q`` [sequences, q_heads, head_dim], ``k``/``v`` [sequences, kv_heads, head_dim], ``lengths`` int32 [sequences]: tokens held before the
     step (the caller advances them); negative: an idle slot of the batch, whose ``out`` row and cache are left as they were (a new ``out``
     is zeroed).  ``positions`` as in ``qk_norm_rope``; default: ``lengths``."""
-    _check_rows(q, "q")
-    _check_rows(k, "k", q)
-    n = q.shape[0]
-    _check_rows(k, "k", q, (n, k.shape[1], q.shape[2]))
-    _check_rows(v, "v", q, k.shape)
-    win = _window_struct(q, q.shape[1], k.shape[1], window, sinks, scale)
-    _check_ints(lengths, "lengths", (n,), q.device)
-    cache = _cache_struct(k_cache, v_cache, q, n, k.shape[1], window + sinks)
+    shape, dtype, device, qr = _head_rows(q, "q")
+    n, q_heads, d = shape
+    kshape, kr = _key_rows(k, "k", n, d, dtype, device)
+    vr = _more_rows(v, "v", kshape, dtype, device)
+    win = _window_packed(dtype, d, q_heads, kshape[1], window, sinks, scale)
+    lp = _ints(lengths, "lengths", n, device)
+    cache = _cache_packed(k_cache, v_cache, (n, kshape[1], window + sinks, d), dtype, device)
     ro, pos, axis_stride = None, None, 0
     if rope is not None:
-        ro = C.byref(rope._struct(q))
+        ro = rope._packed(d, dtype, device)
         if positions is not None:
-            pos, axis_stride = _positions(positions, rope.axes, n, q.device)
+            pos, axis_stride = _positions(positions, rope.axes, n, device)
         elif rope.axes != 1:
             raise ValueError("a rope of several axes needs positions")
     elif positions is not None:
         raise ValueError("positions without rope")
-    out = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-    _check_rows(out, "out", q, q.shape)
-    with torch.cuda.device(q.device):
-        _check_status(lib.sh_window_decode(C.byref(win), n, _rows(q), _rows(k), _rows(v), lengths.data_ptr(), C.byref(cache), ro, pos,
-                                           axis_stride, _rows(out), _on(stream, q.device)), "window_decode")
+    out = q.new_zeros(shape) if out is None else out
+    _launch("window_decode", lib.sh_window_decode, device, stream, win, n, qr, kr, vr, lp, cache, ro, pos, axis_stride,
+            _more_rows(out, "out", shape, dtype, device))
     return out
 
 
 def window_status(device="cuda:0", stream=None) -> None:
     """``sh_window_status``: raise ShError(SH_EDEVICE) if a window kernel on ``device`` gave up one of its bounded waits since the last
     call (its outputs are then incomplete).  Synchronises the stream."""
-    with torch.cuda.device(device):
-        _check_status(lib.sh_window_status(_on(stream, torch.device(device))), "window_status")
+    index = torch.device(device).index
+    _launch("window_status", lib.sh_window_status, _current_device() if index is None else index, stream)
 
 
 class WindowCache:
@@ -631,12 +646,12 @@ class WindowCache:
         dt = INPUT_TORCH_DTYPE[DTYPE_CODE[dtype]] if isinstance(dtype, str) else dtype
         if dt not in _CODE_OF or dtype == "int4" or head_dim not in (64, 128):
             raise ValueError(f"dtype {dtype}, head_dim {head_dim}: need f32, f16 or bf16 and 64 or 128")
+        _window_packed(dt, head_dim, q_heads, kv_heads, window, sinks, scale)
         self.window, self.sinks, self.rope, self.scale, self.q_heads = window, sinks, rope, scale, q_heads
         shape = (sequences, kv_heads, sinks + window, head_dim)
         self.k = torch.zeros(shape, dtype=dt, device=device)
         self.v = torch.zeros(shape, dtype=dt, device=device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
-        _window_struct(self.k[0], q_heads, kv_heads, window, sinks, scale)
 
     def _prompt_positions(self, starts: torch.Tensor, tokens: int) -> torch.Tensor:
         """Position of each row of a chunk tensor: its sequence's length plus its place in the chunk."""

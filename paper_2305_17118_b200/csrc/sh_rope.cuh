@@ -7,11 +7,13 @@
 // 2^31 and a frequency of 1 is off by 2^-52 of itself, below 1e-7 turns, where fp32 would be off by whole turns) and handed to sincospif in fp32.
 #pragma once
 #include "sh_elem.cuh"
+#include "sh_pairs.cuh"
 #include "sh_window.h"
 
 namespace shrope {
 
 using shelem::Vec;
+using namespace shpair;
 
 // Element offsets of this lane's two runs of 8 elements.
 template <int D>
@@ -61,56 +63,96 @@ __device__ __forceinline__ void turns_of_lane(const RopeParams &r, long long t, 
     }
 }
 
-// x[0..7], x[8..15]: the lane's two runs.  Normalise this row if `norm` (w: the weights of the same elements) and rotate.
-// `any` is the same for the whole warp: some row of it is normalised (all lanes then take part in the sums).
-template <int D>
-__device__ __forceinline__ void apply(const RopeParams &r, int p, bool any, bool norm, const float (&w)[16], const float (&c)[8],
-                                      const float (&s)[8], float (&x)[16]) {
+// Sines and cosines arranged for packed pairs of fp32 (Blackwell's two-wide multiply-add): for pairs (i, i + rot/2) two
+// neighbouring i share a register pair, for (2i, 2i + 1) the two members of a pair do.
+template <bool ADJ> struct Turns {
+    static constexpr int N = ADJ ? 8 : 4;
+    uint64_t c[N], s[N], n[N];            // adjacent: n = (-sin, sin), s unused; else n = -s
+    __device__ __forceinline__ void set(const float (&cc)[8], const float (&ss)[8]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (ADJ) {
+                c[i] = f2(cc[i], cc[i]);
+                n[i] = f2(-ss[i], ss[i]);
+            } else {
+                c[i] = f2(cc[2 * i], cc[2 * i + 1]);
+                s[i] = f2(ss[2 * i], ss[2 * i + 1]);
+                n[i] = f2(-ss[2 * i], -ss[2 * i + 1]);
+            }
+        }
+    }
+};
+
+// x: the lane's 16 elements as 8 pairs (4 of each run).  With `any` (the same for the whole warp) the row is normalised: every element
+// times its weight w and the row's 1 / sqrt(mean + eps); a row of such a warp that is not (`norm` false, w = 1) keeps its values.
+template <int D, bool ADJ>
+__device__ __forceinline__ void apply(const RopeParams &r, int p, bool any, bool norm, const uint64_t (&w)[8], const Turns<ADJ> &turn, uint64_t (&x)[8]) {
     if (any) {
-        float ss = 0.f;
+        uint64_t ss = mul2(x[0], x[0]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
+        for (int i = 1; i < 8; ++i) ss = fma2(x[i], x[i], ss);
+        float lo, hi;
+        un2(ss, lo, hi);
+        lo += hi;
 #pragma unroll
-        for (int o = D / 32; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        const float inv = 1.f / sqrtf(ss * (1.f / D) + r.eps);
+        for (int o = D / 32; o; o >>= 1) lo += __shfl_xor_sync(0xffffffffu, lo, o);
+        const float inv = norm ? 1.f / sqrtf(lo * (1.f / D) + r.eps) : 1.f;
+        const uint64_t inv2 = f2(inv, inv);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = norm ? x[i] * inv * w[i] : x[i];
+        for (int i = 0; i < 8; ++i) x[i] = mul2(mul2(x[i], inv2), w[i]);
     }
     if (p >= r.rot / 16) return;
-    if (r.adjacent) {
+    if constexpr (ADJ) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float a = x[2 * i], b = x[2 * i + 1];
-            x[2 * i] = a * c[i] - b * s[i];
-            x[2 * i + 1] = a * s[i] + b * c[i];
+            float a, b;
+            un2(x[i], a, b);
+            x[i] = fma2(f2(b, a), turn.n[i], mul2(x[i], turn.c[i]));
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float a = x[i], b = x[8 + i];
-            x[i] = a * c[i] - b * s[i];
-            x[8 + i] = a * s[i] + b * c[i];
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t a = x[i], b = x[4 + i];
+            x[i] = fma2(b, turn.n[i], mul2(a, turn.c[i]));
+            x[4 + i] = fma2(b, turn.c[i], mul2(a, turn.s[i]));
         }
     }
 }
 
-// The lane's 16 elements of the row at `row` (a row of the element type T), and back.
+// The lane's 16 elements of a row: as 16-byte pieces, and as fp32.
+template <typename T> struct Raw {
+    static constexpr int PIECES = 8 / Vec<T>::N;      // of a run
+    uint4 a[2 * PIECES];
+};
 template <typename T>
-__device__ __forceinline__ void load16(const char *row, int e0, int e1, float (&x)[16]) {
-    constexpr int N = Vec<T>::N;
+__device__ __forceinline__ void load_raw(const char *row, int e0, int e1, Raw<T> &x) {
 #pragma unroll
-    for (int i = 0; i < 8; i += N) {
-        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(row + (e0 + i) * (int)sizeof(T)), x + i);
-        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(row + (e1 + i) * (int)sizeof(T)), x + 8 + i);
+    for (int i = 0; i < Raw<T>::PIECES; ++i) {
+        x.a[i] = *reinterpret_cast<const uint4 *>(row + (e0 + i * Vec<T>::N) * (int)sizeof(T));
+        x.a[Raw<T>::PIECES + i] = *reinterpret_cast<const uint4 *>(row + (e1 + i * Vec<T>::N) * (int)sizeof(T));
     }
 }
 template <typename T>
-__device__ __forceinline__ void store16(char *row, int e0, int e1, const float (&x)[16]) {
+__device__ __forceinline__ void unpack_raw(const Raw<T> &r, uint64_t (&x)[8]) {
     constexpr int N = Vec<T>::N;
 #pragma unroll
+    for (int i = 0; i < 2 * Raw<T>::PIECES; ++i) {
+        float f[N];
+        Vec<T>::unpack(r.a[i], f);
+#pragma unroll
+        for (int e = 0; e < N; e += 2) x[(i * N + e) / 2] = f2(f[e], f[e + 1]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store16(char *row, int e0, int e1, const uint64_t (&x)[8]) {
+    constexpr int N = Vec<T>::N;
+    float f[16];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) un2(x[i], f[2 * i], f[2 * i + 1]);
+#pragma unroll
     for (int i = 0; i < 8; i += N) {
-        *reinterpret_cast<uint4 *>(row + (e0 + i) * (int)sizeof(T)) = Vec<T>::pack(x + i);
-        *reinterpret_cast<uint4 *>(row + (e1 + i) * (int)sizeof(T)) = Vec<T>::pack(x + 8 + i);
+        *reinterpret_cast<uint4 *>(row + (e0 + i) * (int)sizeof(T)) = Vec<T>::pack(f + i);
+        *reinterpret_cast<uint4 *>(row + (e1 + i) * (int)sizeof(T)) = Vec<T>::pack(f + 8 + i);
     }
 }
 

@@ -2,6 +2,8 @@
 #pragma once
 #include <stdint.h>
 
+#include <atomic>
+
 #include "sh_internal.h"
 
 // Kernel-side forms of the public structs: byte strides, resolved options.
@@ -37,8 +39,25 @@ struct WindowParams {
     bool with_rope;
 };
 
+// SMs of the current device, and that a kernel may use `smem` bytes of shared memory there.  Both are facts of the device, asked once
+// (two threads that come first together both ask, and write the same).
+struct ShKernelSetup {
+    static constexpr int DEVICES = 64;
+    std::atomic<bool> done[DEVICES];
+};
+cudaError_t sh_device_sms(int *dev, int *sms);
+template <typename K>
+cudaError_t sh_setup_kernel(ShKernelSetup &setup, K kern, size_t smem, int *sms) {
+    int dev = 0;
+    cudaError_t e = sh_device_sms(&dev, sms);
+    if (e != cudaSuccess || (dev < ShKernelSetup::DEVICES && setup.done[dev].load(std::memory_order_relaxed))) return e;
+    if (smem > 48 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess && dev < ShKernelSetup::DEVICES) setup.done[dev].store(true, std::memory_order_relaxed);
+    return e;
+}
+
 cudaError_t sh_launch_qk_norm_rope(RopeParams p, int dtype, int D, cudaStream_t s);
-cudaError_t sh_launch_window_prefill_simt(const WindowParams &p, int dtype, int D, cudaStream_t s);
+cudaError_t sh_launch_window_prefill_f32(const WindowParams &p, int D, cudaStream_t s);
 // tensor cores: f16 and bf16
 cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int D, cudaStream_t s);
 // code of the first bounded wait that gave up in a window kernel of the current device since the last call (0: none); synchronises

@@ -105,6 +105,19 @@ int done(cudaError_t e) { return e == cudaSuccess ? SH_OK : SH_ECUDA; }
 
 }  // namespace
 
+cudaError_t sh_device_sms(int *dev, int *sms) {
+    static std::atomic<int> known[ShKernelSetup::DEVICES];
+    cudaError_t e = cudaGetDevice(dev);
+    if (e != cudaSuccess) return e;
+    const bool kept = *dev < ShKernelSetup::DEVICES;
+    *sms = kept ? known[*dev].load(std::memory_order_relaxed) : 0;
+    if (*sms == 0) {
+        e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev);
+        if (e == cudaSuccess && kept) known[*dev].store(*sms, std::memory_order_relaxed);
+    }
+    return e;
+}
+
 extern "C" {
 
 int sh_qk_norm_rope(const sh_rope *rope, int tokens, int q_heads, int k_heads, const sh_rows *q, const sh_rows *k, const int32_t *positions_dev,
@@ -145,7 +158,7 @@ int sh_window_prefill(const sh_window *w, int tokens, int sequences, const sh_ro
     p.v = rows(v, tokens, w->kv_heads, D, es);
     p.out = rows(out, tokens, w->q_heads, D, es);
     p.starts = starts_dev; p.lengths = lengths_dev;
-    return done(w->dtype == SH_F32 ? sh_launch_window_prefill_simt(p, w->dtype, D, (cudaStream_t)stream)
+    return done(w->dtype == SH_F32 ? sh_launch_window_prefill_f32(p, D, (cudaStream_t)stream)
                                    : sh_launch_window_prefill_umma(p, w->dtype, D, (cudaStream_t)stream));
 }
 

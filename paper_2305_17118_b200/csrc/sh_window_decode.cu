@@ -30,48 +30,64 @@ constexpr int R = 2;                 // rows in flight per group of eight lanes
 constexpr int BLOCK = 4 * R;         // rows of a warp per pass
 
 // q rows (fp32) and the new token's key and value (as the cache holds them) into shared memory, prepared by `rope` if there is one.
-template <typename T, int D, int WARPS>
-__device__ __forceinline__ void stage_token(const WindowParams &p, int seq, int kvh, int h0, int nq, float qscale, float *qs, float *ks, float *vs) {
+template <typename T, int D, int WARPS, bool ADJ>
+__device__ __forceinline__ void stage_rows(const WindowParams &p, int seq, int kvh, int h0, int nq, float qscale, float *qs, float *ks, float *vs) {
     constexpr int LPR = D / 16, ROWS = 32 / LPR;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pl = lane % LPR, sub = lane / LPR;
     // rows: the nq queries, the key, the value
     if (warp * ROWS >= nq + 2) return;
-    float c[8], s[8];
+    shrope::Turns<ADJ> turn;
     int e0 = 16 * pl, e1 = 16 * pl + 8;
     if (p.with_rope) {
+        float c[8], s[8];
         shrope::runs<D>(p.rope, pl, e0, e1);
         shrope::turns_of_lane<D>(p.rope, seq, lane, c, s);
+        turn.set(c, s);
     }
     for (int base = warp * ROWS; base < nq + 2; base += WARPS * ROWS) {
         const int row = base + sub;
         const bool is_q = row < nq, is_k = row == nq, live = row < nq + 2;
         const char *src = is_q ? p.q.p + seq * p.q.ts + (h0 + row) * p.q.hs
                                : (is_k ? p.k.p + seq * p.k.ts + kvh * p.k.hs : p.v.p + seq * p.v.ts + kvh * p.v.hs);
-        float x[16] = {};
-        if (live) shrope::load16<T>(src, e0, e1, x);
+        shrope::Raw<T> raw = {};
+        if (live) shrope::load_raw<T>(src, e0, e1, raw);
+        uint64_t x[8];
+        shrope::unpack_raw<T>(raw, x);
         if (p.with_rope) {
-            const void *weight = is_q ? p.rope.qw : p.rope.kw;
-            float w[16] = {}, y[16];
+            const void *weight = is_q ? p.rope.qw : (is_k ? p.rope.kw : nullptr);
+            uint64_t w[8], y[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = x[i];
-            if (weight) shrope::load16<T>(static_cast<const char *>(weight), e0, e1, w);
-            shrope::apply<D>(p.rope, pl, p.rope.qw || p.rope.kw, weight != nullptr, w, c, s, y);
+            for (int i = 0; i < 8; ++i) { w[i] = shpair::f2(1.f, 1.f); y[i] = x[i]; }
+            if (weight) {
+                shrope::Raw<T> wr;
+                shrope::load_raw<T>(static_cast<const char *>(weight), e0, e1, wr);
+                shrope::unpack_raw<T>(wr, w);
+            }
+            shrope::apply<D, ADJ>(p.rope, pl, p.rope.qw || p.rope.kw, weight != nullptr, w, turn, y);
             if (is_q || is_k) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = y[i];
+                for (int i = 0; i < 8; ++i) x[i] = y[i];
             }
         }
         if (live) {
-            float *dst = is_q ? qs + row * D : (is_k ? ks : vs);
+            float f[16];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) shpair::un2(x[i], f[2 * i], f[2 * i + 1]);
             if (is_k) {      // the row as it will be read back
 #pragma unroll
-                for (int i = 0; i < 16; i += Vec<T>::N) Vec<T>::unpack(Vec<T>::pack(x + i), x + i);
+                for (int i = 0; i < 16; i += Vec<T>::N) Vec<T>::unpack(Vec<T>::pack(f + i), f + i);
             }
-            const float f = is_q ? qscale : 1.f;
+            float *dst = is_q ? qs + row * D : (is_k ? ks : vs);
+            const float m = is_q ? qscale : 1.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { dst[e0 + i] = x[i] * f; dst[e1 + i] = x[8 + i] * f; }
+            for (int i = 0; i < 8; ++i) { dst[e0 + i] = f[i] * m; dst[e1 + i] = f[8 + i] * m; }
         }
     }
+}
+template <typename T, int D, int WARPS>
+__device__ __forceinline__ void stage_token(const WindowParams &p, int seq, int kvh, int h0, int nq, float qscale, float *qs, float *ks, float *vs) {
+    if (p.with_rope && p.rope.adjacent) stage_rows<T, D, WARPS, true>(p, seq, kvh, h0, nq, qscale, qs, ks, vs);
+    else stage_rows<T, D, WARPS, false>(p, seq, kvh, h0, nq, qscale, qs, ks, vs);
 }
 
 template <typename T, int D, int GQ>
@@ -253,12 +269,20 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
 //
 // Each warp brings its rows in by cp.async, 16 bytes a lane, into a ring of its own (no barrier on the way; pieces permuted by
 // row so that ldmatrix reads without bank conflicts).  Rows that hold no token are filled with zeros and never read.
-constexpr int MW = 4;                // warps of a CTA
+#ifndef MST
+#define MST 3
+#endif
+#ifndef MWARPS
+#define MWARPS 4
+#endif
+#ifndef MAXS
+#define MAXS 8
+#endif
 constexpr int MB = 16;               // rows of a block
 constexpr int MQ = 8;                // query heads of a unit
 
-template <int D> struct Mma {
-    static constexpr int STAGES = D == 128 ? 3 : 6;
+template <int D, int MW> struct Mma {
+    static constexpr int STAGES = (D == 128 ? 1 : 2) * MST;
     static constexpr int ROW = 2 * D, TILE = MB * ROW, STAGE = 2 * TILE;      // bytes: a row, 16 rows, key and value rows of a block
     static constexpr int OFF_Q = MW * STAGES * STAGE;                         // [16][D]: high parts of the queries, low parts
     static constexpr int OFF_NEW = OFF_Q + 16 * ROW;                          // the new token's key and value, 16 bits
@@ -338,9 +362,9 @@ __device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, 
     *reinterpret_cast<uint4 *>(dst + c * 16) = Vec<T>::pack(o);
 }
 
-template <typename T, int D>
+template <typename T, int D, int MW>
 __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __grid_constant__ WindowParams p, int qblocks) {
-    using C = Mma<D>;
+    using C = Mma<D, MW>;
     constexpr int CHUNKS = D / 8;                     // 16-byte pieces of a row
     extern __shared__ __align__(128) unsigned char sm[];
     cg::cluster_group cluster = cg::this_cluster();
@@ -505,8 +529,9 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
         if (d == 0) { cta[q * (D + 2)] = M; cta[q * (D + 2) + 1] = L; }
     }
     cluster.sync();
-    if (rank == 0 && tid / CHUNKS < nq) {             // one CTA finishes: a thread per 8 elements
-        const int q = tid / CHUNKS, d = tid % CHUNKS * 8;
+    // one CTA finishes: a thread per 8 elements
+    if (rank == 0)
+    for (int q = tid / CHUNKS, d = tid % CHUNKS * 8; q < nq; q += MW * 32 / CHUNKS) {
         float M = -CUDART_INF_F, L = 0.f, acc[8] = {};
         for (int r = 0; r < S; ++r) M = fmaxf(M, cluster.map_shared_rank(cta + q * (D + 2), r)[0]);
         const float mb = M == -CUDART_INF_F ? 0.f : M;
@@ -536,16 +561,15 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
 
 // Launch `kern` over units of S CTAs.  S: few units split the axis of keys while that fills SMs (ctas: what the device holds at once)
 // and leaves each CTA `least` rows.
-template <typename K>
-cudaError_t launch_units(K kern, const WindowParams &p, int qblocks, int threads, size_t smem, int per_sm, int least, cudaStream_t s) {
+template <auto kern>
+cudaError_t launch_units(const WindowParams &p, int qblocks, int threads, size_t smem, int per_sm, int least, cudaStream_t s) {
     const long long units = (long long)p.sequences * p.hk * qblocks;
-    int sms = 0, dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess && smem > 48 * 1024) e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static ShKernelSetup setup;
+    int sms = 0;
+    const cudaError_t e = sh_setup_kernel(setup, kern, smem, &sms);
     if (e != cudaSuccess) return e;
     int S = 1;
-    while (S < 8 && units * S * 2 <= (long long)per_sm * sms && p.window + p.sinks >= 2 * S * least) S *= 2;
+    while (S < MAXS && units * S * 2 <= (long long)per_sm * sms && p.window + p.sinks >= 2 * S * least) S *= 2;
     if (units * S > 0x7fffffffll) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(units * S));
@@ -562,7 +586,7 @@ cudaError_t launch_units(K kern, const WindowParams &p, int qblocks, int threads
 
 template <int D, int GQ>
 cudaError_t launch_simt(const WindowParams &p, cudaStream_t s) {
-    return launch_units(sh_window_decode_simt_kernel<float, D, GQ>, p, (p.g + GQ - 1) / GQ, NT, 0, 2, 2 * WARPS * BLOCK, s);
+    return launch_units<sh_window_decode_simt_kernel<float, D, GQ>>(p, (p.g + GQ - 1) / GQ, NT, 0, 2, 2 * WARPS * BLOCK, s);
 }
 template <int D>
 cudaError_t launch_f32(const WindowParams &p, cudaStream_t s) {
@@ -570,7 +594,8 @@ cudaError_t launch_f32(const WindowParams &p, cudaStream_t s) {
 }
 template <typename T, int D>
 cudaError_t launch_mma(const WindowParams &p, cudaStream_t s) {
-    return launch_units(sh_window_decode_mma_kernel<T, D>, p, (p.g + MQ - 1) / MQ, MW * 32, Mma<D>::SMEM, 2, 2 * MW * MB, s);
+    constexpr int MW = MWARPS, per_sm = 233472 / (Mma<D, MW>::SMEM + 1024);
+    return launch_units<sh_window_decode_mma_kernel<T, D, MW>>(p, (p.g + MQ - 1) / MQ, MW * 32, Mma<D, MW>::SMEM, per_sm, 2 * MW * MB, s);
 }
 
 }  // namespace

@@ -208,7 +208,9 @@ template <typename T, int D>
 cudaError_t launch(const WindowParams &p, cudaStream_t s) {
     auto kern = sh_window_prefill_simt_kernel<T, D>;
     constexpr int bytes = smem_floats<D>() * 4;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    static ShKernelSetup setup;
+    int sms = 0;
+    const cudaError_t e = sh_setup_kernel(setup, kern, bytes, &sms);
     if (e != cudaSuccess) return e;
     const long long tiles = (long long)p.tokens * p.g / BM + p.sequences;      // each sequence adds at most one partial tile
     if (tiles > 0x7fffffffll) return cudaErrorInvalidValue;
@@ -216,17 +218,9 @@ cudaError_t launch(const WindowParams &p, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-template <typename T>
-cudaError_t launch_d(const WindowParams &p, int D, cudaStream_t s) {
-    return D == 128 ? launch<T, 128>(p, s) : launch<T, 64>(p, s);
-}
-
 }  // namespace
 
-cudaError_t sh_launch_window_prefill_simt(const WindowParams &p, int dtype, int D, cudaStream_t s) {
-    if (dtype == SH_F32) return launch_d<float>(p, D, s);
-    return dtype == SH_F16 ? launch_d<__half>(p, D, s) : launch_d<__nv_bfloat16>(p, D, s);
-}
+cudaError_t sh_launch_window_prefill_f32(const WindowParams &p, int D, cudaStream_t s) { return D == 128 ? launch<float, 128>(p, s) : launch<float, 64>(p, s); }
 
 cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, cudaStream_t s) {
     const int pieces = D * es / 16;

@@ -34,12 +34,14 @@
 #include <math_constants.h>
 
 #include "sh_elem.cuh"
+#include "sh_pairs.cuh"
 #include "sh_umma.cuh"
 #include "sh_window.cuh"
 
 namespace {
 
 using namespace shasync;
+using namespace shpair;
 using namespace shumma;
 using namespace shwin;
 
@@ -299,23 +301,6 @@ __device__ __forceinline__ uint32_t run_bits(const Runs &r, int base) {
     for (int k = 0; k < 3; ++k) m |= low_bits(r.hi[k] - base) & ~low_bits(r.lo[k] - base);
     return m;
 }
-__device__ __forceinline__ uint64_t f2(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void un2(uint64_t x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -786,10 +771,9 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
         if (!make_map(&mkc, w.kc, 4, dim, st, box) || !make_map(&mvc, w.vc, 4, dim, st, box)) return cudaErrorNotSupported;
     }
     auto kern = sh_window_prefill_umma_kernel<T, D>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::SMEM);
-    int dev = 0, sms = 0;
-    if (e == cudaSuccess) e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    static ShKernelSetup setup;
+    int sms = 0;
+    const cudaError_t e = sh_setup_kernel(setup, kern, Cfg<D>::SMEM, &sms);
     if (e != cudaSuccess) return e;
     // each sequence adds at most one partly filled item
     const long long items = ((long long)w.tokens / (2 * p.tpt) + w.sequences) * w.hk * p.hblocks;
