@@ -448,11 +448,16 @@ int sh_window_append(const sh_window *w, int tokens, int sequences, const sh_row
  * first normalised and rotated, by positions_dev as in sh_qk_norm_rope, or by lengths where that is NULL (one axis); the
  * rotated key is what the cache gets.  lengths_dev: tokens before the step (the caller advances them), below 2^30; negative: an
  * idle slot of the batch, for which nothing is read or written.
- * Errors: SH_EINVAL, SH_ECUDA.
+ * workspace_dev: device memory of sh_window_decode_workspace_bytes(w, sequences) bytes (0 for larger batches), 16-byte aligned, or
+ * NULL.  With it a few sequences over a long axis spread over the whole device; without it they take longer, the result is the
+ * same up to fp32 summation order.  Its contents do not matter; it is in use until `stream` has passed the call, so calls that may
+ * run at once, captured ones included, need one each.
+ * Errors: SH_EINVAL, SH_ENOMEM (workspace too small), SH_ECUDA.
  */
+size_t sh_window_decode_workspace_bytes(const sh_window *w, int sequences);
 int sh_window_decode(const sh_window *w, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *lengths_dev,
                      const sh_window_cache *cache, const sh_rope *rope, const int32_t *positions_dev, long long axis_stride,
-                     const sh_rows *out, void *stream);
+                     const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
  * Did a kernel of the window cache give up one of its bounded waits on the current device since the last call?  Its outputs are

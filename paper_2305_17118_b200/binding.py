@@ -35,7 +35,7 @@ EXPORTS = ["sh_create", "sh_destroy", "sh_workspace_bytes", "sh_bind", "sh_set_o
            "sh_compress", "sh_compress_static", "sh_scores", "sh_select", "sh_state", "sh_export_unit",
            "sh_restore", "sh_launch_count", "sh_decode_kernel_choice", "sh_import_compressed", "sh_prefill_bulk",
            "sh_prefill_bulk_scratch_bytes", "sh_strerror", "sh_last_cuda_error",
-           "sh_qk_norm_rope", "sh_window_prefill", "sh_window_append", "sh_window_decode", "sh_window_status"]
+           "sh_qk_norm_rope", "sh_window_prefill", "sh_window_append", "sh_window_decode", "sh_window_decode_workspace_bytes", "sh_window_status"]
 
 
 class _Rows(C.Structure):
@@ -111,7 +111,9 @@ def declare(lib: C.CDLL) -> C.CDLL:
     lib.sh_window_prefill.argtypes = [window, C.c_int, C.c_int, rows, rows, rows, vp, vp, cache, rows, vp]
     lib.sh_window_append.argtypes = [window, C.c_int, C.c_int, rows, rows, vp, vp, cache, vp]
     lib.sh_window_status.argtypes = [vp]
-    lib.sh_window_decode.argtypes = [window, C.c_int, rows, rows, rows, vp, cache, rope, vp, C.c_longlong, rows, vp]
+    lib.sh_window_decode.argtypes = [window, C.c_int, rows, rows, rows, vp, cache, rope, vp, C.c_longlong, rows, vp, C.c_size_t, vp]
+    lib.sh_window_decode_workspace_bytes.argtypes = [window, C.c_int]
+    lib.sh_window_decode_workspace_bytes.restype = C.c_size_t
     return lib
 
 
@@ -623,8 +625,14 @@ def window_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: to
     elif positions is not None:
         raise ValueError("positions without rope")
     out = q.new_zeros(shape) if out is None else out
-    _launch("window_decode", lib.sh_window_decode, device, stream, win, n, qr, kr, vr, lp, cache, ro, pos, axis_stride,
-            _more_rows(out, "out", shape, dtype, device))
+    outr = _more_rows(out, "out", shape, dtype, device)
+    wp, bytes_ = None, lib.sh_window_decode_workspace_bytes(win, n)
+    if bytes_:
+        work = torch.empty(bytes_, dtype=torch.uint8, device=q.device)      # a tensor of this call's own, ordered by the stream
+        wp = work.data_ptr()
+        if stream is not None:
+            work.record_stream(stream)
+    _launch("window_decode", lib.sh_window_decode, device, stream, win, n, qr, kr, vr, lp, cache, ro, pos, axis_stride, outr, wp, bytes_)
     return out
 
 

@@ -37,6 +37,7 @@ struct WindowParams {
     float scale_log2e;
     RopeParams rope;              // decode only: how the step's q and k are prepared
     bool with_rope;
+    float *part;                  // decode only: scratch of sh_window_decode_scratch bytes, or NULL
 };
 
 // SMs of the current device, and that a kernel may use `smem` bytes of shared memory there.  Both are facts of the device, asked once
@@ -63,4 +64,5 @@ cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int 
 // code of the first bounded wait that gave up in a window kernel of the current device since the last call (0: none); synchronises
 cudaError_t sh_window_error_take(int *code, cudaStream_t s);
 cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, cudaStream_t s);
+size_t sh_window_decode_scratch(int sequences, int hk, int g, int dtype, int D);
 cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, cudaStream_t s);

@@ -179,9 +179,13 @@ int sh_window_append(const sh_window *w, int tokens, int sequences, const sh_row
     return done(sh_launch_window_append(p, es, D, (cudaStream_t)stream));
 }
 
+size_t sh_window_decode_workspace_bytes(const sh_window *w, int sequences) {
+    return good_window(w) && sequences > 0 ? sh_window_decode_scratch(sequences, w->kv_heads, w->q_heads / w->kv_heads, w->dtype, w->head_dim) : 0;
+}
+
 int sh_window_decode(const sh_window *w, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *lengths_dev,
                      const sh_window_cache *cache, const sh_rope *rope, const int32_t *positions_dev, long long axis_stride,
-                     const sh_rows *out, void *stream) {
+                     const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream) {
     if (!good_window(w) || sequences < 0) return SH_EINVAL;
     if (rope && (!good_rope(rope) || rope->dtype != w->dtype || rope->head_dim != w->head_dim)) return SH_EINVAL;
     if (rope && (positions_dev ? !good_positions(positions_dev, axis_stride, rope->axes) : rope->axes != 1)) return SH_EINVAL;
@@ -200,6 +204,12 @@ int sh_window_decode(const sh_window *w, int sequences, const sh_rows *q, const 
     p.out = rows(out, sequences, w->q_heads, D, es);
     p.lengths = lengths_dev;
     p.with_rope = rope != nullptr;
+    if (workspace_dev) {
+        if (!aligned16(workspace_dev)) return SH_EINVAL;
+        const size_t need = sh_window_decode_scratch(sequences, p.hk, p.g, w->dtype, D);
+        if (workspace_bytes < need) return SH_ENOMEM;
+        if (need) p.part = static_cast<float *>(workspace_dev);
+    }
     if (rope) fill_rope(p.rope, rope, positions_dev ? positions_dev : lengths_dev, axis_stride);
     return done(sh_launch_window_decode(p, w->dtype, D, (cudaStream_t)stream));
 }

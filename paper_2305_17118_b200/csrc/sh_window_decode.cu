@@ -11,6 +11,7 @@
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "sh_rope.cuh"
@@ -91,7 +92,7 @@ __device__ __forceinline__ void stage_token(const WindowParams &p, int seq, int 
 }
 
 template <typename T, int D, int GQ>
-__global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowParams p, int qblocks) {
+__global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowParams p, int qblocks, int) {
     constexpr int N = Vec<T>::N, CH = D / N / 8, EL = CH * N;      // 16-byte pieces and elements of a row per lane
     __shared__ __align__(16) float qs[GQ * D], ks[D], vs[D];
     __shared__ float part[WARPS][GQ][D + 2];
@@ -269,20 +270,11 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
 //
 // Each warp brings its rows in by cp.async, 16 bytes a lane, into a ring of its own (no barrier on the way; pieces permuted by
 // row so that ldmatrix reads without bank conflicts).  Rows that hold no token are filled with zeros and never read.
-#ifndef MST
-#define MST 3
-#endif
-#ifndef MWARPS
-#define MWARPS 4
-#endif
-#ifndef MAXS
-#define MAXS 8
-#endif
 constexpr int MB = 16;               // rows of a block
 constexpr int MQ = 8;                // query heads of a unit
 
-template <int D, int MW> struct Mma {
-    static constexpr int STAGES = (D == 128 ? 1 : 2) * MST;
+template <int D, int MW> struct Mma {      // MW: warps of a CTA
+    static constexpr int STAGES = (D == 128 ? 1 : 2) * (MW == 8 ? 3 : 2);
     static constexpr int ROW = 2 * D, TILE = MB * ROW, STAGE = 2 * TILE;      // bytes: a row, 16 rows, key and value rows of a block
     static constexpr int OFF_Q = MW * STAGES * STAGE;                         // [16][D]: high parts of the queries, low parts
     static constexpr int OFF_NEW = OFF_Q + 16 * ROW;                          // the new token's key and value, 16 bits
@@ -326,31 +318,28 @@ template <typename T> __device__ __forceinline__ void split2(float x, float y, u
     lo = Vec<T>::pack2(x - a, y - b);
 }
 
-// One query by the D / 8 lanes that finish it: every live row once, in fp32.
+// One query by the D / 8 lanes that finish it: every live row once, in fp32.  x: this lane's 8 elements of the prepared query; fresh: key and
+// value rows that stand for those of slot snew (NULL: they are in the cache already).
 template <typename T, int D>
-__device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, int live, int snew, const unsigned char *qs, int q, const unsigned char *fresh,
+__device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, int live, int snew, const unsigned char *fresh, const float4 x0, const float4 x1,
                                        char *dst) {
     constexpr int CHUNKS = D / 8;
     const int c = threadIdx.x % CHUNKS;
     const unsigned group = ((1u << CHUNKS) - 1u) << ((threadIdx.x & 31) & ~(CHUNKS - 1));
-    float hi[8], lo[8], o[8], m = -CUDART_INF_F, l = 0.f;
-    Vec<T>::unpack(*reinterpret_cast<const uint4 *>(qs + q * 2 * D + ((c ^ (q & 7)) << 4)), hi);
-    Vec<T>::unpack(*reinterpret_cast<const uint4 *>(qs + (q + 8) * 2 * D + ((c ^ (q & 7)) << 4)), lo);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        hi[e] = (isfinite(hi[e]) ? hi[e] + lo[e] : hi[e]) * p.scale_log2e;
-        o[e] = 0.f;
-    }
+    const float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+    float o[8] = {}, m = -CUDART_INF_F, l = 0.f;
     for (int j = 0; j < live; ++j) {
         const long long off = seq * p.css + kvh * p.chs + j * p.cls + c * 16;
+        const bool f = fresh && j == snew;
         float k[8], v[8];
-        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(j == snew ? reinterpret_cast<const char *>(fresh) + c * 16 : p.kc + off), k);
-        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(j == snew ? reinterpret_cast<const char *>(fresh) + 2 * D + c * 16 : p.vc + off), v);
+        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(f ? reinterpret_cast<const char *>(fresh) + c * 16 : p.kc + off), k);
+        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(f ? reinterpret_cast<const char *>(fresh) + 2 * D + c * 16 : p.vc + off), v);
         float s = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s = fmaf(hi[e], k[e], s);
+        for (int e = 0; e < 8; ++e) s = fmaf(x[e], k[e], s);
 #pragma unroll
-        for (int x = CHUNKS / 2; x; x >>= 1) s += __shfl_xor_sync(group, s, x);
+        for (int i = CHUNKS / 2; i; i >>= 1) s += __shfl_xor_sync(group, s, i);
+        s *= p.scale_log2e;
         const float mn = fmaxf(m, s), b = mn == -CUDART_INF_F ? 0.f : mn, keep = ex2_approx(m - b), w = ex2_approx(s - b);
         m = mn;
         l = l * keep + w;
@@ -363,12 +352,14 @@ __device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, 
 }
 
 template <typename T, int D, int MW>
-__global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __grid_constant__ WindowParams p, int qblocks) {
+__global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __grid_constant__ WindowParams p, int qblocks, int parts) {
     using C = Mma<D, MW>;
     constexpr int CHUNKS = D / 8;                     // 16-byte pieces of a row
     extern __shared__ __align__(128) unsigned char sm[];
     cg::cluster_group cluster = cg::this_cluster();
-    const int S = cluster.num_blocks(), rank = cluster.block_rank();
+    // the CTAs that share a unit's rows: a cluster, which merges by itself, or `parts` CTAs whose results a second kernel merges
+    const int S = parts ? parts : cluster.num_blocks(), rank = parts ? blockIdx.x % parts : cluster.block_rank();
+    if (parts) sh_pdl_launch_dependents();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long unit = blockIdx.x / S;
     const int qb = (int)(unit % qblocks), kvh = (int)(unit / qblocks % p.hk), seq = (int)(unit / qblocks / p.hk);
@@ -528,6 +519,18 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
         cta[q * (D + 2) + 2 + d] = acc;
         if (d == 0) { cta[q * (D + 2)] = M; cta[q * (D + 2) + 1] = L; }
     }
+    if (parts) {                                      // hand the result over, and once the queries (should a row have to be done again)
+        __syncthreads();
+        float *to = p.part + (unit * parts + rank) * (MQ * (D + 2));
+        for (int i = tid; i < nq * (D + 2); i += MW * 32) to[i] = cta[i];
+        if (rank == 0)
+            for (int i = tid; i < nq * D; i += MW * 32) {
+                const int q = i / D, e = i % D, at = q * C::ROW + (((e / 8) ^ (q & 7)) << 4) + e % 8 * 2;
+                const float hi = (float)*reinterpret_cast<const T *>(sm + C::OFF_Q + at), lo = (float)*reinterpret_cast<const T *>(sm + C::OFF_Q + 8 * C::ROW + at);
+                p.part[(long long)(gridDim.x) * (MQ * (D + 2)) + unit * (MQ * D) + i] = isfinite(hi) ? hi + lo : hi;
+            }
+        return;
+    }
     cluster.sync();
     // one CTA finishes: a thread per 8 elements
     if (rank == 0)
@@ -550,29 +553,115 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
         }
         char *dst = p.out.p + seq * p.out.ts + (h0 + q) * p.out.hs;
         // the low part of a weight or of a query may be zero and meet an infinity: such rows are computed again in plain fp32
+        float hi[8], lo[8];
+        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(sm + C::OFF_Q + q * C::ROW + (((d / 8) ^ (q & 7)) << 4)), hi);
+        Vec<T>::unpack(*reinterpret_cast<const uint4 *>(sm + C::OFF_Q + (q + 8) * C::ROW + (((d / 8) ^ (q & 7)) << 4)), lo);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) hi[e] = isfinite(hi[e]) ? hi[e] + lo[e] : hi[e];
+        const float4 x0 = make_float4(hi[0], hi[1], hi[2], hi[3]), x1 = make_float4(hi[4], hi[5], hi[6], hi[7]);
         const unsigned group = ((1u << CHUNKS) - 1u) << (lane & ~(CHUNKS - 1));
         if (__any_sync(group, odd))
-            plain_row<T, D>(p, seq, kvh, live, snew, sm + C::OFF_Q, q, sm + C::OFF_NEW, dst);
+            plain_row<T, D>(p, seq, kvh, live, snew, sm + C::OFF_NEW, x0, x1, dst);
         else
             *reinterpret_cast<uint4 *>(dst + d * 2) = Vec<T>::pack(acc);
     }
     cluster.sync();                                   // nobody's shared memory goes away while it is read
 }
 
-// Launch `kern` over units of S CTAs.  S: few units split the axis of keys while that fills SMs (ctas: what the device holds at once)
-// and leaves each CTA `least` rows.
+// Merge the `parts` results of each unit: a CTA per (unit, query), SLICES groups of D / 8 lanes that take every SLICES-th part each.
+constexpr int SLICES = 8;
+template <typename T, int D>
+__global__ void __launch_bounds__(SLICES * D / 8) sh_window_decode_merge_kernel(const __grid_constant__ WindowParams p, int qblocks, int parts, long long units) {
+    constexpr int CHUNKS = D / 8, N = SLICES * CHUNKS, REC = MQ * (D + 2);
+    __shared__ float top[N / 32], sum[SLICES], out[SLICES][D];
+    const int tid = threadIdx.x, q = blockIdx.x % MQ, slice = tid / CHUNKS, c = tid % CHUNKS;
+    const long long unit = blockIdx.x / MQ;
+    const int qb = (int)(unit % qblocks), kvh = (int)(unit / qblocks % p.hk), seq = (int)(unit / qblocks / p.hk);
+    sh_pdl_wait();
+    const int t = min(p.lengths[seq], MAX_POS);
+    if (t < 0 || q >= min(MQ, p.g - qb * MQ)) return;
+    const float *rec = p.part + unit * parts * REC + q * (D + 2);
+    float M = -CUDART_INF_F;
+    for (int i = tid; i < parts; i += N) M = fmaxf(M, rec[(long long)i * REC]);
+#pragma unroll
+    for (int i = 16; i; i >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, i));
+    if (tid % 32 == 0) top[tid / 32] = M;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N / 32; ++i) M = fmaxf(M, top[i]);
+    const float mb = M == -CUDART_INF_F ? 0.f : M;
+    float L = 0.f, acc[8] = {};
+    for (int i = slice; i < parts; i += SLICES) {
+        const float *r = rec + (long long)i * REC;
+        const float f = ex2_approx(r[0] - mb);
+        L += r[1] * f;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const float2 x = *reinterpret_cast<const float2 *>(r + 2 + c * 8 + e);
+            acc[e] = fmaf(x.x, f, acc[e]);
+            acc[e + 1] = fmaf(x.y, f, acc[e + 1]);
+        }
+    }
+    if (c == 0) sum[slice] = L;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[slice][c * 8 + e] = acc[e];
+    __syncthreads();
+    if (slice) return;
+    L = 0.f;
+#pragma unroll
+    for (int i = 0; i < SLICES; ++i) L += sum[i];
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < SLICES; ++i) x += out[i][c * 8 + e];
+        acc[e] = x / L;
+        odd |= !isfinite(acc[e]);
+    }
+    char *dst = p.out.p + seq * p.out.ts + (long long)(kvh * p.g + qb * MQ + q) * p.out.hs;
+    if (__any_sync((1u << CHUNKS) - 1u, odd)) {
+        const float4 *x = reinterpret_cast<const float4 *>(p.part + units * parts * REC + unit * (MQ * D) + q * D + c * 8);
+        plain_row<T, D>(p, seq, kvh, min(t + 1, p.sinks + p.window), 0, nullptr, x[0], x[1], dst);
+    } else {
+        *reinterpret_cast<uint4 *>(dst + c * 16) = Vec<T>::pack(acc);
+    }
+}
+
+// Parts of all units together; bounds the workspace.
+constexpr int MAX_PARTS = 160;
+
+// How a launch is laid out: S CTAs (a cluster) share the rows of a unit.  `per_sm` CTAs of a kernel fit on an SM, and one of them draws at
+// most `rate` bytes/us, whatever bandwidth is left.
+struct Shape {
+    int S;
+    double us;      // what the launch is expected to take
+};
+// CTAs run in waves of sms * per_sm; those of a wave share the memory bandwidth (6.4 MB/us), and each costs about 2.5 us to start and to
+// merge, half a microsecond more with each doubling of the cluster.  rows * row_bytes is what a unit may have to read.  The number of rows that a sequence really holds is known on the device
+// only, so it is the cache's size that counts here.
+Shape best_split(long long units, long long rows, int row_bytes, int sms, int per_sm, double rate) {
+    Shape best = {1, 1e300};
+    for (int S = 1; S <= 8 && (S == 1 || rows >= 64ll * S); S *= 2) {
+        const long long ctas = units * S, slots = (long long)sms * per_sm, full = (ctas - 1) / slots, rest = ctas - full * slots;
+        const double bytes = (double)rows * row_bytes / S;
+        auto wave = [&](long long n) { return bytes / std::min(6.4e6 / (double)n, rate) + 2.5 + 0.5 * (S > 1) + 0.5 * (S > 2) + 0.5 * (S > 4); };
+        const double us = (full ? full * wave(slots) : 0.0) + wave(rest);
+        if (us < best.us) best = {S, us};
+    }
+    return best;
+}
+
 template <auto kern>
-cudaError_t launch_units(const WindowParams &p, int qblocks, int threads, size_t smem, int per_sm, int least, cudaStream_t s) {
-    const long long units = (long long)p.sequences * p.hk * qblocks;
+cudaError_t launch_units(const WindowParams &p, int qblocks, int threads, size_t smem, int S, int parts, cudaStream_t s) {
+    const long long ctas = (long long)p.sequences * p.hk * qblocks * (parts ? parts : S);
+    if (ctas > 0x7fffffffll) return cudaErrorInvalidValue;
     static ShKernelSetup setup;
     int sms = 0;
     const cudaError_t e = sh_setup_kernel(setup, kern, smem, &sms);
     if (e != cudaSuccess) return e;
-    int S = 1;
-    while (S < MAXS && units * S * 2 <= (long long)per_sm * sms && p.window + p.sinks >= 2 * S * least) S *= 2;
-    if (units * S > 0x7fffffffll) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(units * S));
+    cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -581,27 +670,66 @@ cudaError_t launch_units(const WindowParams &p, int qblocks, int threads, size_t
     attr.val.clusterDim.x = S; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, p, qblocks);
+    return cudaLaunchKernelEx(&cfg, kern, p, qblocks, parts);
 }
 
 template <int D, int GQ>
-cudaError_t launch_simt(const WindowParams &p, cudaStream_t s) {
-    return launch_units<sh_window_decode_simt_kernel<float, D, GQ>>(p, (p.g + GQ - 1) / GQ, NT, 0, 2, 2 * WARPS * BLOCK, s);
+cudaError_t launch_simt(const WindowParams &p, int sms, cudaStream_t s) {
+    const int qblocks = (p.g + GQ - 1) / GQ;
+    const Shape a = best_split((long long)p.sequences * p.hk * qblocks, (long long)p.window + p.sinks, 8 * D, sms, 2, 3.0e4);
+    return launch_units<sh_window_decode_simt_kernel<float, D, GQ>>(p, qblocks, NT, 0, a.S, 0, s);
 }
 template <int D>
-cudaError_t launch_f32(const WindowParams &p, cudaStream_t s) {
-    return p.g == 1 ? launch_simt<D, 1>(p, s) : (p.g == 2 ? launch_simt<D, 2>(p, s) : launch_simt<D, 4>(p, s));
+cudaError_t launch_f32(const WindowParams &p, int sms, cudaStream_t s) {
+    return p.g == 1 ? launch_simt<D, 1>(p, sms, s) : (p.g == 2 ? launch_simt<D, 2>(p, sms, s) : launch_simt<D, 4>(p, sms, s));
 }
+// Two shapes: CTAs of 4 warps, 3 to an SM, each warp with one block of rows in flight besides the one it works on; and CTAs of 8 warps,
+// one to an SM, with two in flight.  Many units want the first (9216 units of 410 rows: 325 against 545 us), few units, which
+// cannot fill the machine, the second, whose CTAs draw more each (8 units of 16384 rows: 34 against 23 us).
 template <typename T, int D>
-cudaError_t launch_mma(const WindowParams &p, cudaStream_t s) {
-    constexpr int MW = MWARPS, per_sm = 233472 / (Mma<D, MW>::SMEM + 1024);
-    return launch_units<sh_window_decode_mma_kernel<T, D, MW>>(p, (p.g + MQ - 1) / MQ, MW * 32, Mma<D, MW>::SMEM, per_sm, 2 * MW * MB, s);
+cudaError_t launch_mma(const WindowParams &p, int sms, cudaStream_t s) {
+    using Small = Mma<D, 4>;
+    using Large = Mma<D, 8>;
+    static_assert(3 * (Small::SMEM + 1024) <= 233472 && Large::SMEM <= 232448, "CTAs per SM");
+    const int qblocks = (p.g + MQ - 1) / MQ;
+    const long long units = (long long)p.sequences * p.hk * qblocks, rows = (long long)p.window + p.sinks;
+    const Shape a = best_split(units, rows, 4 * D, sms, 3, 3.6e4), b = best_split(units, rows, 4 * D, sms, 1, 5.8e4);
+    // Fewer units than SMs: parts whose results a second launch merges (about 3 us) can fill every SM, a cluster of 8 cannot.
+    const long long parts = std::min(std::min((long long)sms, (long long)MAX_PARTS) / units, rows / 64);
+    if (p.part && parts > 1) {
+        const double us = (double)rows * 4 * D / parts / std::min(6.4e6 / (double)(units * parts), 5.8e4) + 5.5;
+        if (us < a.us && us < b.us) {
+            const cudaError_t e = launch_units<sh_window_decode_mma_kernel<T, D, 8>>(p, qblocks, 256, Large::SMEM, 1, (int)parts, s);
+            if (e != cudaSuccess) return e;
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)(units * MQ));
+            cfg.blockDim = dim3(SLICES * D / 8);
+            cfg.stream = s;
+            cudaLaunchAttribute attr = {};
+            attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr.val.programmaticStreamSerializationAllowed = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            return cudaLaunchKernelEx(&cfg, sh_window_decode_merge_kernel<T, D>, p, qblocks, (int)parts, units);
+        }
+    }
+    return a.us <= b.us ? launch_units<sh_window_decode_mma_kernel<T, D, 4>>(p, qblocks, 128, Small::SMEM, a.S, 0, s)
+                        : launch_units<sh_window_decode_mma_kernel<T, D, 8>>(p, qblocks, 256, Large::SMEM, b.S, 0, s);
 }
 
 }  // namespace
 
 cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, cudaStream_t s) {
-    if (dtype == SH_F32) return D == 128 ? launch_f32<128>(p, s) : launch_f32<64>(p, s);
-    if (dtype == SH_F16) return D == 128 ? launch_mma<__half, 128>(p, s) : launch_mma<__half, 64>(p, s);
-    return D == 128 ? launch_mma<__nv_bfloat16, 128>(p, s) : launch_mma<__nv_bfloat16, 64>(p, s);
+    int dev = 0, sms = 0;
+    const cudaError_t e = sh_device_sms(&dev, &sms);
+    if (e != cudaSuccess) return e;
+    if (dtype == SH_F32) return D == 128 ? launch_f32<128>(p, sms, s) : launch_f32<64>(p, sms, s);
+    if (dtype == SH_F16) return D == 128 ? launch_mma<__half, 128>(p, sms, s) : launch_mma<__half, 64>(p, sms, s);
+    return D == 128 ? launch_mma<__nv_bfloat16, 128>(p, sms, s) : launch_mma<__nv_bfloat16, 64>(p, sms, s);
+}
+
+size_t sh_window_decode_scratch(int sequences, int hk, int g, int dtype, int D) {
+    const long long units = (long long)sequences * hk * ((g + MQ - 1) / MQ);
+    if (dtype == SH_F32 || units < 1 || units * 2 > MAX_PARTS) return 0;
+    return sizeof(float) * ((size_t)MAX_PARTS * MQ * (D + 2) + (size_t)units * MQ * D);
 }

@@ -297,8 +297,45 @@ def test_single_tokens(dtype, d, hk, g, window, sinks, rope):
 def test_single_tokens_over_long_axes_and_large_batches(dtype):
     _decode_case(dtype, 128, 2, 4, 5000, 4, [20011], rope=True)              # one sequence: the axis is split
     _decode_case(dtype, 64, 1, 1, 3001, 0, [2500, 7000, -1], seed=22)
+    _decode_case(dtype, 128, 1, 11, 9000, 3, [9100], seed=25, rope=True)
+    _decode_case(dtype, 64, 3, 2, 20000, 0, [-1, 19999, 3], seed=27)
     _decode_case(dtype, 128, 4, 2, 30, 2, [(i * 37) % 90 for i in range(190)], seed=23)
     _decode_case(dtype, 128, 2, 2, 200, 2, [500, 150], seed=24, hot=12.0)    # one key takes nearly all the weight
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_long_axes_with_infinite_values_and_without_a_workspace(dtype):
+    """The axis is split over the device (a second launch merges) or, without a workspace, over a cluster: the same result; values
+    that are infinite come out in their element alone."""
+    import ctypes as C
+    sh, gen, dt = _sh(), _gen(28), DT[dtype]
+    hk, g, d, window, t, inf = 2, 3, 128, 8000, 8100, float("inf")
+    hist = _history(gen, [1], [t], hk, d, dt)
+    hist[0][1][5000, 1, 17], hist[0][1][t, 0, 3], hist[0][1][50, 0, 9] = inf, -inf, inf      # (position 50 has left the window)
+    kc, vc = _caches(hist, [t], hk, d, window, 0, dt, float("nan"))
+    q, k, v = _rnd(gen, 1, hk * g, d, dtype=dt), hist[0][0][t:], hist[0][1][t:]
+    outs = []
+    for work in (True, False):
+        k2, v2 = kc.clone(), vc.clone()
+        if work:
+            out = sh.window_decode(q, k, v, _i32([t]), k2, v2, window=window)
+        else:
+            out, lengths = torch.zeros_like(q), _i32([t])
+            win = sh._Window(sh.DTYPE_CODE[dtype], d, hk * g, hk, window, 0, 0.0)
+            rows = lambda x: C.byref(sh._Rows(x.data_ptr(), x.stride(0), x.stride(1)))
+            cache = sh._WindowCache(k2.data_ptr(), v2.data_ptr(), *k2.stride()[:3])
+            assert sh.lib.sh_window_decode(C.byref(win), 1, rows(q), rows(k), rows(v), lengths.data_ptr(), C.byref(cache), None, None, 0,
+                                           rows(out), None, 0, torch.cuda.current_stream().cuda_stream) == sh.SH_OK
+        outs.append(out.double().cpu())
+    vals = hist[0][1].clone()
+    vals[torch.isinf(vals)] = 0
+    want, vmax, smax = ref.attend_ref(q, [t], hist[0][0], vals, window, 0)
+    tol = ref.attend_tolerance(want, vmax, smax, dt)
+    expect = torch.zeros(hk * g, d, dtype=torch.float64)
+    expect[g:, 17], expect[:g, 3] = inf, -inf
+    for out in outs:
+        assert torch.equal(torch.where(torch.isinf(out[0]), out[0], 0.0), expect)
+        ref.check(torch.where(torch.isinf(out), want, out), want, tol)
 
 
 def test_cache_offsets_pass_32_bits():

@@ -16,7 +16,8 @@ def _sh():
 def _args(sh):
     rows = lambda heads: sh._Rows(FAKE, heads * 64, 64)
     return dict(w=sh._Window(sh.SH_F16, 64, 4, 2, 8, 2, 0.0), q=rows(4), k=rows(2), v=rows(2), out=rows(4), starts=FAKE, lengths=FAKE,
-                cache=sh._WindowCache(FAKE, FAKE, 2 * 10 * 64, 10 * 64, 64), tokens=4, n=3, rope=None, positions=None, axis=0)
+                cache=sh._WindowCache(FAKE, FAKE, 2 * 10 * 64, 10 * 64, 64), tokens=4, n=3, rope=None, positions=None, axis=0,
+                work=None, work_bytes=0)
 
 
 def _rope(sh, **kw):
@@ -35,7 +36,7 @@ def _calls(sh, a):
         append=lambda: lib.sh_window_append(ref(a["w"]), a["tokens"], a["n"], ref(a["k"]), ref(a["v"]), a["starts"], a["lengths"],
                                             ref(a["cache"]), None),
         decode=lambda: lib.sh_window_decode(ref(a["w"]), a["n"], ref(a["q"]), ref(a["k"]), ref(a["v"]), a["lengths"], ref(a["cache"]),
-                                            ref(a["rope"]), a["positions"], a["axis"], ref(a["out"]), None))
+                                            ref(a["rope"]), a["positions"], a["axis"], ref(a["out"]), a["work"], a["work_bytes"], None))
 
 
 ALL, CHUNK = ("prefill", "append", "decode"), ("prefill", "append")
@@ -103,6 +104,21 @@ def test_rope_calls_refuse_rows_and_positions():
     assert _calls(sh, a)["decode"]() == sh.SH_EINVAL
     a["rope"] = _rope(sh, dtype=sh.SH_BF16)                                               # another type than the cache's
     assert _calls(sh, a)["decode"]() == sh.SH_EINVAL
+
+
+def test_decode_workspace():
+    sh = _sh()
+    a = _args(sh)
+    size = sh.lib.sh_window_decode_workspace_bytes
+    need = size(C.byref(a["w"]), 3)
+    assert 0 < need < 1 << 21
+    a["work"], a["work_bytes"] = FAKE, need - 1
+    assert _calls(sh, a)["decode"]() == sh.SH_ENOMEM
+    a["work"], a["work_bytes"] = FAKE + 4, need
+    assert _calls(sh, a)["decode"]() == sh.SH_EINVAL
+    assert size(C.byref(a["w"]), 1000) == 0 and size(C.byref(a["w"]), 0) == 0 and size(None, 3) == 0
+    a["w"].dtype = sh.SH_F32
+    assert size(C.byref(a["w"]), 3) == 0
 
 
 def test_calls_with_nothing_to_do_succeed():
