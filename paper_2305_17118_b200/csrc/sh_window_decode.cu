@@ -631,25 +631,64 @@ __global__ void __launch_bounds__(SLICES * D / 8) sh_window_decode_merge_kernel(
 // Parts of all units together; bounds the workspace.
 constexpr int MAX_PARTS = 160;
 
-// How a launch is laid out: S CTAs (a cluster) share the rows of a unit.  `per_sm` CTAs of a kernel fit on an SM, and one of them draws at
-// most `rate` bytes/us, whatever bandwidth is left.
+// How a launch is laid out: S CTAs (a cluster) share the rows of a unit.  A CTA of a kernel draws at most `rate`
+// bytes/us, whatever bandwidth is left.
 struct Shape {
     int S;
     double us;      // what the launch is expected to take
 };
-// CTAs run in waves of sms * per_sm; those of a wave share the memory bandwidth (6.4 MB/us), and each costs about 2.5 us to start and to
+// CTAs run in waves of slots_of[log2 S], what the device holds at once of such clusters; those of a wave share the memory bandwidth (6.4 MB/us), and each costs about 2.5 us to start and to
 // merge, half a microsecond more with each doubling of the cluster.  rows * row_bytes is what a unit may have to read.  The number of rows that a sequence really holds is known on the device
 // only, so it is the cache's size that counts here.
-Shape best_split(long long units, long long rows, int row_bytes, int sms, int per_sm, double rate) {
+Shape best_split(long long units, long long rows, int row_bytes, const int (&slots_of)[4], double rate) {
     Shape best = {1, 1e300};
-    for (int S = 1; S <= 8 && (S == 1 || rows >= 64ll * S); S *= 2) {
-        const long long ctas = units * S, slots = (long long)sms * per_sm, full = (ctas - 1) / slots, rest = ctas - full * slots;
+    for (int S = 1, i = 0; S <= 8 && (S == 1 || rows >= 64ll * S); S *= 2, ++i) {
+        const long long ctas = units * S, slots = std::max(slots_of[i], S), full = (ctas - 1) / slots, rest = ctas - full * slots;
         const double bytes = (double)rows * row_bytes / S;
         auto wave = [&](long long n) { return bytes / std::min(6.4e6 / (double)n, rate) + 2.5 + 0.5 * (S > 1) + 0.5 * (S > 2) + 0.5 * (S > 4); };
         const double us = (full ? full * wave(slots) : 0.0) + wave(rest);
         if (us < best.us) best = {S, us};
     }
     return best;
+}
+
+cudaLaunchConfig_t cluster_config(unsigned ctas, int threads, size_t smem, int S, cudaLaunchAttribute *attr, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    attr->id = cudaLaunchAttributeClusterDimension;
+    attr->val.clusterDim.x = S; attr->val.clusterDim.y = 1; attr->val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cfg;
+}
+
+// CTAs of `kern` in clusters of 1, 2, 4 and 8 that the current device holds at once (a cluster lies within one group of SMs, so with
+// large CTAs not every SM can be used).  Asked once per device.
+template <auto kern>
+cudaError_t cluster_slots(int threads, size_t smem, int (&slots)[4]) {
+    static std::atomic<int> known[ShKernelSetup::DEVICES][4];
+    static ShKernelSetup setup;
+    int dev = 0, sms = 0;
+    cudaError_t e = sh_device_sms(&dev, &sms);
+    if (e != cudaSuccess) return e;
+    const bool kept = dev < ShKernelSetup::DEVICES;
+    for (int i = 0; i < 4; ++i) {
+        slots[i] = kept ? known[dev][i].load(std::memory_order_relaxed) : 0;
+        if (slots[i]) continue;
+        e = sh_setup_kernel(setup, kern, smem, &sms);
+        if (e != cudaSuccess) return e;
+        cudaLaunchAttribute attr;
+        const cudaLaunchConfig_t cfg = cluster_config(1u << i, threads, smem, 1 << i, &attr, nullptr);
+        int clusters = 0;
+        e = cudaOccupancyMaxActiveClusters(&clusters, kern, &cfg);
+        if (e != cudaSuccess) return e;
+        slots[i] = std::max(clusters, 1) << i;
+        if (kept) known[dev][i].store(slots[i], std::memory_order_relaxed);
+    }
+    return cudaSuccess;
 }
 
 template <auto kern>
@@ -660,46 +699,47 @@ cudaError_t launch_units(const WindowParams &p, int qblocks, int threads, size_t
     int sms = 0;
     const cudaError_t e = sh_setup_kernel(setup, kern, smem, &sms);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = S; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = cluster_config((unsigned)ctas, threads, smem, S, &attr, s);
     return cudaLaunchKernelEx(&cfg, kern, p, qblocks, parts);
 }
 
 template <int D, int GQ>
-cudaError_t launch_simt(const WindowParams &p, int sms, cudaStream_t s) {
+cudaError_t launch_simt(const WindowParams &p, cudaStream_t s) {
+    constexpr auto kern = sh_window_decode_simt_kernel<float, D, GQ>;
     const int qblocks = (p.g + GQ - 1) / GQ;
-    const Shape a = best_split((long long)p.sequences * p.hk * qblocks, (long long)p.window + p.sinks, 8 * D, sms, 2, 3.0e4);
-    return launch_units<sh_window_decode_simt_kernel<float, D, GQ>>(p, qblocks, NT, 0, a.S, 0, s);
+    int slots[4];
+    const cudaError_t e = cluster_slots<kern>(NT, 0, slots);
+    if (e != cudaSuccess) return e;
+    const Shape a = best_split((long long)p.sequences * p.hk * qblocks, (long long)p.window + p.sinks, 8 * D, slots, 3.0e4);
+    return launch_units<kern>(p, qblocks, NT, 0, a.S, 0, s);
 }
 template <int D>
-cudaError_t launch_f32(const WindowParams &p, int sms, cudaStream_t s) {
-    return p.g == 1 ? launch_simt<D, 1>(p, sms, s) : (p.g == 2 ? launch_simt<D, 2>(p, sms, s) : launch_simt<D, 4>(p, sms, s));
+cudaError_t launch_f32(const WindowParams &p, cudaStream_t s) {
+    return p.g == 1 ? launch_simt<D, 1>(p, s) : (p.g == 2 ? launch_simt<D, 2>(p, s) : launch_simt<D, 4>(p, s));
 }
 // Two shapes: CTAs of 4 warps, 3 to an SM, each warp with one block of rows in flight besides the one it works on; and CTAs of 8 warps,
 // one to an SM, with two in flight.  Many units want the first (9216 units of 410 rows: 325 against 545 us), few units, which
 // cannot fill the machine, the second, whose CTAs draw more each (8 units of 16384 rows: 34 against 23 us).
 template <typename T, int D>
-cudaError_t launch_mma(const WindowParams &p, int sms, cudaStream_t s) {
+cudaError_t launch_mma(const WindowParams &p, cudaStream_t s) {
     using Small = Mma<D, 4>;
     using Large = Mma<D, 8>;
     static_assert(3 * (Small::SMEM + 1024) <= 233472 && Large::SMEM <= 232448, "CTAs per SM");
     const int qblocks = (p.g + MQ - 1) / MQ;
     const long long units = (long long)p.sequences * p.hk * qblocks, rows = (long long)p.window + p.sinks;
-    const Shape a = best_split(units, rows, 4 * D, sms, 3, 3.6e4), b = best_split(units, rows, 4 * D, sms, 1, 5.8e4);
+    constexpr auto small = sh_window_decode_mma_kernel<T, D, 4>, large = sh_window_decode_mma_kernel<T, D, 8>;
+    int slots_a[4], slots_b[4];
+    cudaError_t e = cluster_slots<small>(128, Small::SMEM, slots_a);
+    if (e == cudaSuccess) e = cluster_slots<large>(256, Large::SMEM, slots_b);
+    if (e != cudaSuccess) return e;
+    const Shape a = best_split(units, rows, 4 * D, slots_a, 3.6e4), b = best_split(units, rows, 4 * D, slots_b, 5.8e4);
     // Fewer units than SMs: parts whose results a second launch merges (about 3 us) can fill every SM, a cluster of 8 cannot.
-    const long long parts = std::min(std::min((long long)sms, (long long)MAX_PARTS) / units, rows / 64);
+    const long long parts = std::min(std::min((long long)slots_b[0], (long long)MAX_PARTS) / units, rows / 64);
     if (p.part && parts > 1) {
         const double us = (double)rows * 4 * D / parts / std::min(6.4e6 / (double)(units * parts), 5.8e4) + 5.5;
         if (us < a.us && us < b.us) {
-            const cudaError_t e = launch_units<sh_window_decode_mma_kernel<T, D, 8>>(p, qblocks, 256, Large::SMEM, 1, (int)parts, s);
+            e = launch_units<large>(p, qblocks, 256, Large::SMEM, 1, (int)parts, s);
             if (e != cudaSuccess) return e;
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3((unsigned)(units * MQ));
@@ -713,19 +753,16 @@ cudaError_t launch_mma(const WindowParams &p, int sms, cudaStream_t s) {
             return cudaLaunchKernelEx(&cfg, sh_window_decode_merge_kernel<T, D>, p, qblocks, (int)parts, units);
         }
     }
-    return a.us <= b.us ? launch_units<sh_window_decode_mma_kernel<T, D, 4>>(p, qblocks, 128, Small::SMEM, a.S, 0, s)
-                        : launch_units<sh_window_decode_mma_kernel<T, D, 8>>(p, qblocks, 256, Large::SMEM, b.S, 0, s);
+    return a.us <= b.us ? launch_units<small>(p, qblocks, 128, Small::SMEM, a.S, 0, s)
+                        : launch_units<large>(p, qblocks, 256, Large::SMEM, b.S, 0, s);
 }
 
 }  // namespace
 
 cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, cudaStream_t s) {
-    int dev = 0, sms = 0;
-    const cudaError_t e = sh_device_sms(&dev, &sms);
-    if (e != cudaSuccess) return e;
-    if (dtype == SH_F32) return D == 128 ? launch_f32<128>(p, sms, s) : launch_f32<64>(p, sms, s);
-    if (dtype == SH_F16) return D == 128 ? launch_mma<__half, 128>(p, sms, s) : launch_mma<__half, 64>(p, sms, s);
-    return D == 128 ? launch_mma<__nv_bfloat16, 128>(p, sms, s) : launch_mma<__nv_bfloat16, 64>(p, sms, s);
+    if (dtype == SH_F32) return D == 128 ? launch_f32<128>(p, s) : launch_f32<64>(p, s);
+    if (dtype == SH_F16) return D == 128 ? launch_mma<__half, 128>(p, s) : launch_mma<__half, 64>(p, s);
+    return D == 128 ? launch_mma<__nv_bfloat16, 128>(p, s) : launch_mma<__nv_bfloat16, 64>(p, s);
 }
 
 size_t sh_window_decode_scratch(int sequences, int hk, int g, int dtype, int D) {
