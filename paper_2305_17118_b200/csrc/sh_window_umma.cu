@@ -83,7 +83,7 @@ struct Bars {
     uint64_t q_full[2], q_empty[2];        // a query tile landed / its last S has been computed
     uint64_t full[5], empty[5];            // stages: landed / read by the MMAs
     uint64_t s_full[2][2], p_ready[2][2];  // [query tile][buffer of S]
-    uint64_t pv_done[2];
+    uint64_t pv_done[2][2];                // (by buffer too: when a softmax warp waits for P.V(n), only P.V(n-2) is sure to be over)
     uint64_t step_full[STEPS], step_empty[STEPS];
     Step steps[STEPS];
     uint32_t tmem;
@@ -367,8 +367,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     if (tid == 0) {
         for (int t = 0; t < 2; ++t) {
             mbar_init(&bars->q_full[t], 1); mbar_init(&bars->q_empty[t], 1);
-            mbar_init(&bars->pv_done[t], 1);
-            for (int b = 0; b < 2; ++b) { mbar_init(&bars->s_full[t][b], 1); mbar_init(&bars->p_ready[t][b], 4); }
+            for (int b = 0; b < 2; ++b) { mbar_init(&bars->pv_done[t][b], 1); mbar_init(&bars->s_full[t][b], 1); mbar_init(&bars->p_ready[t][b], 4); }
         }
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 2); }
         for (int s = 0; s < STEPS; ++s) { mbar_init(&bars->step_full[s], 1); mbar_init(&bars->step_empty[s], SOFTMAX_WARPS); }
@@ -412,7 +411,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
 #pragma unroll
                 for (int x = 0; x < TN / 16; ++x)     // (the first product of an item overwrites O)
                     umma_ts(C::O_COL + t * D, (2 * t + b) * TN + x * 8, plus(vd, x * 2048), idesc_pv, begun || x > 0);
-                umma_commit(&bars->pv_done[t]);
+                umma_commit(&bars->pv_done[t][b]);
                 umma_commit(&bars->empty[due]);
             }
             __syncwarp();
@@ -625,7 +624,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 if (__any_sync(0xffffffffu, grown)) {
                     const float f = m == -CUDART_INF_F ? 0.f : ex2_approx((m - mn) * c);
                     if (begun) {
-                        ok = wait_for(bars, &bars->pv_done[t], (cnt - 1) & 1, 0x622);      // the product before this one is in O
+                        ok = wait_for(bars, &bars->pv_done[t][buf ^ 1], ((cnt - 1) >> 1) & 1, 0x622);      // the product before this one is in O
                         if (__any_sync(0xffffffffu, !ok)) break;
                         tc_fence_after();
 #pragma unroll
@@ -672,7 +671,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 fetch();
             }
             if (!(flags & STEP_LAST) || !begun) continue;
-            ok = wait_for(bars, &bars->pv_done[t], (cnt - 1) & 1, 0x623);
+            ok = wait_for(bars, &bars->pv_done[t][(cnt - 1) & 1], ((cnt - 1) >> 1) & 1, 0x623);
             tc_fence_after();
             const float inv = 1.f / l;
             if (__any_sync(0xffffffffu, !ok)) break;

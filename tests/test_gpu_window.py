@@ -181,6 +181,33 @@ def test_prompt_chunks_with_large_logits_and_many_sequences(dtype):
     _prefill_case(dtype, 64, 1, 2, 24, 2, lens, [(i * 13) % 70 for i in range(75)], seed=9)
 
 
+@pytest.mark.parametrize("dtype,hk,g,d", [("bf16", 8, 4, 128), ("f16", 16, 1, 128), ("bf16", 4, 7, 64), ("f32", 4, 2, 64)])
+def test_prompts_that_fill_the_device(dtype, hk, g, d):
+    """Many tiles on every SM, short and long sequences mixed: every row against a definition in 64 bits, and run after run the same."""
+    sh, gen, dt = _sh(), _gen(14), DT[dtype]
+    lens, ctx, window, sinks = (1, 200, 777, 1500, 0, 130, 640), (0, 100, 0, 700, 5, 3000, 650), 640, 4
+    hist = _history(gen, lens, ctx, hk, d, dt)
+    kc, vc = _caches(hist, ctx, hk, d, window, sinks, dt, 0.0)
+    k, v = (torch.cat([h[x][c:] for h, c in zip(hist, ctx)]) for x in (0, 1))
+    q = _rnd(gen, sum(lens), hk * g, d, dtype=dt)
+    starts = [sum(lens[:i]) for i in range(len(lens) + 1)]
+    args = dict(window=window, sinks=sinks, lengths=_i32(ctx), k_cache=kc, v_cache=vc)
+    out = sh.window_prefill(q, k, v, _i32(starts), **args)
+    for _ in range(12):
+        assert torch.equal(sh.window_prefill(q, k, v, _i32(starts), **args), out)
+    for i, (n, c) in enumerate(zip(lens, ctx)):
+        if n == 0:
+            continue
+        keys, vals = (x.double().repeat_interleave(g, 1).transpose(0, 1) for x in hist[i])      # [hq, c + n, d]
+        qs = q[starts[i]:starts[i + 1]].double().transpose(0, 1)
+        see = ref.visible(torch.arange(c, c + n)[:, None], torch.arange(c + n)[None], window, sinks).cuda()
+        logits = (qs @ keys.transpose(1, 2) * d ** -0.5).masked_fill(~see, float("-inf"))
+        want = (torch.softmax(logits, -1) @ vals).transpose(0, 1).cpu()
+        vmax = vals.abs().amax((1, 2)).view(1, -1, 1).cpu()
+        smax = (qs.abs().amax((1, 2)) * keys.abs().sum(-1).amax(-1) * d ** -0.5).view(1, -1, 1).cpu()
+        ref.check(out[starts[i]:starts[i + 1]], want, ref.attend_tolerance(want, vmax, smax, dt), f"sequence {i}")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 def test_tokens_out_of_sight_never_matter(dtype, bad):
