@@ -66,4 +66,24 @@ __device__ __forceinline__ int position_in(int s, int cached, int sinks, int win
     return s + (c - 1 - j) / window * window;
 }
 
+// The slots of one cache: [0, min(sinks, cached)) hold the sinks, [sinks, head) the positions cached - (head - slot), and, once the ring
+// has wrapped, [head, sinks + window) the positions cached - window + (slot - head).  Slots from `live` on hold nothing.
+struct Ring {
+    int cached, sinks, window, live, head;
+    bool wrapped;
+    __device__ __forceinline__ Ring() {}
+    __device__ __forceinline__ Ring(int cached_, int sinks_, int window_) : cached(cached_), sinks(sinks_), window(window_) {
+        live = min(cached, sinks + window);
+        wrapped = cached > sinks + window;
+        head = wrapped ? sinks + (cached - sinks) % window : cached;
+    }
+    // do the slots [x, y) hold a sink, or a position from `oldest` on?
+    __device__ __forceinline__ bool any(int x, int y, int oldest) const {
+        y = min(y, live);
+        if (x < min(sinks, cached)) return true;
+        if (wrapped && y > head && cached - window + (y - 1 - head) >= oldest) return true;
+        return x < head && y > sinks && cached - head + min(y, head) - 1 >= oldest;
+    }
+};
+
 }  // namespace shwin

@@ -185,15 +185,13 @@ __device__ __forceinline__ bool elect_one() {
     return p != 0;
 }
 
-// One work item and the key tiles it has to walk over.  Tiles 0 .. ctiles - 1 are blocks of 128 cache slots, tile ctiles + j holds
-// the chunk's rows 128 j ...  In the cache, slots [sinks, head) hold the positions cached - (head - slot), and, once the ring has
-// wrapped, slots [head, sinks + window) the positions cached - window + (slot - head).
-struct Item {
-    int seq, first, count, cached;         // seq < 0: there is no such item
+// One work item and the key tiles it has to walk over.  Tiles 0 .. ctiles - 1 are blocks of TN cache slots, tile ctiles + j holds the
+// chunk's rows TN * j ...
+struct Item : Ring {
+    int seq, first, count;                 // seq < 0: there is no such item
     int kvh, hb;
     int a;                                 // first token of query tile 0, counted in the chunk; tile t starts at a + t * tpt
-    int live, head, ctiles, jlo, jhi, tpt, sinks, window;
-    bool wrapped;
+    int ctiles, jlo, jhi, tpt;
 
     __device__ __forceinline__ int ring2() const { return wrapped ? sinks + window : 0; }
     __device__ __forceinline__ int from(int t) const { return a + t * tpt; }
@@ -203,14 +201,7 @@ struct Item {
     __device__ __forceinline__ bool need(int t, int i) const {
         if (!has(t)) return false;
         const int oldest = cached + from(t) - window + 1;      // position
-        if (i < ctiles) {
-            const int x = i * TN, y = min(x + TN, live);
-            if (x < min(sinks, cached)) return true;
-            if (wrapped && y > head) {
-                if (cached - window + (y - 1 - head) >= oldest) return true;
-            }
-            return x < head && y > sinks && cached - head + min(y, head) - 1 >= oldest;
-        }
+        if (i < ctiles) return any(i * TN, i * TN + TN, oldest);
         const int j = (i - ctiles) * TN;
         return j <= last(t) && (cached + j + TN - 1 >= oldest || cached + j < sinks);
     }
@@ -266,11 +257,8 @@ __device__ __forceinline__ Item find_item(const UmmaParams &p, long long id) {
     }
     if (r.seq < 0) return r;
     r.kvh = in / p.hblocks; r.hb = in % p.hblocks;
-    r.tpt = p.tpt; r.sinks = p.w.sinks; r.window = p.w.window;
-    if (!p.w.kc) r.cached = 0;
-    r.live = min(r.cached, r.sinks + r.window);
-    r.wrapped = r.cached > r.sinks + r.window;
-    r.head = r.wrapped ? r.sinks + (r.cached - r.sinks) % r.window : r.cached;
+    r.tpt = p.tpt;
+    static_cast<Ring &>(r) = Ring(p.w.kc ? r.cached : 0, p.w.sinks, p.w.window);
     r.ctiles = (r.live + TN - 1) / TN;
     r.jlo = max(0, r.a - r.window + 1) / TN;
     r.jhi = r.last(r.has(1) ? 1 : 0) / TN;
