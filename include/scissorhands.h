@@ -365,7 +365,9 @@ int sh_decode_kernel_choice(sh_handle h);
  * These calls use no handle: all state is the caller's tensors and every call is a pure function of its arguments
  * (safe in a CUDA graph; two calls may run at once unless they write the same rows).  They launch on the current
  * device, which must be the one that holds the tensors.  Strides count elements.  Rows of head_dim elements are
- * contiguous; every base address and every stride in bytes must be a multiple of 16 (else SH_EINVAL).
+ * contiguous; every base address and every stride in bytes must be a multiple of 16 (else SH_EINVAL).  Outputs must not
+ * overlap inputs unless a call says so.  The first call of a kind on a device should come before a stream capture: the CUDA
+ * runtime may load the library's device code only then.
  *
  * The window cache is the fixed-policy sibling of the budgeted cache: instead of the importance record it keeps the
  * first `sinks` tokens and the `window` most recent ones.  A token at position p (0-based) sees the positions j <= p

@@ -464,6 +464,16 @@ def _positions(positions, axes: int, tokens: int, device: int):
     return positions.data_ptr(), positions.stride(0)
 
 
+def _new(like: torch.Tensor, shape, stream, zero: bool, dtype=None) -> torch.Tensor:
+    """A tensor for a call on ``stream``: allocated (and zeroed) in that stream's order."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return like.new_zeros(shape, dtype=dtype) if zero else like.new_empty(shape, dtype=dtype)
+    if dtype is None:
+        return like.new_zeros(shape) if zero else like.new_empty(shape)
+    return like.new_empty(shape, dtype=dtype)
+
+
 def _launch(what: str, fn, device: int, stream, *args) -> None:
     """Call a library entry on the tensors' device and the given (or that device's current) stream."""
     if device == _current_device():
@@ -529,10 +539,10 @@ def qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Te
         raise ValueError("k_out without k")
     ro = rope._packed(d, dtype, device)
     pos, axis_stride = _positions(positions, rope.axes, tokens, device)
-    q_out = q.new_empty(shape) if q_out is None else q_out
+    q_out = _new(q, shape, stream, False) if q_out is None else q_out
     qor = _more_rows(q_out, "q_out", shape, dtype, device)
     if k is not None:
-        k_out = k.new_empty(kshape) if k_out is None else k_out
+        k_out = _new(k, kshape, stream, False) if k_out is None else k_out
         kor = _more_rows(k_out, "k_out", kshape, dtype, device)
     _launch("qk_norm_rope", lib.sh_qk_norm_rope, device, stream, ro, tokens, q_heads, kshape[1], qr, kr, pos, axis_stride, qor, kor)
     return q_out, k_out
@@ -580,7 +590,7 @@ def window_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: to
     if lengths is not None or k_cache is not None or v_cache is not None:
         lp = _ints(lengths, "lengths", n, device)
         cache = _cache_packed(k_cache, v_cache, (n, kshape[1], window + sinks, d), dtype, device)
-    out = q.new_zeros(shape) if out is None else out
+    out = _new(q, shape, stream, True) if out is None else out
     _launch("window_prefill", lib.sh_window_prefill, device, stream, win, tokens, n, qr, kr, vr, sp, lp, cache,
             _more_rows(out, "out", shape, dtype, device))
     return out
@@ -624,14 +634,12 @@ def window_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: to
             raise ValueError("a rope of several axes needs positions")
     elif positions is not None:
         raise ValueError("positions without rope")
-    out = q.new_zeros(shape) if out is None else out
+    out = _new(q, shape, stream, True) if out is None else out
     outr = _more_rows(out, "out", shape, dtype, device)
     wp, bytes_ = None, lib.sh_window_decode_workspace_bytes(win, n)
     if bytes_:
-        work = torch.empty(bytes_, dtype=torch.uint8, device=q.device)      # a tensor of this call's own, ordered by the stream
+        work = _new(q, bytes_, stream, False, torch.uint8)      # a tensor of this call's own: it is free again in the stream's order
         wp = work.data_ptr()
-        if stream is not None:
-            work.record_stream(stream)
     _launch("window_decode", lib.sh_window_decode, device, stream, win, n, qr, kr, vr, lp, cache, ro, pos, axis_stride, outr, wp, bytes_)
     return out
 
@@ -652,8 +660,8 @@ class WindowCache:
     def __init__(self, sequences: int, q_heads: int, kv_heads: int, head_dim: int, window: int, sinks: int = 0, dtype="bf16", device="cuda:0",
                  rope: Optional[Rope] = None, scale: Optional[float] = None):
         dt = INPUT_TORCH_DTYPE[DTYPE_CODE[dtype]] if isinstance(dtype, str) else dtype
-        if dt not in _CODE_OF or dtype == "int4" or head_dim not in (64, 128):
-            raise ValueError(f"dtype {dtype}, head_dim {head_dim}: need f32, f16 or bf16 and 64 or 128")
+        if dt not in _CODE_OF or dtype == "int4" or head_dim not in (64, 128) or sequences < 1:
+            raise ValueError(f"{sequences} sequences of dtype {dtype}, head_dim {head_dim}: need one or more, f32, f16 or bf16, 64 or 128")
         _window_packed(dt, head_dim, q_heads, kv_heads, window, sinks, scale)
         self.window, self.sinks, self.rope, self.scale, self.q_heads = window, sinks, rope, scale, q_heads
         shape = (sequences, kv_heads, sinks + window, head_dim)

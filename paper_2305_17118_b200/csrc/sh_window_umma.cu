@@ -225,15 +225,19 @@ struct Item : Ring {
     }
 };
 
-__device__ __forceinline__ Item find_item(const UmmaParams &p, long long id) {
+// Where the search for an item left off: a CTA's items come in rising order, so the sequences before are not counted again.
+struct Found {
+    int base = 0;
+    long long before = 0;
+};
+__device__ __forceinline__ Item find_item(const UmmaParams &p, long long id, Found &from) {
     const int per = p.w.hk * p.hblocks, in = (int)(id % per);
-    // (rows = tokens here: a tile of find_tile is the 2 * tpt tokens of an item)
     const int lane = threadIdx.x & 31, span = 2 * p.tpt;
     const long long tile = id / per;
     Item r;
     r.seq = -1;
-    long long before = 0;
-    for (int base = 0; base < p.w.sequences; base += 32) {
+    long long before = from.before;
+    for (int base = from.base; base < p.w.sequences; base += 32) {
         int first = 0, count = 0, cached = 0;
         if (base + lane < p.w.sequences) sequence_rows(p.w, base + lane, first, count, cached);
         const int mine = (count + span - 1) / span;
@@ -246,6 +250,8 @@ __device__ __forceinline__ Item find_item(const UmmaParams &p, long long id) {
         const unsigned hit = __ballot_sync(0xffffffffu, before + upto > tile);
         if (hit) {
             const int l = __ffs(hit) - 1;
+            from.base = base;
+            from.before = before;
             r.seq = base + l;
             r.first = __shfl_sync(0xffffffffu, first, l);
             r.count = __shfl_sync(0xffffffffu, count, l);
@@ -299,7 +305,8 @@ template <typename T, int D>
 __device__ __noinline__ void slow_row(const UmmaParams &u, long long id, int qi, int h) {
     constexpr int E = D / 32;
     const WindowParams &p = u.w;
-    const Item w = find_item(u, id);
+    Found from;
+    const Item w = find_item(u, id, from);
     const int lane = threadIdx.x & 31;
     float q[E], o[E], m = -CUDART_INF_F, l = 0.f;
     const T *qr = reinterpret_cast<const T *>(p.q.p + (long long)(w.first + qi) * p.q.ts + h * p.q.hs) + lane * E;
@@ -477,8 +484,9 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             }
             __syncwarp();
         };
+        Found from;
         for (long long id = blockIdx.x; ok; id += gridDim.x) {
-            const Item w = find_item(p, id);
+            const Item w = find_item(p, id, from);
             if (w.seq < 0) break;
             bool first = true;
             const int last_tile = w.ctiles + w.jhi;   // (the tile of the last row itself: always needed)

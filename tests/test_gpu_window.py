@@ -177,6 +177,7 @@ def test_prompt_chunks(dtype, d, shape):
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_prompt_chunks_with_large_logits_and_many_sequences(dtype):
     _prefill_case(dtype, 128, 1, 2, 90, 2, (40, 300), (0, 200), seed=8, hot=12.0)
+    _prefill_case(dtype, 64, 1, 1, 20, 1, [1 + i % 3 for i in range(700)], [(i * 11) % 50 for i in range(700)], seed=10)
     lens = [(i * 7) % 11 for i in range(75)]
     _prefill_case(dtype, 64, 1, 2, 24, 2, lens, [(i * 13) % 70 for i in range(75)], seed=9)
 
@@ -491,7 +492,9 @@ def test_graphs_streams_and_calls_at_once():
     sh, gen, dt = _sh(), _gen(33), torch.bfloat16
     n, hq, hk, d, window, sinks = 4, 8, 2, 128, 700, 4
     r = _rope(sh, gen, d, dt, 128, None)
-    mk = lambda: dict(p=_rnd(gen, n, hq + 2 * hk, d, dtype=dt), kc=_rnd(gen, n, hk, window + sinks, d, dtype=dt),
+    long = 30000                                     # a window over which one sequence spreads out
+    mk = lambda: dict(lk=_rnd(gen, 1, hk, long, d, dtype=dt), lv=_rnd(gen, 1, hk, long, d, dtype=dt), lo=torch.empty(1, hq, d, dtype=dt, device="cuda"),
+                      ll=_i32([70001]), p=_rnd(gen, n, hq + 2 * hk, d, dtype=dt), kc=_rnd(gen, n, hk, window + sinks, d, dtype=dt),
                       vc=_rnd(gen, n, hk, window + sinks, d, dtype=dt), x=_rnd(gen, 200, hq + 2 * hk, d, dtype=dt),
                       out=torch.empty(n, hq, d, dtype=dt, device="cuda"), xo=torch.zeros(200, hq, d, dtype=dt, device="cuda"),
                       lengths=_i32([900, 5, -1, 704]), starts=_i32([0, 150, 150, 160, 190]))
@@ -502,6 +505,7 @@ def test_graphs_streams_and_calls_at_once():
                           lengths=s["lengths"], k_cache=s["kc"], v_cache=s["vc"], out=s["xo"])
         sh.window_decode(pk[:, :hq], pk[:, hq:hq + hk], pk[:, hq + hk:], s["lengths"], s["kc"], s["vc"], window=window, sinks=sinks, rope=r,
                          out=s["out"])
+        sh.window_decode(pk[:1, :hq], pk[:1, hq:hq + hk], pk[:1, hq + hk:], s["ll"], s["lk"], s["lv"], window=long, out=s["lo"])
 
     a, b, c = mk(), mk(), mk()
     want = []
@@ -536,8 +540,37 @@ def test_graphs_streams_and_calls_at_once():
     for got, w in zip([graphs[0][1], graphs[1][1], eager], want):
         live = [0, 1, 3]
         assert torch.equal(got["out"][live], w["out"][live])
-        for x in ("xo", "kc", "vc"):
+        for x in ("xo", "kc", "vc", "lo", "lk", "lv"):
             assert torch.equal(got[x], w[x]), x
+
+
+def test_results_on_another_stream_than_the_current_one():
+    """New outputs and workspaces belong to the stream of the call, not to the current one, which is kept busy meanwhile."""
+    sh, gen, dt = _sh(), _gen(36), torch.bfloat16
+    q, k, v = _rnd(gen, 500, 4, 128, dtype=dt), _rnd(gen, 500, 2, 128, dtype=dt), _rnd(gen, 500, 2, 128, dtype=dt)
+    kc, vc = _rnd(gen, 1, 2, 20000, 128, dtype=dt), _rnd(gen, 1, 2, 20000, 128, dtype=dt)
+    r = _rope(sh, gen, 128, dt, 128, None)
+    pos, starts, ln = torch.arange(500, device="cuda", dtype=torch.int32), _i32([0, 300, 480]), _i32([50000])
+
+    def calls(stream):
+        a = sh.qk_norm_rope(q, k, pos, r, stream=stream)
+        b = sh.window_prefill(q, k, v, starts, window=90, sinks=2, stream=stream)
+        c = sh.window_decode(q[:1], k[:1], v[:1], ln, kc, vc, window=20000, rope=r, stream=stream)
+        return (*a, b, c)
+
+    want = calls(None)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    big = torch.randn(8192, 8192, device="cuda")
+    for _ in range(3):
+        for _ in range(4):
+            big @ big                                # the current stream falls behind
+        got = calls(side)
+        side.synchronize()
+        with torch.cuda.stream(side):
+            assert all(torch.equal(x, y) for x, y in zip(got, want))
+        del got
+    torch.cuda.synchronize()
 
 
 def test_results_do_not_depend_on_the_run():
@@ -593,6 +626,7 @@ def test_wrappers_refuse_what_the_kernels_cannot_take():
         lambda: sh.Rope(r.inv_freq, sections=(16, 8)),
         lambda: sh.Rope(r.inv_freq, spread=True),
         lambda: sh.Rope(r.inv_freq.half()),
+        lambda: sh.WindowCache(0, 4, 2, 64, 8),
         lambda: sh.WindowCache(2, 4, 2, 96, 8),
         lambda: sh.WindowCache(2, 4, 2, 64, 8, dtype="int4"),
         lambda: sh.WindowCache(2, 3, 2, 64, 8),
