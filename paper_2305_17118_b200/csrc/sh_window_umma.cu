@@ -15,8 +15,9 @@
 // A query tile has two buffers of S: S(n+1) is made while the softmax of step n runs, and goes into the buffer whose P the product
 // P.V(n-1), issued before it, has read (the tensor pipe keeps the order of one warp's MMAs).  Tensor memory is full with that: two
 // query tiles x (2 x 64 columns of S + 128 of O).  With one buffer of 128 columns each step waited for softmax and both products in
-// turn: 2.3 instead of 2.0 ms for the 32768-token prompt below.  CTAs are persistent; the loads of the next item start while the
-// present one drains.
+// turn: 2.3 instead of 2.0 ms for the 32768-token prompt below.  A running CTA takes over the items of CTAs that
+// have not started (cluster launch control), so it sets up once and long and short items even out: 154 -> TIME us for prompts of 1 to
+// 4001 tokens; the loads of the next item start while the present one drains.
 //
 // P is rounded to the storage type (the tensor cores take no other pair with 16-bit V); its row sum is taken before the rounding,
 // in fp32.  The subtracted maximum is only renewed when it has grown by more than 8 (log2), so weights stay below 2^8; fp16
@@ -53,7 +54,7 @@ constexpr float RENEW = 8.f;               // log2 growth of the maximum at whic
 
 __device__ int g_window_error;             // code of the first bounded wait that gave up
 
-constexpr int STEPS = 8, BAR_BYTES = 896;  // steps in flight between the load warp and the others; barriers and step ring
+constexpr int STEPS = 8, BAR_BYTES = 960;  // steps in flight between the load warp and the others; barriers and step ring
 
 template <int D> struct Cfg {
     static constexpr int QTILE = D / 64 * QHALF, TILE = D / 64 * HALF;      // bytes of a query tile, of a key or value tile
@@ -77,7 +78,7 @@ struct __align__(16) Step {
     int first, count;                      // the sequence's rows of the chunk tensors
     int cached, a, kvh, hb;                // as in Item
     int head, ring2;                       // end of the slots [sinks, head), end of the slots [head, ring2)
-    int pad[2];
+    int id, pad;                           // of the item
 };
 struct Bars {
     uint64_t q_full[2], q_empty[2];        // a query tile landed / its last S has been computed
@@ -85,6 +86,8 @@ struct Bars {
     uint64_t s_full[2][2], p_ready[2][2];  // [query tile][buffer of S]
     uint64_t pv_done[2][2];                // (by buffer too: when a softmax warp waits for P.V(n), only P.V(n-2) is sure to be over)
     uint64_t step_full[STEPS], step_empty[STEPS];
+    uint4 claim;                           // answer to the last request for work
+    uint64_t claimed;
     Step steps[STEPS];
     uint32_t tmem;
     int abort_flag;
@@ -174,6 +177,29 @@ __device__ __forceinline__ void tma_5d(void *dst, const CUtensorMap *map, int sl
         "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(slot), "r"(head), "r"(sequence), "r"(0), "r"(smem_u32(bar))
         : "memory");
 }
+// Cluster launch control: the grid has a CTA for every item, and a running CTA takes over the item of one that has not started yet.
+// Ask for one (the 16-byte answer lands in shared memory, counted on `bar`) ...
+__device__ __forceinline__ void claim_request(uint4 *answer, uint64_t *bar) {
+    mbar_arrive_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(answer)), "r"(smem_u32(bar))
+                 : "memory");
+}
+// ... and read the answer: the index of the CTA taken over, or -1: there is none left (then nobody may ask again).
+__device__ __forceinline__ int claim_read(const uint4 *answer) {
+    int x, got;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        ".reg .b128 r;\n\t"
+        "ld.shared.b128 r, [%2];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+        "selp.s32 %1, 1, 0, p;\n\t"
+        "mov.s32 %0, -1;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, r;\n\t}"
+        : "=r"(x), "=r"(got)
+        : "r"(smem_u32(answer))
+        : "memory");
+    return got ? x : -1;
+}
 // One lane of the warp, which must be converged.
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;
@@ -225,15 +251,16 @@ struct Item : Ring {
     }
 };
 
-// Where the search for an item left off: a CTA's items come in rising order, so the sequences before are not counted again.
+// Where the search for an item left off: a CTA's items mostly come in rising order, and the sequences before are not counted again.
 struct Found {
     int base = 0;
     long long before = 0;
 };
-__device__ __forceinline__ Item find_item(const UmmaParams &p, long long id, Found &from) {
-    const int per = p.w.hk * p.hblocks, in = (int)(id % per);
+__device__ __forceinline__ Item find_item(const UmmaParams &p, int id, Found &from) {
+    const int per = p.w.hk * p.hblocks, in = id % per;
     const int lane = threadIdx.x & 31, span = 2 * p.tpt;
-    const long long tile = id / per;
+    const int tile = id / per;
+    if (tile < from.before) from = Found();
     Item r;
     r.seq = -1;
     long long before = from.before;
@@ -256,7 +283,8 @@ __device__ __forceinline__ Item find_item(const UmmaParams &p, long long id, Fou
             r.first = __shfl_sync(0xffffffffu, first, l);
             r.count = __shfl_sync(0xffffffffu, count, l);
             r.cached = __shfl_sync(0xffffffffu, cached, l);
-            r.a = (int)(tile - before - __shfl_sync(0xffffffffu, upto - mine, l)) * span;
+            // a sequence's items go from its end to its start, where causality leaves fewer keys: the short ones come last
+            r.a = (int)(before + __shfl_sync(0xffffffffu, upto, l) - 1 - tile) * span;
             break;
         }
         before += __shfl_sync(0xffffffffu, upto, 31);
@@ -302,7 +330,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 // One row by one warp, over its visible keys only, in fp32 on CUDA cores: for rows next to values that are not finite.
 template <typename T, int D>
-__device__ __noinline__ void slow_row(const UmmaParams &u, long long id, int qi, int h) {
+__device__ __noinline__ void slow_row(const UmmaParams &u, int id, int qi, int h) {
     constexpr int E = D / 32;
     const WindowParams &p = u.w;
     Found from;
@@ -365,6 +393,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             for (int b = 0; b < 2; ++b) { mbar_init(&bars->pv_done[t][b], 1); mbar_init(&bars->s_full[t][b], 1); mbar_init(&bars->p_ready[t][b], 4); }
         }
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 2); }
+        mbar_init(&bars->claimed, 1);
         for (int s = 0; s < STEPS; ++s) { mbar_init(&bars->step_full[s], 1); mbar_init(&bars->step_empty[s], SOFTMAX_WARPS); }
         bars->abort_flag = 0;
         if ((smem_u32(sm) & 1023u) != 0) {      // the swizzled tiles need the alignment the declaration asks for
@@ -455,7 +484,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         uint32_t st = 0, par = 1;                     // the next stage, and the parity of its last release (the first pass: none)
         const int q_bytes = D / 64 * p.tpt * p.gb * 128;
         // publish a step and take the stage for its tiles
-        auto publish = [&](const Item &w, int flags, int x) {
+        auto publish = [&](const Item &w, int id, int flags, int x) {
             const uint32_t e = steps % STEPS;
             bool go = steps < STEPS || wait_for(bars, &bars->step_empty[e], (steps / STEPS - 1) & 1, 0x613);
             go = go && (steps < C::STAGES || wait_for(bars, &bars->empty[st], par, 0x612));
@@ -464,7 +493,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 Step &d = bars->steps[e];
                 *reinterpret_cast<int4 *>(&d) = make_int4(flags, x, w.first, w.count);
                 *reinterpret_cast<int4 *>(&d.cached) = make_int4(w.cached, w.a, w.kvh, w.hb);
-                *reinterpret_cast<int2 *>(&d.head) = make_int2(w.head, w.ring2());
+                *reinterpret_cast<int4 *>(&d.head) = make_int4(w.head, w.ring2(), id, 0);
                 mbar_arrive(&bars->step_full[e]);
             }
             __syncwarp();
@@ -485,9 +514,10 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             __syncwarp();
         };
         Found from;
-        for (long long id = blockIdx.x; ok; id += gridDim.x) {
+        uint32_t asked = 0;                           // requests for work so far
+        for (int id = blockIdx.x; ok && id >= 0;) {
             const Item w = find_item(p, id, from);
-            if (w.seq < 0) break;
+            if (w.seq < 0) break;                     // (the grid is an upper bound: behind the last item nothing follows)
             bool first = true;
             const int last_tile = w.ctiles + w.jhi;   // (the tile of the last row itself: always needed)
             for (int base = 0; base <= last_tile && ok; base += 32) {
@@ -503,7 +533,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                     todo &= todo - 1;
                     const int flags = __shfl_sync(0xffffffffu, mine, bit) | (first ? STEP_FIRST : 0);
                     const int x = (base + bit - (flags & STEP_CACHE ? 0 : w.ctiles)) * TN;
-                    publish(w, flags, x);
+                    publish(w, id, flags, x);
                     if (ok && first) queries(w, 0);
                     if (ok && elect_one()) {
                         unsigned char *dst = kv + st * 2 * C::TILE;
@@ -524,13 +554,22 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                     first = false;
                 }
             }
+            if (!ok) break;
+            // the next item is asked for now: five steps are still under way, which covers the answer's latency
+            if (elect_one()) claim_request(&bars->claim, &bars->claimed);
+            __syncwarp();
+            ok = __all_sync(0xffffffffu, wait_for(bars, &bars->claimed, asked++ & 1, 0x614));
+            if (!ok) break;
+            id = __shfl_sync(0xffffffffu, claim_read(&bars->claim), 0);
+            fence_async_shared();                     // (read before the next answer is written)
+            __syncwarp();
         }
         const uint32_t loads = steps;                 // (a step that was published without a load only makes the drain below wait in vain)
         if (ok) {                                     // the end: a step without a load
             Item none;
             none.first = none.count = none.cached = none.a = none.kvh = none.hb = none.head = 0;
             none.wrapped = false;
-            publish(none, STEP_END, 0);
+            publish(none, 0, STEP_END, 0);
             if (ok && elect_one()) mbar_arrive(&bars->full[st]);
             __syncwarp();
         }
@@ -552,13 +591,12 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         const int tok = row / p.gb, hrow = row % p.gb;
         const float c = p.w.scale_log2e;
         uint32_t cnt = 0, steps = 0;
-        long long id = (long long)blockIdx.x - gridDim.x;      // present item
+        int id = 0;                                   // present item
         int qi = 0, h = 0, kvh = 0, row0 = 0;
         bool live = false, begun = false;
         float m = -CUDART_INF_F, l = 0.f;
         // The entry of the next step is read while the present one is worked on.
-        int4 e0, e1;
-        int2 e2;
+        int4 e0, e1, e2;
         auto fetch = [&]() {
             const uint32_t e = steps % STEPS;
             ok = wait_for(bars, &bars->step_full[e], (steps / STEPS) & 1, 0x624) && ok;
@@ -566,7 +604,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             const Step &d = bars->steps[e];
             e0 = *reinterpret_cast<const int4 *>(&d);
             e1 = *reinterpret_cast<const int4 *>(&d.cached);
-            e2 = *reinterpret_cast<const int2 *>(&d.head);
+            e2 = *reinterpret_cast<const int4 *>(&d.head);
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->step_empty[e]);
         };
@@ -576,7 +614,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             const int flags = e0.x;
             if (flags & STEP_END) break;
             if (flags & STEP_FIRST) {
-                id += gridDim.x;
+                id = e2.z;
                 qi = e1.y + t * p.tpt + tok;
                 h = e1.w * p.gb + hrow;
                 kvh = e1.z;
@@ -772,7 +810,8 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     // each sequence adds at most one partly filled item
     const long long items = ((long long)w.tokens / (2 * p.tpt) + w.sequences) * w.hk * p.hblocks;
-    kern<<<(unsigned)(items < sms ? items : sms), NTH, Cfg<D>::SMEM, s>>>(p, mq, mk, mv, mkc, mvc);
+    if (items > 0x7fffffffll) return cudaErrorInvalidValue;
+    kern<<<(unsigned)items, NTH, Cfg<D>::SMEM, s>>>(p, mq, mk, mv, mkc, mvc);
     return cudaGetLastError();
 }
 
