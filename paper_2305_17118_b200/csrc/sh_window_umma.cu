@@ -58,8 +58,8 @@ constexpr int STEPS = 8, BAR_BYTES = 960;  // steps in flight between the load w
 
 template <int D> struct Cfg {
     static constexpr int QTILE = D / 64 * QHALF, TILE = D / 64 * HALF;      // bytes of a query tile, of a key or value tile
-    static constexpr int STAGES = 5;                   // steps in flight: a stage holds a key and a value tile
-    static constexpr int OFF_KV = 2 * QTILE;
+    static constexpr int STAGES = D == 128 ? 3 : 6;    // steps in flight: a stage holds a key and a value tile
+    static constexpr int OFF_KV = 4 * QTILE;           // query tiles of two items; a finished item's tiles serve to lay out its output
     static constexpr int OFF_BAR = OFF_KV + STAGES * 2 * TILE;
     static constexpr int SMEM = OFF_BAR + BAR_BYTES;
     static constexpr int O_COL = 4 * TN;               // tensor memory: per query tile two buffers of S (P inside), then O0, O1
@@ -81,8 +81,8 @@ struct __align__(16) Step {
     int id, pad;                           // of the item
 };
 struct Bars {
-    uint64_t q_full[2], q_empty[2];        // a query tile landed / its last S has been computed
-    uint64_t full[5], empty[5];            // stages: landed / read by the MMAs
+    uint64_t q_full[2][2], q_free[2][2];   // [query tile][item mod 2]: landed / its place may be filled again
+    uint64_t full[6], empty[6];            // stages: landed / read by the MMAs
     uint64_t s_full[2][2], p_ready[2][2];  // [query tile][buffer of S]
     uint64_t pv_done[2][2];                // (by buffer too: when a softmax warp waits for P.V(n), only P.V(n-2) is sure to be over)
     uint64_t step_full[STEPS], step_empty[STEPS];
@@ -389,8 +389,10 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     }
     if (tid == 0) {
         for (int t = 0; t < 2; ++t) {
-            mbar_init(&bars->q_full[t], 1); mbar_init(&bars->q_empty[t], 1);
-            for (int b = 0; b < 2; ++b) { mbar_init(&bars->pv_done[t][b], 1); mbar_init(&bars->s_full[t][b], 1); mbar_init(&bars->p_ready[t][b], 4); }
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(&bars->q_full[t][b], 1); mbar_init(&bars->q_free[t][b], 4);
+                mbar_init(&bars->pv_done[t][b], 1); mbar_init(&bars->s_full[t][b], 1); mbar_init(&bars->p_ready[t][b], 4);
+            }
         }
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 2); }
         mbar_init(&bars->claimed, 1);
@@ -425,7 +427,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         uint32_t st = 0, par = 0;                     // stage and parity of the next step
         uint32_t items = 0, steps = 0, done_s = 0, done_pv = 0;      // products S and P.V issued
         uint32_t due = C::STAGES;                     // stage of the step whose P.V is due (STAGES: none)
-        bool begun = false;                           // O holds products of this item
+        bool due_adds = false, begun = false;         // that P.V adds to O (its item's first overwrites it); S of this item was issued
         auto issue_pv = [&]() {
             const uint32_t b = done_pv & 1;
             ok = __all_sync(0xffffffffu, wait_for(bars, &bars->p_ready[t][b], (done_pv >> 1) & 1, 0x604));
@@ -433,24 +435,26 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             if (ok && elect_one()) {
                 const uint64_t vd = plus(v_desc, due * 2 * C::TILE);
 #pragma unroll
-                for (int x = 0; x < TN / 16; ++x)     // (the first product of an item overwrites O)
-                    umma_ts(C::O_COL + t * D, (2 * t + b) * TN + x * 8, plus(vd, x * 2048), idesc_pv, begun || x > 0);
+                for (int x = 0; x < TN / 16; ++x) umma_ts(C::O_COL + t * D, (2 * t + b) * TN + x * 8, plus(vd, x * 2048), idesc_pv, due_adds || x > 0);
                 umma_commit(&bars->pv_done[t][b]);
                 umma_commit(&bars->empty[due]);
             }
             __syncwarp();
             ++done_pv;
-            begun = true;
             due = C::STAGES;
         };
         while (ok) {
             ok = __all_sync(0xffffffffu, wait_for(bars, &bars->full[st], par, 0x603));
             if (!ok) break;
             const int now = __shfl_sync(0xffffffffu, *(volatile int *)&bars->steps[steps++ % STEPS].flags, 0);
-            if (now & STEP_END) break;
+            if (now & STEP_END) {
+                if (due < C::STAGES) issue_pv();
+                break;
+            }
             if (now & STEP_FIRST) {
-                ok = __all_sync(0xffffffffu, wait_for(bars, &bars->q_full[t], items++ & 1, 0x601) && !aborted());
+                ok = __all_sync(0xffffffffu, wait_for(bars, &bars->q_full[t][items & 1], (items >> 1) & 1, 0x601) && !aborted());
                 if (!ok) break;
+                ++items;
                 begun = false;
             }
             const bool need = now & (STEP_NEED0 << t);
@@ -458,25 +462,25 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             if (elect_one()) {
                 if (need) {
                     // S of this step goes into the buffer whose P the last but one P.V has read: the pipe keeps that order
-                    const uint64_t kd = plus(k_desc, st * 2 * C::TILE);
+                    const uint64_t kd = plus(k_desc, st * 2 * C::TILE), qd = plus(q_desc, ((items - 1) & 1) * 2 * C::QTILE);
                     const uint32_t b = done_s & 1;
 #pragma unroll
                     for (int x = 0; x < D / 16; ++x)
-                        umma_f16((2 * t + b) * TN, plus(q_desc, (x >> 2) * QHALF + (x & 3) * 32), plus(kd, (x >> 2) * HALF + (x & 3) * 32), idesc_s, x > 0);
+                        umma_f16((2 * t + b) * TN, plus(qd, (x >> 2) * QHALF + (x & 3) * 32), plus(kd, (x >> 2) * HALF + (x & 3) * 32), idesc_s, x > 0);
                     umma_commit(&bars->s_full[t][b]);
                 } else {
                     mbar_arrive(&bars->empty[st]);
                 }
-                if (now & STEP_LAST) umma_commit(&bars->q_empty[t]);
             }
             __syncwarp();
             if (due < C::STAGES) issue_pv();          // of the step before: its softmax ran while this S was made
             if (need) {
                 ++done_s;
                 due = st;
+                due_adds = begun;
+                begun = true;
             }
             if (++st == C::STAGES) { st = 0; par ^= 1; }
-            if ((now & STEP_LAST) && due < C::STAGES && ok) issue_pv();      // (the next item waits for its queries)
         }
     } else if (warp == SOFTMAX_WARPS + 2) {
         // ------------------------------------------------------------------------------------------------ loads
@@ -500,15 +504,16 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             ++steps;
         };
         auto queries = [&](const Item &w, int t) {
-            ok = __all_sync(0xffffffffu, (items == 0 || wait_for(bars, &bars->q_empty[t], (items - 1) & 1, 0x611)) && !aborted());
+            const uint32_t b = items & 1;
+            ok = __all_sync(0xffffffffu, (items < 2 || wait_for(bars, &bars->q_free[t][b], ((items >> 1) - 1) & 1, 0x611)) && !aborted());
             if (ok && elect_one()) {
                 if (w.has(t)) {
-                    mbar_arrive_expect_tx(&bars->q_full[t], q_bytes);
+                    mbar_arrive_expect_tx(&bars->q_full[t][b], q_bytes);
 #pragma unroll
                     for (int h = 0; h < D / 64; ++h)
-                        tma_3d(sm + t * C::QTILE + h * QHALF, &map_q, h * 64, w.kvh * p.w.g + w.hb * p.gb, w.first + w.from(t), &bars->q_full[t]);
+                        tma_3d(sm + (2 * b + t) * C::QTILE + h * QHALF, &map_q, h * 64, w.kvh * p.w.g + w.hb * p.gb, w.first + w.from(t), &bars->q_full[t][b]);
                 } else {
-                    mbar_arrive(&bars->q_full[t]);
+                    mbar_arrive(&bars->q_full[t][b]);
                 }
             }
             __syncwarp();
@@ -518,7 +523,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         for (int id = blockIdx.x; ok && id >= 0;) {
             const Item w = find_item(p, id, from);
             if (w.seq < 0) break;                     // (the grid is an upper bound: behind the last item nothing follows)
-            bool first = true;
+            bool first = true, ask = true;
             const int last_tile = w.ctiles + w.jhi;   // (the tile of the last row itself: always needed)
             for (int base = 0; base <= last_tile && ok; base += 32) {
                 // 32 tiles at a time, a lane each; what lies between the sinks and the window is passed over
@@ -529,6 +534,13 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                                  (need1 && w.whole(1, i) ? STEP_WHOLE1 : 0) | (i < w.ctiles ? STEP_CACHE : 0) | (i == last_tile ? STEP_LAST : 0);
                 unsigned todo = __ballot_sync(0xffffffffu, need0 || need1);
                 while (todo && ok) {
+                    // the next item is asked for a few steps before the end of this one: soon enough to cover the answer's latency, late
+                    // enough for the next item to go to whoever is done first
+                    if (ask && base + 32 > last_tile && __popc(todo) <= 3) {
+                        if (elect_one()) claim_request(&bars->claim, &bars->claimed);
+                        __syncwarp();
+                        ask = false;
+                    }
                     const int bit = __ffs(todo) - 1;
                     todo &= todo - 1;
                     const int flags = __shfl_sync(0xffffffffu, mine, bit) | (first ? STEP_FIRST : 0);
@@ -555,9 +567,6 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 }
             }
             if (!ok) break;
-            // the next item is asked for now: five steps are still under way, which covers the answer's latency
-            if (elect_one()) claim_request(&bars->claim, &bars->claimed);
-            __syncwarp();
             ok = __all_sync(0xffffffffu, wait_for(bars, &bars->claimed, asked++ & 1, 0x614));
             if (!ok) break;
             id = __shfl_sync(0xffffffffu, claim_read(&bars->claim), 0);
@@ -577,7 +586,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         // published, its stage's earlier load has been waited for)
         if (lane == 0) {
             if (items > 0)
-                for (int t = 0; t < 2; ++t) wait_for(bars, &bars->q_full[t], (items - 1) & 1, 0);
+                for (int t = 0; t < 2; ++t) wait_for(bars, &bars->q_full[t][(items - 1) & 1], ((items - 1) >> 1) & 1, 0);
             for (uint32_t k = 0; k < C::STAGES - (ok ? 1u : 0u) && k < loads; ++k)
                 wait_for(bars, &bars->full[(loads - 1 - k) % C::STAGES], ((loads - 1 - k) / C::STAGES) & 1, 0);
         }
@@ -590,7 +599,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         const uint32_t lanes = tbase + ((uint32_t)((warp & 3) * 32) << 16), s_addr = lanes + 2 * t * TN, o_addr = lanes + C::O_COL + t * D;
         const int tok = row / p.gb, hrow = row % p.gb;
         const float c = p.w.scale_log2e;
-        uint32_t cnt = 0, steps = 0;
+        uint32_t cnt = 0, steps = 0, items = 0;
         int id = 0;                                   // present item
         int qi = 0, h = 0, kvh = 0, row0 = 0;
         bool live = false, begun = false;
@@ -624,6 +633,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 m = -CUDART_INF_F;
                 l = 0.f;
                 ok = !aborted();
+                ++items;
             }
             if (flags & (STEP_NEED0 << t)) {
                 const bool whole = flags & (STEP_WHOLE0 << t);
@@ -704,12 +714,22 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             } else {
                 fetch();
             }
-            if (!(flags & STEP_LAST) || !begun) continue;
+            if (!(flags & STEP_LAST)) continue;
+            const uint32_t qbuf = (items - 1) & 1;
+            if (!begun) {                             // (a query tile without rows)
+                if (lane == 0) mbar_arrive(&bars->q_free[t][qbuf]);
+                continue;
+            }
             ok = wait_for(bars, &bars->pv_done[t][(cnt - 1) & 1], ((cnt - 1) >> 1) & 1, 0x623);
+            if (__any_sync(0xffffffffu, !ok)) break;
             tc_fence_after();
             const float inv = 1.f / l;
-            if (__any_sync(0xffffffffu, !ok)) break;
-            char *dst = p.w.out.p + (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs;
+            // the rows of O, one per thread, are laid out in the place of the item's queries (every S of the item is over) and
+            // leave from there in whole lines: a warp stores 512 bytes of two (four) rows at a time.  16-byte pieces are permuted
+            // by row against bank conflicts.
+            constexpr int CH = D / 8;
+            unsigned char *place = sm + (2 * qbuf + t) * C::QTILE + (warp & 3) * 32 * 2 * D;
+            const long long at = (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs;
             bool odd = false;
 #pragma unroll
             for (int b = 0; b < D / 32; ++b) {
@@ -724,11 +744,21 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                         x[e] = __uint_as_float(o[k + e]) * inv;
                         odd |= !isfinite(x[e]);
                     }
-                    if (live) *reinterpret_cast<uint4 *>(dst + (b * 32 + k) * 2) = shelem::Vec<T>::pack(x);
+                    *reinterpret_cast<uint4 *>(place + lane * 2 * D + (((b * 4 + k / 8) ^ (lane & 7)) << 4)) = shelem::Vec<T>::pack(x);
                 }
             }
             tc_fence_before();      // O has been read before the arrivals that let the next item overwrite it
             __syncwarp();
+#pragma unroll 4
+            for (int r = 0; r < 32; r += 32 / CH) {
+                const int mine = r + lane / CH, c = lane % CH;
+                const long long to = __shfl_sync(0xffffffffu, at, mine);
+                const uint4 x = *reinterpret_cast<const uint4 *>(place + mine * 2 * D + ((c ^ (mine & 7)) << 4));
+                if (__shfl_sync(0xffffffffu, (int)live, mine)) *reinterpret_cast<uint4 *>(p.w.out.p + to + c * 16) = x;
+            }
+            fence_async_shared();   // (the next queries arrive by the asynchronous proxy)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->q_free[t][qbuf]);
             unsigned again = __ballot_sync(0xffffffffu, live && odd);
             while (again) {
                 const int l0 = __ffs(again) - 1;
