@@ -16,8 +16,8 @@
 // P.V(n-1), issued before it, has read (the tensor pipe keeps the order of one warp's MMAs).  Tensor memory is full with that: two
 // query tiles x (2 x 64 columns of S + 128 of O).  With one buffer of 128 columns each step waited for softmax and both products in
 // turn: 2.3 instead of 2.0 ms for the 32768-token prompt below.  A running CTA takes over the items of CTAs that
-// have not started (cluster launch control), so it sets up once and long and short items even out: 154 -> TIME us for prompts of 1 to
-// 4001 tokens; the loads of the next item start while the present one drains.
+// have not started (cluster launch control), so it sets up once and long and short items even out: 153 -> 139 us for prompts of 1 to
+// 4001 tokens, 150 -> 118 us for continued chunks, whose contexts differ most; the loads of the next item start while the present one drains.
 //
 // P is rounded to the storage type (the tensor cores take no other pair with 16-bit V); its row sum is taken before the rounding,
 // in fp32.  The subtracted maximum is only renewed when it has grown by more than 8 (log2), so weights stay below 2^8; fp16
@@ -444,6 +444,9 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             due = C::STAGES;
         };
         while (ok) {
+            // (if the next step is not there yet - the first of an item may be late - the P.V that is due does not wait for it)
+            if (due < C::STAGES && !__all_sync(0xffffffffu, mbar_test(&bars->full[st], par))) issue_pv();
+            if (!ok) break;
             ok = __all_sync(0xffffffffu, wait_for(bars, &bars->full[st], par, 0x603));
             if (!ok) break;
             const int now = __shfl_sync(0xffffffffu, *(volatile int *)&bars->steps[steps++ % STEPS].flags, 0);
@@ -519,7 +522,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             __syncwarp();
         };
         Found from;
-        uint32_t asked = 0;                           // requests for work so far
+        uint32_t asked = 0, answered = 0;             // requests for work, answers read
         for (int id = blockIdx.x; ok && id >= 0;) {
             const Item w = find_item(p, id, from);
             if (w.seq < 0) break;                     // (the grid is an upper bound: behind the last item nothing follows)
@@ -540,6 +543,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                         if (elect_one()) claim_request(&bars->claim, &bars->claimed);
                         __syncwarp();
                         ask = false;
+                        ++asked;
                     }
                     const int bit = __ffs(todo) - 1;
                     todo &= todo - 1;
@@ -567,8 +571,9 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 }
             }
             if (!ok) break;
-            ok = __all_sync(0xffffffffu, wait_for(bars, &bars->claimed, asked++ & 1, 0x614));
+            ok = __all_sync(0xffffffffu, wait_for(bars, &bars->claimed, answered & 1, 0x614));
             if (!ok) break;
+            ++answered;
             id = __shfl_sync(0xffffffffu, claim_read(&bars->claim), 0);
             fence_async_shared();                     // (read before the next answer is written)
             __syncwarp();
@@ -582,9 +587,10 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             if (ok && elect_one()) mbar_arrive(&bars->full[st]);
             __syncwarp();
         }
-        // let the copies requested last land before the CTA goes away (a phase that is past reads as complete; with the last step
+        // let the copies (and the answer) requested last land before the CTA goes away (a phase that is past reads as complete; with the last step
         // published, its stage's earlier load has been waited for)
         if (lane == 0) {
+            if (answered != asked) wait_for(bars, &bars->claimed, answered & 1, 0);
             if (items > 0)
                 for (int t = 0; t < 2; ++t) wait_for(bars, &bars->q_full[t][(items - 1) & 1], ((items - 1) >> 1) & 1, 0);
             for (uint32_t k = 0; k < C::STAGES - (ok ? 1u : 0u) && k < loads; ++k)
@@ -730,7 +736,8 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             constexpr int CH = D / 8;
             unsigned char *place = sm + (2 * qbuf + t) * C::QTILE + (warp & 3) * 32 * 2 * D;
             const long long at = (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs;
-            bool odd = false;
+            const uint64_t inv2 = f2(inv, inv);
+            uint64_t zero = 0;                        // stays zero unless a value is not finite
 #pragma unroll
             for (int b = 0; b < D / 32; ++b) {
                 uint32_t o[32];
@@ -740,13 +747,17 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 for (int k = 0; k < 32; k += 8) {
                     float x[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        x[e] = __uint_as_float(o[k + e]) * inv;
-                        odd |= !isfinite(x[e]);
+                    for (int e = 0; e < 8; e += 2) {
+                        const uint64_t y = mul2(f2(__uint_as_float(o[k + e]), __uint_as_float(o[k + e + 1])), inv2);
+                        zero = fma2(y, 0, zero);
+                        un2(y, x[e], x[e + 1]);
                     }
                     *reinterpret_cast<uint4 *>(place + lane * 2 * D + (((b * 4 + k / 8) ^ (lane & 7)) << 4)) = shelem::Vec<T>::pack(x);
                 }
             }
+            float z0, z1;
+            un2(zero, z0, z1);
+            const bool odd = !(z0 + z1 == 0.f);
             tc_fence_before();      // O has been read before the arrivals that let the next item overwrite it
             __syncwarp();
 #pragma unroll 4
