@@ -49,7 +49,7 @@ using namespace shwin;
 constexpr int TM = 128, TN = 64;           // rows of a query tile, keys of a key tile
 constexpr int QHALF = TM * 128, HALF = TN * 128;      // bytes of a tile's rows x 64 elements
 constexpr int SOFTMAX_WARPS = 8, NTH = 384;      // 8 softmax warps, 2 that issue MMAs, 1 that loads; the last one only makes a whole warpgroup
-constexpr int REGS_SOFTMAX = 216, REGS_OTHER = 72;      // 256 * 216 + 128 * 72 = 384 * 168, what the CTA is launched with
+constexpr int REGS_SOFTMAX = 184, REGS_OTHER = 136;    // 256 * 184 + 128 * 136 = 384 * 168, what the CTA is launched with
 constexpr float RENEW = 8.f;               // log2 growth of the maximum at which O is rescaled
 
 __device__ int g_window_error;             // code of the first bounded wait that gave up
