@@ -1,4 +1,5 @@
-// sh_window_decode on CUDA cores: one token per sequence over the window cache.
+// sh_window_decode: one token per sequence over the window cache.  First the kernel for fp32 rows, on CUDA cores; the one for 16-bit
+// rows follows below, and what they have in common is said here.
 //
 // Let t be the sequence's length before the step and s the slot of position t.  After the append the live slots are
 // 0 .. min(t + 1, sinks + window) - 1, and every one of them holds a token that the query sees (the one that left the window
@@ -270,6 +271,8 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
 //
 // Each warp brings its rows in by cp.async, 16 bytes a lane, into a ring of its own (no barrier on the way; pieces permuted by
 // row so that ldmatrix reads without bank conflicts).  Rows that hold no token are filled with zeros and never read.
+// 128 sequences of up to 4100 rows, 8 key heads of 128, 32 query heads, bf16, with rotation: 295 us, 6.6 TB/s, 1.00 of the measured copy
+// rate (CUDA cores: 699 us); 9216 units of 410 rows, fp16: 325 us, 0.91 (408 us); one sequence of 16388 rows: 19 us, 0.53 (61 us).
 constexpr int MB = 16;               // rows of a block
 constexpr int MQ = 8;                // query heads of a unit
 

@@ -5,7 +5,9 @@
 // works on 4 rows: S for every 16th key, O for 4 neighbouring columns of each 64.  Two elements of d share a register pair (packed
 // multiply-adds), so the operands of S come as they lie in the rows.  Keys and values arrive by cp.async: a block's values while its
 // S is worked out, the next block's keys during P.V; rows in nobody's sight are filled with zeros, whatever they hold.
-// Bound by the issue of multiply-adds, shared-memory reads (8 of 16 bytes for 32 packed multiply-adds) and the tiles' masked parts.
+// 700 + 511 tokens, 16 heads of 64, window 346, 64 sinks: 81 us, 17 TFLOP/s of a possible 74 (the first version, 64-row tiles with
+// transposed operands: 127 us).  Bound by the latency of shared-memory reads at 16 warps an SM (8 of 16 bytes for 32 packed
+// multiply-adds), and by the tiles' masked parts, half again of the work.
 #include <math_constants.h>
 
 #include "sh_pairs.cuh"

@@ -15,9 +15,12 @@
 // A query tile has two buffers of S: S(n+1) is made while the softmax of step n runs, and goes into the buffer whose P the product
 // P.V(n-1), issued before it, has read (the tensor pipe keeps the order of one warp's MMAs).  Tensor memory is full with that: two
 // query tiles x (2 x 64 columns of S + 128 of O).  With one buffer of 128 columns each step waited for softmax and both products in
-// turn: 2.3 instead of 2.0 ms for the 32768-token prompt below.  A running CTA takes over the items of CTAs that
-// have not started (cluster launch control), so it sets up once and long and short items even out: 153 -> 139 us for prompts of 1 to
-// 4001 tokens, 150 -> 118 us for continued chunks, whose contexts differ most; the loads of the next item start while the present one drains.
+// turn: 2.3 instead of 2.0 ms for the 32768-token prompt below.
+//
+// A running CTA takes over the items of CTAs that have not started (cluster launch control), so it sets up once and long and short
+// items even out: 153 -> 139 us for prompts of 1 to 4001 tokens, 150 -> 118 us for continued chunks, whose contexts differ most.
+// The next item's queries have a place of their own, so its first S follows the last one of the present item at once.  What finished
+// leaves by a copy from shared memory (8192 tokens, window 256: 77 -> 71 us against stores by the threads).
 //
 // P is rounded to the storage type (the tensor cores take no other pair with 16-bit V); its row sum is taken before the rounding,
 // in fp32.  The subtracted maximum is only renewed when it has grown by more than 8 (log2), so weights stay below 2^8; fp16
@@ -27,10 +30,12 @@
 // that holds no token, a later token, another sequence's row).  That shows as an O that is not finite; such rows are computed
 // again at the end, one warp per row over the visible keys only.  Rows whose result is rightly not finite take that way too.
 //
-// 32768 tokens, window 4096, 16 sinks, 32 query and 8 key heads of 128, fp16: 2.03 ms, 1017 TFLOP/s.  Bound by shared-memory
-// reads of the operands (48 KB per S of 64 keys, 16 KB per P.V, 32 KB written: about 1250 cycles a step for both query tiles) and
-// by the softmax warps (1024 cycles of exponentials a step on each quarter of the SM), which do not overlap perfectly: a step
-// takes about 1950 cycles, 1600 with the exponentials left out.
+// 32768 tokens, window 4096, 16 sinks, 32 query and 8 key heads of 128, fp16: 1.97 ms, 1050 TFLOP/s, 0.65 of the measured bf16 peak;
+// 8192 tokens, full causal attention, bf16: 0.48 ms, 1150 TFLOP/s.  Bound by the softmax warps and shared memory together: a step
+// takes about 1950 cycles, of which the exponentials need 1024 on each quarter of the SM and the operands' reads (48 KB per S of 64
+// keys, 16 KB per P.V, 32 KB written) 1250; with the exponentials left out it took 1600.  A part of the exponentials on the FMA
+// pipe (a quarter of them by a polynomial) gained nothing at this register split: 473 against 482 us for the 8192 tokens.
+// Items of few steps pay for their ends: 8192 tokens with window 1024 (18 steps an item) run at 850 TFLOP/s, with window 256 at 485.
 #include <cuda.h>
 #include <math_constants.h>
 
@@ -108,6 +113,7 @@ __device__ __forceinline__ bool wait_for(Bars *bars, uint64_t *bar, uint32_t par
 struct UmmaParams {
     WindowParams w;
     int tpt, gb, hblocks;                  // tokens and heads of a tile, head blocks per key head
+    bool copy_out;                         // a warp's 32 rows are whole tokens
 };
 
 __device__ __forceinline__ uint64_t desc_sw128(uint32_t saddr, uint32_t lbo, uint32_t sbo) { return smem_desc(saddr, lbo, sbo) | (2ull << 61); }
@@ -199,6 +205,12 @@ __device__ __forceinline__ int claim_read(const uint4 *answer) {
         : "r"(smem_u32(answer))
         : "memory");
     return got ? x : -1;
+}
+// A tile of output rows, laid out like a query tile, to global memory; tracked by the thread's bulk group.
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, const void *src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(reinterpret_cast<uint64_t>(map)),
+                 "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(src))
+                 : "memory");
 }
 // One lane of the warp, which must be converged.
 __device__ __forceinline__ bool elect_one() {
@@ -375,7 +387,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(NTH, 1)
 sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                               const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_kc,
-                              const __grid_constant__ CUtensorMap map_vc) {
+                              const __grid_constant__ CUtensorMap map_vc, const __grid_constant__ CUtensorMap map_o) {
     using C = Cfg<D>;
     extern __shared__ __align__(1024) unsigned char sm[];
     unsigned char *kv = sm + C::OFF_KV;
@@ -612,7 +624,16 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         float m = -CUDART_INF_F, l = 0.f;
         // The entry of the next step is read while the present one is worked on.
         int4 e0, e1, e2;
+        // The place of an item's queries is given back when its outputs, which were laid out there, have been read: a step later.
+        int owed = -1;                                // (of the lane that stores) the place still to be given back
+        auto give_back = [&]() {
+            if (owed < 0) return;
+            bulk_wait_read_all();
+            mbar_arrive(&bars->q_free[t][owed]);
+            owed = -1;
+        };
         auto fetch = [&]() {
+            give_back();
             const uint32_t e = steps % STEPS;
             ok = wait_for(bars, &bars->step_full[e], (steps / STEPS) & 1, 0x624) && ok;
             ++steps;
@@ -730,11 +751,10 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             if (__any_sync(0xffffffffu, !ok)) break;
             tc_fence_after();
             const float inv = 1.f / l;
-            // the rows of O, one per thread, are laid out in the place of the item's queries (every S of the item is over) and
-            // leave from there in whole lines: a warp stores 512 bytes of two (four) rows at a time.  16-byte pieces are permuted
-            // by row against bank conflicts.
-            constexpr int CH = D / 8;
-            unsigned char *place = sm + (2 * qbuf + t) * C::QTILE + (warp & 3) * 32 * 2 * D;
+            // the rows of O, one per thread, are laid out in the place of the item's queries (every S of the item is over), like a
+            // query tile, and a warp's 32 rows leave from there as one copy if they are whole tokens; rows next to somebody else's,
+            // or that have to be done again, go by the threads, in whole lines
+            unsigned char *place = sm + (2 * qbuf + t) * C::QTILE;
             const long long at = (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs;
             const uint64_t inv2 = f2(inv, inv);
             uint64_t zero = 0;                        // stays zero unless a value is not finite
@@ -752,22 +772,32 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                         zero = fma2(y, 0, zero);
                         un2(y, x[e], x[e + 1]);
                     }
-                    *reinterpret_cast<uint4 *>(place + lane * 2 * D + (((b * 4 + k / 8) ^ (lane & 7)) << 4)) = shelem::Vec<T>::pack(x);
+                    *reinterpret_cast<uint4 *>(place + b / 2 * QHALF + row * 128 + (((b % 2 * 4 + k / 8) ^ (row & 7)) << 4)) = shelem::Vec<T>::pack(x);
                 }
             }
             float z0, z1;
             un2(zero, z0, z1);
             const bool odd = !(z0 + z1 == 0.f);
             tc_fence_before();      // O has been read before the arrivals that let the next item overwrite it
+            fence_async_shared();   // (for the copy, and for the queries that arrive here next)
             __syncwarp();
+            if (!__any_sync(0xffffffffu, !live || odd) && p.copy_out) {
+                if (lane == 0) {
+#pragma unroll
+                    for (int x = 0; x < D / 64; ++x) tma_store_3d(&map_o, place + x * QHALF + (warp & 3) * 32 * 128, x * 64, kvh * p.w.g + h, row0 + qi);
+                    bulk_commit();
+                    owed = qbuf;
+                }
+                continue;
+            }
+            constexpr int CH = D / 8;
 #pragma unroll 4
             for (int r = 0; r < 32; r += 32 / CH) {
-                const int mine = r + lane / CH, c = lane % CH;
+                const int mine = r + lane / CH, c = lane % CH, of = (warp & 3) * 32 + mine;
                 const long long to = __shfl_sync(0xffffffffu, at, mine);
-                const uint4 x = *reinterpret_cast<const uint4 *>(place + mine * 2 * D + ((c ^ (mine & 7)) << 4));
+                const uint4 x = *reinterpret_cast<const uint4 *>(place + c / 8 * QHALF + of * 128 + ((c % 8 ^ (of & 7)) << 4));
                 if (__shfl_sync(0xffffffffu, (int)live, mine)) *reinterpret_cast<uint4 *>(p.w.out.p + to + c * 16) = x;
             }
-            fence_async_shared();   // (the next queries arrive by the asynchronous proxy)
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->q_free[t][qbuf]);
             unsigned again = __ballot_sync(0xffffffffu, live && odd);
@@ -777,6 +807,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 slow_row<T, D>(p, id, __shfl_sync(0xffffffffu, qi, l0), kvh * p.w.g + __shfl_sync(0xffffffffu, h, l0));
             }
         }
+        bulk_wait_all();            // outputs on their way from shared memory
     }
     tc_fence_before();
     __syncthreads();
@@ -832,10 +863,13 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     p.gb = w.g < TM ? w.g : TM;
     p.tpt = TM / p.gb;
     p.hblocks = (w.g + p.gb - 1) / p.gb;
-    CUtensorMap mq, mk, mv, mkc, mvc;
+    CUtensorMap mq, mk, mv, mkc, mvc, mo;
     const uint64_t qdim[2] = {(uint64_t)w.hq, (uint64_t)w.tokens}, qst[2] = {(uint64_t)w.q.hs, (uint64_t)w.q.ts};
     const uint32_t qbox[2] = {(uint32_t)p.gb, (uint32_t)p.tpt};
-    if (!make_map(&mq, w.q.p, 2, qdim, qst, qbox, D) || !keys_map(&mk, w.k, w.hk, w.tokens, D / 64) || !keys_map(&mv, w.v, w.hk, w.tokens, D / 64))
+    p.copy_out = 32 % p.gb == 0;
+    const uint64_t ost[2] = {(uint64_t)w.out.hs, (uint64_t)w.out.ts};
+    const uint32_t obox[2] = {(uint32_t)p.gb, p.copy_out ? 32u / p.gb : 1u};
+    if (!make_map(&mq, w.q.p, 2, qdim, qst, qbox, D) || !make_map(&mo, w.out.p, 2, qdim, ost, obox, D) || !keys_map(&mk, w.k, w.hk, w.tokens, D / 64) || !keys_map(&mv, w.v, w.hk, w.tokens, D / 64))
         return cudaErrorNotSupported;
     mkc = mk; mvc = mv;
     if (w.kc) {
@@ -852,7 +886,7 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     // each sequence adds at most one partly filled item
     const long long items = ((long long)w.tokens / (2 * p.tpt) + w.sequences) * w.hk * p.hblocks;
     if (items > 0x7fffffffll) return cudaErrorInvalidValue;
-    kern<<<(unsigned)items, NTH, Cfg<D>::SMEM, s>>>(p, mq, mk, mv, mkc, mvc);
+    kern<<<(unsigned)items, NTH, Cfg<D>::SMEM, s>>>(p, mq, mk, mv, mkc, mvc, mo);
     return cudaGetLastError();
 }
 
