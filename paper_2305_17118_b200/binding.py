@@ -669,6 +669,10 @@ class WindowCache:
         self.v = torch.zeros(shape, dtype=dt, device=device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
 
+    def _check_heads(self, q: torch.Tensor) -> None:
+        if q.dim() != 3 or q.shape[1] != self.q_heads:
+            _fail("q", f"[tokens, {self.q_heads}, {self.k.shape[3]}]", q)
+
     def _prompt_positions(self, starts: torch.Tensor, tokens: int) -> torch.Tensor:
         """Position of each row of a chunk tensor: its sequence's length plus its place in the chunk."""
         row = torch.arange(tokens, dtype=torch.int32, device=self.k.device)
@@ -678,6 +682,7 @@ class WindowCache:
     def prefill(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, positions: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Chunks of prompts (``window_prefill``), stored and counted.  On the current stream."""
+        self._check_heads(q)
         if self.rope is not None:
             if positions is None:
                 if self.rope.axes != 1:
@@ -693,6 +698,7 @@ class WindowCache:
     def decode(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor] = None,
                out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """One token per sequence (``window_decode``), stored and counted.  On the current stream."""
+        self._check_heads(q)
         out = window_decode(q, k, v, self.lengths, self.k, self.v, window=self.window, sinks=self.sinks, rope=self.rope, positions=positions,
                             scale=self.scale, out=out)
         self.lengths += (self.lengths >= 0).to(torch.int32)

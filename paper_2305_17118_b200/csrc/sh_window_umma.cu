@@ -99,12 +99,13 @@ struct Bars {
 };
 static_assert(sizeof(Bars) <= BAR_BYTES, "barrier block");
 
-// Wait for a phase, bounded like mbar_wait, in few instructions: the code of a wait that gave up goes to the CTA's abort word, and
-// from there to g_window_error at the end.
+// Wait for a phase, bounded by time, in few instructions: the code of a wait that gave up goes to the CTA's abort word, and from
+// there to g_window_error at the end.  The bound has to outlast rows that are done again: 32 of them over a million keys take a second.
+constexpr unsigned long long LIMIT_NS = 8000000000ull;
 __device__ __forceinline__ bool wait_for(Bars *bars, uint64_t *bar, uint32_t parity, int code) {
     if (mbar_try_wait(bar, parity)) return true;
     const unsigned long long t0 = global_ns();
-    while (global_ns() - t0 < WAIT_NS)
+    while (global_ns() - t0 < LIMIT_NS)
         if (mbar_try_wait(bar, parity)) return true;
     if (code) *(volatile int *)&bars->abort_flag = code;
     return false;

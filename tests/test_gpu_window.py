@@ -630,6 +630,8 @@ def test_wrappers_refuse_what_the_kernels_cannot_take():
         lambda: sh.WindowCache(2, 4, 2, 96, 8),
         lambda: sh.WindowCache(2, 4, 2, 64, 8, dtype="int4"),
         lambda: sh.WindowCache(2, 3, 2, 64, 8),
+        lambda: sh.WindowCache(4, 8, 2, 64, 8, dtype=dt).decode(q, k, v),
+        lambda: sh.WindowCache(4, 8, 2, 64, 8, dtype=dt).prefill(q, k, v, st),
     ]
     for i, call in enumerate(bad):
         with pytest.raises(ValueError):
