@@ -341,6 +341,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+
 // One row by one warp, over its visible keys only, in fp32 on CUDA cores: for rows next to values that are not finite.
 template <typename T, int D>
 __device__ __noinline__ void slow_row(const UmmaParams &u, int id, int qi, int h) {
@@ -411,9 +412,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         mbar_init(&bars->claimed, 1);
         for (int s = 0; s < STEPS; ++s) { mbar_init(&bars->step_full[s], 1); mbar_init(&bars->step_empty[s], SOFTMAX_WARPS); }
         bars->abort_flag = 0;
-        if ((smem_u32(sm) & 1023u) != 0) {      // the swizzled tiles need the alignment the declaration asks for
-            bars->abort_flag = 0x620;
-        }
+        if ((smem_u32(sm) & 1023u) != 0) bars->abort_flag = 0x620;      // the swizzled tiles need the alignment the declaration asks for
         fence_barrier_init();
     }
     tc_fence_before();

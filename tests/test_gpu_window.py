@@ -322,6 +322,53 @@ def test_single_tokens(dtype, d, hk, g, window, sinks, rope):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,rot,sections,spread,adjacent,qn,kn", [
+    (128, 128, (24, 20, 20), False, False, True, True),
+    (128, 96, (16, 16, 16), True, True, False, True),
+    (64, 64, (12, 20), False, True, True, False),
+    (64, 32, (6, 5, 5), True, False, False, False),
+])
+def test_single_tokens_prepared_in_the_same_launch(dtype, d, rot, sections, spread, adjacent, qn, kn):
+    """Every form of the preparation inside the step, with positions of their own: the stored key is the prepared one, and the output is
+    that of the prepared query over what is stored."""
+    sh, gen, dt = _sh(), _gen(29), DT[dtype]
+    n, hk, g, window, sinks, c = 3, 2, 5, 40, 3, 57
+    hist = _history(gen, [1] * n, [c] * n, hk, d, dt)
+    kc, vc = _caches(hist, [c] * n, hk, d, window, sinks, dt, float("nan"))
+    q, k, v = _rnd(gen, n, hk * g, d, dtype=dt), _rnd(gen, n, hk, d, dtype=dt), _rnd(gen, n, hk, d, dtype=dt)
+    r = _rope(sh, gen, d, dt, rot, sections, spread, adjacent, qn, kn)
+    pos = torch.randint(0, 1 << 20, (len(sections), n), generator=gen, device="cuda", dtype=torch.int32)
+    out = sh.window_decode(q, k, v, _i32([c] * n), kc, vc, window=window, sinks=sinks, rope=r, positions=pos)
+    args = (pos, r.inv_freq, r.eps, r.sections, spread, adjacent)
+    want_q, _ = ref.rope_ref(q, r.q_weight, *args)
+    want_k, mag = ref.rope_ref(k, r.k_weight, *args)
+    slot = sinks + (c - sinks) % window
+    for i in range(n):
+        stored = kc[i, :, slot]
+        ref.check(stored, want_k[i], ref.rope_tolerance(want_k[i], mag[i], dt), "stored key")
+        hist[i][0][c], hist[i][1][c] = stored, v[i]
+        want, vmax, smax = ref.attend_ref(want_q[i:i + 1], [c], *hist[i], window, sinks)
+        ref.check(out[i:i + 1], want, ref.attend_tolerance(want, vmax, smax, dt))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_other_scales_and_rows_before_the_first_sequence(dtype):
+    sh, gen, dt = _sh(), _gen(30), DT[dtype]
+    q, k, v = _rnd(gen, 90, 4, 64, dtype=dt), _rnd(gen, 90, 2, 64, dtype=dt), _rnd(gen, 90, 2, 64, dtype=dt)
+    out = torch.full_like(q, 7.0)
+    sh.window_prefill(q, k, v, _i32([5, 70, 80]), window=30, sinks=1, scale=0.31, out=out)
+    assert (out[:5] == 7).all() and (out[80:] == 7).all()
+    for a, b in ((5, 70), (70, 80)):
+        want, vmax, smax = ref.attend_ref(q[a:b], range(b - a), k[a:b], v[a:b], 30, 1, scale=0.31)
+        ref.check(out[a:b], want, ref.attend_tolerance(want, vmax, smax, dt))
+    kc, vc = torch.zeros(1, 2, 31, 64, dtype=dt, device="cuda"), torch.zeros(1, 2, 31, 64, dtype=dt, device="cuda")
+    sh.window_append(k, v, _i32([5, 70]), _i32([0]), kc, vc, window=30, sinks=1)
+    step = sh.window_decode(q[70:71], k[70:71], v[70:71], _i32([65]), kc, vc, window=30, sinks=1, scale=0.31)
+    want, vmax, smax = ref.attend_ref(q[70:71], [65], k[5:71], v[5:71], 30, 1, scale=0.31)
+    ref.check(step, want, ref.attend_tolerance(want, vmax, smax, dt))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_single_tokens_over_long_axes_and_large_batches(dtype):
     _decode_case(dtype, 128, 2, 4, 5000, 4, [20011], rope=True)              # one sequence: the axis is split
     _decode_case(dtype, 64, 1, 1, 3001, 0, [2500, 7000, -1], seed=22)
