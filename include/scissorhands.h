@@ -433,10 +433,16 @@ int sh_qk_norm_rope(const sh_rope *rope, int tokens, int q_heads, int k_heads, c
  * length is idle and is skipped.  Rows of `out` that belong to no sequence (before starts[0], from starts[sequences] on) are
  * left as they were.  The cache is only read: sh_window_append stores the chunk afterwards.
  * starts that decrease or leave 0 .. tokens are clamped, so no access leaves the tensors; outputs are then meaningless.
- * lengths[i] plus the chunk's tokens must stay below 2^30.  Errors: SH_EINVAL, SH_ECUDA.
+ * lengths[i] plus the chunk's tokens must stay below 2^30.
+ * workspace_dev: device memory of sh_window_prefill_workspace_bytes(w, tokens, sequences, cache != NULL) bytes (0 unless few rows may
+ * look at many keys), 16-byte aligned, or NULL.  With it a short chunk over a long context spreads over the whole device; without
+ * it it takes longer, the result is the same up to fp32 summation order.  Used as sh_window_decode's.
+ * Errors: SH_EINVAL, SH_ENOMEM (workspace too small), SH_ECUDA.
  */
+size_t sh_window_prefill_workspace_bytes(const sh_window *w, int tokens, int sequences, int with_cache);
 int sh_window_prefill(const sh_window *w, int tokens, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v,
-                      const int32_t *starts_dev, const int32_t *lengths_dev, const sh_window_cache *cache, const sh_rows *out, void *stream);
+                      const int32_t *starts_dev, const int32_t *lengths_dev, const sh_window_cache *cache, const sh_rows *out,
+                      void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
  * Store the chunks' keys and values in the caches (arguments as above, lengths_dev as before the chunk; the caller advances

@@ -35,7 +35,7 @@ EXPORTS = ["sh_create", "sh_destroy", "sh_workspace_bytes", "sh_bind", "sh_set_o
            "sh_compress", "sh_compress_static", "sh_scores", "sh_select", "sh_state", "sh_export_unit",
            "sh_restore", "sh_launch_count", "sh_decode_kernel_choice", "sh_import_compressed", "sh_prefill_bulk",
            "sh_prefill_bulk_scratch_bytes", "sh_strerror", "sh_last_cuda_error",
-           "sh_qk_norm_rope", "sh_window_prefill", "sh_window_append", "sh_window_decode", "sh_window_decode_workspace_bytes", "sh_window_status"]
+           "sh_qk_norm_rope", "sh_window_prefill", "sh_window_append", "sh_window_decode", "sh_window_decode_workspace_bytes", "sh_window_prefill_workspace_bytes", "sh_window_status"]
 
 
 class _Rows(C.Structure):
@@ -108,7 +108,9 @@ def declare(lib: C.CDLL) -> C.CDLL:
     lib.sh_last_cuda_error.restype = C.c_char_p
     rows = cache = window = rope = vp      # (structs arrive as packed bytes or by reference)
     lib.sh_qk_norm_rope.argtypes = [rope, C.c_int, C.c_int, C.c_int, rows, rows, vp, C.c_longlong, rows, rows, vp]
-    lib.sh_window_prefill.argtypes = [window, C.c_int, C.c_int, rows, rows, rows, vp, vp, cache, rows, vp]
+    lib.sh_window_prefill.argtypes = [window, C.c_int, C.c_int, rows, rows, rows, vp, vp, cache, rows, vp, C.c_size_t, vp]
+    lib.sh_window_prefill_workspace_bytes.argtypes = [window, C.c_int, C.c_int, C.c_int]
+    lib.sh_window_prefill_workspace_bytes.restype = C.c_size_t
     lib.sh_window_append.argtypes = [window, C.c_int, C.c_int, rows, rows, vp, vp, cache, vp]
     lib.sh_window_status.argtypes = [vp]
     lib.sh_window_decode.argtypes = [window, C.c_int, rows, rows, rows, vp, cache, rope, vp, C.c_longlong, rows, vp, C.c_size_t, vp]
@@ -591,8 +593,12 @@ def window_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: to
         lp = _ints(lengths, "lengths", n, device)
         cache = _cache_packed(k_cache, v_cache, (n, kshape[1], window + sinks, d), dtype, device)
     out = _new(q, shape, stream, True) if out is None else out
-    _launch("window_prefill", lib.sh_window_prefill, device, stream, win, tokens, n, qr, kr, vr, sp, lp, cache,
-            _more_rows(out, "out", shape, dtype, device))
+    outr = _more_rows(out, "out", shape, dtype, device)
+    wp, bytes_ = None, lib.sh_window_prefill_workspace_bytes(win, tokens, n, cache is not None)
+    if bytes_:
+        work = _new(q, bytes_, stream, False, torch.uint8)      # as in window_decode
+        wp = work.data_ptr()
+    _launch("window_prefill", lib.sh_window_prefill, device, stream, win, tokens, n, qr, kr, vr, sp, lp, cache, outr, wp, bytes_)
     return out
 
 

@@ -37,7 +37,7 @@ struct WindowParams {
     float scale_log2e;
     RopeParams rope;              // decode only: how the step's q and k are prepared
     bool with_rope;
-    float *part;                  // decode only: scratch of sh_window_decode_scratch bytes, or NULL
+    float *part;                  // scratch of sh_window_decode_scratch or sh_window_prefill_scratch bytes, or NULL
 };
 
 // SMs of the current device, and that a kernel may use `smem` bytes of shared memory there.  Both are facts of the device, asked once
@@ -61,6 +61,7 @@ cudaError_t sh_launch_qk_norm_rope(RopeParams p, int dtype, int D, cudaStream_t 
 cudaError_t sh_launch_window_prefill_f32(const WindowParams &p, int D, cudaStream_t s);
 // tensor cores: f16 and bf16
 cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int D, cudaStream_t s);
+size_t sh_window_prefill_scratch(int tokens, int sequences, int hk, int g, int window, int sinks, bool with_cache, int dtype, int D);
 // code of the first bounded wait that gave up in a window kernel of the current device since the last call (0: none); synchronises
 cudaError_t sh_window_error_take(int *code, cudaStream_t s);
 cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, cudaStream_t s);

@@ -141,8 +141,14 @@ int sh_qk_norm_rope(const sh_rope *rope, int tokens, int q_heads, int k_heads, c
     return done(sh_launch_qk_norm_rope(p, rope->dtype, D, (cudaStream_t)stream));
 }
 
+size_t sh_window_prefill_workspace_bytes(const sh_window *w, int tokens, int sequences, int with_cache) {
+    if (!good_window(w) || tokens < 1 || tokens >= MAX_POS || sequences < 1) return 0;
+    return sh_window_prefill_scratch(tokens, sequences, w->kv_heads, w->q_heads / w->kv_heads, w->window, w->sinks, with_cache != 0, w->dtype, w->head_dim);
+}
+
 int sh_window_prefill(const sh_window *w, int tokens, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v,
-                      const int32_t *starts_dev, const int32_t *lengths_dev, const sh_window_cache *cache, const sh_rows *out, void *stream) {
+                      const int32_t *starts_dev, const int32_t *lengths_dev, const sh_window_cache *cache, const sh_rows *out, void *workspace_dev,
+                      size_t workspace_bytes, void *stream) {
     if (!good_window(w) || tokens < 0 || tokens >= MAX_POS || sequences < 0 || (cache == nullptr) != (lengths_dev == nullptr)) return SH_EINVAL;
     if (tokens == 0 || sequences == 0) return SH_OK;
     const int D = w->head_dim, es = elem_size(w->dtype);
@@ -158,6 +164,12 @@ int sh_window_prefill(const sh_window *w, int tokens, int sequences, const sh_ro
     p.v = rows(v, tokens, w->kv_heads, D, es);
     p.out = rows(out, tokens, w->q_heads, D, es);
     p.starts = starts_dev; p.lengths = lengths_dev;
+    if (workspace_dev) {
+        if (!aligned16(workspace_dev)) return SH_EINVAL;
+        const size_t need = sh_window_prefill_workspace_bytes(w, tokens, sequences, cache != nullptr);
+        if (workspace_bytes < need) return SH_ENOMEM;
+        if (need) p.part = static_cast<float *>(workspace_dev);
+    }
     return done(w->dtype == SH_F32 ? sh_launch_window_prefill_f32(p, D, (cudaStream_t)stream)
                                    : sh_launch_window_prefill_umma(p, w->dtype, D, (cudaStream_t)stream));
 }

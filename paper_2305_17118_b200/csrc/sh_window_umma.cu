@@ -39,6 +39,8 @@
 #include <cuda.h>
 #include <math_constants.h>
 
+#include <algorithm>
+
 #include "sh_elem.cuh"
 #include "sh_pairs.cuh"
 #include "sh_umma.cuh"
@@ -76,7 +78,8 @@ template <int D> struct Cfg {
 enum {
     STEP_NEED0 = 1, STEP_NEED1 = 2,        // the query tile sees keys of this step
     STEP_WHOLE0 = 4, STEP_WHOLE1 = 8,      // every row of the query tile sees every key
-    STEP_CACHE = 16, STEP_FIRST = 32, STEP_LAST = 64, STEP_END = 128
+    STEP_CACHE = 16, STEP_FIRST = 32, STEP_LAST = 64, STEP_END = 128,
+    STEP_PART = 256                        // other CTAs have key tiles of this item too
 };
 struct __align__(16) Step {
     int flags, x;                          // first slot of the tile, or its first row in the chunk
@@ -115,7 +118,28 @@ struct UmmaParams {
     WindowParams w;
     int tpt, gb, hblocks;                  // tokens and heads of a tile, head blocks per key head
     bool copy_out;                         // a warp's 32 rows are whole tokens
+    int share;                             // CTAs of the device per item
+    int parts;                             // the most CTAs that an item's key tiles are dealt out to (1: results go straight to the output)
 };
+
+// Few items over many keys: the key tiles of an item are dealt out to several CTAs, 4 tiles each at least, whose results a second
+// launch merges.  It pays when the tiles that no CTA has to walk over any more, at about 1.1 us each, outweigh that launch (2 us where
+// nothing was dealt out, 4 to 7 us else).  An item's count depends on the tiles it needs and on the number of items, not on whether
+// there is a cache.  Measured with 32 query heads over 8, 128 wide, one CTA an item against several: 64 tokens over 32768 538 -> 56 us
+// (18 parts), over 8000 147 -> 28 us; 16 over 2000 34 -> 16 us (7 parts), over 832 18.3 -> 14.5 us (3 parts); 400 over none in a cache
+// of 4100 14.7 -> 17.3 us (the second launch finds nothing to do).
+__host__ __device__ __forceinline__ int parts_of(long long tiles, int share) {
+    const int parts = tiles / 4 < share ? (int)(tiles / 4) : share;
+    return parts >= 2 && tiles - tiles / parts > 8 ? parts : 1;
+}
+
+// What a part leaves for the merge, rows next to each other: O as [item's part][query tile][D / 4][row] of 4 floats, then what its
+// exponents are counted from and its sum (below zero: nothing else was written), then for each item: its parts, its first row, the
+// rows from there to the sequence's end.
+constexpr int MAX_SHARE = 160;             // items times parts
+template <int D> __device__ __forceinline__ float4 *part_o(const UmmaParams &p, int id, int t) { return reinterpret_cast<float4 *>(p.w.part) + (id * 2 + t) * (D / 4) * TM; }
+template <int D> __device__ __forceinline__ float2 *part_sum(const UmmaParams &p, int id, int t) { return reinterpret_cast<float2 *>(p.w.part + MAX_SHARE * 2 * TM * D) + (id * 2 + t) * TM; }
+template <int D> __device__ __forceinline__ int4 *part_item(const UmmaParams &p) { return reinterpret_cast<int4 *>(p.w.part + MAX_SHARE * 2 * TM * (D + 2)); }
 
 __device__ __forceinline__ uint64_t desc_sw128(uint32_t saddr, uint32_t lbo, uint32_t sbo) { return smem_desc(saddr, lbo, sbo) | (2ull << 61); }
 
@@ -228,7 +252,7 @@ __device__ __forceinline__ bool elect_one() {
 // chunk's rows TN * j ...
 struct Item : Ring {
     int seq, first, count;                 // seq < 0: there is no such item
-    int kvh, hb;
+    int kvh, hb, part;
     int a;                                 // first token of query tile 0, counted in the chunk; tile t starts at a + t * tpt
     int ctiles, jlo, jhi, tpt;
 
@@ -270,7 +294,7 @@ struct Found {
     long long before = 0;
 };
 __device__ __forceinline__ Item find_item(const UmmaParams &p, int id, Found &from) {
-    const int per = p.w.hk * p.hblocks, in = id % per;
+    const int per = p.w.hk * p.hblocks * p.parts, in = id % per;
     const int lane = threadIdx.x & 31, span = 2 * p.tpt;
     const int tile = id / per;
     if (tile < from.before) from = Found();
@@ -303,7 +327,8 @@ __device__ __forceinline__ Item find_item(const UmmaParams &p, int id, Found &fr
         before += __shfl_sync(0xffffffffu, upto, 31);
     }
     if (r.seq < 0) return r;
-    r.kvh = in / p.hblocks; r.hb = in % p.hblocks;
+    r.part = in % p.parts;
+    r.kvh = in / p.parts / p.hblocks; r.hb = in / p.parts % p.hblocks;
     r.tpt = p.tpt;
     static_cast<Ring &>(r) = Ring(p.w.kc ? r.cached : 0, p.w.sinks, p.w.window);
     r.ctiles = (r.live + TN - 1) / TN;
@@ -537,17 +562,66 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         uint32_t asked = 0, answered = 0;             // requests for work, answers read
         for (int id = blockIdx.x; ok && id >= 0;) {
             const Item w = find_item(p, id, from);
-            if (w.seq < 0) break;                     // (the grid is an upper bound: behind the last item nothing follows)
+            if (w.seq < 0) {                          // (the grid is an upper bound: behind the last item nothing follows)
+                if (p.parts > 1 && id % p.parts == 0 && elect_one()) part_item<D>(p)[id / p.parts] = make_int4(0, 0, 0, 0);
+                __syncwarp();
+                break;
+            }
             bool first = true, ask = true;
             const int last_tile = w.ctiles + w.jhi;   // (the tile of the last row itself: always needed)
-            for (int base = 0; base <= last_tile && ok; base += 32) {
-                // 32 tiles at a time, a lane each; what lies between the sinks and the window is passed over
-                if (base >= w.ctiles && base - w.ctiles < w.jlo && w.cached + (base - w.ctiles) * TN >= w.sinks) base = w.ctiles + w.jlo;
+            int flags = 0, x = 0;                     // a step that waits to learn whether it is the last
+            // 32 tiles at a time, a lane each; what lies between the sinks and the window is passed over
+            auto skip = [&](int base) {
+                return base >= w.ctiles && base - w.ctiles < w.jlo && w.cached + (base - w.ctiles) * TN >= w.sinks ? w.ctiles + w.jlo : base;
+            };
+            auto needed = [&](int i) { return i <= last_tile && (w.need(0, i) || w.need(1, i)); };
+            int seen = 0, parts = 1;                  // needed tiles so far, CTAs that share them
+            if (p.parts > 1) {
+                int all = 0;
+                for (int base = 0; base <= last_tile; base += 32) {
+                    base = skip(base);
+                    all += __popc(__ballot_sync(0xffffffffu, needed(base + lane)));
+                }
+                parts = min(parts_of(all, p.share), p.parts);
+                if (w.part == 0 && elect_one()) part_item<D>(p)[id / p.parts] = make_int4(parts, w.first + w.a, w.count - w.a, 0);
+                __syncwarp();
+            }
+            const int shared = parts > 1 ? STEP_PART : 0;
+            auto step = [&]() {
+                flags |= (first ? STEP_FIRST : 0) | shared;
+                publish(w, id, flags, x);
+                if (ok && first) queries(w, 0);
+                if (ok && elect_one()) {
+                    unsigned char *dst = kv + st * 2 * C::TILE;
+                    uint64_t *full = &bars->full[st];
+                    mbar_arrive_expect_tx(full, 2 * C::TILE);
+                    if (flags & STEP_CACHE) {
+                        tma_5d(dst, &map_kc, x, w.kvh, w.seq, full);
+                        tma_5d(dst + C::TILE, &map_vc, x, w.kvh, w.seq, full);
+                    } else {
+                        tma_4d(dst, &map_k, w.kvh, w.first + x, full);
+                        tma_4d(dst + C::TILE, &map_v, w.kvh, w.first + x, full);
+                    }
+                }
+                __syncwarp();
+                if (++st == C::STAGES) { st = 0; par ^= 1; }
+                if (ok && first) queries(w, 1);
+                items += first;
+                first = false;
+                flags = 0;
+            };
+            for (int base = w.part < parts ? 0 : last_tile + 1; base <= last_tile && ok; base += 32) {
+                base = skip(base);
                 const int i = base + lane;
                 const bool need0 = i <= last_tile && w.need(0, i), need1 = i <= last_tile && w.need(1, i);
                 const int mine = (need0 ? STEP_NEED0 : 0) | (need1 ? STEP_NEED1 : 0) | (need0 && w.whole(0, i) ? STEP_WHOLE0 : 0) |
-                                 (need1 && w.whole(1, i) ? STEP_WHOLE1 : 0) | (i < w.ctiles ? STEP_CACHE : 0) | (i == last_tile ? STEP_LAST : 0);
+                                 (need1 && w.whole(1, i) ? STEP_WHOLE1 : 0) | (i < w.ctiles ? STEP_CACHE : 0);
                 unsigned todo = __ballot_sync(0xffffffffu, need0 || need1);
+                if (parts > 1) {                      // every parts-th of them is this CTA's
+                    const unsigned all = todo;
+                    todo = __ballot_sync(0xffffffffu, (need0 || need1) && (seen + __popc(all & ((1u << lane) - 1u))) % parts == w.part);
+                    seen += __popc(all);
+                }
                 while (todo && ok) {
                     // the next item is asked for a few steps before the end of this one: soon enough to cover the answer's latency, late
                     // enough for the next item to go to whoever is done first
@@ -557,30 +631,23 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                         ask = false;
                         ++asked;
                     }
+                    if (flags) step();
+                    if (!ok) break;
                     const int bit = __ffs(todo) - 1;
                     todo &= todo - 1;
-                    const int flags = __shfl_sync(0xffffffffu, mine, bit) | (first ? STEP_FIRST : 0);
-                    const int x = (base + bit - (flags & STEP_CACHE ? 0 : w.ctiles)) * TN;
-                    publish(w, id, flags, x);
-                    if (ok && first) queries(w, 0);
-                    if (ok && elect_one()) {
-                        unsigned char *dst = kv + st * 2 * C::TILE;
-                        uint64_t *full = &bars->full[st];
-                        mbar_arrive_expect_tx(full, 2 * C::TILE);
-                        if (flags & STEP_CACHE) {
-                            tma_5d(dst, &map_kc, x, w.kvh, w.seq, full);
-                            tma_5d(dst + C::TILE, &map_vc, x, w.kvh, w.seq, full);
-                        } else {
-                            tma_4d(dst, &map_k, w.kvh, w.first + x, full);
-                            tma_4d(dst + C::TILE, &map_v, w.kvh, w.first + x, full);
-                        }
-                    }
-                    __syncwarp();
-                    if (++st == C::STAGES) { st = 0; par ^= 1; }
-                    if (ok && first) queries(w, 1);
-                    items += first;
-                    first = false;
+                    flags = __shfl_sync(0xffffffffu, mine, bit);
+                    x = (base + bit - (flags & STEP_CACHE ? 0 : w.ctiles)) * TN;
                 }
+            }
+            if (!ok) break;
+            if (w.part < parts) {                     // (a part has 4 tiles at least)
+                flags |= STEP_LAST;
+                step();
+            }
+            if (ok && ask) {
+                if (elect_one()) claim_request(&bars->claim, &bars->claimed);
+                __syncwarp();
+                ++asked;
             }
             if (!ok) break;
             ok = __all_sync(0xffffffffu, wait_for(bars, &bars->claimed, answered & 1, 0x614));
@@ -743,6 +810,30 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             }
             if (!(flags & STEP_LAST)) continue;
             const uint32_t qbuf = (items - 1) & 1;
+            if (flags & STEP_PART) {
+                if (begun) {
+                    ok = wait_for(bars, &bars->pv_done[t][(cnt - 1) & 1], ((cnt - 1) >> 1) & 1, 0x625);
+                    if (__any_sync(0xffffffffu, !ok)) break;
+                    tc_fence_after();
+                    float4 *to = part_o<D>(p, id, t) + row;
+#pragma unroll
+                    for (int b = 0; b < D / 32; ++b) {
+                        uint32_t o[32];
+                        tmem_ld32_nowait(o_addr + b * 32, o);
+                        tmem_wait_ld(o);
+                        if (live) {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                to[(b * 8 + k) * TM] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
+                        }
+                    }
+                    tc_fence_before();
+                }
+                if (live) part_sum<D>(p, id, t)[row] = make_float2(m == -CUDART_INF_F ? m : m * c - Fmt<T>::LIFT, begun ? l : -1.f);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->q_free[t][qbuf]);
+                continue;
+            }
             if (!begun) {                             // (a query tile without rows)
                 if (lane == 0) mbar_arrive(&bars->q_free[t][qbuf]);
                 continue;
@@ -818,6 +909,54 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     }
 }
 
+// Merge the parts of each item: 8 rows of a query tile a CTA, 4 columns a thread (so a part's floats come as runs of 128 bytes).
+template <typename T, int D>
+__global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __grid_constant__ UmmaParams p) {
+    constexpr int ROWS = 8;
+    __shared__ float2 sums[MAX_SHARE][ROWS];
+    __shared__ int odd[ROWS];
+    const int tid = threadIdx.x, r = tid % ROWS, c4 = tid / ROWS;
+    const int t = blockIdx.x / (TM / ROWS) % 2, row0 = blockIdx.x % (TM / ROWS) * ROWS, row = row0 + r;
+    const int item = blockIdx.x / (2 * TM / ROWS), id = item * p.parts;      // id: of its first part
+    const int in = item % (p.w.hk * p.hblocks), kvh = in / p.hblocks, hb = in % p.hblocks;
+    const int tok = t * p.tpt + row / p.gb, h = hb * p.gb + row % p.gb;      // of the item
+    sh_pdl_wait();
+    const int4 w = part_item<D>(p)[item];
+    const int parts = min(w.x, p.parts);
+    if (parts <= 1 || row0 / p.gb >= p.tpt || t * p.tpt + row0 / p.gb >= w.z) return;
+    const bool live = row / p.gb < p.tpt && tok < w.z && h < p.w.g;
+    for (int i = c4; i < parts; i += D / 4) sums[i][r] = live ? part_sum<D>(p, id + i, t)[row] : make_float2(0.f, -1.f);
+    if (tid < ROWS) odd[tid] = 0;
+    __syncthreads();
+    float M = -CUDART_INF_F;
+    for (int i = 0; i < parts; ++i) M = fmaxf(M, sums[i][r].x);
+    float L = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 *at = part_o<D>(p, id, t) + c4 * TM + row;
+#pragma unroll 8
+    for (int i = 0; i < parts; ++i) {
+        const float2 s = sums[i][r];
+        if (s.y < 0.f) continue;                     // (nothing was written)
+        const float4 x = at[(long long)i * 2 * (D / 4) * TM];
+        const float f = s.x == -CUDART_INF_F ? 0.f : ex2_approx(s.x - M);      // (0 times NaN stays one)
+        L += s.y * f;
+        o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+    }
+    const float inv = 1.f / L;                       // (as where there is nothing to merge)
+    o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
+    if (live && !(isfinite(o.x) && isfinite(o.y) && isfinite(o.z) && isfinite(o.w))) odd[r] = 1;
+    __syncthreads();
+    if (live && !odd[r]) {
+        T *dst = reinterpret_cast<T *>(p.w.out.p + (long long)(w.y + tok) * p.w.out.ts + (kvh * p.w.g + h) * p.w.out.hs) + c4 * 4;
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(shelem::Vec<T>::pack2(o.x, o.y), shelem::Vec<T>::pack2(o.z, o.w));
+    }
+    for (int i = tid >> 5; i < ROWS; i += D / 16) {  // rows next to values that are not finite
+        if (!odd[i]) continue;
+        Found from;
+        slow_row<T, D>(p, id, find_item(p, id, from).from(t) + (row0 + i) / p.gb, kvh * p.w.g + hb * p.gb + (row0 + i) % p.gb);
+    }
+}
+
 typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -856,6 +995,21 @@ bool keys_map(CUtensorMap *m, const WinRows &r, int heads, int tokens, uint64_t 
     return make_map(m, r.p, 3, dim, st, box);
 }
 
+// The most items a call can have: c tokens of a sequence make (c - 1) / span + 1.
+long long most_items(int tokens, int sequences, int hk, int g) {
+    const int gb = g < TM ? g : TM;
+    const long long n = std::min(sequences, tokens);
+    return ((tokens - n) / (2 * (TM / gb)) + n) * hk * ((g + gb - 1) / gb);
+}
+// The device's CTAs per item, and the most parts of an item: how many keys there are is known on the device only, but the rows of an
+// item see no more than the window and the sinks hold, and without a cache no more than the call's tokens.
+void share_out(long long items, int tokens, int window, int sinks, int g, bool with_cache, int sms, int &share, int &parts) {
+    const int gb = g < TM ? g : TM;
+    const long long sees = ((long long)window + sinks + 2 * (TM / gb)) / TN + 3, own = ((long long)tokens + TN - 1) / TN;
+    share = (int)(std::min(sms, MAX_SHARE) / items);
+    parts = parts_of(with_cache ? sees : std::min(sees, own), share);
+}
+
 template <typename T, int D>
 cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     UmmaParams p;
@@ -883,11 +1037,24 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     int sms = 0;
     const cudaError_t e = sh_setup_kernel(setup, kern, Cfg<D>::SMEM, &sms);
     if (e != cudaSuccess) return e;
-    // each sequence adds at most one partly filled item
-    const long long items = ((long long)w.tokens / (2 * p.tpt) + w.sequences) * w.hk * p.hblocks;
+    const long long items = most_items(w.tokens, w.sequences, w.hk, w.g);
+    share_out(items, w.tokens, w.window, w.sinks, w.g, w.kc != nullptr, sms, p.share, p.parts);
+    if (!w.part) p.parts = 1;
     if (items > 0x7fffffffll) return cudaErrorInvalidValue;
-    kern<<<(unsigned)items, NTH, Cfg<D>::SMEM, s>>>(p, mq, mk, mv, mkc, mvc, mo);
-    return cudaGetLastError();
+    kern<<<(unsigned)(items * p.parts), NTH, Cfg<D>::SMEM, s>>>(p, mq, mk, mv, mkc, mvc, mo);
+    if (p.parts == 1) return cudaGetLastError();
+    const cudaError_t e2 = cudaGetLastError();
+    if (e2 != cudaSuccess) return e2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(items * (2 * TM / 8)));
+    cfg.blockDim = dim3(2 * D);
+    cfg.stream = s;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, sh_window_prefill_merge_kernel<T, D>, p);
 }
 
 }  // namespace
@@ -895,6 +1062,13 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
 cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int D, cudaStream_t s) {
     if (dtype == SH_F16) return D == 128 ? launch<__half, 128>(p, s) : launch<__half, 64>(p, s);
     return D == 128 ? launch<__nv_bfloat16, 128>(p, s) : launch<__nv_bfloat16, 64>(p, s);
+}
+
+size_t sh_window_prefill_scratch(int tokens, int sequences, int hk, int g, int window, int sinks, bool with_cache, int dtype, int D) {
+    if (dtype == SH_F32 || tokens < 1 || sequences < 1) return 0;
+    int share, parts;
+    share_out(most_items(tokens, sequences, hk, g), tokens, window, sinks, g, with_cache, MAX_SHARE, share, parts);
+    return parts > 1 ? sizeof(float) * MAX_SHARE * (2 * TM * (size_t)(D + 2) + 4) : 0;
 }
 
 cudaError_t sh_window_error_take(int *code, cudaStream_t s) {

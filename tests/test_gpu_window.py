@@ -182,6 +182,68 @@ def test_prompt_chunks_with_large_logits_and_many_sequences(dtype):
     _prefill_case(dtype, 64, 1, 2, 24, 2, lens, [(i * 13) % 70 for i in range(75)], seed=9)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hk,g,window,sinks,lens,ctx", [
+    (1, 2, 2000, 4, (1, 5, 0, 140), (2500, 3, 9, 1000)),       # parts without a tile, and all of them in use
+    (2, 3, 1200, 0, (70,), (5000,)),
+    (1, 71, 1500, 130, (3, 1), (1630, 64)),
+    (1, 130, 2500, 0, (2,), (2400,)),
+    (1, 4, 1100, 1, (1500,), (0,)),                            # a chunk that looks at itself alone
+])
+def test_few_rows_over_many_keys(dtype, d, hk, g, window, sinks, lens, ctx):
+    """Few rows over a long context: the key tiles of a query tile go to several CTAs, whose results are merged."""
+    import ctypes as C
+    sh = _sh()
+    w = sh._Window(sh.DTYPE_CODE[dtype], d, hk * g, hk, window, sinks, 0.0)
+    assert sh.lib.sh_window_prefill_workspace_bytes(C.byref(w), sum(lens), len(lens), 1) > 0
+    _prefill_case(dtype, d, hk, g, window, sinks, lens, ctx, seed=41, pad=0, fill=0.0)
+    _prefill_case(dtype, d, hk, g, window, sinks, lens, ctx, seed=42, hot=8.0)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_few_rows_with_infinite_values_idle_sequences_and_without_a_workspace(dtype):
+    """With and without a workspace the same result: infinite values come out in their element alone, a key that is NaN makes the
+    rows that see it NaN, keys and values out of sight matter to nobody, idle sequences keep their rows, a replayed graph repeats."""
+    import ctypes as C
+    sh, gen, dt = _sh(), _gen(43), DT[dtype]
+    hk, g, d, window, t, n, inf = 2, 3, 128, 2000, 2100, 40, float("inf")
+    hist = _history(gen, [n, n], [t, t], hk, d, dt)
+    vals = hist[0][1].clone()
+    hist[0][1][1500, 1, 17], hist[0][1][t + 20, 0, 3], hist[0][1][50, 0, 9] = inf, -inf, inf      # (position 50 has left the window)
+    kc, vc = _caches(hist, [t, t], hk, d, window, 0, dt, 0.0)
+    k, v = (torch.cat([h[x][t:] for h in hist]) for x in (0, 1))
+    q = _rnd(gen, 2 * n, hk * g, d, dtype=dt)
+    starts, lengths = _i32([0, n, 2 * n]), _i32([t, -1])
+    args = dict(window=window, lengths=lengths, k_cache=kc, v_cache=vc)
+    with_work = torch.full_like(q, 7.0)
+    sh.window_prefill(q, k, v, starts, out=with_work, **args)
+    without = torch.full_like(q, 7.0)
+    win = sh._Window(sh.DTYPE_CODE[dtype], d, hk * g, hk, window, 0, 0.0)
+    rows = lambda x: C.byref(sh._Rows(x.data_ptr(), x.stride(0), x.stride(1)))
+    cache = sh._WindowCache(kc.data_ptr(), vc.data_ptr(), *kc.stride()[:3])
+    assert sh.lib.sh_window_prefill(C.byref(win), 2 * n, 2, rows(q), rows(k), rows(v), starts.data_ptr(), lengths.data_ptr(), C.byref(cache),
+                                    rows(without), None, 0, torch.cuda.current_stream().cuda_stream) == sh.SH_OK
+    replayed, graph = torch.full_like(q, 7.0), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sh.window_prefill(q, k, v, starts, out=replayed, **args)
+    for _ in range(3):
+        graph.replay()
+    assert torch.equal(replayed, with_work)
+    want, vmax, smax = ref.attend_ref(q[:n], range(t, t + n), hist[0][0], vals, window, 0)
+    tol = ref.attend_tolerance(want, vmax, smax, dt)
+    expect = torch.zeros(n, hk * g, d, dtype=torch.float64)
+    expect[:, g:, 17], expect[20:, :g, 3] = inf, -inf
+    for out in (with_work, without):
+        assert (out[n:] == 7).all()
+        got = out[:n].double().cpu()
+        assert torch.equal(torch.where(torch.isinf(got), got, 0.0), expect)
+        ref.check(torch.where(torch.isinf(got), want, got), want, tol)
+    kc[0, 0, (t - 30) % window, 5] = float("nan")
+    sh.window_prefill(q, k, v, starts, out=with_work, **args)
+    assert torch.isnan(with_work[:n, :g]).all() and not torch.isnan(with_work[:n, g:]).any()
+
+
 @pytest.mark.parametrize("dtype,hk,g,d", [("bf16", 8, 4, 128), ("f16", 16, 1, 128), ("bf16", 4, 7, 64), ("f32", 4, 2, 64)])
 def test_prompts_that_fill_the_device(dtype, hk, g, d):
     """Many tiles on every SM, short and long sequences mixed: every row against a definition in 64 bits, and run after run the same."""

@@ -32,7 +32,7 @@ def _calls(sh, a):
     lib = sh.lib
     return dict(
         prefill=lambda: lib.sh_window_prefill(ref(a["w"]), a["tokens"], a["n"], ref(a["q"]), ref(a["k"]), ref(a["v"]), a["starts"],
-                                              a["lengths"], ref(a["cache"]), ref(a["out"]), None),
+                                              a["lengths"], ref(a["cache"]), ref(a["out"]), a["work"], a["work_bytes"], None),
         append=lambda: lib.sh_window_append(ref(a["w"]), a["tokens"], a["n"], ref(a["k"]), ref(a["v"]), a["starts"], a["lengths"],
                                             ref(a["cache"]), None),
         decode=lambda: lib.sh_window_decode(ref(a["w"]), a["n"], ref(a["q"]), ref(a["k"]), ref(a["v"]), a["lengths"], ref(a["cache"]),
@@ -119,6 +119,24 @@ def test_decode_workspace():
     assert size(C.byref(a["w"]), 1000) == 0 and size(C.byref(a["w"]), 0) == 0 and size(None, 3) == 0
     a["w"].dtype = sh.SH_F32
     assert size(C.byref(a["w"]), 3) == 0
+
+
+def test_prefill_workspace():
+    sh = _sh()
+    a = _args(sh)
+    size = sh.lib.sh_window_prefill_workspace_bytes
+    assert size(C.byref(a["w"]), 4, 3, 1) == 0                       # a window of 8: nothing to split
+    a["w"].window = 8000
+    a["cache"] = sh._WindowCache(FAKE, FAKE, 2 * 8002 * 64, 8002 * 64, 64)
+    need = size(C.byref(a["w"]), 4, 3, 1)
+    assert 1 << 20 < need < 1 << 25 and size(C.byref(a["w"]), 4, 3, 0) == 0 and size(C.byref(a["w"]), 1 << 20, 3, 1) == 0
+    assert size(C.byref(a["w"]), 0, 3, 1) == 0 and size(C.byref(a["w"]), 4, 0, 1) == 0 and size(None, 4, 3, 1) == 0
+    a["work"], a["work_bytes"] = FAKE, need - 1
+    assert _calls(sh, a)["prefill"]() == sh.SH_ENOMEM
+    a["work"], a["work_bytes"] = FAKE + 8, need
+    assert _calls(sh, a)["prefill"]() == sh.SH_EINVAL
+    a["w"].dtype = sh.SH_F32
+    assert size(C.byref(a["w"]), 4, 3, 1) == 0
 
 
 def test_calls_with_nothing_to_do_succeed():
