@@ -305,13 +305,18 @@ __device__ __forceinline__ Item find_item(const UmmaParams &p, int id, Found &fr
         int first = 0, count = 0, cached = 0;
         if (base + lane < p.w.sequences) sequence_rows(p.w, base + lane, first, count, cached);
         const int mine = (count + span - 1) / span;
-        long long upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += x;
+        // of 32 sequences those with most cached keys to walk over come first (103 -> 96 us for chunks of 17 to 256 tokens over 1 to
+        // 2052 rows; ordered by the tokens of the chunk too, prompts of 1 to 4001 tokens took 132 instead of 130 us)
+        const unsigned key = (unsigned)(p.w.kc ? min(cached, p.w.sinks + p.w.window) / TN : 0) << 5 | (31 - lane);
+        long long upto = 0, all = 0;
+#pragma unroll 4
+        for (int o = 0; o < min(32, p.w.sequences - base); ++o) {
+            const unsigned other = __shfl_sync(0xffffffffu, key, o);
+            const int x = __shfl_sync(0xffffffffu, mine, o);
+            all += x;
+            if (other >= key) upto += x;
         }
-        const unsigned hit = __ballot_sync(0xffffffffu, before + upto > tile);
+        const unsigned hit = __ballot_sync(0xffffffffu, before + upto > tile && before + upto - mine <= tile);
         if (hit) {
             const int l = __ffs(hit) - 1;
             from.base = base;
@@ -324,7 +329,7 @@ __device__ __forceinline__ Item find_item(const UmmaParams &p, int id, Found &fr
             r.a = (int)(before + __shfl_sync(0xffffffffu, upto, l) - 1 - tile) * span;
             break;
         }
-        before += __shfl_sync(0xffffffffu, upto, 31);
+        before += all;
     }
     if (r.seq < 0) return r;
     r.part = in % p.parts;
