@@ -18,7 +18,8 @@
 // turn: 2.3 instead of 2.0 ms for the 32768-token prompt below.
 //
 // A running CTA takes over the items of CTAs that have not started (cluster launch control), so it sets up once and long and short
-// items even out: 153 -> 139 us for prompts of 1 to 4001 tokens, 150 -> 118 us for continued chunks, whose contexts differ most.
+// items even out: 153 -> 139 us for prompts of 1 to 4001 tokens, 150 -> 118 us for continued chunks, whose contexts differ most (97
+// with the sequences in order of what they have cached).
 // The next item's queries have a place of their own, so its first S follows the last one of the present item at once.  What finished
 // leaves by a copy from shared memory (8192 tokens, window 256: 77 -> 71 us against stores by the threads).
 //

@@ -653,6 +653,44 @@ def test_graphs_streams_and_calls_at_once():
             assert torch.equal(got[x], w[x]), x
 
 
+FIRST_CALLS = """
+import torch
+from paper_2305_17118_b200 import binding as sh
+torch.manual_seed(5)
+for dt, d, axis in ((torch.bfloat16, 128, 30000), (torch.float16, 64, 30000), (torch.bfloat16, 64, 300), (torch.float16, 128, 300), (torch.float32, 64, 300), (torch.float32, 128, 300)):
+    q, k, v = torch.randn(40, 8, d, device="cuda").to(dt), torch.randn(40, 2, d, device="cuda").to(dt), torch.randn(40, 2, d, device="cuda").to(dt)
+    kc, vc = torch.randn(1, 2, axis, d, device="cuda").to(dt), torch.randn(1, 2, axis, d, device="cuda").to(dt)
+    r = sh.Rope(torch.rand(d // 2, device="cuda"), q_weight=torch.ones(d, device="cuda", dtype=dt))
+    pos, starts, ln = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (list(range(40)), [0, 40], [70001]))
+    def calls(kc, vc):
+        a, b = sh.qk_norm_rope(q, k, pos, r)
+        c = sh.window_prefill(a, b, v, starts, window=axis, lengths=ln, k_cache=kc, v_cache=vc)
+        sh.window_append(b, v, starts, ln, kc, vc, window=axis)
+        return c, sh.window_decode(q[:1], k[:1], v[:1], ln + 40, kc, vc, window=axis, rope=r)
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    mine = kc.clone(), vc.clone()
+    ln + 40
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=side):      # the first call of each kernel is captured
+        got = calls(*mine)
+    mine[0].copy_(kc), mine[1].copy_(vc)
+    g.replay()
+    torch.cuda.synchronize()
+    for x, y in zip(got, calls(kc, vc)):
+        assert torch.equal(x, y)
+    sh.window_status()
+print("same")
+"""
+
+
+def test_the_first_calls_of_a_process_can_be_captured():
+    import pathlib
+    import subprocess
+    import sys
+    done = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=pathlib.Path(__file__).parent.parent, capture_output=True, text=True, timeout=240)
+    assert done.returncode == 0 and done.stdout.strip() == "same", done.stderr[-2000:]
+
+
 def test_results_on_another_stream_than_the_current_one():
     """New outputs and workspaces belong to the stream of the call, not to the current one, which is kept busy meanwhile."""
     sh, gen, dt = _sh(), _gen(36), torch.bfloat16
