@@ -63,6 +63,9 @@ constexpr int REGS_SOFTMAX = 184, REGS_OTHER = 136;    // 256 * 184 + 128 * 136 
 constexpr float RENEW = 8.f;               // log2 growth of the maximum at which O is rescaled
 
 __device__ int g_window_error;             // code of the first bounded wait that gave up
+#ifdef SH_DEBUG_BOUNDS
+__device__ int g_window_selftest = -1;     // self-test: the work item whose load warp gives up before it has listed the item
+#endif
 
 constexpr int STEPS = 8, BAR_BYTES = 960;  // steps in flight between the load warp and the others; barriers and step ring
 
@@ -109,7 +112,11 @@ static_assert(sizeof(Bars) <= BAR_BYTES, "barrier block");
 
 // Wait for a phase, bounded by time, in few instructions: the code of a wait that gave up goes to the CTA's abort word, and from
 // there to g_window_error at the end.  The bound has to outlast rows that are done again: 32 of them over a million keys take a second.
+#ifdef SH_DEBUG_BOUNDS
+constexpr unsigned long long LIMIT_NS = 200000000ull;      // (its self-test waits for it)
+#else
 constexpr unsigned long long LIMIT_NS = 8000000000ull;
+#endif
 __device__ __forceinline__ bool wait_for(Bars *bars, uint64_t *bar, uint32_t parity, int code) {
     if (mbar_try_wait(bar, parity)) return true;
     const unsigned long long t0 = global_ns();
@@ -305,6 +312,7 @@ __device__ __forceinline__ Item find_item(const UmmaParams &p, int id, Found &fr
     if (tile < from.before) from = Found();
     Item r;
     r.seq = -1;
+    r.a = r.tpt = r.count = 0;
     long long before = from.before;
     for (int base = from.base; base < p.w.sequences; base += 32) {
         int first = 0, count = 0, cached = 0;
@@ -384,6 +392,7 @@ __device__ __noinline__ void slow_row(const UmmaParams &u, int id, int qi, int h
     const WindowParams &p = u.w;
     Found from;
     const Item w = find_item(u, id, from);
+    if (w.seq < 0 || qi < 0 || qi >= w.count) return;      // (only where a CTA gave up a wait)
     const int lane = threadIdx.x & 31;
     float q[E], o[E], m = -CUDART_INF_F, l = 0.f;
     const T *qr = reinterpret_cast<const T *>(p.q.p + (long long)(w.first + qi) * p.q.ts + h * p.q.hs) + lane * E;
@@ -569,15 +578,27 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             __syncwarp();
         };
         Found from;
+        // an item that nobody works on any more: the merge finds nothing to do
+        auto drop = [&](int i) {
+            if (p.parts > 1 && i >= 0 && i % p.parts == 0) part_item<D>(p)[i / p.parts] = make_int4(0, 0, 0, 0);
+        };
+        if (!ok && lane == 0) drop(blockIdx.x);
         uint32_t asked = 0, answered = 0;             // requests for work, answers read
         uint32_t cleaned = 0;                         // tiles with dead rows
         for (int id = blockIdx.x; ok && id >= 0;) {
             const Item w = find_item(p, id, from);
             if (w.seq < 0) {                          // (the grid is an upper bound: behind the last item nothing follows)
-                if (p.parts > 1 && id % p.parts == 0 && elect_one()) part_item<D>(p)[id / p.parts] = make_int4(0, 0, 0, 0);
+                if (elect_one()) drop(id);
                 __syncwarp();
                 break;
             }
+#ifdef SH_DEBUG_BOUNDS
+            if (id == g_window_selftest) {
+                *(volatile int *)&bars->abort_flag = 0x6ff;
+                ok = false;
+                break;
+            }
+#endif
             bool first = true, ask = true;
             const int last_tile = w.ctiles + w.jhi;   // (the tile of the last row itself: always needed)
             int flags = 0, x = 0;                     // a step that waits to learn whether it is the last
@@ -696,7 +717,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         // let the copies (and the answer) requested last land before the CTA goes away (a phase that is past reads as complete; with the last step
         // published, its stage's earlier load has been waited for)
         if (lane == 0) {
-            if (answered != asked) wait_for(bars, &bars->claimed, answered & 1, 0);
+            if (answered != asked && wait_for(bars, &bars->claimed, answered & 1, 0)) drop(claim_read(&bars->claim));
             if (items > 0)
                 for (int t = 0; t < 2; ++t) wait_for(bars, &bars->q_full[t][(items - 1) & 1], ((items - 1) >> 1) & 1, 0);
             for (uint32_t k = 0; k < C::STAGES - (ok ? 1u : 0u) && k < loads; ++k)
@@ -950,6 +971,8 @@ __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __
     sh_pdl_wait();
     const int4 w = part_item<D>(p)[item];
     const int parts = min(w.x, p.parts);
+    // (the entry of an item that was lost with a CTA that gave up a wait holds anything)
+    if (w.y < 0 || w.y > p.w.tokens || w.z > p.w.tokens - w.y) return;
     if (parts <= 1 || row0 / p.gb >= p.tpt || t * p.tpt + row0 / p.gb >= w.z) return;
     const bool live = row / p.gb < p.tpt && tok < w.z && h < p.w.g;
     for (int i = c4; i < parts; i += D / 4) sums[i][r] = live ? part_sum<D>(p, id + i, t)[row] : make_float2(0.f, -1.f);
@@ -1097,6 +1120,14 @@ size_t sh_window_prefill_scratch(int tokens, int sequences, int hk, int g, int w
     share_out(most_items(tokens, sequences, hk, g), tokens, window, sinks, g, with_cache, MAX_SHARE, share, parts);
     return parts > 1 ? sizeof(float) * MAX_SHARE * (2 * TM * (size_t)(D + 2) + 4) : 0;
 }
+
+#ifdef SH_DEBUG_BOUNDS
+// Self-test of the give-up path of the waits (bounds-checked build only): the next launches' CTA that takes work item `item` gives up;
+// -1: none.
+extern "C" int sh_window_selftest(int item) {
+    return cudaMemcpyToSymbol(g_window_selftest, &item, sizeof(int)) == cudaSuccess ? SH_OK : SH_ECUDA;
+}
+#endif
 
 cudaError_t sh_window_error_take(int *code, cudaStream_t s) {
     cudaError_t e = cudaMemcpyFromSymbolAsync(code, g_window_error, sizeof(int), 0, cudaMemcpyDeviceToHost, s);
