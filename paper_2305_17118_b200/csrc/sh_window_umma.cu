@@ -67,7 +67,8 @@ __device__ int g_window_error;             // code of the first bounded wait tha
 __device__ int g_window_selftest = -1;     // self-test: the work item whose load warp gives up before it has listed the item
 #endif
 
-constexpr int STEPS = 8, BAR_BYTES = 960;  // steps in flight between the load warp and the others; barriers and step ring
+constexpr int STEPS = 8, BAR_BYTES = 2048; // steps in flight between the load warp and the others; barriers, step ring, rows to do again
+constexpr int AGAIN = 16;                  // items of a warp with such rows, at most: see Bars
 
 template <int D> struct Cfg {
     static constexpr int QTILE = D / 64 * QHALF, TILE = D / 64 * HALF;      // bytes of a query tile, of a key or value tile
@@ -105,13 +106,20 @@ struct Bars {
     uint64_t claimed;
     uint64_t landed;                       // a tile whose dead rows are zeroed before anybody reads it
     Step steps[STEPS];
+    // Rows to be computed again wait for the end of the CTA's items, when nobody waits for their warps any more: 32 of them over a million
+    // keys take up to 19 s.  An item that begins after the first of them was noted asks for no further one (CTAs that have not started
+    // take the rest).  So a softmax warp may still come to the item of the step it has read ahead, those of STEPS published steps
+    // behind that, the item being published and the one asked for already.
+    int2 again[SOFTMAX_WARPS][AGAIN];      // (item, rows of the warp)
+    int again_count[SOFTMAX_WARPS], no_more;
     uint32_t tmem;
     int abort_flag;
 };
+static_assert(AGAIN >= STEPS + 4, "see Bars");
 static_assert(sizeof(Bars) <= BAR_BYTES, "barrier block");
 
 // Wait for a phase, bounded by time, in few instructions: the code of a wait that gave up goes to the CTA's abort word, and from
-// there to g_window_error at the end.  The bound has to outlast rows that are done again: 32 of them over a million keys take a second.
+// there to g_window_error at the end.
 #ifdef SH_DEBUG_BOUNDS
 constexpr unsigned long long LIMIT_NS = 200000000ull;      // (its self-test waits for it)
 #else
@@ -425,6 +433,35 @@ __device__ __noinline__ void slow_row(const UmmaParams &u, int id, int qi, int h
     for (int e = 0; e < E; ++e) dst[e] = (T)(o[e] / l);
 }
 
+// Note rows of a softmax warp that have to be computed again, and do them.  (Calls, as inlined they cost the loop over the steps
+// 3 %: 534 against 518 us for 8192 tokens, full causal attention.)
+__device__ __noinline__ void note_again(Bars *bars, int warp, int id, unsigned rows) {
+    if ((threadIdx.x & 31) == 0) {
+        const int n = bars->again_count[warp];
+        if (n < AGAIN) {
+            bars->again[warp][n] = make_int2(id, (int)rows);
+            bars->again_count[warp] = n + 1;
+            *(volatile int *)&bars->no_more = 1;
+        } else {
+            *(volatile int *)&bars->abort_flag = 0x626;
+        }
+    }
+    __syncwarp();
+}
+
+template <typename T, int D>
+__device__ __noinline__ void do_again(const UmmaParams &p, const int2 *list, int count, int t, int quarter) {
+    for (int i = 0; i < count; ++i) {
+        const int2 e = list[i];
+        Found from;
+        const Item w = find_item(p, e.x, from);
+        for (unsigned rows = (unsigned)e.y; rows; rows &= rows - 1) {
+            const int r = quarter * 32 + __ffs(rows) - 1;
+            slow_row<T, D>(p, e.x, w.from(t) + r / p.gb, w.kvh * p.w.g + w.hb * p.gb + r % p.gb);
+        }
+    }
+}
+
 template <typename T> struct Fmt;
 template <> struct Fmt<__half> { static constexpr int CODE = 0; static constexpr float LIFT = 7.f; };
 template <> struct Fmt<__nv_bfloat16> { static constexpr int CODE = 1; static constexpr float LIFT = 0.f; };
@@ -455,7 +492,8 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(&bars->full[s], 1); mbar_init(&bars->empty[s], 2); }
         mbar_init(&bars->claimed, 1); mbar_init(&bars->landed, 1);
         for (int s = 0; s < STEPS; ++s) { mbar_init(&bars->step_full[s], 1); mbar_init(&bars->step_empty[s], SOFTMAX_WARPS); }
-        bars->abort_flag = 0;
+        for (int w = 0; w < SOFTMAX_WARPS; ++w) bars->again_count[w] = 0;
+        bars->abort_flag = bars->no_more = 0;
         if ((smem_u32(sm) & 1023u) != 0) bars->abort_flag = 0x620;      // the swizzled tiles need the alignment the declaration asks for
         fence_barrier_init();
     }
@@ -599,7 +637,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 break;
             }
 #endif
-            bool first = true, ask = true;
+            bool first = true, ask = __shfl_sync(0xffffffffu, *(volatile int *)&bars->no_more, 0) == 0;
             const int last_tile = w.ctiles + w.jhi;   // (the tile of the last row itself: always needed)
             int flags = 0, x = 0;                     // a step that waits to learn whether it is the last
             // 32 tiles at a time, a lane each; what lies between the sinks and the window is passed over
@@ -697,7 +735,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 __syncwarp();
                 ++asked;
             }
-            if (!ok) break;
+            if (!ok || asked == answered) break;
             ok = __all_sync(0xffffffffu, wait_for(bars, &bars->claimed, answered & 1, 0x614));
             if (!ok) break;
             ++answered;
@@ -939,13 +977,11 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->q_free[t][qbuf]);
-            unsigned again = __ballot_sync(0xffffffffu, live && odd);
-            while (again) {
-                const int l0 = __ffs(again) - 1;
-                again &= again - 1;
-                slow_row<T, D>(p, id, __shfl_sync(0xffffffffu, qi, l0), kvh * p.w.g + __shfl_sync(0xffffffffu, h, l0));
-            }
+            const unsigned again = __ballot_sync(0xffffffffu, live && odd);
+            if (again) note_again(bars, warp, id, again);
         }
+        __syncwarp();
+        do_again<T, D>(p, bars->again[warp], bars->again_count[warp], t, warp & 3);
         bulk_wait_all();            // outputs on their way from shared memory
     }
     tc_fence_before();

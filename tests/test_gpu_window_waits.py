@@ -74,3 +74,26 @@ def test_a_lost_item_leaves_the_rows_of_others_alone(shb, dtype, d):
         assert _prefill(sh, q, k, v, starts, lengths, kc, vc, window, out, work) == sh.SH_OK
         sh.window_status()
         assert torch.equal(out, whole) and (memory[n:] == 7).all()
+
+
+def test_rows_computed_again_do_not_run_out_the_waits(shb):
+    """An infinite value that every row sees sends every row through the slow path: a warp's rows take longer than the waits of this
+    build last, while the other warps wait for its next item.  All rows come out."""
+    sh, dt, d, n = shb, torch.float16, 64, 160000
+    gen = torch.Generator(device="cuda").manual_seed(52)
+    q, k, v = (torch.randn(n, 1, d, generator=gen, device="cuda").to(dt) for _ in range(3))
+    starts = _i32([0, n])
+    clean = v.clone()
+    v[0, 0, 3] = float("inf")
+    out = sh.window_prefill(q, k, v, starts, window=1 << 20)
+    sh.window_status()
+    assert torch.isposinf(out[:, 0, 3]).all()
+    assert torch.isfinite(out[:, 0, :3]).all() and torch.isfinite(out[:, 0, 4:]).all()
+    clean[0, 0, 3] = 0
+    for i in (0, 1, 255, 256, 70001, n - 257, n - 1):
+        want, vmax, smax = ref.attend_ref(q[i:i + 1], [i], k[:i + 1], clean[:i + 1], 1 << 20, 0)
+        got = out[i:i + 1].clone()
+        got[0, 0, 3] = want[0, 0, 3]
+        tol = ref.attend_tolerance(want, vmax, smax, dt)
+        tol[0, 0, 3] = 1.0
+        ref.check(got, want, tol)
