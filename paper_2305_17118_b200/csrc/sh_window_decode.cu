@@ -266,8 +266,13 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
 // A warp takes blocks of 16 rows: S[q][key] = Q.K^T with the queries as M, O^T[d][q] += V^T.P^T with d as M, so that the
 // accumulators of S are, lane by lane, the B operand of the second product.  Up to 8 query heads share a pass over the rows.  The
 // other 8 rows of M hold what rounding a prepared query to 16 bits leaves (zero for queries that come as they are), and P enters as
-// two 16-bit parts, so the step is as exact as fp32 arithmetic on the stored rows.  The arithmetic is a fifth of what the
+// two 16-bit parts, so what is left of those roundings is 2^-18 of a weight or of an element of the query (bf16; fp16: 2^-24).  The arithmetic is a fifth of what the
 // tensor pipe can do; the kernel is bound by HBM.
+//
+// Two fp16 parts hold a weight to 2^-25, however small it is, and thousands of small weights beside one large one (a sink) carry what
+// the large one's value leaves out.  So fp16 weights are lifted: the maximum is renewed whenever it grows (weights are at most 1), and they
+// carry a factor 2^15, which cancels in O / l.  A weight down to 2^-25 of its warp's largest then keeps 15 bits, one of 2^-29 keeps 11, and
+// below it counts to 2^-40.  bf16 has the range of fp32.
 //
 // Each warp brings its rows in by cp.async, 16 bytes a lane, into a ring of its own (no barrier on the way; pieces permuted by
 // row so that ldmatrix reads without bank conflicts).  Rows that hold no token are filled with zeros and never read.
@@ -275,6 +280,9 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
 // rate (CUDA cores: 699 us); 9216 units of 410 rows, fp16: 325 us, 0.91 (408 us); one sequence of 16388 rows: 19 us, 0.53 (61 us).
 constexpr int MB = 16;               // rows of a block
 constexpr int MQ = 8;                // query heads of a unit
+// log2: growth at which the subtracted maximum is renewed (weights stay below 2^RENEW), and the factor of the weights
+template <typename T> struct Weights { static constexpr float RENEW = 8.f, LIFT = 0.f; };
+template <> struct Weights<__half> { static constexpr float RENEW = 0.f, LIFT = 15.f; };
 
 template <int D, int MW> struct Mma {      // MW: warps of a CTA
     static constexpr int STAGES = (D == 128 ? 1 : 2) * (MW == 8 ? 3 : 2);
@@ -466,8 +474,7 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
         float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        // the subtracted maximum is renewed when it has grown by more than 8 (log2): weights stay below 2^8
-        if (__any_sync(0xffffffffu, mx - m > 8.f)) {
+        if (__any_sync(0xffffffffu, mx - m > Weights<T>::RENEW)) {
             const float mn = fmaxf(m, mx), f = mn == -CUDART_INF_F ? 1.f : ex2_approx(m - mn);
             m = mn;
             l *= f;
@@ -475,7 +482,7 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) { o[k][0] *= f0; o[k][1] *= f1; o[k][2] *= f0; o[k][3] *= f1; }
         }
-        const float mb = m == -CUDART_INF_F ? 0.f : m;
+        const float mb = m == -CUDART_INF_F ? 0.f : m - Weights<T>::LIFT;
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = ex2_approx(x[e] - mb);
         l += (x[0] + x[1]) + (x[2] + x[3]);
