@@ -18,6 +18,7 @@
 #include "sh_rope.cuh"
 #include "sh_umma.cuh"
 #include "sh_window.cuh"
+#include "sh_window_split.h"
 
 namespace cg = cooperative_groups;
 
@@ -641,27 +642,6 @@ __global__ void __launch_bounds__(SLICES * D / 8) sh_window_decode_merge_kernel(
 // Parts of all units together; bounds the workspace.
 constexpr int MAX_PARTS = 160;
 
-// How a launch is laid out: S CTAs (a cluster) share the rows of a unit.  A CTA of a kernel draws at most `rate`
-// bytes/us, whatever bandwidth is left.
-struct Shape {
-    int S;
-    double us;      // what the launch is expected to take
-};
-// CTAs run in waves of slots_of[log2 S], what the device holds at once of such clusters; those of a wave share the memory bandwidth (6.4 MB/us), and each costs about 2.5 us to start and to
-// merge, half a microsecond more with each doubling of the cluster.  rows * row_bytes is what a unit may have to read.  The number of rows that a sequence really holds is known on the device
-// only, so it is the cache's size that counts here.
-Shape best_split(long long units, long long rows, int row_bytes, const int (&slots_of)[4], double rate) {
-    Shape best = {1, 1e300};
-    for (int S = 1, i = 0; S <= 8 && (S == 1 || rows >= 64ll * S); S *= 2, ++i) {
-        const long long ctas = units * S, slots = std::max(slots_of[i], S), full = (ctas - 1) / slots, rest = ctas - full * slots;
-        const double bytes = (double)rows * row_bytes / S;
-        auto wave = [&](long long n) { return bytes / std::min(6.4e6 / (double)n, rate) + 2.5 + 0.5 * (S > 1) + 0.5 * (S > 2) + 0.5 * (S > 4); };
-        const double us = (full ? full * wave(slots) : 0.0) + wave(rest);
-        if (us < best.us) best = {S, us};
-    }
-    return best;
-}
-
 cudaLaunchConfig_t cluster_config(unsigned ctas, int threads, size_t smem, int S, cudaLaunchAttribute *attr, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
@@ -676,18 +656,18 @@ cudaLaunchConfig_t cluster_config(unsigned ctas, int threads, size_t smem, int S
 }
 
 // CTAs of `kern` in clusters of 1, 2, 4 and 8 that the current device holds at once (a cluster lies within one group of SMs, so with
-// large CTAs not every SM can be used).  Asked once per device.
+// large CTAs not every SM can be used, and a size may have no place at all: 0).  Asked once per device.
 template <auto kern>
 cudaError_t cluster_slots(int threads, size_t smem, int (&slots)[4]) {
-    static std::atomic<int> known[ShKernelSetup::DEVICES][4];
+    static std::atomic<int> known[ShKernelSetup::DEVICES][4];      // one more than the answer; 0: not asked yet
     static ShKernelSetup setup;
     int dev = 0, sms = 0;
     cudaError_t e = sh_device_sms(&dev, &sms);
     if (e != cudaSuccess) return e;
     const bool kept = dev < ShKernelSetup::DEVICES;
     for (int i = 0; i < 4; ++i) {
-        slots[i] = kept ? known[dev][i].load(std::memory_order_relaxed) : 0;
-        if (slots[i]) continue;
+        slots[i] = (kept ? known[dev][i].load(std::memory_order_relaxed) : 0) - 1;
+        if (slots[i] >= 0) continue;
         e = sh_setup_kernel(setup, kern, smem, &sms);
         if (e != cudaSuccess) return e;
         cudaLaunchAttribute attr;
@@ -695,8 +675,8 @@ cudaError_t cluster_slots(int threads, size_t smem, int (&slots)[4]) {
         int clusters = 0;
         e = cudaOccupancyMaxActiveClusters(&clusters, kern, &cfg);
         if (e != cudaSuccess) return e;
-        slots[i] = std::max(clusters, 1) << i;
-        if (kept) known[dev][i].store(slots[i], std::memory_order_relaxed);
+        slots[i] = std::max(clusters, 0) << i;
+        if (kept) known[dev][i].store(slots[i] + 1, std::memory_order_relaxed);
     }
     return cudaSuccess;
 }

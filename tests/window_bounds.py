@@ -16,7 +16,7 @@ import torch
 
 import window_reference as ref
 
-LIFT_STEP, LIFT_PROMPT = 15, 11      # log2 factors of fp16 weights
+LIFT_STEP, LIFT_PROMPT = 15, 7      # log2 factors of fp16 weights
 
 
 def attend(q, qpos, keys, vals, window, sinks, scale=None, at=None):
