@@ -519,11 +519,11 @@ class Rope:
 
     def _packed(self, d: int, dtype, device: int) -> bytes:
         f, qw, kw = self.inv_freq, self.q_weight, self.k_weight
-        if f.get_device() != device or 2 * f.numel() != self._head[0]:
-            _fail("rope", f"{self._head[0] // 2} frequencies on cuda:{device}", f)
+        if f.get_device() != device or f.dtype is not torch.float32 or f.shape != (self._head[0] // 2,) or (f.numel() > 1 and f.stride(0) != 1):
+            _fail("rope", f"a contiguous vector of {self._head[0] // 2} fp32 frequencies on cuda:{device}", f)
         for w in (qw, kw):
-            if w is not None and (w.dtype is not dtype or w.shape != (d,) or w.get_device() != device):
-                _fail("weight", f"[{d}] of {dtype} on cuda:{device}", w)
+            if w is not None and (w.dtype is not dtype or w.shape != (d,) or w.get_device() != device or w.stride(0) != 1):
+                _fail("weight", f"contiguous [{d}] of {dtype} on cuda:{device}", w)
         return _pack_rope(_CODE_OF[dtype], d, *self._head, f.data_ptr(), 0 if qw is None else qw.data_ptr(), 0 if kw is None else kw.data_ptr())
 
 
