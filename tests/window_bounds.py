@@ -59,3 +59,17 @@ def step_tolerance(x, dtype):
 def prompt_tolerance(x, dtype):
     """Prompts: weights rounded once."""
     return tolerance(x, dtype, 1, LIFT_PROMPT)
+
+
+def marks(n, heads, d, dtype, device="cpu"):
+    """Values [n, heads, d] that name their block of 16 keys: 1 in column (block mod d), 0 elsewhere.  What comes out is each block's share."""
+    v = torch.zeros(n, heads, d, dtype=dtype, device=device)
+    j = torch.arange(n, device=device)
+    v[j, :, j // 16 % d] = 1
+    return v
+
+
+def repeated(rows, n):
+    """n rows that take the given ones in turn: keys that weigh the same are rounded the same way, so that errors of weights add up instead of
+    evening out over a long axis."""
+    return rows[torch.arange(n, device=rows.device) % rows.shape[0]]
