@@ -374,7 +374,7 @@ int sh_decode_kernel_choice(sh_handle h);
  * with j < sinks or j > p - window.  The cache has sinks + window slots per (sequence, key head): position j lives in
  * slot j when j < sinks, else in slot sinks + (j - sinks) % window.  Slots that hold no token are never used,
  * whatever they contain, and neither are keys and values outside of a query's sight (infinities and NaN included; rows next
- * to such values, and rows whose result is not finite, take a slower path).
+ * to such values, and rows whose result is not finite, take a slower path: up to half a microsecond a row and key).
  */
 
 /* [tokens][heads][head_dim] rows: element (t, h, i) is data[t * token_stride + h * head_stride + i]. */
@@ -469,8 +469,9 @@ int sh_window_decode(const sh_window *w, int sequences, const sh_rows *q, const 
                      const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
- * Did a kernel of the window cache give up one of its bounded waits (some seconds) on the current device since the last call?  Its outputs are
- * then incomplete.  Synchronises `stream`.  SH_OK, SH_EDEVICE or SH_ECUDA.
+ * Did a kernel of the window cache give up one of its bounded waits (some seconds; none lasts as long unless the device or the
+ * kernel is broken) on the current device since the last call?  Its outputs are then incomplete, while the call itself has returned SH_OK:
+ * only this call tells.  Synchronises `stream`.  SH_OK, SH_EDEVICE or SH_ECUDA.
  */
 int sh_window_status(void *stream);
 

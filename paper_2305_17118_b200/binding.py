@@ -580,7 +580,8 @@ def window_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: to
     ``q`` [tokens, q_heads, head_dim], ``k``/``v`` [tokens, kv_heads, head_dim]; the tokens ``starts[i] .. starts[i+1] - 1`` (int32, on the
     device) continue sequence i, which holds ``lengths[i]`` tokens in ``k_cache``/``v_cache`` [sequences, kv_heads, sinks + window, head_dim]
     (all three None: fresh prompts).  A token sees those before it among the first ``sinks`` positions and the last ``window``, itself
-    included.  Rows of ``out`` that belong to no sequence are left as they were (a new ``out`` is zeroed)."""
+    included.  Rows of ``out`` that belong to no sequence are left as they were (a new ``out`` is zeroed).  ``out`` must not overlap the
+    inputs.  16-bit types: the weights are rounded once to the type.  A broken device shows in ``window_status`` alone."""
     shape, dtype, device, qr = _head_rows(q, "q")
     tokens, q_heads, d = shape
     kshape, kr = _key_rows(k, "k", tokens, d, dtype, device)
@@ -652,7 +653,8 @@ def window_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: to
 
 def window_status(device="cuda:0", stream=None) -> None:
     """``sh_window_status``: raise ShError(SH_EDEVICE) if a window kernel on ``device`` gave up one of its bounded waits since the last
-    call (its outputs are then incomplete).  Synchronises the stream."""
+    call (its outputs are then incomplete, though ``window_prefill`` and ``WindowCache.prefill`` returned as usual: they do not
+    synchronise, and ask for nothing).  Synchronises the stream."""
     index = torch.device(device).index
     _launch("window_status", lib.sh_window_status, _current_device() if index is None else index, stream)
 

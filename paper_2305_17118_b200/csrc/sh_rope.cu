@@ -3,7 +3,7 @@
 // A warp takes one token and walks over groups of its heads (4 heads of 128 elements or 8 of 64 at a time, D / 16 lanes a
 // row), query heads first, then key heads; sines and cosines are made once per token and warp.  The rows of UNROLL groups are
 // requested before the first is worked on.  Bound by HBM: each row is read and written once.
-// 16384 tokens of 40 + 8 heads of 128 (bf16, views of a packed projection): 73.5 us, 5.48 TB/s, 0.84 of the measured copy
+// 16384 tokens of 40 + 8 heads of 128 (bf16, views of a packed projection): 73 us, 5.5 TB/s, 0.84 of the measured copy
 // rate.  Instructions come next (two thirds of the issue slots before the arithmetic went to packed pairs: 85 us).  UNROLL 3 / 4 / 6
 // at 5 or 6 blocks an SM: 73.1 / 73.5 / 97 us there, 17.2 / 15.9 / 20.2 us for 5003 tokens of 28 + 4 heads (fp16, three axes).
 #include "sh_rope.cuh"

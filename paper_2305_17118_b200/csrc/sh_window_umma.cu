@@ -23,20 +23,26 @@
 // The next item's queries have a place of their own, so its first S follows the last one of the present item at once.  What finished
 // leaves by a copy from shared memory (8192 tokens, window 256: 77 -> 71 us against stores by the threads).
 //
-// P is rounded to the storage type (the tensor cores take no other pair with 16-bit V); its row sum is taken before the rounding,
-// in fp32.  The subtracted maximum is only renewed when it has grown by more than 8 (log2), so weights stay below 2^8; fp16
-// weights carry a factor 2^7 (at most 2^15) that keeps small ones out of the subnormal numbers; it cancels in O / l.
+// P is rounded once, to the storage type; its row sum is taken before the rounding, in fp32.  That is a price paid for speed: the
+// single-token kernels hold P in two 16-bit parts, and here too the low part would have a place (the columns of S that P leaves free), but
+// P.V would be issued twice and every weight split.  Measured with one part and with two: 132 and 151 us for prompts of 1 to 4001 tokens,
+// 1.88 and 2.53 ms for the 32768 tokens below, 97 and 113 us for continued chunks.  With one the error against 64 bits is 1.2 to 1.4 times
+// that of the output's rounding alone.
+// The subtracted maximum is only renewed when it has grown by more than 8 (log2), so weights stay below 2^8; fp16 weights carry a
+// factor 2^7 (at most 2^15), which cancels in O / l: weights down to 2^-21 of the row's largest keep 11 bits, below that they are multiples
+// of 2^-31 of it.  (Renewing at 4, with a factor of 2^11, would reach 2^-25 and cost fp16 prompts 2 to 3 %.)
 //
 // Weights of unseen keys are zero, but 0 * NaN is NaN: a value row that is not finite poisons rows that do not see it (a slot
 // that holds no token, a later token, another sequence's row).  That shows as an O that is not finite; such rows are computed
-// again at the end, one warp per row over the visible keys only.  Rows whose result is rightly not finite take that way too.  As that
-// is slow, and slots that hold no token may hold anything, the load warp zeroes the rows of a value tile behind the sequence's last
+// again after the CTA's last item, one warp per row over the visible keys only.  Rows whose result is rightly not finite take that way
+// too.  As that is slow (0.1 to 0.6 us a row and key), and slots that hold no token may hold anything, the load warp zeroes the rows of a value tile behind the sequence's last
 // slot or token before it hands the tile on (512 tokens over 1000 in a cache with NaN behind them: 3655 -> 34 us).
 //
-// 32768 tokens, window 4096, 16 sinks, 32 query and 8 key heads of 128, fp16: 1.97 ms, 1050 TFLOP/s, 0.65 of the measured bf16 peak;
-// 8192 tokens, full causal attention, bf16: 0.48 ms, 1150 TFLOP/s.  Bound by the softmax warps and shared memory together: a step
-// takes about 1950 cycles, of which the exponentials need 1024 on each quarter of the SM and the operands' reads (48 KB per S of 64
-// keys, 16 KB per P.V, 32 KB written) 1250; with the exponentials left out it took 1600.  A part of the exponentials on the FMA
+// 32768 tokens, window 4096, 16 sinks, 32 query and 8 key heads of 128, fp16: 1.84 to 1.90 ms replayed from a graph, 1100 TFLOP/s, 0.68 to
+// 0.70 of the measured bf16 peak (2.14 ms a call when calls follow for seconds, under the power cap); 8192 tokens, full causal
+// attention, bf16: 0.48 ms, 1150 TFLOP/s.  Bound by the operands' reads from shared memory and the chain around them: a step takes about
+// 1950 cycles, of which the operands (48 KB per S of 64 keys, 16 KB per P.V, 32 KB written) need 1250 and the exponentials 1024 on each
+// quarter of the SM; with the exponentials left out it took 1600.  A part of the exponentials on the FMA
 // pipe (a quarter of them by a polynomial) gained nothing at this register split: 473 against 482 us for the 8192 tokens.
 // Items of few steps pay for their ends: 8192 tokens with window 1024 (18 steps an item) run at 850 TFLOP/s, with window 256 at 485.
 #include <cuda.h>
@@ -434,7 +440,7 @@ __device__ __noinline__ void slow_row(const UmmaParams &u, int id, int qi, int h
 }
 
 // Note rows of a softmax warp that have to be computed again, and do them.  (Calls, as inlined they cost the loop over the steps
-// 3 %: 534 against 518 us for 8192 tokens, full causal attention.)
+// 3 %: 534 against 518 us for 8192 tokens, full causal attention, with their append.)
 __device__ __noinline__ void note_again(Bars *bars, int warp, int id, unsigned rows) {
     if ((threadIdx.x & 31) == 0) {
         const int n = bars->again_count[warp];
