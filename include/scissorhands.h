@@ -475,6 +475,90 @@ int sh_window_decode(const sh_window *w, int sequences, const sh_rows *q, const 
  */
 int sh_window_status(void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Shared contexts and the cache with accumulated weights.  The rules of the window calls above hold here too: no handle, tensors in,
+ * tensors out, 16-byte addresses and strides, safe in a CUDA graph.
+ *
+ * The cache with accumulated weights keeps the rows that have received most attention: every slot has a mass, the sum of the weights that
+ * the tokens so far have given it (over the query heads that share the key head), and the position of its token.  Slots [0, lengths[i])
+ * of a (sequence, key head) are live, in no particular order; every token sees all of them.  All key heads of a sequence hold the same
+ * number of rows, each its own.  A batch's tokens may share a prefix besides: it is attended to as a context, for all tokens at once, and the calls
+ * below continue from that result (`prior`): the softmax, and with it every weight, then goes over both.
+ */
+
+/* Shape of the attention; query head h reads key head h / (q_heads / kv_heads). */
+typedef struct {
+    int dtype;            /* SH_F32, SH_F16 or SH_BF16: q, k, v, caches and outputs alike */
+    int head_dim;         /* 64 or 128 */
+    int q_heads, kv_heads;
+    int slots;            /* rows of a cache, or of a context: 1 .. 2^30 - 1 */
+    double scale;         /* of the logits, 1e-30 to 1e30; 0: 1/sqrt(head_dim) */
+} sh_attention;
+
+/* Records of a cache: entry (sequence, head, slot) is at sequence * sequence_stride + head * head_stride + slot, for both. */
+typedef struct {
+    float *mass;
+    int32_t *positions;
+    long long sequence_stride, head_stride;
+} sh_records;
+
+/*
+ * Attention to contexts that are complete: a prefix that a batch has in common, a sequence's encoder states.  The tokens
+ * starts[i] .. starts[i+1] - 1 see the rows [0, lengths[i]) of context i, all of them.  starts_dev: int32 [contexts + 1], or NULL: one context that
+ * all tokens share, or (contexts == tokens) one of its own for each token.  lengths_dev: int32 [contexts], or NULL: `slots` rows each;
+ * lengths outside of 0 .. slots are clamped.  Outputs: out, and lse_dev [tokens][q_heads], the natural logs of the sums of exponentials.  A
+ * context of length 0 gives zeros and -infinity; rows that belong to no context are left as they were.  starts that decrease or leave 0 .. tokens are clamped, outputs are then meaningless.
+ * 16-bit types: the weights are rounded once to the type (one token of each context: held in two parts).
+ * workspace_dev: sh_context_attention_workspace_bytes(a, tokens, contexts, starts_dev != NULL) bytes of device memory, 16-byte aligned, or NULL; used
+ * as sh_window_prefill's.
+ * Errors: SH_EINVAL, SH_ENOMEM (workspace too small), SH_ECUDA; bounded waits as in sh_window_status.
+ */
+size_t sh_context_attention_workspace_bytes(const sh_attention *a, int tokens, int contexts, int with_starts);
+int sh_context_attention(const sh_attention *a, int tokens, int contexts, const sh_rows *q, const sh_window_cache *context, const int32_t *starts_dev,
+                         const int32_t *lengths_dev, const sh_rows *out, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * Prompt chunks: the tokens starts[i] .. starts[i+1] - 1 continue sequence i, which holds lengths[i] rows and has seen seen[i] tokens.  They are
+ * stored in the slots from lengths[i] on (positions from seen[i] on); each sees the live slots and the chunk up to itself, and every
+ * slot's mass grows by the weights it gets from them (new slots start at 0).  The caller advances lengths and seen.  A sequence of
+ * negative length is idle, and one whose chunk has no room (lengths[i] + tokens > slots) takes no part either: nothing of it is read or written.
+ * prior, prior_lse_dev [tokens][q_heads]: what the tokens have seen elsewhere (out and lse of sh_context_attention), or both NULL.
+ * The rows are rounded to the type before a prior joins them, and once more after.
+ * workspace_dev: sh_mass_prefill_workspace_bytes(a, tokens, sequences) bytes of device memory, 16-byte aligned; in use until `stream` has passed
+ * the call, so calls that may run at once need one each.
+ * Errors: SH_EINVAL, SH_ENOMEM, SH_ECUDA (a call that fails midway may have stored the chunk); bounded waits as in sh_window_status.
+ */
+size_t sh_mass_prefill_workspace_bytes(const sh_attention *a, int tokens, int sequences);
+int sh_mass_prefill(const sh_attention *a, int tokens, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *starts_dev,
+                    const int32_t *lengths_dev, const int32_t *seen_dev, const sh_window_cache *cache, const sh_records *rec, const sh_rows *prior,
+                    const float *prior_lse_dev, const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * One token per sequence, as above: token i goes to slot lengths[i] of sequence i with position seen[i].  A sequence of negative length, or
+ * whose cache is full (lengths[i] >= slots), takes no part.
+ * workspace_dev: sh_mass_decode_workspace_bytes(a, sequences) bytes, 16-byte aligned; used as sh_mass_prefill's.
+ */
+size_t sh_mass_decode_workspace_bytes(const sh_attention *a, int sequences);
+int sh_mass_decode(const sh_attention *a, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *lengths_dev,
+                   const int32_t *seen_dev, const sh_window_cache *cache, const sh_records *rec, const sh_rows *prior, const float *prior_lse_dev,
+                   const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * Eviction: every (sequence, key head) with more than `keep` live rows keeps `keep` of them: first those whose position lies within the `recent`
+ * newest ones (positions > the largest - recent), then those with the largest mass; among equal ones the lowest slots.  (A mass that is NaN
+ * counts as larger than every number.)  In place (into, into_rec NULL): the rows that stay below slot `keep` do not move, and the others
+ * move, in the order of their slots, into the holes, in theirs; slots from `keep` on are left as they were.  Into another cache of
+ * into_slots >= keep slots, which must not overlap the first: the rows that stay go, in the order of their slots, to its slots from 0 on, all live
+ * rows of a sequence that has no more than `keep`; its other slots are left as they were.
+ * left_dev [sequences]: the new lengths, min(lengths[i], keep); may be lengths_dev itself.  1 <= keep <= slots, 0 <= recent <= keep.
+ * workspace_dev: sh_mass_evict_workspace_bytes(a, sequences, keep, into == NULL) bytes, 16-byte aligned; used as sh_mass_prefill's.
+ * Errors: SH_EINVAL, SH_ENOMEM, SH_ECUDA.
+ */
+size_t sh_mass_evict_workspace_bytes(const sh_attention *a, int sequences, int keep, int in_place);
+int sh_mass_evict(const sh_attention *a, int sequences, const int32_t *lengths_dev, const sh_window_cache *cache, const sh_records *rec, int keep, int recent,
+                  const sh_window_cache *into, const sh_records *into_rec, int into_slots, int32_t *left_dev, void *workspace_dev, size_t workspace_bytes,
+                  void *stream);
+
 /* Text for a status code; never NULL. */
 const char *sh_strerror(int status);
 

@@ -35,7 +35,9 @@ EXPORTS = ["sh_create", "sh_destroy", "sh_workspace_bytes", "sh_bind", "sh_set_o
            "sh_compress", "sh_compress_static", "sh_scores", "sh_select", "sh_state", "sh_export_unit",
            "sh_restore", "sh_launch_count", "sh_decode_kernel_choice", "sh_import_compressed", "sh_prefill_bulk",
            "sh_prefill_bulk_scratch_bytes", "sh_strerror", "sh_last_cuda_error",
-           "sh_qk_norm_rope", "sh_window_prefill", "sh_window_append", "sh_window_decode", "sh_window_decode_workspace_bytes", "sh_window_prefill_workspace_bytes", "sh_window_status"]
+           "sh_qk_norm_rope", "sh_window_prefill", "sh_window_append", "sh_window_decode", "sh_window_decode_workspace_bytes", "sh_window_prefill_workspace_bytes", "sh_window_status",
+           "sh_context_attention", "sh_context_attention_workspace_bytes", "sh_mass_prefill", "sh_mass_prefill_workspace_bytes", "sh_mass_decode",
+           "sh_mass_decode_workspace_bytes", "sh_mass_evict", "sh_mass_evict_workspace_bytes"]
 
 
 class _Rows(C.Structure):
@@ -56,6 +58,14 @@ class _Rope(C.Structure):
     _fields_ = [("dtype", C.c_int), ("head_dim", C.c_int), ("rot_dim", C.c_int), ("axes", C.c_int), ("sections", C.c_int * 3),
                 ("spread", C.c_int), ("adjacent_pairs", C.c_int), ("eps", C.c_float), ("inv_freq_dev", C.c_void_p),
                 ("q_weight_dev", C.c_void_p), ("k_weight_dev", C.c_void_p)]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("head_dim", C.c_int), ("q_heads", C.c_int), ("kv_heads", C.c_int), ("slots", C.c_int), ("scale", C.c_double)]
+
+
+class _Records(C.Structure):
+    _fields_ = [("mass", C.c_void_p), ("positions", C.c_void_p), ("sequence_stride", C.c_longlong), ("head_stride", C.c_longlong)]
 
 
 def _load() -> C.CDLL:
@@ -116,6 +126,18 @@ def declare(lib: C.CDLL) -> C.CDLL:
     lib.sh_window_decode.argtypes = [window, C.c_int, rows, rows, rows, vp, cache, rope, vp, C.c_longlong, rows, vp, C.c_size_t, vp]
     lib.sh_window_decode_workspace_bytes.argtypes = [window, C.c_int]
     lib.sh_window_decode_workspace_bytes.restype = C.c_size_t
+    attention = records = vp
+    lib.sh_context_attention.argtypes = [attention, C.c_int, C.c_int, rows, cache, vp, vp, rows, vp, vp, C.c_size_t, vp]
+    lib.sh_context_attention_workspace_bytes.argtypes = [attention, C.c_int, C.c_int, C.c_int]
+    lib.sh_mass_prefill.argtypes = [attention, C.c_int, C.c_int, rows, rows, rows, vp, vp, vp, cache, records, rows, vp, rows, vp, C.c_size_t, vp]
+    lib.sh_mass_prefill_workspace_bytes.argtypes = [attention, C.c_int, C.c_int]
+    lib.sh_mass_decode.argtypes = [attention, C.c_int, rows, rows, rows, vp, vp, cache, records, rows, vp, rows, vp, C.c_size_t, vp]
+    lib.sh_mass_decode_workspace_bytes.argtypes = [attention, C.c_int]
+    lib.sh_mass_evict.argtypes = [attention, C.c_int, vp, cache, records, C.c_int, C.c_int, cache, records, C.c_int, vp, vp, C.c_size_t, vp]
+    lib.sh_mass_evict_workspace_bytes.argtypes = [attention, C.c_int, C.c_int, C.c_int]
+    for fn in (lib.sh_context_attention_workspace_bytes, lib.sh_mass_prefill_workspace_bytes, lib.sh_mass_decode_workspace_bytes,
+               lib.sh_mass_evict_workspace_bytes):
+        fn.restype = C.c_size_t
     return lib
 
 
@@ -711,3 +733,173 @@ class WindowCache:
                             scale=self.scale, out=out)
         self.lengths += (self.lengths >= 0).to(torch.int32)
         return out
+
+
+# -- shared contexts and the cache with accumulated weights ------------------------------------------------------------
+_pack_attention, _pack_records = struct.Struct("iiiiid").pack, struct.Struct("PPqq").pack
+
+
+def _attention_packed(dtype, d: int, q_heads: int, kv_heads: int, slots: int, scale: Optional[float]) -> bytes:
+    if kv_heads < 1 or q_heads < 1 or q_heads % kv_heads:
+        raise ValueError(f"{q_heads} query heads, {kv_heads} key heads: the first must be a multiple of the second")
+    if not 1 <= slots < 1 << 30:
+        raise ValueError(f"{slots} rows: need 1 .. 2^30 - 1")
+    if scale is not None and not (1e-30 < scale < 1e30):
+        raise ValueError(f"scale {scale}: need a number between 1e-30 and 1e30")
+    return _pack_attention(_CODE_OF[dtype], d, q_heads, kv_heads, slots, 0.0 if scale is None else scale)
+
+
+def _slots_of(k_cache, what: str, n: Optional[int], kv_heads: Optional[int], d: Optional[int], dtype, device: int):
+    """Shape of a cache [sequences, key heads, slots, head_dim] whose other sizes are given (None: free)."""
+    if isinstance(k_cache, torch.Tensor) and k_cache.dim() == 4:
+        s = k_cache.shape
+        if (n is None or s[0] == n) and (kv_heads is None or s[1] == kv_heads) and (s[3] == d if d is not None else s[3] in (64, 128)):
+            return s
+    _fail(what, f"[{n or 'sequences'}, {kv_heads or 'key heads'}, slots, {d or '64 or 128'}] of {dtype} on cuda:{device}", k_cache)
+
+
+def _records_packed(mass, positions, shape, device: int) -> bytes:
+    for t, what, dt in ((mass, "mass", torch.float32), (positions, "positions", torch.int32)):
+        if not (isinstance(t, torch.Tensor) and t.dtype is dt and t.get_device() == device and t.shape == shape and (shape[2] <= 1 or t.stride(2) == 1)):
+            _fail(what, f"[sequences, key heads, slots] = {tuple(shape)} of {dt} on cuda:{device}, contiguous along its last dimension", t)
+    ms, ps = mass.stride(), positions.stride()
+    if any(ms[i] != ps[i] for i in range(2) if shape[i] > 1):
+        _fail("positions", f"the strides of mass, {ms}", positions)
+    return _pack_records(mass.data_ptr(), positions.data_ptr(), ms[0], ms[1])
+
+
+def _prior_packed(prior, shape, dtype, device: int):
+    if prior is None:
+        return None, None
+    if not (isinstance(prior, (tuple, list)) and len(prior) == 2):
+        _fail("prior", "a pair (out, lse)", prior)
+    rows = _more_rows(prior[0], "prior", shape, dtype, device)
+    return rows, _logs(prior[1], "prior's lse", shape, device)
+
+
+def _logs(t, what: str, shape, device: int) -> int:
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.float32 and t.get_device() == device and t.shape == shape[:2] and t.is_contiguous()):
+        _fail(what, f"a contiguous fp32 tensor {tuple(shape[:2])} on cuda:{device}", t)
+    return t.data_ptr()
+
+
+def context_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None,
+                      lengths: Optional[torch.Tensor] = None, *, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """``sh_context_attention``: attention to contexts that are complete: a prefix that a whole batch shares, or each sequence's encoder states
+    (cross attention).
+
+    ``q`` [tokens, q_heads, head_dim], ``k``/``v`` [contexts, kv_heads, rows, head_dim].  The tokens ``starts[i] .. starts[i+1] - 1`` (int32, on the
+    device) see the first ``lengths[i]`` rows of context i (None: all), all of them.  ``starts`` None: one context that all tokens share, or
+    one for each token.  Returns ``out`` and ``lse`` fp32 [tokens, q_heads], the logs of the rows' sums of exponentials, from which
+    ``mass_decode`` and ``mass_prefill`` continue (``prior``).  A context of length 0 gives zeros and -inf; rows that belong to no
+    context are left as they were (new tensors: zeros and -inf)."""
+    shape, dtype, device, qr = _head_rows(q, "q")
+    tokens, q_heads, d = shape
+    kshape = _slots_of(k, "k", None, None, d, dtype, device)
+    n, kv_heads, rows = kshape[0], kshape[1], kshape[2]
+    at = _attention_packed(dtype, d, q_heads, kv_heads, rows, scale)
+    cache = _cache_packed(k, v, kshape, dtype, device)
+    sp = None
+    if starts is not None:
+        sp = _ints(starts, "starts", n + 1, device)
+    elif n != 1 and n != tokens:
+        raise ValueError(f"{n} contexts for {tokens} tokens: without starts there must be one, or one for each token")
+    lp = None if lengths is None else _ints(lengths, "lengths", n, device)
+    out = _new(q, shape, stream, sp is not None) if out is None else out
+    outr = _more_rows(out, "out", shape, dtype, device)
+    if lse is None:
+        lse = _new(q, shape[:2], stream, False, torch.float32)
+        if sp is not None:
+            with torch.cuda.stream(stream):
+                lse.fill_(float("-inf"))
+    wp, bytes_ = None, lib.sh_context_attention_workspace_bytes(at, tokens, n, sp is not None)
+    if bytes_:
+        work = _new(q, bytes_, stream, False, torch.uint8)
+        wp = work.data_ptr()
+    _launch("context_attention", lib.sh_context_attention, device, stream, at, tokens, n, qr, cache, sp, lp, outr, _logs(lse, "lse", shape, device), wp, bytes_)
+    return out, lse
+
+
+def mass_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, k_cache: torch.Tensor,
+                 v_cache: torch.Tensor, mass: torch.Tensor, positions: torch.Tensor, seen: torch.Tensor, *, prior=None,
+                 scale: Optional[float] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``sh_mass_prefill``: prompt chunks over a cache with accumulated weights.
+
+    ``q`` [tokens, q_heads, head_dim], ``k``/``v`` [tokens, kv_heads, head_dim]; the tokens ``starts[i] .. starts[i+1] - 1`` are stored in the slots of
+    ``k_cache``/``v_cache`` [sequences, kv_heads, slots, head_dim] from ``lengths[i]`` on, with positions from ``seen[i]`` on (the caller advances both);
+    each sees the live slots and the chunk up to itself, and ``mass`` fp32 [sequences, kv_heads, slots] grows by the weights that the rows get.
+    ``prior``: (out, lse) of ``context_attention`` for the same tokens; the softmax goes over both.  A sequence of negative length, or
+    whose chunk has no room, takes no part; its rows of ``out``, and those of no sequence, are left as they were (a new ``out`` is
+    zeroed)."""
+    shape, dtype, device, qr = _head_rows(q, "q")
+    tokens, q_heads, d = shape
+    kshape, kr = _key_rows(k, "k", tokens, d, dtype, device)
+    vr = _more_rows(v, "v", kshape, dtype, device)
+    n = _sequences(starts)
+    cshape = _slots_of(k_cache, "k_cache", n, kshape[1], d, dtype, device)
+    at = _attention_packed(dtype, d, q_heads, kshape[1], cshape[2], scale)
+    cache, rec = _cache_packed(k_cache, v_cache, cshape, dtype, device), _records_packed(mass, positions, cshape[:3], device)
+    pr, pl = _prior_packed(prior, shape, dtype, device)
+    out = _new(q, shape, stream, True) if out is None else out
+    outr = _more_rows(out, "out", shape, dtype, device)
+    bytes_ = lib.sh_mass_prefill_workspace_bytes(at, tokens, n)
+    work = _new(q, bytes_, stream, False, torch.uint8)
+    _launch("mass_prefill", lib.sh_mass_prefill, device, stream, at, tokens, n, qr, kr, vr, _ints(starts, "starts", n + 1, device),
+            _ints(lengths, "lengths", n, device), _ints(seen, "seen", n, device), cache, rec, pr, pl, outr, work.data_ptr(), bytes_)
+    return out
+
+
+def mass_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                mass: torch.Tensor, positions: torch.Tensor, seen: torch.Tensor, *, prior=None, scale: Optional[float] = None,
+                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``sh_mass_decode``: one token per sequence over a cache with accumulated weights (arguments as ``mass_prefill``, ``q`` [sequences, q_heads,
+    head_dim]): stored in slot ``lengths[i]``, attends over the live slots and itself, and the masses grow by its weights.  A sequence of
+    negative length, or whose cache is full, takes no part."""
+    shape, dtype, device, qr = _head_rows(q, "q")
+    n, q_heads, d = shape
+    kshape, kr = _key_rows(k, "k", n, d, dtype, device)
+    vr = _more_rows(v, "v", kshape, dtype, device)
+    cshape = _slots_of(k_cache, "k_cache", n, kshape[1], d, dtype, device)
+    at = _attention_packed(dtype, d, q_heads, kshape[1], cshape[2], scale)
+    cache, rec = _cache_packed(k_cache, v_cache, cshape, dtype, device), _records_packed(mass, positions, cshape[:3], device)
+    pr, pl = _prior_packed(prior, shape, dtype, device)
+    out = _new(q, shape, stream, True) if out is None else out
+    outr = _more_rows(out, "out", shape, dtype, device)
+    bytes_ = lib.sh_mass_decode_workspace_bytes(at, n)
+    work = _new(q, bytes_, stream, False, torch.uint8)
+    _launch("mass_decode", lib.sh_mass_decode, device, stream, at, n, qr, kr, vr, _ints(lengths, "lengths", n, device),
+            _ints(seen, "seen", n, device), cache, rec, pr, pl, outr, work.data_ptr(), bytes_)
+    return out
+
+
+def mass_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, mass: torch.Tensor, positions: torch.Tensor, lengths: torch.Tensor, *, keep: int,
+               recent: int = 0, into=None, left: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``sh_mass_evict``: every (sequence, key head) with more than ``keep`` live rows keeps that many: the ``recent`` newest positions, then the
+    largest masses, among equal ones the lowest slots.
+
+    In place, or ``into`` = (k_cache, v_cache, mass, positions) of a cache with at least ``keep`` slots, which must not overlap the first.  Returns
+    the new lengths, ``min(lengths, keep)`` (``left``: where to put them; may be ``lengths``)."""
+    if not (isinstance(k_cache, torch.Tensor) and k_cache.dtype in _CODE_OF and k_cache.is_cuda):
+        _fail("k_cache", "a CUDA tensor [sequences, key heads, slots, 64 or 128] of f32, f16 or bf16", k_cache)
+    dtype, device = k_cache.dtype, k_cache.get_device()
+    shape = _slots_of(k_cache, "k_cache", None, None, None, dtype, device)
+    n, heads, slots, d = shape
+    room = slots
+    cache, rec, to, to_rec = _cache_packed(k_cache, v_cache, shape, dtype, device), _records_packed(mass, positions, shape[:3], device), None, None
+    if into is not None:
+        if not (isinstance(into, (tuple, list)) and len(into) == 4):
+            _fail("into", "(k_cache, v_cache, mass, positions)", into)
+        tshape = _slots_of(into[0], "into", n, heads, d, dtype, device)
+        room = tshape[2]
+        to, to_rec = _cache_packed(into[0], into[1], tshape, dtype, device), _records_packed(into[2], into[3], tshape[:3], device)
+    if not (1 <= keep <= room and 0 <= recent <= keep):
+        raise ValueError(f"keep {keep}, recent {recent}: need 1 <= keep <= {room} slots and 0 <= recent <= keep")
+    at = _attention_packed(dtype, d, heads, heads, slots, None)
+    lp = _ints(lengths, "lengths", n, device)
+    left = _new(lengths, lengths.shape, stream, False) if left is None else left
+    bytes_ = lib.sh_mass_evict_workspace_bytes(at, n, keep, into is None)
+    work = _new(k_cache, bytes_, stream, False, torch.uint8)
+    _launch("mass_evict", lib.sh_mass_evict, device, stream, at, n, lp, cache, rec, keep, recent, to, to_rec, room, _ints(left, "left", n, device),
+            work.data_ptr(), bytes_)
+    return left

@@ -8,13 +8,16 @@ constexpr int MAX_POS = 1 << 30;
 
 // The rows [first, first + count) of the chunk tensors that belong to sequence i (starts that decrease or leave the tensor are
 // clamped), and the tokens its cache holds.  An idle sequence (negative length) has no rows.
+// MODE: what is attended to (sh_window.h).  Contexts without starts: all tokens share the one there is, or each has its own.
+template <int MODE = ATTEND_WINDOW>
 __device__ __forceinline__ void sequence_rows(const WindowParams &p, int i, int &first, int &count, int &cached) {
-    const int a = min(max(p.starts[i], 0), p.tokens);
-    const int b = min(max(p.starts[i + 1], a), p.tokens);
-    cached = p.lengths ? p.lengths[i] : 0;
+    const int a = MODE == ATTEND_CONTEXT && !p.starts ? (p.sequences == 1 ? 0 : i) : min(max(p.starts[i], 0), p.tokens);
+    const int b = MODE == ATTEND_CONTEXT && !p.starts ? (p.sequences == 1 ? p.tokens : i + 1) : min(max(p.starts[i + 1], a), p.tokens);
+    cached = p.lengths ? p.lengths[i] : (MODE == ATTEND_CONTEXT ? p.slots : 0);
     first = a;
-    count = cached < 0 ? 0 : b - a;
-    cached = min(max(cached, 0), MAX_POS);
+    count = MODE != ATTEND_CONTEXT && cached < 0 ? 0 : b - a;
+    cached = min(max(cached, 0), MODE == ATTEND_CONTEXT ? p.slots : MAX_POS);
+    if (MODE == ATTEND_MASS && count > p.fit - cached) count = 0;
 }
 
 struct Tile {
@@ -26,13 +29,14 @@ struct Tile {
 
 // The tile-th block of `bm` rows over all sequences.  A row is (token, query head of the group), heads innermost: the heads that
 // share a key head sit in one tile and a tile spans few tokens, so few keys.  One warp, all lanes.
+template <int MODE = ATTEND_WINDOW>
 __device__ __forceinline__ Tile find_tile(const WindowParams &p, long long tile, int bm) {
     const int lane = threadIdx.x & 31;
     Tile r = {-1, 0, 0, 0, 0};
     long long before = 0;
     for (int base = 0; base < p.sequences; base += 32) {
         int first = 0, count = 0, cached = 0;
-        if (base + lane < p.sequences) sequence_rows(p, base + lane, first, count, cached);
+        if (base + lane < p.sequences) sequence_rows<MODE>(p, base + lane, first, count, cached);
         const long long mine = ((long long)count * p.g + bm - 1) / bm;
         long long upto = mine;
 #pragma unroll
@@ -53,6 +57,19 @@ __device__ __forceinline__ Tile find_tile(const WindowParams &p, long long tile,
         before += __shfl_sync(0xffffffffu, upto, 31);
     }
     return r;
+}
+
+// Does token `tok` belong to a sequence?  Found by bisection of `starts`; its number and rows come back.
+template <int MODE = ATTEND_WINDOW>
+__device__ __forceinline__ bool sequence_of(const WindowParams &p, long long tok, int &seq, int &first, int &count, int &cached) {
+    int lo = 0, hi = p.sequences;      // the last sequence that starts at or before tok (empty ones before it are passed over)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p.starts[mid] <= tok) lo = mid; else hi = mid;
+    }
+    seq = lo;
+    sequence_rows<MODE>(p, lo, first, count, cached);
+    return tok >= first && tok < (long long)first + count;
 }
 
 // Slot of position p.

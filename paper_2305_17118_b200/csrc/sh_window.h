@@ -38,7 +38,23 @@ struct WindowParams {
     RopeParams rope;              // decode only: how the step's q and k are prepared
     bool with_rope;
     float *part;                  // scratch of sh_window_decode_scratch or sh_window_prefill_scratch bytes, or NULL
+    // what only the shared contexts and the cache with accumulated weights use
+    int slots;                    // slots of a cache (the window calls: window + sinks)
+    int fit;                      // > 0: a sequence whose chunk leaves `fit` slots takes no part
+    float *lse;                   // [tokens][hq]: log of each row's sum of exponentials, or NULL
+    WinRows prior;                // rows to continue from, with prior_lse [tokens][hq], or NULL
+    const float *prior_lse;
+    float *scores, *total;        // single tokens: [sequences][hq][score_stride] logits, [sequences][hq] logs of their sums (base 2)
+    long long score_stride;
+    const int32_t *seen;          // [sequences]: position of a sequence's next token
+    float *mass;                  // [sequences][hk][slots] with the strides below, in elements; positions alike
+    int32_t *held;
+    long long rss, rhs;
 };
+
+// What a kernel attends to and leaves: the window's calls; the same over a cache with accumulated weights (every live slot is in sight,
+// the logs of the rows' sums are kept); a context that all its tokens see in full.
+enum { ATTEND_WINDOW = 0, ATTEND_MASS = 1, ATTEND_CONTEXT = 2 };
 
 // SMs of the current device, and that a kernel may use `smem` bytes of shared memory there.  Both are facts of the device, asked once
 // (two threads that come first together both ask, and write the same).
@@ -58,12 +74,12 @@ cudaError_t sh_setup_kernel(ShKernelSetup &setup, K kern, size_t smem, int *sms)
 }
 
 cudaError_t sh_launch_qk_norm_rope(RopeParams p, int dtype, int D, cudaStream_t s);
-cudaError_t sh_launch_window_prefill_f32(const WindowParams &p, int D, cudaStream_t s);
+cudaError_t sh_launch_window_prefill_f32(const WindowParams &p, int D, int mode, cudaStream_t s);
 // tensor cores: f16 and bf16
-cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int D, cudaStream_t s);
+cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int D, int mode, cudaStream_t s);
 size_t sh_window_prefill_scratch(int tokens, int sequences, int hk, int g, int window, int sinks, bool with_cache, int dtype, int D);
 // code of the first bounded wait that gave up in a window kernel of the current device since the last call (0: none); synchronises
 cudaError_t sh_window_error_take(int *code, cudaStream_t s);
-cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, cudaStream_t s);
+cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, int mode, cudaStream_t s);      // (ATTEND_MASS: and the new rows' records)
 size_t sh_window_decode_scratch(int sequences, int hk, int g, int dtype, int D);
-cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, cudaStream_t s);
+cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, int mode, cudaStream_t s);

@@ -32,13 +32,14 @@ constexpr int WARPS = 8, NT = WARPS * 32;
 constexpr int R = 2;                 // rows in flight per group of eight lanes
 constexpr int BLOCK = 4 * R;         // rows of a warp per pass
 
-// q rows (fp32) and the new token's key and value (as the cache holds them) into shared memory, prepared by `rope` if there is one.
-template <typename T, int D, int WARPS, bool ADJ>
+// q rows (fp32) and (KV) the new token's key and value (as the cache holds them) into shared memory, prepared by `rope` if there is one.
+template <typename T, int D, int WARPS, bool KV, bool ADJ>
 __device__ __forceinline__ void stage_rows(const WindowParams &p, int seq, int kvh, int h0, int nq, float qscale, float *qs, float *ks, float *vs) {
     constexpr int LPR = D / 16, ROWS = 32 / LPR;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pl = lane % LPR, sub = lane / LPR;
     // rows: the nq queries, the key, the value
-    if (warp * ROWS >= nq + 2) return;
+    const int rows = KV ? nq + 2 : nq;
+    if (warp * ROWS >= rows) return;
     shrope::Turns<ADJ> turn;
     int e0 = 16 * pl, e1 = 16 * pl + 8;
     if (p.with_rope) {
@@ -47,9 +48,9 @@ __device__ __forceinline__ void stage_rows(const WindowParams &p, int seq, int k
         shrope::turns_of_lane<D>(p.rope, seq, lane, c, s);
         turn.set(c, s);
     }
-    for (int base = warp * ROWS; base < nq + 2; base += WARPS * ROWS) {
+    for (int base = warp * ROWS; base < rows; base += WARPS * ROWS) {
         const int row = base + sub;
-        const bool is_q = row < nq, is_k = row == nq, live = row < nq + 2;
+        const bool is_q = row < nq, is_k = row == nq, live = row < rows;
         const char *src = is_q ? p.q.p + seq * p.q.ts + (h0 + row) * p.q.hs
                                : (is_k ? p.k.p + seq * p.k.ts + kvh * p.k.hs : p.v.p + seq * p.v.ts + kvh * p.v.hs);
         shrope::Raw<T> raw = {};
@@ -87,13 +88,48 @@ __device__ __forceinline__ void stage_rows(const WindowParams &p, int seq, int k
         }
     }
 }
-template <typename T, int D, int WARPS>
+template <typename T, int D, int WARPS, int MODE>
 __device__ __forceinline__ void stage_token(const WindowParams &p, int seq, int kvh, int h0, int nq, float qscale, float *qs, float *ks, float *vs) {
-    if (p.with_rope && p.rope.adjacent) stage_rows<T, D, WARPS, true>(p, seq, kvh, h0, nq, qscale, qs, ks, vs);
-    else stage_rows<T, D, WARPS, false>(p, seq, kvh, h0, nq, qscale, qs, ks, vs);
+    if (MODE == ATTEND_WINDOW && p.with_rope && p.rope.adjacent) stage_rows<T, D, WARPS, true, true>(p, seq, kvh, h0, nq, qscale, qs, ks, vs);
+    else stage_rows<T, D, WARPS, MODE != ATTEND_CONTEXT, false>(p, seq, kvh, h0, nq, qscale, qs, ks, vs);
 }
 
-template <typename T, int D, int GQ>
+// Rows that a sequence holds before the step (below zero: it takes no part).
+template <int MODE>
+__device__ __forceinline__ int rows_before(const WindowParams &p, int seq) {
+    if (MODE == ATTEND_CONTEXT) return p.lengths ? min(max(p.lengths[seq], 0), p.slots) : p.slots;
+    const int t = min(p.lengths[seq], MAX_POS);
+    return MODE == ATTEND_MASS && t >= p.slots ? -1 : t;      // (a full cache has no place for the token)
+}
+
+// The last step for N elements of a row, from d on: `base` + log2(L) is the log of its sum, x its unnormalised output.  Over a cache with
+// accumulated weights the row continues from the prior's, if there is one, and leaves that log; a context's goes to the caller.
+template <typename T, int MODE, int N>
+__device__ __forceinline__ void close_row(const WindowParams &p, int seq, int h, int d, float base, float L, bool empty, float (&x)[N]) {
+    const long long at = (long long)seq * p.hq + h;
+    if (MODE == ATTEND_MASS && p.prior_lse) {
+        const float pl = p.prior_lse[at] * 1.4426950408889634f;
+        if (pl != -CUDART_INF_F) {                                  // (nothing was seen there: its row does not matter)
+            const float top = fmaxf(base, pl), f = ex2_approx(base - top), g = ex2_approx(pl - top);
+            const char *row = p.prior.p + seq * p.prior.ts + h * p.prior.hs + d * (int)sizeof(T);
+            L = fmaf(L, f, g);
+#pragma unroll
+            for (int i = 0; i < N; i += Vec<T>::N) {
+                float y[Vec<T>::N];
+                Vec<T>::unpack(*reinterpret_cast<const uint4 *>(row + i * (int)sizeof(T)), y);
+#pragma unroll
+                for (int e = 0; e < Vec<T>::N; ++e) x[i + e] = fmaf(y[e], g, x[i + e] * f);
+            }
+            base = top;
+        }
+    }
+    if (MODE == ATTEND_MASS && d == 0) p.total[at] = base + log2f(L);
+    if (MODE == ATTEND_CONTEXT && d == 0) p.lse[at] = empty ? -CUDART_INF_F : 0.69314718055994531f * (base + log2f(L));
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = MODE == ATTEND_CONTEXT && empty ? 0.f : x[e] / L;
+}
+
+template <typename T, int D, int GQ, int MODE>
 __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowParams p, int qblocks, int) {
     constexpr int N = Vec<T>::N, CH = D / N / 8, EL = CH * N;      // 16-byte pieces and elements of a row per lane
     __shared__ __align__(16) float qs[GQ * D], ks[D], vs[D];
@@ -104,13 +140,13 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, l8 = lane & 7, grp = lane >> 3;
     const long long unit = blockIdx.x / S;
     const int qb = (int)(unit % qblocks), kvh = (int)(unit / qblocks % p.hk), seq = (int)(unit / qblocks / p.hk);
-    const int t = min(p.lengths[seq], MAX_POS);
+    const int t = rows_before<MODE>(p, seq);
     if (t < 0) return;                                              // idle: the whole cluster leaves
     const int h0 = kvh * p.g + qb * GQ, nq = min(GQ, p.g - qb * GQ);
-    const int live = min(t, p.sinks + p.window), snew = slot_of(t, p.sinks, p.window);
+    const int live = min(t, p.sinks + p.window), snew = MODE == ATTEND_CONTEXT ? -1 : slot_of(t, p.sinks, p.window);
     for (int i = tid; i < GQ * D; i += NT) qs[i] = 0.f;
     __syncthreads();
-    stage_token<T, D, WARPS>(p, seq, kvh, h0, nq, p.scale_log2e, qs, ks, vs);
+    stage_token<T, D, WARPS, MODE>(p, seq, kvh, h0, nq, p.scale_log2e, qs, ks, vs);
     __syncthreads();
 
     float m[GQ], l[GQ], o[GQ][EL];
@@ -120,8 +156,8 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
 #pragma unroll
         for (int e = 0; e < EL; ++e) o[q][e] = 0.f;
     }
-    // fold R rows (k, v: this lane's elements; valid: the group's row is to be used) into the running state
-    auto fold = [&](const float (&k)[R][EL], const float (&v)[R][EL], const bool (&valid)[R]) {
+    // fold R rows (k, v: this lane's elements; valid: the group's row, slot first + 4 r, is to be used) into the running state
+    auto fold = [&](const float (&k)[R][EL], const float (&v)[R][EL], const bool (&valid)[R], int first) {
 #pragma unroll
         for (int q = 0; q < GQ; ++q) {
             float s[R];
@@ -142,6 +178,7 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
                 s[r] += __shfl_xor_sync(0xffffffffu, s[r], 2);
                 s[r] += __shfl_xor_sync(0xffffffffu, s[r], 4);
                 if (valid[r]) mn = fmaxf(mn, s[r]);
+                if (MODE == ATTEND_MASS && valid[r] && l8 == 0 && q < nq) p.scores[((long long)seq * p.hq + h0 + q) * p.score_stride + first + 4 * r] = s[r];
             }
             const float base = mn == -CUDART_INF_F ? 0.f : mn, keep = ex2_approx(m[q] - base);
             m[q] = mn;
@@ -186,9 +223,9 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
                 Vec<T>::unpack(kr[r][c], k[r] + c * N);
                 Vec<T>::unpack(vr[r][c], v[r] + c * N);
             }
-        fold(k, v, valid);
+        fold(k, v, valid, base + grp);
     }
-    if (rank == 0 && warp == 0) {      // the new token: one group counts it, and the first query block stores it
+    if (MODE != ATTEND_CONTEXT && rank == 0 && warp == 0) {      // the new token: one group counts it, and the first query block stores it
         float k[R][EL] = {}, v[R][EL] = {};
         bool valid[R] = {};
         valid[0] = grp == 0;
@@ -199,7 +236,7 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
                 k[0][c * N + e] = ks[(c * 8 + l8) * N + e];
                 v[0][c * N + e] = valid[0] ? vs[(c * 8 + l8) * N + e] : 0.f;
             }
-        fold(k, v, valid);
+        fold(k, v, valid, snew);
         if (qb == 0 && grp == 0) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
@@ -254,8 +291,7 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
 #pragma unroll
             for (int e = 0; e < N; ++e) x[e] = fmaf(c[2 + d + e], f, x[e]);
         }
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] /= L;
+        close_row<T, MODE>(p, seq, h0 + q, d, M, L, live == 0, x);
         *reinterpret_cast<uint4 *>(p.out.p + seq * p.out.ts + (h0 + q) * p.out.hs + d * (int)sizeof(T)) = Vec<T>::pack(x);
     }
     cluster.sync();      // nobody's shared memory goes away while it is read
@@ -332,8 +368,8 @@ template <typename T> __device__ __forceinline__ void split2(float x, float y, u
 
 // One query by the D / 8 lanes that finish it: every live row once, in fp32.  x: this lane's 8 elements of the prepared query; fresh: key and
 // value rows that stand for those of slot snew (NULL: they are in the cache already).
-template <typename T, int D>
-__device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, int live, int snew, const unsigned char *fresh, const float4 x0, const float4 x1,
+template <typename T, int D, int MODE>
+__device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, int h, int live, int snew, const unsigned char *fresh, const float4 x0, const float4 x1,
                                        char *dst) {
     constexpr int CHUNKS = D / 8;
     const int c = threadIdx.x % CHUNKS;
@@ -352,18 +388,18 @@ __device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, 
 #pragma unroll
         for (int i = CHUNKS / 2; i; i >>= 1) s += __shfl_xor_sync(group, s, i);
         s *= p.scale_log2e;
+        if (MODE == ATTEND_MASS && c == 0) p.scores[((long long)seq * p.hq + h) * p.score_stride + j] = s;
         const float mn = fmaxf(m, s), b = mn == -CUDART_INF_F ? 0.f : mn, keep = ex2_approx(m - b), w = ex2_approx(s - b);
         m = mn;
         l = l * keep + w;
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = fmaf(w, v[e], o[e] * keep);
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] /= l;
+    close_row<T, MODE>(p, seq, h, c * 8, m, l, false, o);
     *reinterpret_cast<uint4 *>(dst + c * 16) = Vec<T>::pack(o);
 }
 
-template <typename T, int D, int MW>
+template <typename T, int D, int MW, int MODE>
 __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __grid_constant__ WindowParams p, int qblocks, int parts) {
     using C = Mma<D, MW>;
     constexpr int CHUNKS = D / 8;                     // 16-byte pieces of a row
@@ -375,10 +411,11 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long unit = blockIdx.x / S;
     const int qb = (int)(unit % qblocks), kvh = (int)(unit / qblocks % p.hk), seq = (int)(unit / qblocks / p.hk);
-    const int t = min(p.lengths[seq], MAX_POS);
+    const int t = rows_before<MODE>(p, seq);
     if (t < 0) return;                                // idle: the whole cluster leaves
     const int h0 = kvh * p.g + qb * MQ, nq = min(MQ, p.g - qb * MQ);
-    const int live = min(t + 1, p.sinks + p.window), snew = slot_of(t, p.sinks, p.window);      // rows after the append
+    const int live = MODE == ATTEND_CONTEXT ? t : min(t + 1, p.sinks + p.window);      // rows after the append
+    const int snew = MODE == ATTEND_CONTEXT ? -1 : slot_of(t, p.sinks, p.window);
     const char *kc = p.kc + seq * p.css + kvh * p.chs, *vc = p.vc + seq * p.css + kvh * p.chs;
     const uint32_t ring = shasync::smem_u32(sm) + warp * C::STAGES * C::STAGE;
 
@@ -404,12 +441,12 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
     }
     // the token: prepared in fp32, then queries as two 16-bit parts, key and value as the cache holds them
     float *rows = reinterpret_cast<float *>(sm + C::OFF_F32);
-    stage_token<T, D, MW>(p, seq, kvh, h0, nq, 1.f, rows, rows + MQ * D, rows + (MQ + 1) * D);
+    stage_token<T, D, MW, MODE>(p, seq, kvh, h0, nq, 1.f, rows, rows + MQ * D, rows + (MQ + 1) * D);
     __syncthreads();
     for (int i = tid; i < (MQ + 2) * CHUNKS; i += MW * 32) {
         const int r = i / CHUNKS, c = i % CHUNKS;
         uint32_t hi[4] = {}, lo[4] = {};
-        if (r < nq || r >= MQ) {
+        if (r < nq || (MODE != ATTEND_CONTEXT && r >= MQ)) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) split2<T>(rows[r * D + c * 8 + 2 * e], rows[r * D + c * 8 + 2 * e + 1], hi[e], lo[e]);
         }
@@ -472,6 +509,11 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
         for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) x[2 * n + e] = j + 8 * n + e < live ? (s[n][e] + s[n][2 + e]) * p.scale_log2e : -CUDART_INF_F;
+        if (MODE == ATTEND_MASS && (lane >> 2) < nq) {      // (a row of scores has a place for every row of the last block)
+            float *to = p.scores + ((long long)seq * p.hq + h0 + (lane >> 2)) * p.score_stride + j;
+            *reinterpret_cast<float2 *>(to) = make_float2(x[0], x[1]);
+            *reinterpret_cast<float2 *>(to + 8) = make_float2(x[2], x[3]);
+        }
         float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
@@ -557,11 +599,9 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
             for (int e = 0; e < 8; ++e) acc[e] = fmaf(c[2 + d + e], f, acc[e]);
         }
         bool odd = false;
+        close_row<T, MODE>(p, seq, h0 + q, d, M - Weights<T>::LIFT, L, live == 0, acc);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            acc[e] /= L;
-            odd |= !isfinite(acc[e]);
-        }
+        for (int e = 0; e < 8; ++e) odd |= !isfinite(acc[e]);
         char *dst = p.out.p + seq * p.out.ts + (h0 + q) * p.out.hs;
         // the low part of a weight or of a query may be zero and meet an infinity: such rows are computed again in plain fp32
         float hi[8], lo[8];
@@ -572,7 +612,7 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
         const float4 x0 = make_float4(hi[0], hi[1], hi[2], hi[3]), x1 = make_float4(hi[4], hi[5], hi[6], hi[7]);
         const unsigned group = ((1u << CHUNKS) - 1u) << (lane & ~(CHUNKS - 1));
         if (__any_sync(group, odd))
-            plain_row<T, D>(p, seq, kvh, live, snew, sm + C::OFF_NEW, x0, x1, dst);
+            plain_row<T, D, MODE>(p, seq, kvh, h0 + q, live, snew, MODE == ATTEND_CONTEXT ? nullptr : sm + C::OFF_NEW, x0, x1, dst);
         else
             *reinterpret_cast<uint4 *>(dst + d * 2) = Vec<T>::pack(acc);
     }
@@ -581,7 +621,7 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
 
 // Merge the `parts` results of each unit: a CTA per (unit, query), SLICES groups of D / 8 lanes that take every SLICES-th part each.
 constexpr int SLICES = 8;
-template <typename T, int D>
+template <typename T, int D, int MODE>
 __global__ void __launch_bounds__(SLICES * D / 8) sh_window_decode_merge_kernel(const __grid_constant__ WindowParams p, int qblocks, int parts, long long units) {
     constexpr int CHUNKS = D / 8, N = SLICES * CHUNKS, REC = MQ * (D + 2);
     __shared__ float top[N / 32], sum[SLICES], out[SLICES][D];
@@ -589,7 +629,7 @@ __global__ void __launch_bounds__(SLICES * D / 8) sh_window_decode_merge_kernel(
     const long long unit = blockIdx.x / MQ;
     const int qb = (int)(unit % qblocks), kvh = (int)(unit / qblocks % p.hk), seq = (int)(unit / qblocks / p.hk);
     sh_pdl_wait();
-    const int t = min(p.lengths[seq], MAX_POS);
+    const int t = rows_before<MODE>(p, seq);
     if (t < 0 || q >= min(MQ, p.g - qb * MQ)) return;
     const float *rec = p.part + unit * parts * REC + q * (D + 2);
     float M = -CUDART_INF_F;
@@ -627,13 +667,16 @@ __global__ void __launch_bounds__(SLICES * D / 8) sh_window_decode_merge_kernel(
         float x = 0.f;
 #pragma unroll
         for (int i = 0; i < SLICES; ++i) x += out[i][c * 8 + e];
-        acc[e] = x / L;
-        odd |= !isfinite(acc[e]);
+        acc[e] = x;
     }
-    char *dst = p.out.p + seq * p.out.ts + (long long)(kvh * p.g + qb * MQ + q) * p.out.hs;
+    const int h = kvh * p.g + qb * MQ + q;
+    close_row<T, MODE>(p, seq, h, c * 8, M - Weights<T>::LIFT, L, t == 0, acc);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) odd |= !isfinite(acc[e]);
+    char *dst = p.out.p + seq * p.out.ts + (long long)h * p.out.hs;
     if (__any_sync((1u << CHUNKS) - 1u, odd)) {
         const float4 *x = reinterpret_cast<const float4 *>(p.part + units * parts * REC + unit * (MQ * D) + q * D + c * 8);
-        plain_row<T, D>(p, seq, kvh, min(t + 1, p.sinks + p.window), 0, nullptr, x[0], x[1], dst);
+        plain_row<T, D, MODE>(p, seq, kvh, h, MODE == ATTEND_CONTEXT ? t : min(t + 1, p.sinks + p.window), 0, nullptr, x[0], x[1], dst);
     } else {
         *reinterpret_cast<uint4 *>(dst + c * 16) = Vec<T>::pack(acc);
     }
@@ -694,9 +737,9 @@ cudaError_t launch_units(const WindowParams &p, int qblocks, int threads, size_t
     return cudaLaunchKernelEx(&cfg, kern, p, qblocks, parts);
 }
 
-template <int D, int GQ>
+template <int D, int GQ, int MODE>
 cudaError_t launch_simt(const WindowParams &p, cudaStream_t s) {
-    constexpr auto kern = sh_window_decode_simt_kernel<float, D, GQ>;
+    constexpr auto kern = sh_window_decode_simt_kernel<float, D, GQ, MODE>;
     const int qblocks = (p.g + GQ - 1) / GQ;
     int slots[4];
     const cudaError_t e = cluster_slots<kern>(NT, 0, slots);
@@ -704,21 +747,21 @@ cudaError_t launch_simt(const WindowParams &p, cudaStream_t s) {
     const Shape a = best_split((long long)p.sequences * p.hk * qblocks, (long long)p.window + p.sinks, 8 * D, slots, 3.0e4);
     return launch_units<kern>(p, qblocks, NT, 0, a.S, 0, s);
 }
-template <int D>
+template <int D, int MODE>
 cudaError_t launch_f32(const WindowParams &p, cudaStream_t s) {
-    return p.g == 1 ? launch_simt<D, 1>(p, s) : (p.g == 2 ? launch_simt<D, 2>(p, s) : launch_simt<D, 4>(p, s));
+    return p.g == 1 ? launch_simt<D, 1, MODE>(p, s) : (p.g == 2 ? launch_simt<D, 2, MODE>(p, s) : launch_simt<D, 4, MODE>(p, s));
 }
 // Two shapes: CTAs of 4 warps, 3 to an SM, each warp with one block of rows in flight besides the one it works on; and CTAs of 8 warps,
 // one to an SM, with two in flight.  Many units want the first (9216 units of 410 rows: 325 against 545 us), few units, which
 // cannot fill the machine, the second, whose CTAs draw more each (8 units of 16384 rows: 34 against 23 us).
-template <typename T, int D>
+template <typename T, int D, int MODE>
 cudaError_t launch_mma(const WindowParams &p, cudaStream_t s) {
     using Small = Mma<D, 4>;
     using Large = Mma<D, 8>;
     static_assert(3 * (Small::SMEM + 1024) <= 233472 && Large::SMEM <= 232448, "CTAs per SM");
     const int qblocks = (p.g + MQ - 1) / MQ;
     const long long units = (long long)p.sequences * p.hk * qblocks, rows = (long long)p.window + p.sinks;
-    constexpr auto small = sh_window_decode_mma_kernel<T, D, 4>, large = sh_window_decode_mma_kernel<T, D, 8>;
+    constexpr auto small = sh_window_decode_mma_kernel<T, D, 4, MODE>, large = sh_window_decode_mma_kernel<T, D, 8, MODE>;
     int slots_a[4], slots_b[4];
     cudaError_t e = cluster_slots<small>(128, Small::SMEM, slots_a);
     if (e == cudaSuccess) e = cluster_slots<large>(256, Large::SMEM, slots_b);
@@ -740,7 +783,7 @@ cudaError_t launch_mma(const WindowParams &p, cudaStream_t s) {
             attr.val.programmaticStreamSerializationAllowed = 1;
             cfg.attrs = &attr;
             cfg.numAttrs = 1;
-            return cudaLaunchKernelEx(&cfg, sh_window_decode_merge_kernel<T, D>, p, qblocks, (int)parts, units);
+            return cudaLaunchKernelEx(&cfg, sh_window_decode_merge_kernel<T, D, MODE>, p, qblocks, (int)parts, units);
         }
     }
     return a.us <= b.us ? launch_units<small>(p, qblocks, 128, Small::SMEM, a.S, 0, s)
@@ -749,10 +792,15 @@ cudaError_t launch_mma(const WindowParams &p, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, cudaStream_t s) {
-    if (dtype == SH_F32) return D == 128 ? launch_f32<128>(p, s) : launch_f32<64>(p, s);
-    if (dtype == SH_F16) return D == 128 ? launch_mma<__half, 128>(p, s) : launch_mma<__half, 64>(p, s);
-    return D == 128 ? launch_mma<__nv_bfloat16, 128>(p, s) : launch_mma<__nv_bfloat16, 64>(p, s);
+template <int MODE>
+static cudaError_t launch_type(const WindowParams &p, int dtype, int D, cudaStream_t s) {
+    if (dtype == SH_F32) return D == 128 ? launch_f32<128, MODE>(p, s) : launch_f32<64, MODE>(p, s);
+    if (dtype == SH_F16) return D == 128 ? launch_mma<__half, 128, MODE>(p, s) : launch_mma<__half, 64, MODE>(p, s);
+    return D == 128 ? launch_mma<__nv_bfloat16, 128, MODE>(p, s) : launch_mma<__nv_bfloat16, 64, MODE>(p, s);
+}
+cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, int mode, cudaStream_t s) {
+    if (mode == ATTEND_CONTEXT) return launch_type<ATTEND_CONTEXT>(p, dtype, D, s);
+    return mode == ATTEND_MASS ? launch_type<ATTEND_MASS>(p, dtype, D, s) : launch_type<ATTEND_WINDOW>(p, dtype, D, s);
 }
 
 size_t sh_window_decode_scratch(int sequences, int hk, int g, int dtype, int D) {

@@ -33,7 +33,7 @@ __device__ __forceinline__ void cp16_or_zero(void *dst, const void *src, bool ta
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(shasync::smem_u32(dst)), "l"(src), "r"(take ? 16 : 0) : "memory");
 }
 
-template <int D>
+template <int D, int MODE>
 __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const WindowParams p) {
     using C = Simt<D>;
     constexpr int BN = C::BN, NC = C::NC, LDK = C::LDK, LDP = C::LDP;
@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int kvh = blockIdx.y;
     if (tid < 32) {
-        const Tile t = find_tile(p, blockIdx.x, BM);
+        const Tile t = find_tile<MODE>(p, blockIdx.x, BM);
         if (tid == 0) tile_sh = t;
     }
     __syncthreads();
@@ -54,13 +54,13 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
     const int qlo = (int)(t.row0 / p.g), qhi = (int)((min(t.row0 + BM, rows) - 1) / p.g);      // the tile's first and last token in the chunk
     const int oldest = t.cached + qlo - p.window + 1;                // the first row's window starts here
     const Ring ring(p.kc ? t.cached : 0, p.sinks, p.window);
-    const int cblocks = (ring.live + BN - 1) / BN, blocks = cblocks + qhi / BN + 1;
+    const int cblocks = (ring.live + BN - 1) / BN, blocks = cblocks + (MODE == ATTEND_CONTEXT ? 0 : qhi / BN + 1);
     // the first block from b on with a key in sight
     auto seek = [&](int b) {
         for (; b < cblocks; ++b)
             if (ring.any(b * BN, b * BN + BN, oldest)) return b;
         const int lo = max(0, qlo - p.window + 1) / BN;              // (what lies between the sinks and the window is passed over)
-        return b - cblocks < lo && t.cached + (b - cblocks) * BN >= p.sinks ? cblocks + lo : b;
+        return MODE != ATTEND_CONTEXT && b - cblocks < lo && t.cached + (b - cblocks) * BN >= p.sinks ? cblocks + lo : b;
     };
     auto position = [&](int b, int j) {
         int pos;
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
         for (int i = 0; i < C::EACH; ++i) {
             const int j = tid / PIECES + i * STEP;
             const bool take = kpos[turn * BN + j] >= 0;
-            cp16_or_zero(value ? Vs + j * D + c * 4 : Ks + j * LDK + c * 4, take ? src + j * stride + c * 16 : (value ? p.v.p : p.k.p), take);
+            cp16_or_zero(value ? Vs + j * D + c * 4 : Ks + j * LDK + c * 4, take ? src + j * stride + c * 16 : p.q.p, take);
         }
         shumma::cp_async_commit();
     };
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
         cp16_or_zero(Qs + r * LDK + c * 4, take ? p.q.p + tok * p.q.ts + (kvh * p.g + (int)(row % p.g)) * p.q.hs + c * 16 : p.q.p, take);
     }
     __syncthreads();
-    request(b, 0, false);
+    if (MODE != ATTEND_CONTEXT || b < blocks) request(b, 0, false);      // (a context may have no rows)
     int qp[R];
     float m[R], l[R];
     uint64_t o[R][D / 32];                                           // pairs of columns
@@ -111,6 +111,7 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) o[a][c] = 0;
     }
+    if (MODE == ATTEND_CONTEXT && b >= blocks) shumma::cp_async_wait_all();
     while (b < blocks) {
         shumma::cp_async_wait_all();
         __syncthreads();                                             // the keys are there; the last block's P.V is done
@@ -216,6 +217,11 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
 #pragma unroll
         for (int off = 8; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
         if (qp[a] < 0) continue;
+        if (MODE != ATTEND_WINDOW && tx == 0) {
+            const long long row = t.row0 + ty * R + a;
+            p.lse[(t.first + row / p.g) * p.hq + kvh * p.g + (int)(row % p.g)] = 0.69314718055994531f * (m[a] + log2f(sum));
+        }
+        if (MODE == ATTEND_CONTEXT && blocks == 0) sum = 1.f;         // no rows: zeros
         const long long row = t.row0 + ty * R + a, tok = t.first + row / p.g;
         float *dst = reinterpret_cast<float *>(p.out.p + tok * p.out.ts + (kvh * p.g + (int)(row % p.g)) * p.out.hs);
 #pragma unroll
@@ -229,7 +235,8 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
 }
 
 // Copy the rows that a later token can see into their slots: PIECES lanes move one token's key and value row of one head.
-// Rows are found by bisection of `starts`; a warp's rows are neighbouring heads of the same token.
+// A warp's rows are neighbouring heads of the same token.
+template <int MODE>
 __global__ void __launch_bounds__(256) sh_window_append_kernel(const WindowParams p, int pieces) {
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
     const int c = (int)(id % pieces);
@@ -237,14 +244,8 @@ __global__ void __launch_bounds__(256) sh_window_append_kernel(const WindowParam
     const int h = (int)(rh % p.hk);
     const long long tok = rh / p.hk;
     if (tok >= p.tokens) return;
-    int lo = 0, hi = p.sequences;      // the last sequence that starts at or before tok (empty ones before it are passed over)
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.starts[mid] <= tok) lo = mid; else hi = mid;
-    }
-    int first, count, cached;
-    sequence_rows(p, lo, first, count, cached);
-    if (tok < first || tok >= (long long)first + count) return;
+    int lo, first, count, cached;
+    if (!sequence_of<MODE>(p, tok, lo, first, count, cached)) return;
     const int pos = cached + (int)(tok - first), end = cached + count;
     if (pos >= p.sinks && pos < end - p.window) return;      // pushed out of the window by the chunk itself
     const long long slot = slot_of(pos, p.sinks, p.window);
@@ -253,11 +254,16 @@ __global__ void __launch_bounds__(256) sh_window_append_kernel(const WindowParam
     const uint4 vv = *reinterpret_cast<const uint4 *>(p.v.p + tok * p.v.ts + h * p.v.hs + c * 16);
     *reinterpret_cast<uint4 *>(p.kc + at) = kk;
     *reinterpret_cast<uint4 *>(p.vc + at) = vv;
+    if (MODE == ATTEND_MASS && c == 0) {
+        const long long r = lo * p.rss + h * p.rhs + slot;
+        p.mass[r] = 0.f;
+        p.held[r] = p.seen[lo] + (int)(tok - first);
+    }
 }
 
-template <int D>
+template <int D, int MODE>
 cudaError_t launch(const WindowParams &p, cudaStream_t s) {
-    auto kern = sh_window_prefill_f32_kernel<D>;
+    auto kern = sh_window_prefill_f32_kernel<D, MODE>;
     constexpr int bytes = Simt<D>::FLOATS * 4;
     static ShKernelSetup setup;
     int sms = 0;
@@ -271,12 +277,17 @@ cudaError_t launch(const WindowParams &p, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t sh_launch_window_prefill_f32(const WindowParams &p, int D, cudaStream_t s) { return D == 128 ? launch<128>(p, s) : launch<64>(p, s); }
+cudaError_t sh_launch_window_prefill_f32(const WindowParams &p, int D, int mode, cudaStream_t s) {
+    if (mode == ATTEND_CONTEXT) return D == 128 ? launch<128, ATTEND_CONTEXT>(p, s) : launch<64, ATTEND_CONTEXT>(p, s);
+    if (mode == ATTEND_MASS) return D == 128 ? launch<128, ATTEND_MASS>(p, s) : launch<64, ATTEND_MASS>(p, s);
+    return D == 128 ? launch<128, ATTEND_WINDOW>(p, s) : launch<64, ATTEND_WINDOW>(p, s);
+}
 
-cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, cudaStream_t s) {
+cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, int mode, cudaStream_t s) {
     const int pieces = D * es / 16;
     const long long blocks = ((long long)p.tokens * p.hk * pieces + 255) / 256;
     if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
-    sh_window_append_kernel<<<(unsigned)blocks, 256, 0, s>>>(p, pieces);
+    if (mode == ATTEND_MASS) sh_window_append_kernel<ATTEND_MASS><<<(unsigned)blocks, 256, 0, s>>>(p, pieces);
+    else sh_window_append_kernel<ATTEND_WINDOW><<<(unsigned)blocks, 256, 0, s>>>(p, pieces);
     return cudaGetLastError();
 }

@@ -319,6 +319,7 @@ struct Found {
     int base = 0;
     long long before = 0;
 };
+template <int MODE>
 __device__ __forceinline__ Item find_item(const UmmaParams &p, int id, Found &from) {
     const int per = p.w.hk * p.hblocks * p.parts, in = id % per;
     const int lane = threadIdx.x & 31, span = 2 * p.tpt;
@@ -330,7 +331,7 @@ __device__ __forceinline__ Item find_item(const UmmaParams &p, int id, Found &fr
     long long before = from.before;
     for (int base = from.base; base < p.w.sequences; base += 32) {
         int first = 0, count = 0, cached = 0;
-        if (base + lane < p.w.sequences) sequence_rows(p.w, base + lane, first, count, cached);
+        if (base + lane < p.w.sequences) sequence_rows<MODE>(p.w, base + lane, first, count, cached);
         const int mine = (count + span - 1) / span;
         // of 32 sequences those with most cached keys to walk over come first (103 -> 96 us for chunks of 17 to 256 tokens over 1 to
         // 2052 rows; ordered by the tokens of the chunk too, prompts of 1 to 4001 tokens took 132 instead of 130 us)
@@ -365,7 +366,7 @@ __device__ __forceinline__ Item find_item(const UmmaParams &p, int id, Found &fr
     static_cast<Ring &>(r) = Ring(p.w.kc ? r.cached : 0, p.w.sinks, p.w.window);
     r.ctiles = (r.live + TN - 1) / TN;
     r.jlo = max(0, r.a - r.window + 1) / TN;
-    r.jhi = r.last(r.has(1) ? 1 : 0) / TN;
+    r.jhi = MODE == ATTEND_CONTEXT ? -1 : r.last(r.has(1) ? 1 : 0) / TN;      // (a context has no rows of the chunk)
     return r;
 }
 
@@ -399,13 +400,17 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
+// Where the log of a row's sum goes (natural units; kernels count exponents in base 2).
+constexpr float LN2 = 0.69314718055994531f;
+__device__ __forceinline__ float *lse_of(const WindowParams &p, int token, int head) { return p.lse + (long long)token * p.hq + head; }
+
 // One row by one warp, over its visible keys only, in fp32 on CUDA cores: for rows next to values that are not finite.
-template <typename T, int D>
+template <typename T, int D, int MODE>
 __device__ __noinline__ void slow_row(const UmmaParams &u, int id, int qi, int h) {
     constexpr int E = D / 32;
     const WindowParams &p = u.w;
     Found from;
-    const Item w = find_item(u, id, from);
+    const Item w = find_item<MODE>(u, id, from);
     if (w.seq < 0 || qi < 0 || qi >= w.count) return;      // (only where a CTA gave up a wait)
     const int lane = threadIdx.x & 31;
     float q[E], o[E], m = -CUDART_INF_F, l = 0.f;
@@ -437,6 +442,7 @@ __device__ __noinline__ void slow_row(const UmmaParams &u, int id, int qi, int h
     T *dst = reinterpret_cast<T *>(p.out.p + (long long)(w.first + qi) * p.out.ts + h * p.out.hs) + lane * E;
 #pragma unroll
     for (int e = 0; e < E; ++e) dst[e] = (T)(o[e] / l);
+    if (MODE != ATTEND_WINDOW && lane == 0) *lse_of(p, w.first + qi, h) = LN2 * (m + log2f(l));
 }
 
 // Note rows of a softmax warp that have to be computed again, and do them.  (Calls, as inlined they cost the loop over the steps
@@ -455,15 +461,15 @@ __device__ __noinline__ void note_again(Bars *bars, int warp, int id, unsigned r
     __syncwarp();
 }
 
-template <typename T, int D>
+template <typename T, int D, int MODE>
 __device__ __noinline__ void do_again(const UmmaParams &p, const int2 *list, int count, int t, int quarter) {
     for (int i = 0; i < count; ++i) {
         const int2 e = list[i];
         Found from;
-        const Item w = find_item(p, e.x, from);
+        const Item w = find_item<MODE>(p, e.x, from);
         for (unsigned rows = (unsigned)e.y; rows; rows &= rows - 1) {
             const int r = quarter * 32 + __ffs(rows) - 1;
-            slow_row<T, D>(p, e.x, w.from(t) + r / p.gb, w.kvh * p.w.g + w.hb * p.gb + r % p.gb);
+            slow_row<T, D, MODE>(p, e.x, w.from(t) + r / p.gb, w.kvh * p.w.g + w.hb * p.gb + r % p.gb);
         }
     }
 }
@@ -472,7 +478,7 @@ template <typename T> struct Fmt;
 template <> struct Fmt<__half> { static constexpr int CODE = 0; static constexpr float LIFT = 7.f; };
 template <> struct Fmt<__nv_bfloat16> { static constexpr int CODE = 1; static constexpr float LIFT = 0.f; };
 
-template <typename T, int D>
+template <typename T, int D, int MODE>
 __global__ void __launch_bounds__(NTH, 1)
 sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                               const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_kc,
@@ -630,7 +636,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
         uint32_t asked = 0, answered = 0;             // requests for work, answers read
         uint32_t cleaned = 0;                         // tiles with dead rows
         for (int id = blockIdx.x; ok && id >= 0;) {
-            const Item w = find_item(p, id, from);
+            const Item w = find_item<MODE>(p, id, from);
             if (w.seq < 0) {                          // (the grid is an upper bound: behind the last item nothing follows)
                 if (elect_one()) drop(id);
                 __syncwarp();
@@ -652,7 +658,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             };
             // (what lies outside the tensors is zeros already)
             auto dead = [&](int i) {
-                return i < w.ctiles ? i * TN + TN > w.live && w.live < w.sinks + w.window : (i - w.ctiles) * TN + TN > w.count && w.first + w.count < p.w.tokens;
+                return i < w.ctiles ? i * TN + TN > w.live && w.live < (MODE == ATTEND_CONTEXT ? p.w.slots : w.sinks + w.window) : (i - w.ctiles) * TN + TN > w.count && w.first + w.count < p.w.tokens;
             };
             auto needed = [&](int i) { return i <= last_tile && (w.need(0, i) || w.need(1, i)); };
             int seen = 0, parts = 1;                  // needed tiles so far, CTAs that share them
@@ -733,6 +739,10 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             }
             if (!ok) break;
             if (w.part < parts) {                     // (a part has 4 tiles at least)
+                if (MODE == ATTEND_CONTEXT && w.ctiles == 0) {      // a context without rows: a step that nobody looks at
+                    flags = STEP_CACHE;
+                    x = 0;
+                }
                 flags |= STEP_LAST;
                 step();
             }
@@ -927,6 +937,12 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                 continue;
             }
             if (!begun) {                             // (a query tile without rows)
+                if (MODE == ATTEND_CONTEXT && live) { // (a context without rows)
+                    uint4 *dst = reinterpret_cast<uint4 *>(p.w.out.p + (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs);
+                    for (int i = 0; i < D / 8; ++i) dst[i] = make_uint4(0, 0, 0, 0);
+                    *lse_of(p.w, row0 + qi, kvh * p.w.g + h) = -CUDART_INF_F;
+                }
+                __syncwarp();
                 if (lane == 0) mbar_arrive(&bars->q_free[t][qbuf]);
                 continue;
             }
@@ -934,6 +950,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             if (__any_sync(0xffffffffu, !ok)) break;
             tc_fence_after();
             const float inv = 1.f / l;
+            if (MODE != ATTEND_WINDOW && live) *lse_of(p.w, row0 + qi, kvh * p.w.g + h) = LN2 * (m * c - Fmt<T>::LIFT + log2f(l));
             // the rows of O, one per thread, are laid out in the place of the item's queries (every S of the item is over), like a
             // query tile, and a warp's 32 rows leave from there as one copy if they are whole tokens; rows next to somebody else's,
             // or that have to be done again, go by the threads, in whole lines
@@ -987,7 +1004,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             if (again) note_again(bars, warp, id, again);
         }
         __syncwarp();
-        do_again<T, D>(p, bars->again[warp], bars->again_count[warp], t, warp & 3);
+        do_again<T, D, MODE>(p, bars->again[warp], bars->again_count[warp], t, warp & 3);
         bulk_wait_all();            // outputs on their way from shared memory
     }
     tc_fence_before();
@@ -1000,7 +1017,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
 }
 
 // Merge the parts of each item: 8 rows of a query tile a CTA, 4 columns a thread (so a part's floats come as runs of 128 bytes).
-template <typename T, int D>
+template <typename T, int D, int MODE>
 __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __grid_constant__ UmmaParams p) {
     constexpr int ROWS = 8;
     __shared__ float2 sums[MAX_SHARE][ROWS];
@@ -1035,6 +1052,7 @@ __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __
         o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
     }
     const float inv = 1.f / L;                       // (as where there is nothing to merge)
+    if (MODE != ATTEND_WINDOW && live && c4 == 0) *lse_of(p.w, w.y + tok, kvh * p.w.g + h) = LN2 * (M + log2f(L));
     o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
     if (live && !(isfinite(o.x) && isfinite(o.y) && isfinite(o.z) && isfinite(o.w))) odd[r] = 1;
     __syncthreads();
@@ -1045,7 +1063,7 @@ __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __
     for (int i = tid >> 5; i < ROWS; i += D / 16) {  // rows next to values that are not finite
         if (!odd[i]) continue;
         Found from;
-        slow_row<T, D>(p, id, find_item(p, id, from).from(t) + (row0 + i) / p.gb, kvh * p.w.g + hb * p.gb + (row0 + i) % p.gb);
+        slow_row<T, D, MODE>(p, id, find_item<MODE>(p, id, from).from(t) + (row0 + i) / p.gb, kvh * p.w.g + hb * p.gb + (row0 + i) % p.gb);
     }
 }
 
@@ -1102,7 +1120,7 @@ void share_out(long long items, int tokens, int window, int sinks, int g, bool w
     parts = parts_of(with_cache ? sees : std::min(sees, own), share);
 }
 
-template <typename T, int D>
+template <typename T, int D, int MODE>
 cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     UmmaParams p;
     p.w = w;
@@ -1115,22 +1133,26 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     p.copy_out = 32 % p.gb == 0;
     const uint64_t ost[2] = {(uint64_t)w.out.hs, (uint64_t)w.out.ts};
     const uint32_t obox[2] = {(uint32_t)p.gb, p.copy_out ? 32u / p.gb : 1u};
-    if (!make_map(&mq, w.q.p, 2, qdim, qst, qbox, D) || !make_map(&mo, w.out.p, 2, qdim, ost, obox, D) || !keys_map(&mk, w.k, w.hk, w.tokens, D / 64) || !keys_map(&mv, w.v, w.hk, w.tokens, D / 64))
+    if (!make_map(&mq, w.q.p, 2, qdim, qst, qbox, D) || !make_map(&mo, w.out.p, 2, qdim, ost, obox, D))
         return cudaErrorNotSupported;
-    mkc = mk; mvc = mv;
+    if (MODE != ATTEND_CONTEXT) {
+        if (!keys_map(&mk, w.k, w.hk, w.tokens, D / 64) || !keys_map(&mv, w.v, w.hk, w.tokens, D / 64)) return cudaErrorNotSupported;
+        mkc = mk; mvc = mv;
+    }
     if (w.kc) {
-        const uint64_t dim[4] = {(uint64_t)w.sinks + w.window, (uint64_t)w.hk, (uint64_t)w.sequences, D / 64};
+        const uint64_t dim[4] = {(uint64_t)w.slots, (uint64_t)w.hk, (uint64_t)w.sequences, D / 64};
         const uint64_t st[4] = {(uint64_t)w.cls, (uint64_t)w.chs, (uint64_t)w.css, 128};
         const uint32_t box[4] = {TN, 1, 1, D / 64};
         if (!make_map(&mkc, w.kc, 4, dim, st, box) || !make_map(&mvc, w.vc, 4, dim, st, box)) return cudaErrorNotSupported;
+        if (MODE == ATTEND_CONTEXT) { mk = mkc; mv = mvc; }
     }
-    auto kern = sh_window_prefill_umma_kernel<T, D>;
+    auto kern = sh_window_prefill_umma_kernel<T, D, MODE>;
     static ShKernelSetup setup;
     int sms = 0;
     const cudaError_t e = sh_setup_kernel(setup, kern, Cfg<D>::SMEM, &sms);
     if (e != cudaSuccess) return e;
     const long long items = most_items(w.tokens, w.sequences, w.hk, w.g);
-    share_out(items, w.tokens, w.window, w.sinks, w.g, w.kc != nullptr, sms, p.share, p.parts);
+    share_out(items, w.tokens, MODE == ATTEND_CONTEXT ? w.slots : w.window, w.sinks, w.g, w.kc != nullptr, sms, p.share, p.parts);
     if (!w.part) p.parts = 1;
     if (items > 0x7fffffffll) return cudaErrorInvalidValue;
     kern<<<(unsigned)(items * p.parts), NTH, Cfg<D>::SMEM, s>>>(p, mq, mk, mv, mkc, mvc, mo);
@@ -1146,14 +1168,19 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, sh_window_prefill_merge_kernel<T, D>, p);
+    return cudaLaunchKernelEx(&cfg, sh_window_prefill_merge_kernel<T, D, MODE>, p);
 }
 
 }  // namespace
 
-cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int D, cudaStream_t s) {
-    if (dtype == SH_F16) return D == 128 ? launch<__half, 128>(p, s) : launch<__half, 64>(p, s);
-    return D == 128 ? launch<__nv_bfloat16, 128>(p, s) : launch<__nv_bfloat16, 64>(p, s);
+template <int MODE>
+static cudaError_t launch_type(const WindowParams &p, int dtype, int D, cudaStream_t s) {
+    if (dtype == SH_F16) return D == 128 ? launch<__half, 128, MODE>(p, s) : launch<__half, 64, MODE>(p, s);
+    return D == 128 ? launch<__nv_bfloat16, 128, MODE>(p, s) : launch<__nv_bfloat16, 64, MODE>(p, s);
+}
+cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int D, int mode, cudaStream_t s) {
+    if (mode == ATTEND_CONTEXT) return launch_type<ATTEND_CONTEXT>(p, dtype, D, s);
+    return mode == ATTEND_MASS ? launch_type<ATTEND_MASS>(p, dtype, D, s) : launch_type<ATTEND_WINDOW>(p, dtype, D, s);
 }
 
 size_t sh_window_prefill_scratch(int tokens, int sequences, int hk, int g, int window, int sinks, bool with_cache, int dtype, int D) {
