@@ -508,29 +508,30 @@ typedef struct {
  * all tokens share, or (contexts == tokens) one of its own for each token.  lengths_dev: int32 [contexts], or NULL: `slots` rows each;
  * lengths outside of 0 .. slots are clamped.  Outputs: out, and lse_dev [tokens][q_heads], the natural logs of the sums of exponentials.  A
  * context of length 0 gives zeros and -infinity; rows that belong to no context are left as they were.  starts that decrease or leave 0 .. tokens are clamped, outputs are then meaningless.
- * 16-bit types: the weights are rounded once to the type (one token of each context: held in two parts).
+ * 16-bit types: the weights are rounded once to the type (one token of each context: held in two parts).  out_dtype: a->dtype, or SH_F32
+ * for a result that something continues from (it is then not rounded before it joins the rest).
  * workspace_dev: sh_context_attention_workspace_bytes(a, tokens, contexts, starts_dev != NULL) bytes of device memory, 16-byte aligned, or NULL; used
  * as sh_window_prefill's.
  * Errors: SH_EINVAL, SH_ENOMEM (workspace too small), SH_ECUDA; bounded waits as in sh_window_status.
  */
 size_t sh_context_attention_workspace_bytes(const sh_attention *a, int tokens, int contexts, int with_starts);
 int sh_context_attention(const sh_attention *a, int tokens, int contexts, const sh_rows *q, const sh_window_cache *context, const int32_t *starts_dev,
-                         const int32_t *lengths_dev, const sh_rows *out, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+                         const int32_t *lengths_dev, const sh_rows *out, int out_dtype, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
  * Prompt chunks: the tokens starts[i] .. starts[i+1] - 1 continue sequence i, which holds lengths[i] rows and has seen seen[i] tokens.  They are
  * stored in the slots from lengths[i] on (positions from seen[i] on); each sees the live slots and the chunk up to itself, and every
  * slot's mass grows by the weights it gets from them (new slots start at 0).  The caller advances lengths and seen.  A sequence of
  * negative length is idle, and one whose chunk has no room (lengths[i] + tokens > slots) takes no part either: nothing of it is read or written.
- * prior, prior_lse_dev [tokens][q_heads]: what the tokens have seen elsewhere (out and lse of sh_context_attention), or both NULL.
- * The rows are rounded to the type before a prior joins them, and once more after.
+ * prior (rows of prior_dtype: a->dtype or SH_F32), prior_lse_dev [tokens][q_heads]: what the tokens have seen elsewhere (out and lse of
+ * sh_context_attention), or both NULL.
  * workspace_dev: sh_mass_prefill_workspace_bytes(a, tokens, sequences) bytes of device memory, 16-byte aligned; in use until `stream` has passed
  * the call, so calls that may run at once need one each.
  * Errors: SH_EINVAL, SH_ENOMEM, SH_ECUDA (a call that fails midway may have stored the chunk); bounded waits as in sh_window_status.
  */
 size_t sh_mass_prefill_workspace_bytes(const sh_attention *a, int tokens, int sequences);
 int sh_mass_prefill(const sh_attention *a, int tokens, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *starts_dev,
-                    const int32_t *lengths_dev, const int32_t *seen_dev, const sh_window_cache *cache, const sh_records *rec, const sh_rows *prior,
+                    const int32_t *lengths_dev, const int32_t *seen_dev, const sh_window_cache *cache, const sh_records *rec, const sh_rows *prior, int prior_dtype,
                     const float *prior_lse_dev, const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
@@ -540,8 +541,8 @@ int sh_mass_prefill(const sh_attention *a, int tokens, int sequences, const sh_r
  */
 size_t sh_mass_decode_workspace_bytes(const sh_attention *a, int sequences);
 int sh_mass_decode(const sh_attention *a, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *lengths_dev,
-                   const int32_t *seen_dev, const sh_window_cache *cache, const sh_records *rec, const sh_rows *prior, const float *prior_lse_dev,
-                   const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream);
+                   const int32_t *seen_dev, const sh_window_cache *cache, const sh_records *rec, const sh_rows *prior, int prior_dtype,
+                   const float *prior_lse_dev, const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /*
  * Eviction: every (sequence, key head) with more than `keep` live rows keeps `keep` of them: first those whose position lies within the `recent`

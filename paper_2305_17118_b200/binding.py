@@ -127,11 +127,11 @@ def declare(lib: C.CDLL) -> C.CDLL:
     lib.sh_window_decode_workspace_bytes.argtypes = [window, C.c_int]
     lib.sh_window_decode_workspace_bytes.restype = C.c_size_t
     attention = records = vp
-    lib.sh_context_attention.argtypes = [attention, C.c_int, C.c_int, rows, cache, vp, vp, rows, vp, vp, C.c_size_t, vp]
+    lib.sh_context_attention.argtypes = [attention, C.c_int, C.c_int, rows, cache, vp, vp, rows, C.c_int, vp, vp, C.c_size_t, vp]
     lib.sh_context_attention_workspace_bytes.argtypes = [attention, C.c_int, C.c_int, C.c_int]
-    lib.sh_mass_prefill.argtypes = [attention, C.c_int, C.c_int, rows, rows, rows, vp, vp, vp, cache, records, rows, vp, rows, vp, C.c_size_t, vp]
+    lib.sh_mass_prefill.argtypes = [attention, C.c_int, C.c_int, rows, rows, rows, vp, vp, vp, cache, records, rows, C.c_int, vp, rows, vp, C.c_size_t, vp]
     lib.sh_mass_prefill_workspace_bytes.argtypes = [attention, C.c_int, C.c_int]
-    lib.sh_mass_decode.argtypes = [attention, C.c_int, rows, rows, rows, vp, vp, cache, records, rows, vp, rows, vp, C.c_size_t, vp]
+    lib.sh_mass_decode.argtypes = [attention, C.c_int, rows, rows, rows, vp, vp, cache, records, rows, C.c_int, vp, rows, vp, C.c_size_t, vp]
     lib.sh_mass_decode_workspace_bytes.argtypes = [attention, C.c_int]
     lib.sh_mass_evict.argtypes = [attention, C.c_int, vp, cache, records, C.c_int, C.c_int, cache, records, C.c_int, vp, vp, C.c_size_t, vp]
     lib.sh_mass_evict_workspace_bytes.argtypes = [attention, C.c_int, C.c_int, C.c_int]
@@ -495,7 +495,7 @@ def _new(like: torch.Tensor, shape, stream, zero: bool, dtype=None) -> torch.Ten
             return like.new_zeros(shape, dtype=dtype) if zero else like.new_empty(shape, dtype=dtype)
     if dtype is None:
         return like.new_zeros(shape) if zero else like.new_empty(shape)
-    return like.new_empty(shape, dtype=dtype)
+    return like.new_zeros(shape, dtype=dtype) if zero else like.new_empty(shape, dtype=dtype)
 
 
 def _launch(what: str, fn, device: int, stream, *args) -> None:
@@ -770,11 +770,11 @@ def _records_packed(mass, positions, shape, device: int) -> bytes:
 
 def _prior_packed(prior, shape, dtype, device: int):
     if prior is None:
-        return None, None
-    if not (isinstance(prior, (tuple, list)) and len(prior) == 2):
+        return None, 0, None
+    if not (isinstance(prior, (tuple, list)) and len(prior) == 2 and isinstance(prior[0], torch.Tensor)):
         _fail("prior", "a pair (out, lse)", prior)
-    rows = _more_rows(prior[0], "prior", shape, dtype, device)
-    return rows, _logs(prior[1], "prior's lse", shape, device)
+    dt = torch.float32 if prior[0].dtype is torch.float32 else dtype
+    return _more_rows(prior[0], "prior", shape, dt, device), _CODE_OF[dt], _logs(prior[1], "prior's lse", shape, device)
 
 
 def _logs(t, what: str, shape, device: int) -> int:
@@ -784,15 +784,15 @@ def _logs(t, what: str, shape, device: int) -> int:
 
 
 def context_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None,
-                      lengths: Optional[torch.Tensor] = None, *, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
-                      lse: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+                      lengths: Optional[torch.Tensor] = None, *, scale: Optional[float] = None, partial: bool = False,
+                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """``sh_context_attention``: attention to contexts that are complete: a prefix that a whole batch shares, or each sequence's encoder states
     (cross attention).
 
     ``q`` [tokens, q_heads, head_dim], ``k``/``v`` [contexts, kv_heads, rows, head_dim].  The tokens ``starts[i] .. starts[i+1] - 1`` (int32, on the
     device) see the first ``lengths[i]`` rows of context i (None: all), all of them.  ``starts`` None: one context that all tokens share, or
     one for each token.  Returns ``out`` and ``lse`` fp32 [tokens, q_heads], the logs of the rows' sums of exponentials, from which
-    ``mass_decode`` and ``mass_prefill`` continue (``prior``).  A context of length 0 gives zeros and -inf; rows that belong to no
+    ``mass_decode`` and ``mass_prefill`` continue (``prior``); with ``partial`` ``out`` is fp32, so that nothing is rounded on the way.  A context of length 0 gives zeros and -inf; rows that belong to no
     context are left as they were (new tensors: zeros and -inf)."""
     shape, dtype, device, qr = _head_rows(q, "q")
     tokens, q_heads, d = shape
@@ -806,8 +806,9 @@ def context_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts:
     elif n != 1 and n != tokens:
         raise ValueError(f"{n} contexts for {tokens} tokens: without starts there must be one, or one for each token")
     lp = None if lengths is None else _ints(lengths, "lengths", n, device)
-    out = _new(q, shape, stream, sp is not None) if out is None else out
-    outr = _more_rows(out, "out", shape, dtype, device)
+    odt = torch.float32 if partial else dtype
+    out = _new(q, shape, stream, sp is not None, odt) if out is None else out
+    outr = _more_rows(out, "out", shape, odt, device)
     if lse is None:
         lse = _new(q, shape[:2], stream, False, torch.float32)
         if sp is not None:
@@ -817,7 +818,7 @@ def context_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts:
     if bytes_:
         work = _new(q, bytes_, stream, False, torch.uint8)
         wp = work.data_ptr()
-    _launch("context_attention", lib.sh_context_attention, device, stream, at, tokens, n, qr, cache, sp, lp, outr, _logs(lse, "lse", shape, device), wp, bytes_)
+    _launch("context_attention", lib.sh_context_attention, device, stream, at, tokens, n, qr, cache, sp, lp, outr, _CODE_OF[odt], _logs(lse, "lse", shape, device), wp, bytes_)
     return out, lse
 
 
@@ -829,7 +830,7 @@ def mass_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torc
     ``q`` [tokens, q_heads, head_dim], ``k``/``v`` [tokens, kv_heads, head_dim]; the tokens ``starts[i] .. starts[i+1] - 1`` are stored in the slots of
     ``k_cache``/``v_cache`` [sequences, kv_heads, slots, head_dim] from ``lengths[i]`` on, with positions from ``seen[i]`` on (the caller advances both);
     each sees the live slots and the chunk up to itself, and ``mass`` fp32 [sequences, kv_heads, slots] grows by the weights that the rows get.
-    ``prior``: (out, lse) of ``context_attention`` for the same tokens; the softmax goes over both.  A sequence of negative length, or
+    ``prior``: (out, lse) of ``context_attention(..., partial=True)`` for the same tokens; the softmax goes over both.  A sequence of negative length, or
     whose chunk has no room, takes no part; its rows of ``out``, and those of no sequence, are left as they were (a new ``out`` is
     zeroed)."""
     shape, dtype, device, qr = _head_rows(q, "q")
@@ -840,13 +841,13 @@ def mass_prefill(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torc
     cshape = _slots_of(k_cache, "k_cache", n, kshape[1], d, dtype, device)
     at = _attention_packed(dtype, d, q_heads, kshape[1], cshape[2], scale)
     cache, rec = _cache_packed(k_cache, v_cache, cshape, dtype, device), _records_packed(mass, positions, cshape[:3], device)
-    pr, pl = _prior_packed(prior, shape, dtype, device)
+    pr, pt, pl = _prior_packed(prior, shape, dtype, device)
     out = _new(q, shape, stream, True) if out is None else out
     outr = _more_rows(out, "out", shape, dtype, device)
     bytes_ = lib.sh_mass_prefill_workspace_bytes(at, tokens, n)
     work = _new(q, bytes_, stream, False, torch.uint8)
     _launch("mass_prefill", lib.sh_mass_prefill, device, stream, at, tokens, n, qr, kr, vr, _ints(starts, "starts", n + 1, device),
-            _ints(lengths, "lengths", n, device), _ints(seen, "seen", n, device), cache, rec, pr, pl, outr, work.data_ptr(), bytes_)
+            _ints(lengths, "lengths", n, device), _ints(seen, "seen", n, device), cache, rec, pr, pt, pl, outr, work.data_ptr(), bytes_)
     return out
 
 
@@ -863,13 +864,13 @@ def mass_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lengths: torc
     cshape = _slots_of(k_cache, "k_cache", n, kshape[1], d, dtype, device)
     at = _attention_packed(dtype, d, q_heads, kshape[1], cshape[2], scale)
     cache, rec = _cache_packed(k_cache, v_cache, cshape, dtype, device), _records_packed(mass, positions, cshape[:3], device)
-    pr, pl = _prior_packed(prior, shape, dtype, device)
+    pr, pt, pl = _prior_packed(prior, shape, dtype, device)
     out = _new(q, shape, stream, True) if out is None else out
     outr = _more_rows(out, "out", shape, dtype, device)
     bytes_ = lib.sh_mass_decode_workspace_bytes(at, n)
     work = _new(q, bytes_, stream, False, torch.uint8)
     _launch("mass_decode", lib.sh_mass_decode, device, stream, at, n, qr, kr, vr, _ints(lengths, "lengths", n, device),
-            _ints(seen, "seen", n, device), cache, rec, pr, pl, outr, work.data_ptr(), bytes_)
+            _ints(seen, "seen", n, device), cache, rec, pr, pt, pl, outr, work.data_ptr(), bytes_)
     return out
 
 

@@ -1,12 +1,11 @@
 // The records of the cache with accumulated weights: mass[j] += sum over queries and heads of p_j, p_j = exp(s_j - log sum of the row).
 // Weights are only known when the row's sum is, so they are worked out after the attention has left those logs: single tokens from
-// the scores that it stored on its way (sh_mass_fold_kernel), prompts from queries and keys once more (the columns kernels).
+// the scores that it stored on its way (sh_mass_fold_kernel), prompts from queries and keys once more (the columns kernels; the one for 16-bit types is in sh_mass_columns.cu).
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
 #include <algorithm>
 
-#include "sh_elem.cuh"
 #include "sh_mass.h"
 #include "sh_pairs.cuh"
 #include "sh_umma.cuh"
@@ -16,12 +15,11 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-using shelem::Vec;
 using shumma::ex2_approx;
 using namespace shpair;
 using namespace shwin;
 
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
+constexpr float LOG2E = 1.4426950408889634f;
 
 // ---------------------------------------------------------------------------------------------------------------- single tokens
 constexpr int FOLD = 128, EACH = 4;      // threads, slots of a thread
@@ -54,37 +52,13 @@ __global__ void __launch_bounds__(FOLD) sh_mass_fold_kernel(const __grid_constan
 }
 
 // ---------------------------------------------------------------------------------------------------------------- prompts
-// A row continues from the prior's: out = (out 2^l + prior 2^pl) / (2^l + 2^pl).  The attention's rows are rounded to the type before
-// (half a step of their share), the result once more; D / N lanes a row.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) sh_mass_join_kernel(const __grid_constant__ WindowParams p) {
-    constexpr int N = Vec<T>::N, CH = D / N;
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int c = (int)(id % CH), h = (int)(id / CH % p.hq);
-    const long long tok = id / CH / p.hq;
-    int seq, first, count, cached;
-    const bool mine = tok < p.tokens && sequence_of<ATTEND_MASS>(p, tok, seq, first, count, cached);
-    float *lse = p.lse + tok * p.hq + h;
-    const float pl = mine ? p.prior_lse[tok * p.hq + h] * LOG2E : 0.f, l = mine ? *lse * LOG2E : 0.f;
-    __syncwarp();                        // (a row's lanes have read its log before one of them renews it)
-    if (!mine || pl == -CUDART_INF_F) return;
-    const float top = fmaxf(l, pl), f = ex2_approx(l - top), g = ex2_approx(pl - top), sum = f + g;
-    uint4 *out = reinterpret_cast<uint4 *>(p.out.p + tok * p.out.ts + h * p.out.hs) + c;
-    float x[N], y[N];
-    Vec<T>::unpack(*out, x);
-    Vec<T>::unpack(*(reinterpret_cast<const uint4 *>(p.prior.p + tok * p.prior.ts + h * p.prior.hs) + c), y);
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = (x[e] * f + y[e] * g) / sum;
-    *out = Vec<T>::pack(x);
-    if (c == 0) *lse = LN2 * (top + log2f(sum));
-}
+constexpr int CNT = 256, BK = 64, BQ = 64;      // threads, keys and rows of a tile
 
 // Blocks of BK slots of a sequence that takes part, over all key heads; one warp, all lanes.  The first blocks of a sequence see most
 // queries and come first.
 struct Keys {
     int seq, first, count, cached, slot0;      // seq < 0: no such block
 };
-template <int BK>
 __device__ __forceinline__ Keys find_keys(const WindowParams &p, long long tile) {
     const int lane = threadIdx.x & 31;
     Keys r = {-1, 0, 0, 0, 0};
@@ -114,15 +88,14 @@ __device__ __forceinline__ Keys find_keys(const WindowParams &p, long long tile)
     return r;
 }
 
-// On CUDA cores: a cluster of S CTAs takes 64 keys, its CTAs take the row tiles (64 rows of token x head of the group) in turn; a thread
+// fp32, on CUDA cores: a cluster of S CTAs takes 64 keys, its CTAs take the row tiles (64 rows of token x head of the group) in turn; a thread
 // works on 4 keys x 4 rows and keeps its keys' sums; threads, then CTAs, are added up in a fixed order.
-constexpr int CNT = 256, BK = 64, BQ = 64;
 template <int D> struct Cols {
     static constexpr int LD = D + 4, BYTES = (BK + BQ) * LD * 4;
 };
-template <typename T, int D>
-__global__ void __launch_bounds__(CNT) sh_mass_columns_simt_kernel(const __grid_constant__ WindowParams p) {
-    constexpr int LD = Cols<D>::LD, N = Vec<T>::N, CH = D / N;
+template <int D>
+__global__ void __launch_bounds__(CNT) sh_mass_columns_f32_kernel(const __grid_constant__ WindowParams p) {
+    constexpr int LD = Cols<D>::LD, CH = D / 4;
     extern __shared__ __align__(16) float sm[];
     float *Ks = sm, *Qs = sm + BK * LD;
     __shared__ float log_of[BQ], red[16][BK], part[BK];
@@ -134,7 +107,7 @@ __global__ void __launch_bounds__(CNT) sh_mass_columns_simt_kernel(const __grid_
     for (long long item = blockIdx.x / S;; item += gridDim.x / S) {
         const int kvh = (int)(item % p.hk);
         if (tid < 32) {
-            const Keys k = find_keys<BK>(p, item / p.hk);
+            const Keys k = find_keys(p, item / p.hk);
             if (tid == 0) keys_sh = k;
         }
         __syncthreads();
@@ -143,20 +116,18 @@ __global__ void __launch_bounds__(CNT) sh_mass_columns_simt_kernel(const __grid_
         const int n = w.cached + w.count, rows = w.count * p.g;
         for (int i = tid; i < BK * CH; i += CNT) {
             const int r = i / CH, c = i % CH;
-            float x[N] = {};
-            if (w.slot0 + r < n) Vec<T>::unpack(*reinterpret_cast<const uint4 *>(p.kc + w.seq * p.css + kvh * p.chs + (long long)(w.slot0 + r) * p.cls + c * 16), x);
-#pragma unroll
-            for (int e = 0; e < N; ++e) Ks[r * LD + c * N + e] = x[e];
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (w.slot0 + r < n) x = *reinterpret_cast<const uint4 *>(p.kc + w.seq * p.css + kvh * p.chs + (long long)(w.slot0 + r) * p.cls + c * 16);
+            *reinterpret_cast<uint4 *>(Ks + r * LD + c * 4) = x;
         }
         float acc[4] = {};
         for (int base = max(0, w.slot0 - w.cached) * p.g + rank * BQ; base < rows; base += S * BQ) {
             __syncthreads();
             for (int i = tid; i < BQ * CH; i += CNT) {
                 const int r = i / CH, c = i % CH, row = base + r;
-                float x[N] = {};
-                if (row < rows) Vec<T>::unpack(*reinterpret_cast<const uint4 *>(p.q.p + (long long)(w.first + row / p.g) * p.q.ts + (kvh * p.g + row % p.g) * p.q.hs + c * 16), x);
-#pragma unroll
-                for (int e = 0; e < N; ++e) Qs[r * LD + c * N + e] = x[e];
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (row < rows) x = *reinterpret_cast<const uint4 *>(p.q.p + (long long)(w.first + row / p.g) * p.q.ts + (kvh * p.g + row % p.g) * p.q.hs + c * 16);
+                *reinterpret_cast<uint4 *>(Qs + r * LD + c * 4) = x;
             }
             if (tid < BQ) {
                 const int row = base + tid;
@@ -209,9 +180,9 @@ __global__ void __launch_bounds__(CNT) sh_mass_columns_simt_kernel(const __grid_
     }
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t launch_columns(const WindowParams &p, cudaStream_t s) {
-    auto kern = sh_mass_columns_simt_kernel<T, D>;
+    auto kern = sh_mass_columns_f32_kernel<D>;
     static ShKernelSetup setup;
     int sms = 0;
     const cudaError_t e = sh_setup_kernel(setup, kern, Cols<D>::BYTES, &sms);
@@ -233,14 +204,6 @@ cudaError_t launch_columns(const WindowParams &p, cudaStream_t s) {
     return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
-template <typename T, int D>
-cudaError_t launch_join(const WindowParams &p, cudaStream_t s) {
-    const long long blocks = ((long long)p.tokens * p.hq * (D / Vec<T>::N) + 255) / 256;
-    if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
-    sh_mass_join_kernel<T, D><<<(unsigned)blocks, 256, 0, s>>>(p);
-    return cudaGetLastError();
-}
-
 }  // namespace
 
 cudaError_t sh_launch_mass_fold(const WindowParams &p, cudaStream_t s) {
@@ -258,14 +221,4 @@ cudaError_t sh_launch_mass_fold(const WindowParams &p, cudaStream_t s) {
     return cudaLaunchKernelEx(&cfg, sh_mass_fold_kernel, p, (int)blocks);
 }
 
-cudaError_t sh_launch_mass_join(const WindowParams &p, int dtype, int D, cudaStream_t s) {
-    if (dtype == SH_F32) return D == 128 ? launch_join<float, 128>(p, s) : launch_join<float, 64>(p, s);
-    if (dtype == SH_F16) return D == 128 ? launch_join<__half, 128>(p, s) : launch_join<__half, 64>(p, s);
-    return D == 128 ? launch_join<__nv_bfloat16, 128>(p, s) : launch_join<__nv_bfloat16, 64>(p, s);
-}
-
-cudaError_t sh_launch_mass_columns(const WindowParams &p, int dtype, int D, cudaStream_t s) {
-    if (dtype == SH_F32) return D == 128 ? launch_columns<float, 128>(p, s) : launch_columns<float, 64>(p, s);
-    if (dtype == SH_F16) return D == 128 ? launch_columns<__half, 128>(p, s) : launch_columns<__half, 64>(p, s);
-    return D == 128 ? launch_columns<__nv_bfloat16, 128>(p, s) : launch_columns<__nv_bfloat16, 64>(p, s);
-}
+cudaError_t sh_launch_mass_columns_f32(const WindowParams &p, int D, cudaStream_t s) { return D == 128 ? launch_columns<128>(p, s) : launch_columns<64>(p, s); }

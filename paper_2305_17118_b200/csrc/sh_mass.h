@@ -27,7 +27,8 @@ cudaError_t sh_launch_mass_evict(const EvictParams &p, cudaStream_t s);
 
 // Single tokens: add the step's weights to the masses, from the scores and totals that the attention has left.
 cudaError_t sh_launch_mass_fold(const WindowParams &p, cudaStream_t s);
-// Prompts: let finished rows continue from the prior's (outputs and logs of their sums).
-cudaError_t sh_launch_mass_join(const WindowParams &p, int dtype, int D, cudaStream_t s);
 // Prompts: add the weights of the chunk's rows to the masses of the keys they see; the chunk is in the cache already.
-cudaError_t sh_launch_mass_columns(const WindowParams &p, int dtype, int D, cudaStream_t s);
+cudaError_t sh_launch_mass_columns_f32(const WindowParams &p, int D, cudaStream_t s);
+cudaError_t sh_launch_mass_columns_umma(const WindowParams &p, int dtype, int D, cudaStream_t s);      // f16 and bf16
+// as sh_window_error_take
+cudaError_t sh_mass_error_take(int *code, cudaStream_t s);

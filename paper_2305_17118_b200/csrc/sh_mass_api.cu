@@ -30,9 +30,16 @@ void fill_records(WindowParams &p, const sh_records *r, int sequences) {
     const MassRecords m = records(r, p.hk, sequences);
     p.mass = m.mass; p.held = m.positions; p.rss = m.ss; p.rhs = m.hs;
 }
-// A prior: rows like the queries and the logs of their sums, both or neither.
-bool good_prior(const sh_rows *r, const float *lse, int tokens, int heads, int D, int es) {
-    return r ? rows_in(r, tokens, heads, D, es) && lse && ((uintptr_t)lse & 3) == 0 : lse == nullptr;
+// A prior: rows like the queries, or in fp32, and the logs of their sums, both or neither.
+bool good_prior(const sh_rows *r, int dtype, const float *lse, const sh_attention *a, int tokens) {
+    if (!r) return lse == nullptr;
+    return (dtype == SH_F32 || dtype == a->dtype) && rows_in(r, tokens, a->q_heads, a->head_dim, elem_size(dtype)) && lse && ((uintptr_t)lse & 3) == 0;
+}
+void fill_prior(WindowParams &p, const sh_rows *r, int dtype, const float *lse, const sh_attention *a, int tokens) {
+    if (!r) return;
+    p.prior = rows(r, tokens, a->q_heads, a->head_dim, elem_size(dtype));
+    p.prior_lse = lse;
+    p.prior_f32 = dtype == SH_F32;
 }
 size_t up(size_t x, size_t to) { return (x + to - 1) / to * to; }
 long long score_stride(const sh_attention *a) { return ((long long)a->slots + 15) / 16 * 16; }
@@ -49,12 +56,12 @@ size_t sh_context_attention_workspace_bytes(const sh_attention *a, int tokens, i
 }
 
 int sh_context_attention(const sh_attention *a, int tokens, int contexts, const sh_rows *q, const sh_window_cache *context, const int32_t *starts_dev,
-                         const int32_t *lengths_dev, const sh_rows *out, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream) {
-    if (!good_attention(a) || tokens < 0 || tokens >= MAX_POS || contexts < 0) return SH_EINVAL;
+                         const int32_t *lengths_dev, const sh_rows *out, int out_dtype, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream) {
+    if (!good_attention(a) || (out_dtype != SH_F32 && out_dtype != a->dtype) || tokens < 0 || tokens >= MAX_POS || contexts < 0) return SH_EINVAL;
     if (!starts_dev && contexts != 1 && contexts != tokens) return SH_EINVAL;
     if (tokens == 0 || contexts == 0) return SH_OK;
     const int D = a->head_dim, es = elem_size(a->dtype);
-    if (!rows_in(q, tokens, a->q_heads, D, es) || !rows_out(out, tokens, a->q_heads, D, es) || !cache_in(context, a->kv_heads, D, es, a->slots, contexts) ||
+    if (!rows_in(q, tokens, a->q_heads, D, es) || !rows_out(out, tokens, a->q_heads, D, elem_size(out_dtype)) || !cache_in(context, a->kv_heads, D, es, a->slots, contexts) ||
         (starts_dev && !good_ints(starts_dev)) || (lengths_dev && !good_ints(lengths_dev)) || !lse_dev || ((uintptr_t)lse_dev & 3))
         return SH_EINVAL;
     const sh_window w = as_window(a);
@@ -62,7 +69,8 @@ int sh_context_attention(const sh_attention *a, int tokens, int contexts, const 
     fill_window(p, &w, context, contexts);
     p.tokens = tokens;
     p.q = rows(q, tokens, a->q_heads, D, es);
-    p.out = rows(out, tokens, a->q_heads, D, es);
+    p.out = rows(out, tokens, a->q_heads, D, elem_size(out_dtype));
+    p.out_f32 = out_dtype == SH_F32;
     p.starts = starts_dev; p.lengths = lengths_dev;
     p.lse = lse_dev;
     if (workspace_dev) {
@@ -85,14 +93,14 @@ size_t sh_mass_prefill_workspace_bytes(const sh_attention *a, int tokens, int se
 }
 
 int sh_mass_prefill(const sh_attention *a, int tokens, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *starts_dev,
-                    const int32_t *lengths_dev, const int32_t *seen_dev, const sh_window_cache *cache, const sh_records *rec, const sh_rows *prior,
+                    const int32_t *lengths_dev, const int32_t *seen_dev, const sh_window_cache *cache, const sh_records *rec, const sh_rows *prior, int prior_dtype,
                     const float *prior_lse_dev, const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream) {
     if (!good_attention(a) || tokens < 0 || tokens >= MAX_POS || sequences < 0) return SH_EINVAL;
     if (tokens == 0 || sequences == 0) return SH_OK;
     const int D = a->head_dim, es = elem_size(a->dtype);
     const sh_window w = as_window(a);
     if (!rows_in(q, tokens, a->q_heads, D, es) || !rows_in(k, tokens, a->kv_heads, D, es) || !rows_in(v, tokens, a->kv_heads, D, es) ||
-        !rows_out(out, tokens, a->q_heads, D, es) || !good_prior(prior, prior_lse_dev, tokens, a->q_heads, D, es) || !good_cache(cache, &w, sequences) ||
+        !rows_out(out, tokens, a->q_heads, D, es) || !good_prior(prior, prior_dtype, prior_lse_dev, a, tokens) || !good_cache(cache, &w, sequences) ||
         !good_records(rec, a->slots, a->kv_heads, sequences) || !good_ints(starts_dev) || !good_ints(lengths_dev) || !good_ints(seen_dev) ||
         !aligned16(workspace_dev))
         return SH_EINVAL;
@@ -111,15 +119,11 @@ int sh_mass_prefill(const sh_attention *a, int tokens, int sequences, const sh_r
     const size_t lse_bytes = up(sizeof(float) * (size_t)tokens * a->q_heads, 256);
     if (need > lse_bytes) p.part = static_cast<float *>(workspace_dev);
     p.lse = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + need - lse_bytes);
-    if (prior) {
-        p.prior = rows(prior, tokens, a->q_heads, D, es);
-        p.prior_lse = prior_lse_dev;
-    }
+    fill_prior(p, prior, prior_dtype, prior_lse_dev, a, tokens);
     const cudaStream_t s = (cudaStream_t)stream;
     cudaError_t e = a->dtype == SH_F32 ? sh_launch_window_prefill_f32(p, D, ATTEND_MASS, s) : sh_launch_window_prefill_umma(p, a->dtype, D, ATTEND_MASS, s);
     if (e == cudaSuccess) e = sh_launch_window_append(p, es, D, ATTEND_MASS, s);
-    if (e == cudaSuccess && prior) e = sh_launch_mass_join(p, a->dtype, D, s);
-    if (e == cudaSuccess) e = sh_launch_mass_columns(p, a->dtype, D, s);
+    if (e == cudaSuccess) e = a->dtype == SH_F32 ? sh_launch_mass_columns_f32(p, D, s) : sh_launch_mass_columns_umma(p, a->dtype, D, s);
     return done(e);
 }
 
@@ -130,14 +134,14 @@ size_t sh_mass_decode_workspace_bytes(const sh_attention *a, int sequences) {
 }
 
 int sh_mass_decode(const sh_attention *a, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *lengths_dev,
-                   const int32_t *seen_dev, const sh_window_cache *cache, const sh_records *rec, const sh_rows *prior, const float *prior_lse_dev,
-                   const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream) {
+                   const int32_t *seen_dev, const sh_window_cache *cache, const sh_records *rec, const sh_rows *prior, int prior_dtype,
+                   const float *prior_lse_dev, const sh_rows *out, void *workspace_dev, size_t workspace_bytes, void *stream) {
     if (!good_attention(a) || sequences < 0) return SH_EINVAL;
     if (sequences == 0) return SH_OK;
     const int D = a->head_dim, es = elem_size(a->dtype);
     const sh_window w = as_window(a);
     if (!rows_in(q, sequences, a->q_heads, D, es) || !rows_in(k, sequences, a->kv_heads, D, es) || !rows_in(v, sequences, a->kv_heads, D, es) ||
-        !rows_out(out, sequences, a->q_heads, D, es) || !good_prior(prior, prior_lse_dev, sequences, a->q_heads, D, es) || !good_cache(cache, &w, sequences) ||
+        !rows_out(out, sequences, a->q_heads, D, es) || !good_prior(prior, prior_dtype, prior_lse_dev, a, sequences) || !good_cache(cache, &w, sequences) ||
         !good_records(rec, a->slots, a->kv_heads, sequences) || !good_ints(lengths_dev) || !good_ints(seen_dev) || !aligned16(workspace_dev))
         return SH_EINVAL;
     const size_t need = sh_mass_decode_workspace_bytes(a, sequences);
@@ -156,10 +160,7 @@ int sh_mass_decode(const sh_attention *a, int sequences, const sh_rows *q, const
     p.score_stride = score_stride(a);
     p.scores = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + part);
     p.total = p.scores + (size_t)sequences * p.hq * p.score_stride;
-    if (prior) {
-        p.prior = rows(prior, sequences, a->q_heads, D, es);
-        p.prior_lse = prior_lse_dev;
-    }
+    fill_prior(p, prior, prior_dtype, prior_lse_dev, a, sequences);
     const cudaStream_t s = (cudaStream_t)stream;
     cudaError_t e = sh_launch_window_decode(p, a->dtype, D, ATTEND_MASS, s);
     if (e == cudaSuccess) e = sh_launch_mass_fold(p, s);

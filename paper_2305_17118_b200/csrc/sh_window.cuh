@@ -1,5 +1,9 @@
 // Device helpers of the window cache kernels: which rows a tile holds and which positions a block of keys has.
 #pragma once
+#include <math_constants.h>
+
+#include "sh_elem.cuh"
+#include "sh_umma.cuh"
 #include "sh_window.h"
 
 namespace shwin {
@@ -102,5 +106,52 @@ struct Ring {
         return x < head && y > sinks && cached - head + min(y, head) - 1 >= oldest;
     }
 };
+
+// The end of a row: its unnormalised output times `own`, plus the prior's row times `other` (0: there is none, or it has seen nothing, and
+// its row does not matter).  `total`: the log (base 2) of the sum of exponentials that this is divided by.
+struct Close {
+    float own, other, total;
+};
+// `base` + log2(L) is the log of the row's own sum.
+template <int MODE>
+__device__ __forceinline__ Close close_row(const WindowParams &p, long long token, int h, float base, float L) {
+    Close r = {1.f / L, 0.f, 0.f};
+    if (MODE == ATTEND_MASS && p.prior_lse) {
+        const float pl = p.prior_lse[token * p.hq + h] * 1.4426950408889634f;
+        if (pl != -CUDART_INF_F) {
+            const float top = fmaxf(base, pl), f = shumma::ex2_approx(base - top), g = shumma::ex2_approx(pl - top);
+            L = fmaf(L, f, g);
+            r.own = f / L;
+            r.other = g / L;
+            base = top;
+        }
+    }
+    if (MODE != ATTEND_WINDOW) r.total = base + log2f(L);
+    return r;
+}
+// N elements of the prior's row, from d on.
+template <typename T, int N>
+__device__ __forceinline__ void prior_row(const WindowParams &p, long long token, int h, int d, float (&y)[N]) {
+    const char *row = p.prior.p + token * p.prior.ts + h * p.prior.hs;
+    if (p.prior_f32) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) shelem::Vec<float>::unpack(*reinterpret_cast<const uint4 *>(row + (d + i) * 4), y + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += shelem::Vec<T>::N) shelem::Vec<T>::unpack(*reinterpret_cast<const uint4 *>(row + (d + i) * (int)sizeof(T)), y + i);
+    }
+}
+// N elements of a row of `out`, from d on.
+template <typename T, int MODE, int N>
+__device__ __forceinline__ void store_row(const WindowParams &p, long long token, int h, int d, const float (&x)[N]) {
+    char *row = p.out.p + token * p.out.ts + h * p.out.hs;
+    if (MODE == ATTEND_CONTEXT && p.out_f32) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *reinterpret_cast<uint4 *>(row + (d + i) * 4) = shelem::Vec<float>::pack(x + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += shelem::Vec<T>::N) *reinterpret_cast<uint4 *>(row + (d + i) * (int)sizeof(T)) = shelem::Vec<T>::pack(x + i);
+    }
+}
 
 }  // namespace shwin

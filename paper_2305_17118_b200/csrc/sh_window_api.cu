@@ -1,5 +1,6 @@
 // Entry points of the query/key preparation and of the window cache: argument checks and parameter blocks.
 #include "sh_args.h"
+#include "sh_mass.h"
 
 namespace {
 
@@ -160,8 +161,9 @@ int sh_window_decode(const sh_window *w, int sequences, const sh_rows *q, const 
 
 int sh_window_status(void *stream) {
     int code = 0;
-    if (sh_window_error_take(&code, (cudaStream_t)stream) != cudaSuccess) return SH_ECUDA;
-    return code ? SH_EDEVICE : SH_OK;
+    int other = 0;      // (of the cache with accumulated weights)
+    if (sh_window_error_take(&code, (cudaStream_t)stream) != cudaSuccess || sh_mass_error_take(&other, (cudaStream_t)stream) != cudaSuccess) return SH_ECUDA;
+    return code || other ? SH_EDEVICE : SH_OK;
 }
 
 }  // extern "C"

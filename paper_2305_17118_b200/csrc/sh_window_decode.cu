@@ -103,30 +103,21 @@ __device__ __forceinline__ int rows_before(const WindowParams &p, int seq) {
 }
 
 // The last step for N elements of a row, from d on: `base` + log2(L) is the log of its sum, x its unnormalised output.  Over a cache with
-// accumulated weights the row continues from the prior's, if there is one, and leaves that log; a context's goes to the caller.
+// accumulated weights the row continues from the prior's, if there is one, and leaves that log for the masses; a context's goes to the caller.
 template <typename T, int MODE, int N>
-__device__ __forceinline__ void close_row(const WindowParams &p, int seq, int h, int d, float base, float L, bool empty, float (&x)[N]) {
-    const long long at = (long long)seq * p.hq + h;
-    if (MODE == ATTEND_MASS && p.prior_lse) {
-        const float pl = p.prior_lse[at] * 1.4426950408889634f;
-        if (pl != -CUDART_INF_F) {                                  // (nothing was seen there: its row does not matter)
-            const float top = fmaxf(base, pl), f = ex2_approx(base - top), g = ex2_approx(pl - top);
-            const char *row = p.prior.p + seq * p.prior.ts + h * p.prior.hs + d * (int)sizeof(T);
-            L = fmaf(L, f, g);
+__device__ __forceinline__ void finish(const WindowParams &p, int seq, int h, int d, float base, float L, bool empty, float (&x)[N]) {
+    if constexpr (MODE == ATTEND_WINDOW) {
 #pragma unroll
-            for (int i = 0; i < N; i += Vec<T>::N) {
-                float y[Vec<T>::N];
-                Vec<T>::unpack(*reinterpret_cast<const uint4 *>(row + i * (int)sizeof(T)), y);
+        for (int e = 0; e < N; ++e) x[e] /= L;
+    } else {
+        const Close c = close_row<MODE>(p, seq, h, base, L);
+        if (MODE == ATTEND_MASS && d == 0) p.total[(long long)seq * p.hq + h] = c.total;
+        if (MODE == ATTEND_CONTEXT && d == 0) p.lse[(long long)seq * p.hq + h] = empty ? -CUDART_INF_F : 0.69314718055994531f * c.total;
+        float y[N] = {};
+        if (c.other != 0.f) prior_row<T>(p, seq, h, d, y);
 #pragma unroll
-                for (int e = 0; e < Vec<T>::N; ++e) x[i + e] = fmaf(y[e], g, x[i + e] * f);
-            }
-            base = top;
-        }
+        for (int e = 0; e < N; ++e) x[e] = MODE == ATTEND_CONTEXT && empty ? 0.f : fmaf(y[e], c.other, x[e] * c.own);
     }
-    if (MODE == ATTEND_MASS && d == 0) p.total[at] = base + log2f(L);
-    if (MODE == ATTEND_CONTEXT && d == 0) p.lse[at] = empty ? -CUDART_INF_F : 0.69314718055994531f * (base + log2f(L));
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = MODE == ATTEND_CONTEXT && empty ? 0.f : x[e] / L;
 }
 
 template <typename T, int D, int GQ, int MODE>
@@ -291,8 +282,8 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
 #pragma unroll
             for (int e = 0; e < N; ++e) x[e] = fmaf(c[2 + d + e], f, x[e]);
         }
-        close_row<T, MODE>(p, seq, h0 + q, d, M, L, live == 0, x);
-        *reinterpret_cast<uint4 *>(p.out.p + seq * p.out.ts + (h0 + q) * p.out.hs + d * (int)sizeof(T)) = Vec<T>::pack(x);
+        finish<T, MODE>(p, seq, h0 + q, d, M, L, live == 0, x);
+        store_row<T, MODE>(p, seq, h0 + q, d, x);
     }
     cluster.sync();      // nobody's shared memory goes away while it is read
 }
@@ -369,8 +360,7 @@ template <typename T> __device__ __forceinline__ void split2(float x, float y, u
 // One query by the D / 8 lanes that finish it: every live row once, in fp32.  x: this lane's 8 elements of the prepared query; fresh: key and
 // value rows that stand for those of slot snew (NULL: they are in the cache already).
 template <typename T, int D, int MODE>
-__device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, int h, int live, int snew, const unsigned char *fresh, const float4 x0, const float4 x1,
-                                       char *dst) {
+__device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, int h, int live, int snew, const unsigned char *fresh, const float4 x0, const float4 x1) {
     constexpr int CHUNKS = D / 8;
     const int c = threadIdx.x % CHUNKS;
     const unsigned group = ((1u << CHUNKS) - 1u) << ((threadIdx.x & 31) & ~(CHUNKS - 1));
@@ -395,8 +385,8 @@ __device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, 
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = fmaf(w, v[e], o[e] * keep);
     }
-    close_row<T, MODE>(p, seq, h, c * 8, m, l, false, o);
-    *reinterpret_cast<uint4 *>(dst + c * 16) = Vec<T>::pack(o);
+    finish<T, MODE>(p, seq, h, c * 8, m, l, false, o);
+    store_row<T, MODE>(p, seq, h, c * 8, o);
 }
 
 template <typename T, int D, int MW, int MODE>
@@ -599,10 +589,9 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
             for (int e = 0; e < 8; ++e) acc[e] = fmaf(c[2 + d + e], f, acc[e]);
         }
         bool odd = false;
-        close_row<T, MODE>(p, seq, h0 + q, d, M - Weights<T>::LIFT, L, live == 0, acc);
+        finish<T, MODE>(p, seq, h0 + q, d, M - Weights<T>::LIFT, L, live == 0, acc);
 #pragma unroll
         for (int e = 0; e < 8; ++e) odd |= !isfinite(acc[e]);
-        char *dst = p.out.p + seq * p.out.ts + (h0 + q) * p.out.hs;
         // the low part of a weight or of a query may be zero and meet an infinity: such rows are computed again in plain fp32
         float hi[8], lo[8];
         Vec<T>::unpack(*reinterpret_cast<const uint4 *>(sm + C::OFF_Q + q * C::ROW + (((d / 8) ^ (q & 7)) << 4)), hi);
@@ -612,9 +601,9 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
         const float4 x0 = make_float4(hi[0], hi[1], hi[2], hi[3]), x1 = make_float4(hi[4], hi[5], hi[6], hi[7]);
         const unsigned group = ((1u << CHUNKS) - 1u) << (lane & ~(CHUNKS - 1));
         if (__any_sync(group, odd))
-            plain_row<T, D, MODE>(p, seq, kvh, h0 + q, live, snew, MODE == ATTEND_CONTEXT ? nullptr : sm + C::OFF_NEW, x0, x1, dst);
+            plain_row<T, D, MODE>(p, seq, kvh, h0 + q, live, snew, MODE == ATTEND_CONTEXT ? nullptr : sm + C::OFF_NEW, x0, x1);
         else
-            *reinterpret_cast<uint4 *>(dst + d * 2) = Vec<T>::pack(acc);
+            store_row<T, MODE>(p, seq, h0 + q, d, acc);
     }
     cluster.sync();                                   // nobody's shared memory goes away while it is read
 }
@@ -670,15 +659,14 @@ __global__ void __launch_bounds__(SLICES * D / 8) sh_window_decode_merge_kernel(
         acc[e] = x;
     }
     const int h = kvh * p.g + qb * MQ + q;
-    close_row<T, MODE>(p, seq, h, c * 8, M - Weights<T>::LIFT, L, t == 0, acc);
+    finish<T, MODE>(p, seq, h, c * 8, M - Weights<T>::LIFT, L, t == 0, acc);
 #pragma unroll
     for (int e = 0; e < 8; ++e) odd |= !isfinite(acc[e]);
-    char *dst = p.out.p + seq * p.out.ts + (long long)h * p.out.hs;
     if (__any_sync((1u << CHUNKS) - 1u, odd)) {
         const float4 *x = reinterpret_cast<const float4 *>(p.part + units * parts * REC + unit * (MQ * D) + q * D + c * 8);
-        plain_row<T, D, MODE>(p, seq, kvh, h, MODE == ATTEND_CONTEXT ? t : min(t + 1, p.sinks + p.window), 0, nullptr, x[0], x[1], dst);
+        plain_row<T, D, MODE>(p, seq, kvh, h, MODE == ATTEND_CONTEXT ? t : min(t + 1, p.sinks + p.window), 0, nullptr, x[0], x[1]);
     } else {
-        *reinterpret_cast<uint4 *>(dst + c * 16) = Vec<T>::pack(acc);
+        store_row<T, MODE>(p, seq, h, c * 8, acc);
     }
 }
 

@@ -217,19 +217,29 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
 #pragma unroll
         for (int off = 8; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
         if (qp[a] < 0) continue;
-        if (MODE != ATTEND_WINDOW && tx == 0) {
-            const long long row = t.row0 + ty * R + a;
-            p.lse[(t.first + row / p.g) * p.hq + kvh * p.g + (int)(row % p.g)] = 0.69314718055994531f * (m[a] + log2f(sum));
-        }
-        if (MODE == ATTEND_CONTEXT && blocks == 0) sum = 1.f;         // no rows: zeros
         const long long row = t.row0 + ty * R + a, tok = t.first + row / p.g;
-        float *dst = reinterpret_cast<float *>(p.out.p + tok * p.out.ts + (kvh * p.g + (int)(row % p.g)) * p.out.hs);
+        const int h = kvh * p.g + (int)(row % p.g);
+        Close end = {};
+        if constexpr (MODE != ATTEND_WINDOW) {
+            end = close_row<MODE>(p, tok, h, m[a], sum);
+            if (tx == 0) p.lse[tok * p.hq + h] = 0.69314718055994531f * end.total;
+            if (MODE == ATTEND_CONTEXT && blocks == 0) end.own = 1.f;      // no rows: zeros
+        }
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
             float x[4];
             un2(o[a][2 * c], x[0], x[1]);
             un2(o[a][2 * c + 1], x[2], x[3]);
-            *reinterpret_cast<float4 *>(dst + c * 64 + tx * 4) = make_float4(x[0] / sum, x[1] / sum, x[2] / sum, x[3] / sum);
+            if constexpr (MODE == ATTEND_WINDOW) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] /= sum;
+            } else {
+                float y[4] = {};
+                if (end.other != 0.f) prior_row<float>(p, tok, h, c * 64 + tx * 4, y);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = fmaf(y[e], end.other, x[e] * end.own);
+            }
+            store_row<float, MODE>(p, tok, h, c * 64 + tx * 4, x);
         }
     }
 }

@@ -45,13 +45,13 @@
 // quarter of the SM; with the exponentials left out it took 1600.  A part of the exponentials on the FMA
 // pipe (a quarter of them by a polynomial) gained nothing at this register split: 473 against 482 us for the 8192 tokens.
 // Items of few steps pay for their ends: 8192 tokens with window 1024 (18 steps an item) run at 850 TFLOP/s, with window 256 at 485.
-#include <cuda.h>
 #include <math_constants.h>
 
 #include <algorithm>
 
 #include "sh_elem.cuh"
 #include "sh_pairs.cuh"
+#include "sh_tiles.cuh"
 #include "sh_umma.cuh"
 #include "sh_window.cuh"
 
@@ -59,6 +59,7 @@ namespace {
 
 using namespace shasync;
 using namespace shpair;
+using namespace shtile;
 using namespace shumma;
 using namespace shwin;
 
@@ -167,8 +168,6 @@ template <int D> __device__ __forceinline__ float4 *part_o(const UmmaParams &p, 
 template <int D> __device__ __forceinline__ float2 *part_sum(const UmmaParams &p, int id, int t) { return reinterpret_cast<float2 *>(p.w.part + MAX_SHARE * 2 * TM * D) + (id * 2 + t) * TM; }
 template <int D> __device__ __forceinline__ int4 *part_item(const UmmaParams &p) { return reinterpret_cast<int4 *>(p.w.part + MAX_SHARE * 2 * TM * (D + 2)); }
 
-__device__ __forceinline__ uint64_t desc_sw128(uint32_t saddr, uint32_t lbo, uint32_t sbo) { return smem_desc(saddr, lbo, sbo) | (2ull << 61); }
-
 __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
@@ -176,24 +175,6 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
         "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
-}
-__device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, uint32_t *r) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr));
-}
-// Wait for this thread's tensor-memory loads; the values pass through the asm, so that no use of them moves before the wait.
-template <int N>
-__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[N]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
 }
 __device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, uint32_t *r) {
     asm volatile(
@@ -213,25 +194,12 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-__device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *map, int c0, int c1, int c2, uint64_t *bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-                     smem_u32(dst)),
-                 "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
-                 : "memory");
-}
 // Key and value tiles: the halves of a row are the outermost dimension of the map, so one copy brings both.
 __device__ __forceinline__ void tma_4d(void *dst, const CUtensorMap *map, int head, int token, uint64_t *bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
             smem_u32(dst)),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(head), "r"(token), "r"(0), "r"(smem_u32(bar))
-        : "memory");
-}
-__device__ __forceinline__ void tma_5d(void *dst, const CUtensorMap *map, int slot, int head, int sequence, uint64_t *bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
-            smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(slot), "r"(head), "r"(sequence), "r"(0), "r"(smem_u32(bar))
         : "memory");
 }
 // Cluster launch control: the grid has a CTA for every item, and a running CTA takes over the item of one that has not started yet.
@@ -263,17 +231,6 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, const void 
                  "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(src))
                  : "memory");
 }
-// One lane of the warp, which must be converged.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "elect.sync _|p, 0xffffffff;\n\t"
-        "selp.b32 %0, 1, 0, p;\n\t}"
-        : "=r"(p));
-    return p != 0;
-}
-
 // One work item and the key tiles it has to walk over.  Tiles 0 .. ctiles - 1 are blocks of TN cache slots, tile ctiles + j holds the
 // chunk's rows TN * j ...
 struct Item : Ring {
@@ -439,10 +396,23 @@ __device__ __noinline__ void slow_row(const UmmaParams &u, int id, int qi, int h
             for (int e = 0; e < E; ++e) o[e] = fmaf(e1, (float)vr[e], o[e] * keep);
         }
     }
-    T *dst = reinterpret_cast<T *>(p.out.p + (long long)(w.first + qi) * p.out.ts + h * p.out.hs) + lane * E;
+    char *dst = p.out.p + (long long)(w.first + qi) * p.out.ts + h * p.out.hs;
+    if constexpr (MODE == ATTEND_WINDOW) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) dst[e] = (T)(o[e] / l);
-    if (MODE != ATTEND_WINDOW && lane == 0) *lse_of(p, w.first + qi, h) = LN2 * (m + log2f(l));
+        for (int e = 0; e < E; ++e) reinterpret_cast<T *>(dst)[lane * E + e] = (T)(o[e] / l);
+    } else {
+        const Close end = close_row<MODE>(p, w.first + qi, h, m, l);
+        if (lane == 0) *lse_of(p, w.first + qi, h) = LN2 * end.total;
+        const char *prior = p.prior.p + (long long)(w.first + qi) * p.prior.ts + h * p.prior.hs;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int d = lane * E + e;
+            const float y = end.other == 0.f ? 0.f : (p.prior_f32 ? reinterpret_cast<const float *>(prior)[d] : (float)reinterpret_cast<const T *>(prior)[d]);
+            const float x = fmaf(y, end.other, o[e] * end.own);
+            if (MODE == ATTEND_CONTEXT && p.out_f32) reinterpret_cast<float *>(dst)[d] = x;
+            else reinterpret_cast<T *>(dst)[d] = (T)x;
+        }
+    }
 }
 
 // Note rows of a softmax warp that have to be computed again, and do them.  (Calls, as inlined they cost the loop over the steps
@@ -938,8 +908,8 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             }
             if (!begun) {                             // (a query tile without rows)
                 if (MODE == ATTEND_CONTEXT && live) { // (a context without rows)
-                    uint4 *dst = reinterpret_cast<uint4 *>(p.w.out.p + (long long)(row0 + qi) * p.w.out.ts + (long long)(kvh * p.w.g + h) * p.w.out.hs);
-                    for (int i = 0; i < D / 8; ++i) dst[i] = make_uint4(0, 0, 0, 0);
+                    const float none[8] = {};
+                    for (int i = 0; i < D; i += 8) store_row<T, MODE>(p.w, row0 + qi, kvh * p.w.g + h, i, none);
                     *lse_of(p.w, row0 + qi, kvh * p.w.g + h) = -CUDART_INF_F;
                 }
                 __syncwarp();
@@ -949,8 +919,35 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             ok = wait_for(bars, &bars->pv_done[t][(cnt - 1) & 1], ((cnt - 1) >> 1) & 1, 0x623);
             if (__any_sync(0xffffffffu, !ok)) break;
             tc_fence_after();
-            const float inv = 1.f / l;
-            if (MODE != ATTEND_WINDOW && live) *lse_of(p.w, row0 + qi, kvh * p.w.g + h) = LN2 * (m * c - Fmt<T>::LIFT + log2f(l));
+            float inv = 1.f / l, other = 0.f;         // (of the row's own output, of the prior's)
+            if (MODE != ATTEND_WINDOW && live) {
+                const Close end = close_row<MODE>(p.w, row0 + qi, kvh * p.w.g + h, m * c - Fmt<T>::LIFT, l);
+                *lse_of(p.w, row0 + qi, kvh * p.w.g + h) = LN2 * end.total;
+                inv = end.own;
+                other = end.other;
+            }
+            if (MODE == ATTEND_CONTEXT && p.w.out_f32) {      // fp32 rows leave by their threads
+                float zero = 0.f;
+#pragma unroll
+                for (int b = 0; b < D / 32; ++b) {
+                    uint32_t o[32];
+                    tmem_ld32_nowait(o_addr + b * 32, o);
+                    tmem_wait_ld(o);
+                    float x[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        x[k] = __uint_as_float(o[k]) * inv;
+                        zero = fmaf(x[k], 0.f, zero);
+                    }
+                    if (live) store_row<T, MODE>(p.w, row0 + qi, kvh * p.w.g + h, b * 32, x);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->q_free[t][qbuf]);
+                const unsigned again = __ballot_sync(0xffffffffu, live && !(zero == 0.f));
+                if (again) note_again(bars, warp, id, again);
+                continue;
+            }
             // the rows of O, one per thread, are laid out in the place of the item's queries (every S of the item is over), like a
             // query tile, and a warp's 32 rows leave from there as one copy if they are whole tokens; rows next to somebody else's,
             // or that have to be done again, go by the threads, in whole lines
@@ -971,6 +968,12 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
                         const uint64_t y = mul2(f2(__uint_as_float(o[k + e]), __uint_as_float(o[k + e + 1])), inv2);
                         zero = fma2(y, 0, zero);
                         un2(y, x[e], x[e + 1]);
+                    }
+                    if (MODE == ATTEND_MASS && other != 0.f) {      // (a prior that is not finite needs no second look at the keys)
+                        float y[8];
+                        prior_row<T>(p.w, row0 + qi, kvh * p.w.g + h, b * 32 + k, y);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = fmaf(y[e], other, x[e]);
                     }
                     *reinterpret_cast<uint4 *>(place + b / 2 * QHALF + row * 128 + (((b % 2 * 4 + k / 8) ^ (row & 7)) << 4)) = shelem::Vec<T>::pack(x);
                 }
@@ -1051,14 +1054,27 @@ __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __
         L += s.y * f;
         o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
     }
-    const float inv = 1.f / L;                       // (as where there is nothing to merge)
-    if (MODE != ATTEND_WINDOW && live && c4 == 0) *lse_of(p.w, w.y + tok, kvh * p.w.g + h) = LN2 * (M + log2f(L));
+    float inv = 1.f / L;                             // (as where there is nothing to merge)
+    float4 prior = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (MODE != ATTEND_WINDOW && live) {
+        const Close end = close_row<MODE>(p.w, w.y + tok, kvh * p.w.g + h, M, L);
+        if (c4 == 0) *lse_of(p.w, w.y + tok, kvh * p.w.g + h) = LN2 * end.total;
+        inv = end.own;
+        if (end.other != 0.f) {
+            const char *row = p.w.prior.p + (long long)(w.y + tok) * p.w.prior.ts + (kvh * p.w.g + h) * p.w.prior.hs;
+            float *y = &prior.x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = end.other * (p.w.prior_f32 ? reinterpret_cast<const float *>(row)[c4 * 4 + e] : (float)reinterpret_cast<const T *>(row)[c4 * 4 + e]);
+        }
+    }
     o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
     if (live && !(isfinite(o.x) && isfinite(o.y) && isfinite(o.z) && isfinite(o.w))) odd[r] = 1;
     __syncthreads();
+    o.x += prior.x; o.y += prior.y; o.z += prior.z; o.w += prior.w;
     if (live && !odd[r]) {
-        T *dst = reinterpret_cast<T *>(p.w.out.p + (long long)(w.y + tok) * p.w.out.ts + (kvh * p.w.g + h) * p.w.out.hs) + c4 * 4;
-        *reinterpret_cast<uint2 *>(dst) = make_uint2(shelem::Vec<T>::pack2(o.x, o.y), shelem::Vec<T>::pack2(o.z, o.w));
+        char *row = p.w.out.p + (long long)(w.y + tok) * p.w.out.ts + (kvh * p.w.g + h) * p.w.out.hs;
+        if (MODE == ATTEND_CONTEXT && p.w.out_f32) reinterpret_cast<float4 *>(row)[c4] = o;
+        else *reinterpret_cast<uint2 *>(row + c4 * 8) = make_uint2(shelem::Vec<T>::pack2(o.x, o.y), shelem::Vec<T>::pack2(o.z, o.w));
     }
     for (int i = tid >> 5; i < ROWS; i += D / 16) {  // rows next to values that are not finite
         if (!odd[i]) continue;
@@ -1067,37 +1083,6 @@ __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __
     }
 }
 
-typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's tensor-map encoder, looked up through the runtime (the library does not link against the driver).
-EncodeTiled encoder() {
-    static EncodeTiled fn = [] {
-        void *sym = nullptr;
-        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
-            sym = nullptr;
-        return reinterpret_cast<EncodeTiled>(sym);
-    }();
-    return fn;
-}
-
-// Map over rows of 16-bit elements, 64 of them innermost: dims and byte strides of what lies outside of them, the box's extents
-// there; 128-byte swizzle, zeros outside the tensor.
-bool make_map(CUtensorMap *m, const void *base, int outer, const uint64_t *dim, const uint64_t *stride, const uint32_t *extent, uint64_t inner = 64) {
-    EncodeTiled enc = encoder();
-    if (!enc) return false;
-    cuuint64_t gdim[5] = {inner}, gstride[4];
-    cuuint32_t box[5] = {64u}, one[5] = {1u, 1u, 1u, 1u, 1u};
-    for (int i = 0; i < outer; ++i) {
-        gdim[i + 1] = dim[i];
-        gstride[i] = stride[i];
-        box[i + 1] = extent[i];
-    }
-    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, outer + 1, const_cast<void *>(base), gdim, gstride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 // [half][token][head][64]: all halves of TN tokens of one head are one copy
 bool keys_map(CUtensorMap *m, const WinRows &r, int heads, int tokens, uint64_t halves) {
     const uint64_t dim[3] = {(uint64_t)heads, (uint64_t)tokens, halves}, st[3] = {(uint64_t)r.hs, (uint64_t)r.ts, 128};

@@ -51,10 +51,9 @@ def chain(x):
     return (x["keys"] / 16 + 64) * 2.0 ** -23
 
 
-def out_tolerance(x, dtype, parts, lift, joined=0.0):
-    """joined: roundings of the row before a prior joined it (0 or 1)."""
+def out_tolerance(x, dtype, parts, lift, out_dtype=None):
     half = ref.half_step(dtype)
-    tol = ref.rounding(x["out"], dtype) + (logit_error(x, dtype) + chain(x)) * (x["mass"] + x["out"].abs()) + joined * half * x["mass"]
+    tol = ref.rounding(x["out"], out_dtype or dtype) + (logit_error(x, dtype) + chain(x)) * (x["mass"] + x["out"].abs())
     if dtype != torch.float32:
         tol = tol + half ** parts * x["mass"]
     if dtype == torch.float16:

@@ -36,7 +36,7 @@ def _check_context(q, k, v, ranges, lengths, out, lse, dtype, kind, scale=None):
             assert (out[a:b] == 0).all() and (lse[a:b] == -INF).all()
             continue
         x = mr.attend(q[a:b], k[i, :, :n].transpose(0, 1), v[i, :, :n].transpose(0, 1), torch.ones(b - a, n, dtype=torch.bool), scale)
-        ref.check(out[a:b], x["out"], mr.out_tolerance(x, dtype, **kind), f"context {i}")
+        ref.check(out[a:b], x["out"], mr.out_tolerance(x, dtype, out_dtype=out.dtype, **kind), f"context {i}")
         ref.check(lse[a:b], x["lse"], mr.lse_tolerance(x, dtype), f"lse of context {i}")
 
 
@@ -50,8 +50,10 @@ def test_one_token_of_each_context(dtype, d, hk, g, rows, lengths):
     q, k, v = rnd(n, hk * g, d, dtype=dt), rnd(n, hk, rows, d, dtype=dt), rnd(n, hk, rows, d, dtype=dt)
     for i, x in enumerate(lengths):                              # what lies behind a context is not looked at
         k[i, :, max(x, 0):], v[i, :, max(x, 0):] = NAN, INF
-    out, lse = sh.context_attention(q, k, v, lengths=_i32(lengths))
-    _check_context(q, k, v, [(i, i + 1) for i in range(n)], lengths, out, lse, dt, STEP)
+    for partial in (False, True):
+        out, lse = sh.context_attention(q, k, v, lengths=_i32(lengths), partial=partial)
+        assert out.dtype == (torch.float32 if partial else dt)
+        _check_context(q, k, v, [(i, i + 1) for i in range(n)], lengths, out, lse, dt, STEP)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
@@ -78,6 +80,8 @@ def test_prompts_over_contexts(dtype, d, hk, g, rows, counts, lengths):
     for x in (out, lse):
         assert (x[:before] == 7).all() and (x[total - behind:] == 7).all()
     fresh = sh.context_attention(q, k, v, _i32(starts), _i32(lengths), scale=0.2)
+    part = sh.context_attention(q, k, v, _i32(starts), _i32(lengths), scale=0.2, partial=True)
+    _check_context(q, k, v, list(zip(starts, starts[1:])), lengths, *part, dt, PROMPT, 0.2)
     assert torch.equal(fresh[0][before:total - behind], out[before:total - behind]) and (fresh[0][:before] == 0).all() and (fresh[1][:before] == -INF).all()
 
 
@@ -87,8 +91,9 @@ def test_a_shared_prefix(dtype, d, hk, g, rows, tokens):
     sh, rnd, dt = _sh(), _rnd(rows), DT[dtype]
     q, k, v = rnd(tokens, hk * g, d, dtype=dt), rnd(1, hk, rows, d, dtype=dt), rnd(1, hk, rows, d, dtype=dt)
     for lengths in ([rows], [rows - 7], [0]):
-        out, lse = sh.context_attention(q, k, v, lengths=_i32(lengths))
-        _check_context(q, k, v, [(0, tokens)], lengths, out, lse, dt, PROMPT)
+        for partial in (False, True):
+            out, lse = sh.context_attention(q, k, v, lengths=_i32(lengths), partial=partial)
+            _check_context(q, k, v, [(0, tokens)], lengths, out, lse, dt, PROMPT)
     whole = sh.context_attention(q, k, v)
     again = sh.context_attention(q, k, v, starts=_i32([0, tokens]))
     assert torch.equal(whole[0], again[0]) and torch.equal(whole[1], again[1])
@@ -123,7 +128,7 @@ def _check_sequence(old, new, i, c, rows, q, kn, vn, out, seen, g, dt, kind, pri
     assert torch.equal(positions[i, :, c:end], (seen + torch.arange(rows, dtype=torch.int32, device="cuda")).expand(hk, rows))
     sees = torch.arange(end)[None] <= torch.arange(c, end)[:, None]
     x = mr.attend(q, k[i, :, :end].transpose(0, 1), v[i, :, :end].transpose(0, 1), sees, scale, prior)
-    ref.check(out, x["out"], mr.out_tolerance(x, dt, joined=float(prior is not None and kind is PROMPT), **kind), f"sequence {i}")
+    ref.check(out, x["out"], mr.out_tolerance(x, dt, **kind), f"sequence {i}")
     before = old[2][i].T.double().cpu()[:end].clone()
     before[c:] = 0
     ref.check(mass[i, :, :end].T, before + mr.mass_of(x, g), mr.mass_tolerance(x, g, dt, before), f"mass of sequence {i}")
@@ -141,7 +146,7 @@ def test_single_tokens(dtype, d, hk, g, slots, held):
     q, kn, vn = packed[:, :hk * g], packed[:, hk * g:hk * (g + 1)], packed[:, hk * (g + 1):]
     seen = _i32([max(c, 0) * 2 + 5 for c in held])
     pk, pv = rnd(1, hk, 50, d, dtype=dt), rnd(1, hk, 50, d, dtype=dt)
-    for prior in (None, sh.context_attention(q, pk, pv)):
+    for prior in (None, sh.context_attention(q, pk, pv, partial=True), sh.context_attention(q, pk, pv)):
         old = _cache(_rnd(slots), n, hk, slots, d, dt, held)
         new = tuple(x.clone() for x in old[:2]) + _cache(_rnd(slots), n, hk, slots, d, dt, held)[2:]
         new[3].copy_(old[3])
@@ -173,7 +178,7 @@ def test_prompts(dtype, d, hk, g, slots, counts, held):
     q, kn, vn = packed[:, :hk * g], packed[:, hk * g:hk * (g + 1)], packed[:, hk * (g + 1):]
     seen = _i32([max(c, 0) * 2 + 5 for c in held])
     pk, pv = rnd(1, hk, 50, d, dtype=dt), rnd(1, hk, 50, d, dtype=dt)
-    for prior in (None, sh.context_attention(q, pk, pv)):
+    for prior in (None, sh.context_attention(q, pk, pv, partial=True), sh.context_attention(q, pk, pv)):
         old = _cache(_rnd(slots), n, hk, slots, d, dt, held)
         new = tuple(x.clone() for x in old[:2]) + _cache(_rnd(slots), n, hk, slots, d, dt, held)[2:]
         new[3].copy_(old[3])
@@ -241,7 +246,7 @@ def test_run_together(dtype):
     lengths, seen = _i32([0, 0, 0]), _i32([0, 0, 0])
     old = [x.clone() for x in state]
     q, kn, vn = rnd(83, hk * g, d, dtype=dt), rnd(83, hk, d, dtype=dt), rnd(83, hk, d, dtype=dt)
-    prior = sh.context_attention(q, pk, pv)
+    prior = sh.context_attention(q, pk, pv, partial=True)
     out = sh.mass_prefill(q, kn, vn, starts, lengths, *state, seen, prior=prior)
     a = 0
     for i, c in enumerate(counts):
@@ -266,7 +271,7 @@ def test_run_together(dtype):
                     newest = set(range(int(seen[i]) - min(recent, held[i]), int(seen[i])))
                     assert newest <= set(state[3][i, h, :held[i]].tolist())
         q, kn, vn = rnd(n, hk * g, d, dtype=dt), rnd(n, hk, d, dtype=dt), rnd(n, hk, d, dtype=dt)
-        prior = sh.context_attention(q, pk, pv)
+        prior = sh.context_attention(q, pk, pv, partial=True)
         old = [x.clone() for x in state]
         out = sh.mass_decode(q, kn, vn, lengths, *state, seen, prior=prior)
         for i in range(n):
