@@ -208,7 +208,7 @@ def _own_run(st):
         left = sh.mass_evict(st["k"], st["v"], st["mass"], st["positions"], st["lengths"], keep=case["keep"], recent=case["recent"])
         return left, st["k"], st["v"], st["mass"], st["positions"]
     if case["op"] == "step":
-        prior = sh.context_attention(st["q"], st["prefix_k"], st["prefix_v"]) if case["prefix"] else None
+        prior = sh.context_attention(st["q"], st["prefix_k"], st["prefix_v"], partial=True) if case["prefix"] else None
         sh.mass_decode(st["q"], st["k"], st["v"], st["lengths"], st["k_cache"], st["v_cache"], st["mass"], st["positions"], st["seen"],
                        prior=prior, out=st["out"])
     else:
