@@ -30,5 +30,6 @@ cudaError_t sh_launch_mass_fold(const WindowParams &p, cudaStream_t s);
 // Prompts: add the weights of the chunk's rows to the masses of the keys they see; the chunk is in the cache already.
 cudaError_t sh_launch_mass_columns_f32(const WindowParams &p, int D, cudaStream_t s);
 cudaError_t sh_launch_mass_columns_umma(const WindowParams &p, int dtype, int D, cudaStream_t s);      // f16 and bf16
+size_t sh_mass_columns_scratch(int tokens, int sequences, int hk, int g, int slots);      // bytes of `part` that either wants
 // as sh_window_error_take
 cudaError_t sh_mass_error_take(int *code, cudaStream_t s);

@@ -88,7 +88,10 @@ int sh_context_attention(const sh_attention *a, int tokens, int contexts, const 
 // The workspaces of the calls below: what their attention needs, then the logs and scores.
 size_t sh_mass_prefill_workspace_bytes(const sh_attention *a, int tokens, int sequences) {
     if (!good_attention(a) || tokens < 1 || tokens >= MAX_POS || sequences < 1) return 0;
-    return up(sh_window_prefill_scratch(tokens, sequences, a->kv_heads, a->q_heads / a->kv_heads, a->slots, 0, true, a->dtype, a->head_dim), 256) +
+    const int g = a->q_heads / a->kv_heads;
+    // (the columns kernel comes after the attention: they share a place)
+    return up(std::max(sh_window_prefill_scratch(tokens, sequences, a->kv_heads, g, a->slots, 0, true, a->dtype, a->head_dim),
+                       a->dtype == SH_F32 ? 0 : sh_mass_columns_scratch(tokens, sequences, a->kv_heads, g, a->slots)), 256) +
            up(sizeof(float) * (size_t)tokens * a->q_heads, 256);
 }
 
@@ -183,6 +186,7 @@ int sh_mass_evict(const sh_attention *a, int sequences, const int32_t *lengths_d
     if (!(into ? cache_in(cache, a->kv_heads, D, es, a->slots, sequences) : good_cache(cache, &w, sequences)) ||
         !good_records(rec, a->slots, a->kv_heads, sequences) || !good_ints(lengths_dev) || !good_ints(left_dev) || !aligned16(workspace_dev))
         return SH_EINVAL;
+    if (left_dev != lengths_dev && left_dev < lengths_dev + sequences && lengths_dev < left_dev + sequences) return SH_EINVAL;
     EvictParams p = {};
     WindowParams from = {}, to = {};
     fill_window(from, &w, cache, sequences);

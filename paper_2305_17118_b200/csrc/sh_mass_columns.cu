@@ -5,27 +5,25 @@
 // then owns a key, one lane of tensor memory, and its sum never leaves a register.  Nothing of size keys x rows leaves the SM.  The chunk is
 // in the cache already, so all keys come from there.
 //
-//   warps 0-3, 4-7   sums: thread = key; the two groups take the row tiles in turn.  S from tensor memory, exponentials, addition
-//   warp 8           issues the MMAs (both operands in shared memory, K-major)
-//   warp 9           finds the items (128 keys of a key head), publishes them in a ring and requests the tiles (TMA, 128-byte swizzle)
+//   warps 0-15       sums: thread = key; the four groups of four warps take the row tiles in turn.  S from tensor memory, exponentials, addition
+//   warp 16          issues the MMAs (both operands in shared memory, K-major)
+//   warp 17          finds the items (128 keys of a key head), publishes them in a ring and requests the tiles (TMA, 128-byte swizzle)
 //
 // Four buffers of S fill tensor memory.  The rows' logs are read from global memory two tiles ahead by the group that needs them, a thread
 // a row, and handed around in shared memory.  A CTA walks over items in a fixed order, from the ends of the list in turn (the first
-// key blocks of a sequence are seen by all its rows, the last by few); when there are fewer items than SMs, the CTAs of a cluster share an
-// item's row tiles and are added up in their order.  So results do not depend on the launch.
+// key blocks of a sequence are seen by all its rows, the last by few).  Where an item would be long against what an SM has to do in all, its
+// row tiles are dealt out to several items, whose sums a second launch adds up in their order: no atomics, the same result every time.
 //
 // Bound by the exponentials: a tile has 16384, at 16 a cycle on an SM, while its MMAs take 256 cycles (D = 128).
-#include <cooperative_groups.h>
 #include <math_constants.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "sh_mass.h"
 #include "sh_pairs.cuh"
 #include "sh_tiles.cuh"
 #include "sh_window.cuh"
-
-namespace cg = cooperative_groups;
 
 namespace {
 
@@ -37,7 +35,7 @@ using namespace shwin;
 
 constexpr int KEYS = 128, ROWS = 128;              // of a tile of S
 constexpr int HALF = 128 * 128;                    // bytes of a tile's rows x 64 elements
-constexpr int SUM_WARPS = 8, NTH = 384;            // (the last two warps only make whole warpgroups)
+constexpr int GROUPS = 4, SUM_WARPS = 4 * GROUPS, NTH = 32 * (SUM_WARPS + 2);
 constexpr int STAGES = 4, BUFS = 4, RING = 4;      // row tiles in flight, buffers of S, items in flight
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -45,14 +43,15 @@ __device__ int g_mass_error;                       // code of the first bounded 
 
 struct __align__(16) ColItem {
     int seq, first, count, cached;                 // seq < 0: the end
-    int slot0, kvh, tok0, tiles;                   // first key, key head, first token that sees it, row tiles of this CTA
+    int slot0, kvh, tok0, tiles;                   // first key, key head, first token that sees it, row tiles
+    int part, pad[3];
 };
 struct ColBars {
     uint64_t k_full[2], k_free[2], q_full[STAGES], q_free[STAGES], s_full[BUFS], s_free[BUFS], item_full[RING], item_free[RING];
-    uint64_t logs_full[2], part_full;              // a group's logs, an item's sums are there
+    uint64_t logs_full[GROUPS], part_full;              // a group's logs, an item's sums are there
     ColItem items[RING];
-    float logs[2][2][ROWS];                        // [group][tile mod 2]: minus the rows' logs, base 2
-    float part[2][2][KEYS];                        // [item mod 2][group]: sums
+    float logs[GROUPS][2][ROWS];                   // [group][its tile mod 2]: minus the rows' logs, base 2
+    float part[2][GROUPS][KEYS];                        // [item mod 2][group]: sums
     uint32_t tmem;
     int abort_flag;
 };
@@ -64,7 +63,8 @@ template <int D> struct ColCfg {
 struct ColParams {
     WindowParams w;
     int tpt, gb, hblocks;                          // tokens and heads of a row tile, head blocks per key head
-};
+    int parts;                                     // items that share the row tiles of 128 keys; more than one: they leave their sums in
+};                                                 // w.part, [part][sequence][key head][slot]
 
 constexpr unsigned long long LIMIT_NS = 8000000000ull;
 __device__ __forceinline__ bool wait_for(ColBars *bars, uint64_t *bar, uint32_t parity, int code) {
@@ -78,10 +78,10 @@ __device__ __forceinline__ bool wait_for(ColBars *bars, uint64_t *bar, uint32_t 
 // The n-th item of this CTA among all CTAs of the launch.
 __device__ __forceinline__ long long item_of(long long n, int cta, int ctas) { return n * ctas + (n & 1 ? ctas - 1 - cta : cta); }
 
-__device__ __forceinline__ ColItem find_item(const ColParams &p, long long id, int rank, int S) {
+__device__ __forceinline__ ColItem find_item(const ColParams &p, long long id) {
     ColItem r = {};
     const int lane = threadIdx.x & 31;
-    const long long tile = id / p.w.hk;
+    const long long tile = id / p.parts / p.w.hk;
     r.seq = -1;
     long long before = 0;
     for (int base = 0; base < p.w.sequences; base += 32) {
@@ -102,10 +102,11 @@ __device__ __forceinline__ ColItem find_item(const ColParams &p, long long id, i
             r.count = __shfl_sync(0xffffffffu, count, l);
             r.cached = __shfl_sync(0xffffffffu, cached, l);
             r.slot0 = (int)(tile - before - __shfl_sync(0xffffffffu, upto - mine, l)) * KEYS;
-            r.kvh = (int)(id % p.w.hk);
+            r.kvh = (int)(id / p.parts % p.w.hk);
+            r.part = (int)(id % p.parts);
             r.tok0 = max(0, r.slot0 - r.cached);
             const int all = (r.count - r.tok0 + p.tpt - 1) / p.tpt * p.hblocks;
-            r.tiles = (all - rank + S - 1) / S;
+            r.tiles = (all - r.part + p.parts - 1) / p.parts;
             return r;
         }
         before += __shfl_sync(0xffffffffu, upto, 31);
@@ -115,9 +116,16 @@ __device__ __forceinline__ ColItem find_item(const ColParams &p, long long id, i
 
 // Row tile n of an item: its first token (in the chunk), its first head, and how many of its rows there are.
 __device__ __forceinline__ void tile_of(const ColParams &p, const ColItem &w, int n, int &tok, int &h, int &rows) {
-    tok = w.tok0 + n / p.hblocks * p.tpt;
-    h = n % p.hblocks * p.gb;
-    rows = p.hblocks > 1 ? min(p.gb, p.w.g - h) : min(p.tpt, w.count - tok) * p.gb;      // (several blocks: a tile is one token)
+    n = n * p.parts + w.part;
+    if (p.hblocks > 1) {                           // a tile is one token
+        tok = w.tok0 + n / p.hblocks;
+        h = n % p.hblocks * p.gb;
+        rows = min(p.gb, p.w.g - h);
+    } else {
+        tok = w.tok0 + n * p.tpt;
+        h = 0;
+        rows = min(p.tpt, w.count - tok) * p.gb;
+    }
 }
 
 template <int FMT, int D>
@@ -126,8 +134,6 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
     using C = ColCfg<D>;
     extern __shared__ __align__(1024) unsigned char sm[];
     ColBars *bars = reinterpret_cast<ColBars *>(sm + C::OFF_BAR);
-    cg::cluster_group cluster = cg::this_cluster();
-    const int S = cluster.num_blocks(), rank = cluster.block_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     auto aborted = [&]() { return *(volatile int *)&bars->abort_flag != 0; };
     if (warp == 0) {
@@ -139,7 +145,8 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
         for (int i = 0; i < STAGES; ++i) { mbar_init(&bars->q_full[i], 1); mbar_init(&bars->q_free[i], 1); }
         for (int i = 0; i < BUFS; ++i) { mbar_init(&bars->s_full[i], 1); mbar_init(&bars->s_free[i], 4); }
         for (int i = 0; i < RING; ++i) { mbar_init(&bars->item_full[i], 1); mbar_init(&bars->item_free[i], SUM_WARPS + 1); }
-        mbar_init(&bars->logs_full[0], 4); mbar_init(&bars->logs_full[1], 4); mbar_init(&bars->part_full, SUM_WARPS);
+        for (int i = 0; i < GROUPS; ++i) mbar_init(&bars->logs_full[i], 4);
+        mbar_init(&bars->part_full, SUM_WARPS);
         bars->abort_flag = (smem_u32(sm) & 1023u) != 0 ? 0x630 : 0;      // the swizzled tiles need the alignment the declaration asks for
         fence_barrier_init();
     }
@@ -192,10 +199,7 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
         uint32_t it = 0, tiles = 0, loads = 0;
         bool more = true;
         while (ok && more) {
-            ColItem w = {};
-            w.seq = -1;
-            if (S == 1) w = find_item(p, item_of(it, blockIdx.x, gridDim.x), 0, 1);
-            else if (it == 0) w = find_item(p, blockIdx.x / S, rank, S);      // (a cluster has one item)
+            const ColItem w = find_item(p, item_of(it, blockIdx.x, gridDim.x));
             more = w.seq >= 0;
             ok = __all_sync(0xffffffffu, it < RING || wait_for(bars, &bars->item_free[it % RING], (it / RING - 1) & 1, 0x636));
             if (!ok) break;
@@ -220,7 +224,7 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
                 ok = __all_sync(0xffffffffu, (tiles < STAGES || wait_for(bars, &bars->q_free[st], (tiles / STAGES - 1) & 1, 0x638)) && !aborted());
                 if (!ok) break;
                 int tok, h, rows;
-                tile_of(p, w, n * S + rank, tok, h, rows);
+                tile_of(p, w, n, tok, h, rows);
                 if (elect_one()) {
                     mbar_arrive_expect_tx(&bars->q_full[st], q_bytes);
 #pragma unroll
@@ -238,7 +242,7 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
         __syncwarp();
     } else if (warp < SUM_WARPS) {
         // ------------------------------------------------------------------------------------------------ sums
-        const int grp = warp >> 2, key = tid & 127;
+        const int grp = warp >> 2, key = tid & 127, key_tok = key / p.gb, key_head = key % p.gb;      // (and of the row whose log it fetches)
         const uint32_t s_addr = tbase + ((uint32_t)((warp & 3) * 32) << 16);
         const float c = p.w.scale_log2e;
         const uint64_t c2 = f2(c, c);
@@ -257,28 +261,28 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
             auto log_of = [&](int n) {
                 int tok, h, rows;
                 if (n >= w.tiles) return 0.f;
-                tile_of(p, w, n * S + rank, tok, h, rows);
+                tile_of(p, w, n, tok, h, rows);
                 if (key >= rows) return 0.f;
-                return -LOG2E * p.w.lse[(long long)(w.first + tok + key / p.gb) * p.w.hq + w.kvh * p.w.g + h + key % p.gb];
+                return -LOG2E * p.w.lse[(long long)(w.first + tok + key_tok) * p.w.hq + w.kvh * p.w.g + h + key_head];
             };
             uint64_t sum0 = 0, sum1 = 0;
-            int n = (grp ^ tiles) & 1;                                   // this group takes the tiles of its parity, counted over the CTA
-            float mine = log_of(n), next = log_of(n + 2);
-            for (; n < w.tiles; n += 2) {
+            int n = (grp - (int)(tiles % GROUPS) + GROUPS) % GROUPS;     // this group takes every fourth tile, counted over the CTA
+            float mine = log_of(n), next = log_of(n + GROUPS);
+            for (; n < w.tiles; n += GROUPS) {
                 const uint32_t t = tiles + n, b = t % BUFS;
-                float *logs = bars->logs[grp][t >> 1 & 1];
+                float *logs = bars->logs[grp][t / GROUPS & 1];
                 logs[key] = mine;
                 mine = next;
-                next = log_of(n + 4);
+                next = log_of(n + 2 * GROUPS);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars->logs_full[grp]);
                 int tok, h, rows;
-                tile_of(p, w, n * S + rank, tok, h, rows);
+                tile_of(p, w, n, tok, h, rows);
                 const bool whole = rows == ROWS && w.slot0 + KEYS - 1 <= w.cached + tok;
                 // rows that see this key: from the token at its slot on
                 const int lo = p.hblocks > 1 ? (slot <= w.cached + tok ? 0 : ROWS) : max(0, slot - w.cached - tok) * p.gb;
                 // (whoever has passed the wait for its logs knows that the group is done with those of the tile before, whose place comes next)
-                ok = wait_for(bars, &bars->logs_full[grp], t >> 1 & 1, 0x63d) && wait_for(bars, &bars->s_full[b], t / BUFS & 1, 0x63c) && ok;
+                ok = wait_for(bars, &bars->logs_full[grp], t / GROUPS & 1, 0x63d) && wait_for(bars, &bars->s_full[b], t / BUFS & 1, 0x63c) && ok;
                 if (__any_sync(0xffffffffu, !ok)) break;
                 tc_fence_after();
 #pragma unroll
@@ -322,37 +326,46 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
             float a, b;
             un2(add2(sum0, sum1), a, b);
             bars->part[turn][grp][key] = a + b;
-            if (S == 1) {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars->part_full);
-                ok = wait_for(bars, &bars->part_full, turn, 0x63e);
-                if (__any_sync(0xffffffffu, !ok)) break;
-                if (grp == (int)turn && slot < n_keys) p.w.mass[w.seq * p.w.rss + w.kvh * p.w.rhs + slot] += bars->part[turn][0][key] + bars->part[turn][1][key];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->part_full);
+            ok = wait_for(bars, &bars->part_full, turn, 0x63e);
+            if (__any_sync(0xffffffffu, !ok)) break;
+            if (grp == (int)(it % GROUPS) && slot < n_keys) {
+                const float x = (bars->part[turn][0][key] + bars->part[turn][1][key]) + (bars->part[turn][2][key] + bars->part[turn][3][key]);
+                if (p.parts == 1) p.w.mass[w.seq * p.w.rss + w.kvh * p.w.rhs + slot] += x;
+                else p.w.part[(((long long)w.part * p.w.sequences + w.seq) * p.w.hk + w.kvh) * p.w.slots + slot] = x;
             }
         }
         __syncwarp();
     }
     tc_fence_before();
     __syncthreads();
-    if (S > 1) {
-        cluster.sync();
-        const ColItem w = bars->items[0];
-        const bool fine = !aborted();
-        if (rank == 0 && fine && w.seq >= 0 && tid < KEYS && w.slot0 + tid < w.cached + w.count) {
-            float x = 0.f;
-            for (int r = 0; r < S; ++r) {
-                const float *part = cluster.map_shared_rank(&bars->part[0][0][0], r);
-                x += part[tid] + part[KEYS + tid];
-            }
-            p.w.mass[w.seq * p.w.rss + w.kvh * p.w.rhs + w.slot0 + tid] += x;
-        }
-        cluster.sync();                            // nobody's shared memory goes away while it is read
-    }
     if (tid == 0 && bars->abort_flag) atomicCAS(&g_mass_error, 0, bars->abort_flag);
     if (warp == 0) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512) : "memory");
     }
+}
+
+// The parts' sums, in their order.
+constexpr int ADD = 256;
+__global__ void __launch_bounds__(ADD) sh_mass_columns_add_kernel(const __grid_constant__ WindowParams p, int blocks, int parts) {
+    const int kvh = blockIdx.x / blocks % p.hk, seq = blockIdx.x / blocks / p.hk, slot = blockIdx.x % blocks * ADD + threadIdx.x;
+    int first, count, cached;
+    sequence_rows<ATTEND_MASS>(p, seq, first, count, cached);
+    sh_pdl_wait();
+    if (count == 0 || slot >= cached + count) return;
+    float x = 0.f;
+    for (int i = 0; i < parts; ++i) x += p.part[(((long long)i * p.sequences + seq) * p.hk + kvh) * p.slots + slot];
+    p.mass[seq * p.rss + kvh * p.rhs + slot] += x;
+}
+
+// How many items share the row tiles of a key block.  The longest item has the rows of all tokens if they are one sequence's; then an SM has
+// about `load` tiles in all (half of them are behind the diagonal), and an item should be a quarter of that.  Four tiles an item at least.
+int parts_of(int tokens, int sequences, int hk, int g, int slots) {
+    const double tiles = (double)tokens * g / ROWS, load = tiles * hk * ((double)tokens / KEYS + 1) / 2 / 148;
+    const double most = std::min(std::min(8.0, tiles / 4), (double)(64 << 20) / (4.0 * sequences * hk * slots));      // (64 MB of sums)
+    return (int)std::max(1.0, std::min(most, std::ceil(4 * tiles / std::max(load, 1.0))));
 }
 
 template <int FMT, int D>
@@ -374,20 +387,23 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     int sms = 0;
     const cudaError_t e = sh_setup_kernel(setup, kern, ColCfg<D>::SMEM, &sms);
     if (e != cudaSuccess) return e;
-    const long long items = (long long)std::min(w.sequences, w.tokens) * ((w.slots + KEYS - 1) / KEYS) * w.hk;      // at most
-    int S = 1;
-    while (S < 8 && items * S * 2 <= sms && (long long)w.tokens * w.g >= 2ll * S * ROWS) S *= 2;
+    p.parts = parts_of(w.tokens, w.sequences, w.hk, w.g, w.slots);
+    const long long items = (long long)std::min(w.sequences, w.tokens) * ((w.slots + KEYS - 1) / KEYS) * w.hk * p.parts;      // at most
+    kern<<<(unsigned)std::min<long long>(items, sms), NTH, ColCfg<D>::SMEM, s>>>(p, mq, mk);
+    const cudaError_t e2 = cudaGetLastError();
+    if (e2 != cudaSuccess || p.parts == 1) return e2;
+    const long long blocks = (w.slots + ADD - 1) / ADD;
+    if (blocks * w.sequences * w.hk > 0x7fffffffll) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(S > 1 ? items * S : std::min<long long>(items, sms)));
-    cfg.blockDim = dim3(NTH);
-    cfg.dynamicSmemBytes = ColCfg<D>::SMEM;
+    cfg.gridDim = dim3((unsigned)(blocks * w.sequences * w.hk));
+    cfg.blockDim = dim3(ADD);
     cfg.stream = s;
     cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = S; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kern, p, mq, mk);
+    return cudaLaunchKernelEx(&cfg, sh_mass_columns_add_kernel, w, (int)blocks, p.parts);
 }
 
 }  // namespace
@@ -404,4 +420,9 @@ cudaError_t sh_mass_error_take(int *code, cudaStream_t s) {
     static const int zero = 0;
     e = cudaMemcpyToSymbolAsync(g_mass_error, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, s);
     return e == cudaSuccess ? cudaStreamSynchronize(s) : e;
+}
+
+size_t sh_mass_columns_scratch(int tokens, int sequences, int hk, int g, int slots) {
+    const int parts = parts_of(tokens, sequences, hk, g, slots);
+    return parts > 1 ? sizeof(float) * parts * (size_t)sequences * hk * slots : 0;
 }

@@ -1,88 +1,212 @@
 // sh_mass_evict: of every (sequence, key head) keep the `recent` newest rows and those with the largest mass, `keep` in all.
 //
 // Rows are ordered by one 32-bit key: the newest come first, then masses from large to small (fp32 as an unsigned number of the same
-// order; NaN before everything else), among equal keys the lower slot.  The keep-th largest key is found by radix selection, 8 bits a pass
-// from the top; a last pass over the slots in order gives every row its place.  In place a survivor from behind slot keep - 1 moves into
-// the hole of a row that goes, the lowest hole taking the lowest of them, so no more rows move than go; into another cache survivors are
-// written in the order of their slots.  A second launch moves the rows.  Bound by HBM: the records are read once, moved rows read and written.
+// order; NaN before everything else), among equal keys the lower slot.  The keep-th largest key is searched for, then a pass over the slots in
+// order gives every row its place.  In place a survivor from behind slot keep - 1 moves into the hole of a row that goes, the lowest hole
+// taking the lowest of them, so no more rows move than go; into another cache survivors are written in the order of their slots.
+//
+// Short caches (1024 slots): a warp takes a unit, its keys in registers, and settles one bit of the key after the other by counting; no
+// barrier on the way.  Long ones: a cluster takes a unit and settles 8 bits at a time by histograms in shared memory, added up through
+// distributed shared memory.  Rows are moved by a second launch, with a CTA for 64 moves; many short units move their own.
+// Bound by HBM: the records are read once, moved rows read and written.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "sh_mass.h"
 
+namespace cg = cooperative_groups;
+
 namespace {
 
-constexpr int NT = 512, WARPS = NT / 32;
 constexpr unsigned NEWEST = 0xffffffffu, NOT_A_NUMBER = 0xfffffffeu;
-constexpr int MAX_KEYS = 48 * 1024;      // keys that are kept in shared memory; longer caches read the records again in every pass
 
+// Never 0: that stands for no row at all.
 __device__ __forceinline__ unsigned order_of(float x) {
     if (x != x) return NOT_A_NUMBER;
     const unsigned b = __float_as_uint(x + 0.f);      // (-0 counts as 0)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-
-// Sums over the CTA, for every thread; `sh` holds a word per warp.
-__device__ __forceinline__ int block_max(int x, int *sh) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
-    __syncthreads();
-    x = sh[0];
-#pragma unroll
-    for (int i = 1; i < WARPS; ++i) x = max(x, sh[i]);
-    return x;
+__device__ __forceinline__ unsigned key_of(const EvictParams &p, const float *mass, const int32_t *positions, int j, int newest) {
+    if (p.recent > 0 && (long long)positions[j] > (long long)newest - p.recent) return NEWEST;
+    return order_of(mass[j]);
 }
+
+// The rows of a unit (16-byte pieces) and their records, from slot m.y to slot m.x; `lanes` threads take them in turn, AHEAD of a thread's in flight.
+template <int AHEAD, typename Moves>
+__device__ __forceinline__ void move_rows(const EvictParams &p, int seq, int kvh, int count, int lane, int lanes, Moves move) {
+    const long long from = seq * p.ss + kvh * p.hs, to = seq * p.oss + kvh * p.ohs;
+    const int shift = p.row_bytes == 512 ? 5 : (p.row_bytes == 256 ? 4 : 3);      // log2 of a row's pieces
+    for (int i0 = lane; i0 < count << shift; i0 += lanes * AHEAD) {
+        uint4 a[AHEAD], b[AHEAD];
+        long long at[AHEAD];
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) {
+            const int i = i0 + x * lanes;
+            if (i >= count << shift) break;
+            const int2 m = move(i >> shift);
+            const int c = (i & ((1 << shift) - 1)) * 16;
+            a[x] = *reinterpret_cast<const uint4 *>(p.k + from + m.y * p.ls + c);
+            b[x] = *reinterpret_cast<const uint4 *>(p.v + from + m.y * p.ls + c);
+            at[x] = to + m.x * p.ols + c;
+        }
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x) {
+            if (i0 + x * lanes >= count << shift) break;
+            *reinterpret_cast<uint4 *>(p.ko + at[x]) = a[x];
+            *reinterpret_cast<uint4 *>(p.vo + at[x]) = b[x];
+        }
+    }
+    for (int i = lane; i < count; i += lanes) {
+        const int2 m = move(i);
+        const long long x = seq * p.rec.ss + kvh * p.rec.hs + m.y, y = seq * p.out.ss + kvh * p.out.hs + m.x;
+        p.out.mass[y] = p.rec.mass[x];
+        p.out.positions[y] = p.rec.positions[x];
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- short caches
+constexpr int SHORT = 1024, SHORT_WARPS = 4;
+
+template <int EACH>      // keys of a lane
+__global__ void __launch_bounds__(SHORT_WARPS * 32) sh_mass_select_short_kernel(const __grid_constant__ EvictParams p, int units, bool fused) {
+    __shared__ unsigned short holes_sh[SHORT_WARPS][EACH * 32], movers_sh[SHORT_WARPS][EACH * 32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int unit = blockIdx.x * SHORT_WARPS + warp, kvh = unit % p.heads, seq = unit / p.heads;
+    if (!fused) sh_pdl_launch_dependents();
+    if (unit >= units) return;
+    const int n = min(p.lengths[seq], p.slots);
+    unsigned short *holes = holes_sh[warp], *movers = movers_sh[warp];
+    int count = 0;                             // rows that move
+    const bool whole = n <= p.keep;            // nothing goes
+    if (whole) {
+        count = p.in_place ? 0 : max(n, 0);
+    } else {
+        const float *mass = p.rec.mass + seq * p.rec.ss + kvh * p.rec.hs;
+        const int32_t *positions = p.rec.positions + seq * p.rec.ss + kvh * p.rec.hs;
+        unsigned key[EACH];
+        int newest = 0x80000000;
+        if (p.recent > 0) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (i * 32 + lane < n) newest = max(newest, positions[i * 32 + lane]);
+            newest = __reduce_max_sync(0xffffffffu, newest);
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) key[i] = i * 32 + lane < n ? key_of(p, mass, positions, i * 32 + lane, newest) : 0u;
+        // the keep-th largest key, from its top bit down; done early where a bit parts the rows as wanted
+        unsigned at = 0;
+        bool parted = false;
+#pragma unroll 1
+        for (unsigned bit = 0x80000000u; bit && !parted; bit >>= 1) {
+            const unsigned next = at | bit;
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) c += key[i] >= next;
+            c = __reduce_add_sync(0xffffffffu, c);
+            if (c >= p.keep) at = next;
+            parted = c == p.keep;
+        }
+        int want = p.keep;                     // rows equal to it that stay, the lowest slots
+        {
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) c += key[i] > at;
+            want -= __reduce_add_sync(0xffffffffu, c);
+        }
+        int ties = 0, h = 0, m = 0;
+        const unsigned below = (1u << lane) - 1u;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int j = i * 32 + lane;
+            const bool tie = key[i] == at;
+            const unsigned tie_bits = __ballot_sync(0xffffffffu, tie);
+            const bool stays = key[i] > at || (tie && ties + __popc(tie_bits & below) < want);
+            ties += __popc(tie_bits);
+            const bool hole = p.in_place && j < p.keep && !stays, mover = stays && (!p.in_place || j >= p.keep);      // (keep < n)
+            const unsigned hole_bits = __ballot_sync(0xffffffffu, hole), mover_bits = __ballot_sync(0xffffffffu, mover);
+            if (hole) holes[h + __popc(hole_bits & below)] = (unsigned short)j;
+            if (mover) movers[m + __popc(mover_bits & below)] = (unsigned short)j;
+            h += __popc(hole_bits);
+            m += __popc(mover_bits);
+        }
+        count = m;                             // (as many holes in place: keep rows stay)
+        __syncwarp();
+    }
+    if (fused && kvh == 0 && lane == 0 && p.left != p.lengths) p.left[seq] = min(p.lengths[seq], p.keep);
+    auto move = [&](int i) { return whole ? make_int2(i, i) : make_int2(p.in_place ? holes[i] : i, movers[i]); };
+    if (fused) {
+        move_rows<4>(p, seq, kvh, count, lane, 32, move);
+        return;
+    }
+    if (lane == 0) p.count[unit] = count;
+    for (int i = lane; i < count; i += 32) p.moves[(long long)unit * p.most + i] = move(i);
+}
+
+// ---------------------------------------------------------------------------------------------------------------- long caches
+constexpr int NT = 1024, WARPS = NT / 32, MAX_CLUSTER = 8;
+constexpr int MAX_KEYS = 48 * 1024;      // keys that a CTA keeps in shared memory; beyond it the records are read again in every pass
 
 __global__ void __launch_bounds__(NT) sh_mass_select_kernel(const __grid_constant__ EvictParams p, int cached_keys) {
     extern __shared__ unsigned keys[];
-    __shared__ int hist[256], warp_sums[3][WARPS], found[3];
+    __shared__ int hist[4][256], sums[WARPS], found[2], newest_sh;
+    __shared__ int4 tally[WARPS];              // of a warp's rows: above the key below and from slot keep on, equal to it likewise
+    __shared__ int4 bases[WARPS * MAX_CLUSTER];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int S = cluster.num_blocks(), rank = cluster.block_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int unit = blockIdx.x, kvh = unit % p.heads, seq = unit / p.heads;
+    const int unit = blockIdx.x / S, kvh = unit % p.heads, seq = unit / p.heads;
     sh_pdl_launch_dependents();
     const int n = min(p.lengths[seq], p.slots);
-    if (n <= p.keep) {                         // nothing goes
-        if (tid == 0) p.count[unit] = p.in_place ? 0 : max(n, 0);
+    int2 *moves = p.moves + (long long)unit * p.most;
+    if (n <= p.keep) {                         // nothing goes (the same for the whole cluster)
+        if (tid == 0 && rank == 0) p.count[unit] = p.in_place ? 0 : max(n, 0);
         if (!p.in_place)
-            for (int i = tid; i < n; i += NT) p.moves[(long long)unit * p.most + i] = make_int2(i, i);
+            for (int i = rank * NT + tid; i < n; i += S * NT) moves[i] = make_int2(i, i);
         return;
     }
     const float *mass = p.rec.mass + seq * p.rec.ss + kvh * p.rec.hs;
     const int32_t *positions = p.rec.positions + seq * p.rec.ss + kvh * p.rec.hs;
+    const int each = (n + S * NT - 1) / (S * NT) * 32, per = each * WARPS;      // rows of a warp, of a CTA, in the order of their slots
+    const int lo = min(n, rank * per), hi = min(n, lo + per);
+    for (int i = tid; i < 4 * 256; i += NT) hist[i >> 8][i & 255] = 0;
     int newest = 0x80000000;
     if (p.recent > 0) {
-        for (int j = tid; j < n; j += NT) newest = max(newest, positions[j]);
-        newest = block_max(newest, warp_sums[0]);
+        for (int j = lo + tid; j < hi; j += NT) newest = max(newest, positions[j]);
+        newest = __reduce_max_sync(0xffffffffu, newest);
+        if (lane == 0) sums[warp] = newest;
+        __syncthreads();
+        if (warp == 0) {
+            newest = __reduce_max_sync(0xffffffffu, sums[lane]);
+            if (lane == 0) newest_sh = newest;
+        }
+        cluster.sync();
+        for (int r = 0; r < S; ++r) newest = max(newest, *cluster.map_shared_rank(&newest_sh, r));
     }
-    auto read_key = [&](int j) {
-        if (p.recent > 0 && (long long)positions[j] > (long long)newest - p.recent) return NEWEST;
-        return order_of(mass[j]);
-    };
     if (cached_keys)
-        for (int j = tid; j < n; j += NT) keys[j] = read_key(j);
-    auto key = [&](int j) { return cached_keys ? keys[j] : read_key(j); };
-    // the keep-th largest key: its top bits pass by pass
+        for (int j = lo + tid; j < hi; j += NT) keys[j - lo] = key_of(p, mass, positions, j, newest);
+    auto key = [&](int j) { return cached_keys ? keys[j - lo] : key_of(p, mass, positions, j, newest); };
+    __syncthreads();
+    // the keep-th largest key: 8 bits a pass
     unsigned prefix = 0, known = 0;
     int want = p.keep;                         // place of the key among those that share the known bits
 #pragma unroll 1
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += NT) hist[i] = 0;
-        __syncthreads();
-        for (int j0 = warp * 32; j0 < n; j0 += NT) {
-            const int j = j0 + lane;
-            const unsigned k = j < n ? key(j) : 0u;
-            const bool in = j < n && (k & known) == prefix;
-            const unsigned who = __ballot_sync(0xffffffffu, in);
-            if (in) {                          // one count for all lanes of the warp with the same digit
-                const unsigned same = __match_any_sync(who, (k >> shift) & 255u);
-                if (lane == __ffs(same) - 1) atomicAdd(&hist[(k >> shift) & 255u], __popc(same));
-            }
+    for (int pass = 0; pass < 4; ++pass) {
+        const int shift = 24 - 8 * pass;
+        for (int j = lo + tid; j < hi; j += NT) {
+            const unsigned k = key(j);
+            if ((k & known) == prefix) atomicAdd(&hist[pass][(k >> shift) & 255u], 1);
         }
-        __syncthreads();
+        cluster.sync();
         if (warp == 0) {                       // from the largest digit down: lane l has 8 of them
-            int mine[8], sum = 0;
+            int mine[8] = {}, sum = 0;
+            for (int r = 0; r < S; ++r) {
+                const int *h = cluster.map_shared_rank(&hist[pass][0], r);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { mine[i] = hist[255 - (lane * 8 + i)]; sum += mine[i]; }
+                for (int i = 0; i < 8; ++i) mine[i] += h[255 - (lane * 8 + i)];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += mine[i];
             int upto = sum;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -100,71 +224,112 @@ __global__ void __launch_bounds__(NT) sh_mass_select_kernel(const __grid_constan
         prefix |= (unsigned)found[0] << shift;
         known |= 255u << shift;
         want = found[1];
+        __syncthreads();
     }
-    // Slots in order: rows above the threshold stay, and the first `want` of those equal to it.
-    int equal = 0, holes = 0, movers = 0;      // so far; movers: rows that stay (another cache), or those of them behind the last kept slot
-    int2 *moves = p.moves + (long long)unit * p.most;
-    for (int j0 = 0; j0 < n; j0 += NT) {
-        const int j = j0 + tid;
-        const unsigned k = j < n ? key(j) : 0u;
-        const bool tie = j < n && k == prefix;
-        const unsigned ties = __ballot_sync(0xffffffffu, tie);
-        __syncthreads();
-        if (lane == 0) warp_sums[0][warp] = __popc(ties);
-        __syncthreads();
-        int before = equal, all = 0;
+    // Rows above that key stay, and the first `want` of those equal to it.  Every warp counts its own ...
+    const int from = lo + warp * each, to = min(hi, from + each);
+    int4 t = make_int4(0, 0, 0, 0);
+    for (int j = from + lane; j < to; j += 32) {
+        const unsigned k = key(j);
+        if (j < p.keep) { t.x += k > prefix; t.z += k == prefix; }
+        else { t.y += k > prefix; t.w += k == prefix; }
+    }
+    t = make_int4(__reduce_add_sync(0xffffffffu, t.x), __reduce_add_sync(0xffffffffu, t.y), __reduce_add_sync(0xffffffffu, t.z), __reduce_add_sync(0xffffffffu, t.w));
+    if (lane == 0) tally[warp] = t;
+    cluster.sync();
+    // ... and a warp of each CTA works out what comes before whom: rows equal to the key, holes, rows that move.  Lane l has S warps of the cluster.
+    if (warp == 0) {
+        auto of = [&](int w) { return *cluster.map_shared_rank(&tally[w % WARPS], w / WARPS); };
+        int ties = 0;
+        for (int i = 0; i < S; ++i) { const int4 x = of(lane * S + i); ties += x.z + x.w; }
+        int upto = ties;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            if (w < warp) before += warp_sums[0][w];
-            all += warp_sums[0][w];
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
         }
-        equal += all;
-        const bool stays = j < n && (k > prefix || (tie && before + __popc(ties & ((1u << lane) - 1u)) < want));
-        const bool hole = p.in_place && j < p.keep && !stays, mover = stays && (!p.in_place || j >= p.keep);
+        ties = upto - ties;
+        int h = 0, m = 0;
+        for (int i = 0; i < S; ++i) {          // (counted from this lane's first warp)
+            const int w = lane * S + i;
+            const int4 x = of(w);
+            const int low = min(max(want - ties, 0), x.z), high = min(max(want - ties - x.z, 0), x.w);      // equal ones that stay
+            bases[w] = make_int4(ties, h, m, 0);
+            ties += x.z + x.w;
+            h += min(max(min(n, p.keep) - w * each, 0), each) - (x.x + low);      // (slots below keep that this warp has)
+            m += x.y + high + (p.in_place ? 0 : x.x + low);
+        }
+        int h0 = h, m0 = m;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, h0, o), y = __shfl_up_sync(0xffffffffu, m0, o);
+            if (lane >= o) { h0 += x; m0 += y; }
+        }
+        if (lane == 31 && rank == 0) p.count[unit] = m0;
+        for (int i = 0; i < S; ++i) { bases[lane * S + i].y += h0 - h; bases[lane * S + i].z += m0 - m; }
+    }
+    __syncthreads();
+    int ties = bases[rank * WARPS + warp].x, h = bases[rank * WARPS + warp].y, m = bases[rank * WARPS + warp].z;
+    const unsigned below = (1u << lane) - 1u;
+    for (int j0 = from; j0 < to; j0 += 32) {
+        const int j = j0 + lane;
+        const unsigned k = j < to ? key(j) : 0u;
+        const bool tie = j < to && k == prefix;
+        const unsigned tie_bits = __ballot_sync(0xffffffffu, tie);
+        const bool stays = j < to && (k > prefix || (tie && ties + __popc(tie_bits & below) < want));
+        const bool hole = p.in_place && j < to && j < p.keep && !stays, mover = stays && (!p.in_place || j >= p.keep);
         const unsigned hole_bits = __ballot_sync(0xffffffffu, hole), mover_bits = __ballot_sync(0xffffffffu, mover);
-        if (lane == 0) { warp_sums[1][warp] = __popc(hole_bits); warp_sums[2][warp] = __popc(mover_bits); }
-        __syncthreads();
-        int h = holes, m = movers;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            if (w < warp) { h += warp_sums[1][w]; m += warp_sums[2][w]; }
-            holes += warp_sums[1][w];
-            movers += warp_sums[2][w];
-        }
-        const unsigned below = (1u << lane) - 1u;
         if (hole) moves[h + __popc(hole_bits & below)].x = j;
         if (mover) {
             const int at = m + __popc(mover_bits & below);
             moves[at].y = j;
             if (!p.in_place) moves[at].x = at;
         }
+        ties += __popc(tie_bits);
+        h += __popc(hole_bits);
+        m += __popc(mover_bits);
     }
-    if (tid == 0) p.count[unit] = movers;      // (as many holes as movers: keep rows stay)
+    cluster.sync();                            // nobody's shared memory goes away while it is read
 }
 
-// Lanes of 16 bytes move the rows: MOVE_WARPS * 32 threads take ROWS moves of a unit.
+// ---------------------------------------------------------------------------------------------------------------- moves
 constexpr int MOVE_NT = 256, ROWS = 64;
 __global__ void __launch_bounds__(MOVE_NT) sh_mass_move_kernel(const __grid_constant__ EvictParams p, int blocks) {
     const int unit = blockIdx.x / blocks, block = blockIdx.x % blocks, kvh = unit % p.heads, seq = unit / p.heads;
-    const int pieces = p.row_bytes / 16, tid = threadIdx.x;
     sh_pdl_wait();                             // (the moves)
-    if (block == 0 && kvh == 0 && tid == 0) p.left[seq] = min(p.lengths[seq], p.keep);      // (may be the place of the lengths: nobody reads them any more)
+    if (block == 0 && kvh == 0 && threadIdx.x == 0) p.left[seq] = min(p.lengths[seq], p.keep);      // (may be the place of the lengths: nobody else reads them any more)
     const int count = min(p.count[unit] - block * ROWS, ROWS);
     const int2 *moves = p.moves + (long long)unit * p.most + block * ROWS;
-    const long long from = seq * p.ss + kvh * p.hs, to = seq * p.oss + kvh * p.ohs;
-    for (int i = tid; i < count * pieces; i += MOVE_NT) {
-        const int2 m = moves[i / pieces];
-        const int c = i % pieces * 16;
-        const uint4 a = *reinterpret_cast<const uint4 *>(p.k + from + m.y * p.ls + c), b = *reinterpret_cast<const uint4 *>(p.v + from + m.y * p.ls + c);
-        *reinterpret_cast<uint4 *>(p.ko + to + m.x * p.ols + c) = a;
-        *reinterpret_cast<uint4 *>(p.vo + to + m.x * p.ols + c) = b;
-    }
-    for (int i = tid; i < count; i += MOVE_NT) {
-        const int2 m = moves[i];
-        const long long x = seq * p.rec.ss + kvh * p.rec.hs + m.y, y = seq * p.out.ss + kvh * p.out.hs + m.x;
-        p.out.mass[y] = p.rec.mass[x];
-        p.out.positions[y] = p.rec.positions[x];
-    }
+    move_rows<1>(p, seq, kvh, count, threadIdx.x, MOVE_NT, [&](int i) { return moves[i]; });
+}
+// Where the units have moved their rows themselves, and the new lengths take the place of the old ones.
+__global__ void sh_mass_left_kernel(const __grid_constant__ EvictParams p) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    sh_pdl_wait();
+    if (i < p.sequences) p.left[i] = min(p.lengths[i], p.keep);
+}
+
+template <typename... A>
+cudaError_t launch(void (*kern)(A...), unsigned ctas, int threads, size_t smem, cudaLaunchAttributeID id, int cluster, cudaStream_t s, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr = {};
+    attr.id = id;
+    if (id == cudaLaunchAttributeClusterDimension) { attr.val.clusterDim.x = cluster; attr.val.clusterDim.y = attr.val.clusterDim.z = 1; }
+    else attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+constexpr auto AFTER = cudaLaunchAttributeProgrammaticStreamSerialization;
+
+template <int EACH>
+cudaError_t select_short(const EvictParams &p, int units, bool fused, cudaStream_t s) {
+    sh_mass_select_short_kernel<EACH><<<(units + SHORT_WARPS - 1) / SHORT_WARPS, SHORT_WARPS * 32, 0, s>>>(p, units, fused);
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -172,24 +337,28 @@ __global__ void __launch_bounds__(MOVE_NT) sh_mass_move_kernel(const __grid_cons
 size_t sh_mass_evict_scratch(long long units, int most) { return (size_t)units * ((size_t)most * sizeof(int2) + sizeof(int)) + 16; }
 
 cudaError_t sh_launch_mass_evict(const EvictParams &p, cudaStream_t s) {
-    const long long units = (long long)p.sequences * p.heads, blocks = (p.most + ROWS - 1) / ROWS;
-    if (units * std::max(blocks, 1ll) > 0x7fffffffll) return cudaErrorInvalidValue;
-    static ShKernelSetup setup;
-    int sms = 0;
-    cudaError_t e = sh_setup_kernel(setup, sh_mass_select_kernel, MAX_KEYS * sizeof(unsigned), &sms);
+    const long long units = (long long)p.sequences * p.heads, blocks = std::max((p.most + ROWS - 1) / ROWS, 1);
+    if (units * blocks > 0x7fffffffll || units * MAX_CLUSTER > 0x7fffffffll) return cudaErrorInvalidValue;
+    int dev = 0, sms = 0;
+    cudaError_t e = sh_device_sms(&dev, &sms);
     if (e != cudaSuccess) return e;
-    const bool cached = p.slots <= MAX_KEYS;
-    sh_mass_select_kernel<<<(unsigned)units, NT, cached ? p.slots * sizeof(unsigned) : 0, s>>>(p, cached);
-    e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(units * std::max(blocks, 1ll)));
-    cfg.blockDim = dim3(MOVE_NT);
-    cfg.stream = s;
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, sh_mass_move_kernel, p, (int)std::max(blocks, 1ll));
+    if (p.slots <= SHORT) {
+        // a warp has few copies in flight: units move their own rows when there are several for each place of the device, or next to none to move
+        const bool fused = units >= 16ll * sms || p.most <= 4;
+        const int n = (int)units;
+        e = p.slots <= 128 ? select_short<4>(p, n, fused, s) : p.slots <= 256 ? select_short<8>(p, n, fused, s) : p.slots <= 512 ? select_short<16>(p, n, fused, s) : select_short<32>(p, n, fused, s);
+        if (e != cudaSuccess) return e;
+        if (fused) return p.left != p.lengths ? cudaSuccess : launch(sh_mass_left_kernel, (unsigned)((p.sequences + 127) / 128), 128, 0, AFTER, 0, s, p);
+    } else {
+        int S = 1;
+        while (S < MAX_CLUSTER && units * S * 2 <= 2ll * sms && p.slots >= 2 * S * NT) S *= 2;
+        const int most = (p.slots + S * NT - 1) / (S * NT) * NT;      // rows of a CTA
+        const bool cached = most <= MAX_KEYS;
+        static ShKernelSetup setup;
+        e = sh_setup_kernel(setup, sh_mass_select_kernel, MAX_KEYS * sizeof(unsigned), &sms);
+        if (e != cudaSuccess) return e;
+        e = launch(sh_mass_select_kernel, (unsigned)(units * S), NT, cached ? most * sizeof(unsigned) : 0, cudaLaunchAttributeClusterDimension, S, s, p, (int)cached);
+        if (e != cudaSuccess) return e;
+    }
+    return launch(sh_mass_move_kernel, (unsigned)(units * blocks), MOVE_NT, 0, AFTER, 0, s, p, (int)blocks);
 }
