@@ -5,8 +5,8 @@
 // order gives every row its place.  In place a survivor from behind slot keep - 1 moves into the hole of a row that goes, the lowest hole
 // taking the lowest of them, so no more rows move than go; into another cache survivors are written in the order of their slots.
 //
-// Short caches (1024 slots): a warp takes a unit, its keys in registers, and settles one bit of the key after the other by counting; no
-// barrier on the way.  Long ones: a cluster takes a unit and settles 8 bits at a time by histograms in shared memory, added up through
+// Short caches (1024 slots): a small CTA takes a unit, its keys in registers, and settles one bit of the key after the other by counting.
+// Long ones: a cluster takes a unit and settles 11 bits at a time by histograms in shared memory, added up through
 // distributed shared memory.  Rows are moved by a second launch, with a CTA for 64 moves; many short units move their own.
 // Bound by HBM: the records are read once, moved rows read and written.
 #include <cooperative_groups.h>
@@ -66,17 +66,16 @@ __device__ __forceinline__ void move_rows(const EvictParams &p, int seq, int kvh
 }
 
 // ---------------------------------------------------------------------------------------------------------------- short caches
-constexpr int SHORT = 1024, SHORT_WARPS = 4;
+constexpr int SHORT = 1024, SHORT_WARPS = 4, SHORT_NT = 32 * SHORT_WARPS;
 
-template <int EACH>      // keys of a lane
-__global__ void __launch_bounds__(SHORT_WARPS * 32) sh_mass_select_short_kernel(const __grid_constant__ EvictParams p, int units, bool fused) {
-    __shared__ unsigned short holes_sh[SHORT_WARPS][EACH * 32], movers_sh[SHORT_WARPS][EACH * 32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int unit = blockIdx.x * SHORT_WARPS + warp, kvh = unit % p.heads, seq = unit / p.heads;
+template <int EACH>      // keys of a thread; a warp has EACH * 32 neighbouring slots
+__global__ void __launch_bounds__(SHORT_NT) sh_mass_select_short_kernel(const __grid_constant__ EvictParams p, bool fused) {
+    __shared__ unsigned short holes[EACH * SHORT_NT], movers[EACH * SHORT_NT];
+    __shared__ int counts[2][SHORT_WARPS], ties_of[SHORT_WARPS], holes_of[SHORT_WARPS], movers_of[SHORT_WARPS];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int unit = blockIdx.x, kvh = unit % p.heads, seq = unit / p.heads;
     if (!fused) sh_pdl_launch_dependents();
-    if (unit >= units) return;
     const int n = min(p.lengths[seq], p.slots);
-    unsigned short *holes = holes_sh[warp], *movers = movers_sh[warp];
     int count = 0;                             // rows that move
     const bool whole = n <= p.keep;            // nothing goes
     if (whole) {
@@ -84,72 +83,138 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32) sh_mass_select_short_kernel(
     } else {
         const float *mass = p.rec.mass + seq * p.rec.ss + kvh * p.rec.hs;
         const int32_t *positions = p.rec.positions + seq * p.rec.ss + kvh * p.rec.hs;
+        const int j0 = warp * EACH * 32 + lane;
         unsigned key[EACH];
-        int newest = 0x80000000;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) key[i] = j0 + i * 32 < n ? order_of(mass[j0 + i * 32]) : 0u;
         if (p.recent > 0) {
+            int pos[EACH], newest = 0x80000000;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                pos[i] = j0 + i * 32 < n ? positions[j0 + i * 32] : 0x80000000;
+                newest = max(newest, pos[i]);
+            }
+            newest = __reduce_max_sync(0xffffffffu, newest);
+            if (lane == 0) ties_of[warp] = newest;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < SHORT_WARPS; ++w) newest = max(newest, ties_of[w]);
+            __syncthreads();
 #pragma unroll
             for (int i = 0; i < EACH; ++i)
-                if (i * 32 + lane < n) newest = max(newest, positions[i * 32 + lane]);
-            newest = __reduce_max_sync(0xffffffffu, newest);
+                if (j0 + i * 32 < n && (long long)pos[i] > (long long)newest - p.recent) key[i] = NEWEST;
         }
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) key[i] = i * 32 + lane < n ? key_of(p, mass, positions, i * 32 + lane, newest) : 0u;
         // the keep-th largest key, from its top bit down; done early where a bit parts the rows as wanted
         unsigned at = 0;
         bool parted = false;
+        int turn = 0;
+        auto sum = [&](int c) {                // over the CTA
+            c = __reduce_add_sync(0xffffffffu, c);
+            if (lane == 0) counts[turn][warp] = c;
+            __syncthreads();
+            c = 0;
+#pragma unroll
+            for (int w = 0; w < SHORT_WARPS; ++w) c += counts[turn][w];
+            turn ^= 1;
+            return c;
+        };
 #pragma unroll 1
         for (unsigned bit = 0x80000000u; bit && !parted; bit >>= 1) {
-            const unsigned next = at | bit;
             int c = 0;
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) c += key[i] >= next;
-            c = __reduce_add_sync(0xffffffffu, c);
-            if (c >= p.keep) at = next;
+            for (int i = 0; i < EACH; ++i) c += key[i] >= (at | bit);
+            c = sum(c);
+            if (c >= p.keep) at |= bit;
             parted = c == p.keep;
         }
-        int want = p.keep;                     // rows equal to it that stay, the lowest slots
-        {
-            int c = 0;
+        int c = 0, t = 0;
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) c += key[i] > at;
-            want -= __reduce_add_sync(0xffffffffu, c);
+        for (int i = 0; i < EACH; ++i) {
+            c += key[i] > at;
+            t += __popc(__ballot_sync(0xffffffffu, key[i] == at));
         }
-        int ties = 0, h = 0, m = 0;
+        if (lane == 0) ties_of[warp] = t;
+        const int want = p.keep - sum(c);      // rows equal to that key that stay, the lowest slots
+        int ties = 0;
+#pragma unroll
+        for (int w = 0; w < SHORT_WARPS; ++w)
+            if (w < warp) ties += ties_of[w];
+        unsigned hole_bits[EACH], mover_bits[EACH];
+        int h = 0, m = 0;
         const unsigned below = (1u << lane) - 1u;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int j = i * 32 + lane;
+            const int j = j0 + i * 32;
             const bool tie = key[i] == at;
             const unsigned tie_bits = __ballot_sync(0xffffffffu, tie);
             const bool stays = key[i] > at || (tie && ties + __popc(tie_bits & below) < want);
             ties += __popc(tie_bits);
-            const bool hole = p.in_place && j < p.keep && !stays, mover = stays && (!p.in_place || j >= p.keep);      // (keep < n)
-            const unsigned hole_bits = __ballot_sync(0xffffffffu, hole), mover_bits = __ballot_sync(0xffffffffu, mover);
-            if (hole) holes[h + __popc(hole_bits & below)] = (unsigned short)j;
-            if (mover) movers[m + __popc(mover_bits & below)] = (unsigned short)j;
-            h += __popc(hole_bits);
-            m += __popc(mover_bits);
+            hole_bits[i] = __ballot_sync(0xffffffffu, p.in_place && j < p.keep && !stays);      // (keep < n)
+            mover_bits[i] = __ballot_sync(0xffffffffu, stays && (!p.in_place || j >= p.keep));
+            h += __popc(hole_bits[i]);
+            m += __popc(mover_bits[i]);
         }
-        count = m;                             // (as many holes in place: keep rows stay)
-        __syncwarp();
+        if (lane == 0) { holes_of[warp] = h; movers_of[warp] = m; }
+        __syncthreads();
+        h = m = 0;
+#pragma unroll
+        for (int w = 0; w < SHORT_WARPS; ++w) {
+            if (w < warp) { h += holes_of[w]; m += movers_of[w]; }
+            count += movers_of[w];             // (as many holes in place: keep rows stay)
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (hole_bits[i] >> lane & 1u) holes[h + __popc(hole_bits[i] & below)] = (unsigned short)(j0 + i * 32);
+            if (mover_bits[i] >> lane & 1u) movers[m + __popc(mover_bits[i] & below)] = (unsigned short)(j0 + i * 32);
+            h += __popc(hole_bits[i]);
+            m += __popc(mover_bits[i]);
+        }
+        __syncthreads();
     }
-    if (fused && kvh == 0 && lane == 0 && p.left != p.lengths) p.left[seq] = min(p.lengths[seq], p.keep);
+    if (fused && kvh == 0 && tid == 0 && p.left != p.lengths) p.left[seq] = min(p.lengths[seq], p.keep);
     auto move = [&](int i) { return whole ? make_int2(i, i) : make_int2(p.in_place ? holes[i] : i, movers[i]); };
     if (fused) {
-        move_rows<4>(p, seq, kvh, count, lane, 32, move);
+        move_rows<2>(p, seq, kvh, count, tid, SHORT_NT, move);
         return;
     }
-    if (lane == 0) p.count[unit] = count;
-    for (int i = lane; i < count; i += 32) p.moves[(long long)unit * p.most + i] = move(i);
+    if (tid == 0) p.count[unit] = count;
+    for (int i = tid; i < count; i += SHORT_NT) p.moves[(long long)unit * p.most + i] = move(i);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- long caches
-constexpr int NT = 1024, WARPS = NT / 32, MAX_CLUSTER = 8;
-constexpr int MAX_KEYS = 48 * 1024;      // keys that a CTA keeps in shared memory; beyond it the records are read again in every pass
+constexpr int NT = 1024, WARPS = NT / 32, MAX_CLUSTER = 8, PASSES = 3, BINS = 2 * NT;
+constexpr int MAX_KEYS = 45 * 1024;      // keys that a CTA keeps in shared memory; beyond it the records are read again in every pass
+
+// What all CTAs of the cluster have at the place of `mine`, added up.  (The loads are in flight together: one remote latency, not S.)
+template <typename T, typename F>
+__device__ __forceinline__ void over_cluster(cg::cluster_group &cluster, T *mine, int S, F f) {
+    T x[MAX_CLUSTER];
+#pragma unroll
+    for (int r = 0; r < MAX_CLUSTER; ++r)
+        if (r < S) x[r] = *cluster.map_shared_rank(mine, r);
+#pragma unroll
+    for (int r = 0; r < MAX_CLUSTER; ++r)
+        if (r < S) f(r, x[r]);
+}
+// Sum of x over the threads before this one.
+__device__ __forceinline__ int before_me(int x, int *sums) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int upto = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+    }
+    if (lane == 31) sums[warp] = upto;
+    __syncthreads();
+    const int all = sums[lane];
+    const int ahead = __reduce_add_sync(0xffffffffu, lane < warp ? all : 0);
+    return ahead + upto - x;
+}
 
 __global__ void __launch_bounds__(NT) sh_mass_select_kernel(const __grid_constant__ EvictParams p, int cached_keys) {
     extern __shared__ unsigned keys[];
-    __shared__ int hist[4][256], sums[WARPS], found[2], newest_sh;
+    __shared__ int hist[PASSES][BINS], sums[PASSES][WARPS], found[PASSES][2], newest_sh;
     __shared__ int4 tally[WARPS];              // of a warp's rows: above the key below and from slot keep on, equal to it likewise
     __shared__ int4 bases[WARPS * MAX_CLUSTER];
     cg::cluster_group cluster = cg::this_cluster();
@@ -169,62 +234,61 @@ __global__ void __launch_bounds__(NT) sh_mass_select_kernel(const __grid_constan
     const int32_t *positions = p.rec.positions + seq * p.rec.ss + kvh * p.rec.hs;
     const int each = (n + S * NT - 1) / (S * NT) * 32, per = each * WARPS;      // rows of a warp, of a CTA, in the order of their slots
     const int lo = min(n, rank * per), hi = min(n, lo + per);
-    for (int i = tid; i < 4 * 256; i += NT) hist[i >> 8][i & 255] = 0;
+    for (int i = tid; i < PASSES * BINS; i += NT) (&hist[0][0])[i] = 0;
     int newest = 0x80000000;
     if (p.recent > 0) {
-        for (int j = lo + tid; j < hi; j += NT) newest = max(newest, positions[j]);
+#pragma unroll 8
+        for (int j = lo + tid; j < hi; j += NT) {
+            newest = max(newest, positions[j]);
+            if (cached_keys) keys[j - lo] = order_of(mass[j]);
+        }
         newest = __reduce_max_sync(0xffffffffu, newest);
-        if (lane == 0) sums[warp] = newest;
+        if (lane == 0) sums[0][warp] = newest;
         __syncthreads();
         if (warp == 0) {
-            newest = __reduce_max_sync(0xffffffffu, sums[lane]);
+            newest = __reduce_max_sync(0xffffffffu, sums[0][lane]);
             if (lane == 0) newest_sh = newest;
         }
         cluster.sync();
-        for (int r = 0; r < S; ++r) newest = max(newest, *cluster.map_shared_rank(&newest_sh, r));
+        over_cluster(cluster, &newest_sh, S, [&](int, int x) { newest = max(newest, x); });
     }
-    if (cached_keys)
-        for (int j = lo + tid; j < hi; j += NT) keys[j - lo] = key_of(p, mass, positions, j, newest);
+    if (cached_keys) {
+#pragma unroll 8
+        for (int j = lo + tid; j < hi; j += NT) {
+            if (p.recent == 0) keys[j - lo] = order_of(mass[j]);
+            else if ((long long)positions[j] > (long long)newest - p.recent) keys[j - lo] = NEWEST;
+        }
+    }
     auto key = [&](int j) { return cached_keys ? keys[j - lo] : key_of(p, mass, positions, j, newest); };
     __syncthreads();
-    // the keep-th largest key: 8 bits a pass
+    // the keep-th largest key: 11, 11 and 10 bits a pass.  (The first has sign, exponent and two bits more: with fewer, most rows would meet
+    // in a few places of the histogram.)
     unsigned prefix = 0, known = 0;
     int want = p.keep;                         // place of the key among those that share the known bits
-#pragma unroll 1
-    for (int pass = 0; pass < 4; ++pass) {
-        const int shift = 24 - 8 * pass;
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+        constexpr int SHIFT[PASSES] = {21, 10, 0};
+        const int shift = SHIFT[pass];
+        const unsigned mask = pass == 2 ? BINS / 2 - 1 : BINS - 1;
+#pragma unroll 4
         for (int j = lo + tid; j < hi; j += NT) {
             const unsigned k = key(j);
-            if ((k & known) == prefix) atomicAdd(&hist[pass][(k >> shift) & 255u], 1);
+            if ((k & known) == prefix) atomicAdd(&hist[pass][k >> shift & mask], 1);
         }
         cluster.sync();
-        if (warp == 0) {                       // from the largest digit down: lane l has 8 of them
-            int mine[8] = {}, sum = 0;
-            for (int r = 0; r < S; ++r) {
-                const int *h = cluster.map_shared_rank(&hist[pass][0], r);
+        int mine[2] = {};                      // from the largest digit down, a thread has two
 #pragma unroll
-                for (int i = 0; i < 8; ++i) mine[i] += h[255 - (lane * 8 + i)];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += mine[i];
-            int upto = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int x = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += x;
-            }
-            int before = upto - sum;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (before < want && want <= before + mine[i]) { found[0] = 255 - (lane * 8 + i); found[1] = want - before; }
-                before += mine[i];
-            }
+        for (int i = 0; i < 2; ++i) over_cluster(cluster, &hist[pass][BINS - 1 - (2 * tid + i)], S, [&](int, int x) { mine[i] += x; });
+        const int before = before_me(mine[0] + mine[1], sums[pass]);
+        if (before < want && want <= before + mine[0] + mine[1]) {
+            const int second = want > before + mine[0];
+            found[pass][0] = BINS - 1 - (2 * tid + second);
+            found[pass][1] = want - before - (second ? mine[0] : 0);
         }
         __syncthreads();
-        prefix |= (unsigned)found[0] << shift;
-        known |= 255u << shift;
-        want = found[1];
-        __syncthreads();
+        prefix |= (unsigned)found[pass][0] << shift;
+        known |= mask << shift;
+        want = found[pass][1];
     }
     // Rows above that key stay, and the first `want` of those equal to it.  Every warp counts its own ...
     const int from = lo + warp * each, to = min(hi, from + each);
@@ -237,36 +301,30 @@ __global__ void __launch_bounds__(NT) sh_mass_select_kernel(const __grid_constan
     t = make_int4(__reduce_add_sync(0xffffffffu, t.x), __reduce_add_sync(0xffffffffu, t.y), __reduce_add_sync(0xffffffffu, t.z), __reduce_add_sync(0xffffffffu, t.w));
     if (lane == 0) tally[warp] = t;
     cluster.sync();
-    // ... and a warp of each CTA works out what comes before whom: rows equal to the key, holes, rows that move.  Lane l has S warps of the cluster.
+    // ... and a warp of each CTA works out what comes before whom: rows equal to the key, holes, rows that move.  Warp w of CTA r is the
+    // (32 r + w)-th; lane l takes the l-th of each CTA, one CTA after the other.
     if (warp == 0) {
-        auto of = [&](int w) { return *cluster.map_shared_rank(&tally[w % WARPS], w / WARPS); };
-        int ties = 0;
-        for (int i = 0; i < S; ++i) { const int4 x = of(lane * S + i); ties += x.z + x.w; }
-        int upto = ties;
+        int ties = 0, h = 0, m = 0;            // before the CTA
+        over_cluster(cluster, &tally[lane], S, [&](int r, int4 x) {
+            auto scan = [&](int v) {
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += x;
-        }
-        ties = upto - ties;
-        int h = 0, m = 0;
-        for (int i = 0; i < S; ++i) {          // (counted from this lane's first warp)
-            const int w = lane * S + i;
-            const int4 x = of(w);
-            const int low = min(max(want - ties, 0), x.z), high = min(max(want - ties - x.z, 0), x.w);      // equal ones that stay
-            bases[w] = make_int4(ties, h, m, 0);
-            ties += x.z + x.w;
-            h += min(max(min(n, p.keep) - w * each, 0), each) - (x.x + low);      // (slots below keep that this warp has)
-            m += x.y + high + (p.in_place ? 0 : x.x + low);
-        }
-        int h0 = h, m0 = m;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, h0, o), y = __shfl_up_sync(0xffffffffu, m0, o);
-            if (lane >= o) { h0 += x; m0 += y; }
-        }
-        if (lane == 31 && rank == 0) p.count[unit] = m0;
-        for (int i = 0; i < S; ++i) { bases[lane * S + i].y += h0 - h; bases[lane * S + i].z += m0 - m; }
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, v, o);
+                    if (lane >= o) v += y;
+                }
+                return v;
+            };
+            const int w = r * WARPS + lane, both = x.z + x.w, t1 = scan(both), mine = ties + t1 - both;
+            const int low = min(max(want - mine, 0), x.z), high = min(max(want - mine - x.z, 0), x.w);      // equal ones that stay
+            const int hh = min(max(p.keep - w * each, 0), each) - (x.x + low);      // (slots below keep that this warp has; keep < n)
+            const int mm = x.y + high + (p.in_place ? 0 : x.x + low);
+            const int h1 = scan(hh), m1 = scan(mm);
+            bases[w] = make_int4(mine, h + h1 - hh, m + m1 - mm, 0);
+            ties += __shfl_sync(0xffffffffu, t1, 31);
+            h += __shfl_sync(0xffffffffu, h1, 31);
+            m += __shfl_sync(0xffffffffu, m1, 31);
+        });
+        if (lane == 0 && rank == 0) p.count[unit] = m;
     }
     __syncthreads();
     int ties = bases[rank * WARPS + warp].x, h = bases[rank * WARPS + warp].y, m = bases[rank * WARPS + warp].z;
@@ -328,7 +386,7 @@ constexpr auto AFTER = cudaLaunchAttributeProgrammaticStreamSerialization;
 
 template <int EACH>
 cudaError_t select_short(const EvictParams &p, int units, bool fused, cudaStream_t s) {
-    sh_mass_select_short_kernel<EACH><<<(units + SHORT_WARPS - 1) / SHORT_WARPS, SHORT_WARPS * 32, 0, s>>>(p, units, fused);
+    sh_mass_select_short_kernel<EACH><<<units, SHORT_NT, 0, s>>>(p, fused);
     return cudaGetLastError();
 }
 
@@ -343,15 +401,15 @@ cudaError_t sh_launch_mass_evict(const EvictParams &p, cudaStream_t s) {
     cudaError_t e = sh_device_sms(&dev, &sms);
     if (e != cudaSuccess) return e;
     if (p.slots <= SHORT) {
-        // a warp has few copies in flight: units move their own rows when there are several for each place of the device, or next to none to move
-        const bool fused = units >= 16ll * sms || p.most <= 4;
+        // units move their own rows when there are several for each place of the device, or few to move
+        const bool fused = units >= 8ll * sms || p.most <= 16;
         const int n = (int)units;
-        e = p.slots <= 128 ? select_short<4>(p, n, fused, s) : p.slots <= 256 ? select_short<8>(p, n, fused, s) : p.slots <= 512 ? select_short<16>(p, n, fused, s) : select_short<32>(p, n, fused, s);
+        e = p.slots <= SHORT_NT ? select_short<1>(p, n, fused, s) : p.slots <= 2 * SHORT_NT ? select_short<2>(p, n, fused, s) : p.slots <= 4 * SHORT_NT ? select_short<4>(p, n, fused, s) : select_short<8>(p, n, fused, s);
         if (e != cudaSuccess) return e;
         if (fused) return p.left != p.lengths ? cudaSuccess : launch(sh_mass_left_kernel, (unsigned)((p.sequences + 127) / 128), 128, 0, AFTER, 0, s, p);
     } else {
         int S = 1;
-        while (S < MAX_CLUSTER && units * S * 2 <= 2ll * sms && p.slots >= 2 * S * NT) S *= 2;
+        while (S < MAX_CLUSTER && units * S * 2 <= sms && p.slots >= 2 * S * NT) S *= 2;
         const int most = (p.slots + S * NT - 1) / (S * NT) * NT;      // rows of a CTA
         const bool cached = most <= MAX_KEYS;
         static ShKernelSetup setup;
