@@ -583,9 +583,10 @@ def _window_packed(dtype, d: int, q_heads: int, kv_heads: int, window: int, sink
 
 
 def _cache_packed(k_cache, v_cache, shape, dtype, device: int) -> bytes:
-    for t, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape):
-            _fail(what, f"[sequences, key heads, sinks + window, head_dim] = {shape} of {dtype} on cuda:{device}", t)
+    if not (isinstance(k_cache, torch.Tensor) and k_cache.dtype is dtype and k_cache.get_device() == device and k_cache.shape == shape):
+        _fail("k_cache", f"[sequences, key heads, slots, head_dim] = {tuple(shape)} of {dtype} on cuda:{device}", k_cache)
+    if not (isinstance(v_cache, torch.Tensor) and v_cache.dtype is dtype and v_cache.get_device() == device and v_cache.shape == shape):
+        _fail("v_cache", f"[sequences, key heads, slots, head_dim] = {tuple(shape)} of {dtype} on cuda:{device}", v_cache)
     ks, vs = k_cache.stride(), v_cache.stride()
     if ks[3] != 1 and k_cache.numel():
         _fail("k_cache", "contiguous rows", k_cache)
@@ -759,11 +760,14 @@ def _slots_of(k_cache, what: str, n: Optional[int], kv_heads: Optional[int], d: 
 
 
 def _records_packed(mass, positions, shape, device: int) -> bytes:
-    for t, what, dt in ((mass, "mass", torch.float32), (positions, "positions", torch.int32)):
-        if not (isinstance(t, torch.Tensor) and t.dtype is dt and t.get_device() == device and t.shape == shape and (shape[2] <= 1 or t.stride(2) == 1)):
-            _fail(what, f"[sequences, key heads, slots] = {tuple(shape)} of {dt} on cuda:{device}, contiguous along its last dimension", t)
+    if not (isinstance(mass, torch.Tensor) and mass.dtype is torch.float32 and mass.get_device() == device and mass.shape == shape):
+        _fail("mass", f"[sequences, key heads, slots] = {tuple(shape)} of fp32 on cuda:{device}", mass)
+    if not (isinstance(positions, torch.Tensor) and positions.dtype is torch.int32 and positions.get_device() == device and positions.shape == shape):
+        _fail("positions", f"[sequences, key heads, slots] = {tuple(shape)} of int32 on cuda:{device}", positions)
     ms, ps = mass.stride(), positions.stride()
-    if any(ms[i] != ps[i] for i in range(2) if shape[i] > 1):
+    if ms[2] != 1 and shape[2] > 1:
+        _fail("mass", "contiguous slots", mass)
+    if ms != ps and any(ms[i] != ps[i] for i in range(3) if shape[i] > 1):
         _fail("positions", f"the strides of mass, {ms}", positions)
     return _pack_records(mass.data_ptr(), positions.data_ptr(), ms[0], ms[1])
 

@@ -25,7 +25,7 @@ struct EvictParams {
 size_t sh_mass_evict_scratch(long long units, int most);
 cudaError_t sh_launch_mass_evict(const EvictParams &p, cudaStream_t s);
 
-// Single tokens: add the step's weights to the masses, from the scores and totals that the attention has left.
+// Single tokens: add the step's weights to the masses, from the scores and totals that the attention has left (where it has not done so).
 cudaError_t sh_launch_mass_fold(const WindowParams &p, cudaStream_t s);
 // Prompts: add the weights of the chunk's rows to the masses of the keys they see; the chunk is in the cache already.
 cudaError_t sh_launch_mass_columns_f32(const WindowParams &p, int D, cudaStream_t s);

@@ -164,10 +164,7 @@ int sh_mass_decode(const sh_attention *a, int sequences, const sh_rows *q, const
     p.scores = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + part);
     p.total = p.scores + (size_t)sequences * p.hq * p.score_stride;
     fill_prior(p, prior, prior_dtype, prior_lse_dev, a, sequences);
-    const cudaStream_t s = (cudaStream_t)stream;
-    cudaError_t e = sh_launch_window_decode(p, a->dtype, D, ATTEND_MASS, s);
-    if (e == cudaSuccess) e = sh_launch_mass_fold(p, s);
-    return done(e);
+    return done(sh_launch_window_decode(p, a->dtype, D, ATTEND_MASS, (cudaStream_t)stream));
 }
 
 size_t sh_mass_evict_workspace_bytes(const sh_attention *a, int sequences, int keep, int in_place) {

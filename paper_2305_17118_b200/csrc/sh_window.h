@@ -47,6 +47,7 @@ struct WindowParams {
     bool out_f32, prior_f32;      // the rows of out (contexts), of the prior are fp32 whatever the type is
     float *scores, *total;        // single tokens: [sequences][hq][score_stride] logits, [sequences][hq] logs of their sums (base 2)
     long long score_stride;
+    bool add_here;                // the single-token kernel adds the weights to the masses itself
     const int32_t *seen;          // [sequences]: position of a sequence's next token
     float *mass;                  // [sequences][hk][slots] with the strides below, in elements; positions alike
     int32_t *held;

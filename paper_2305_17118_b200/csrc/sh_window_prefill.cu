@@ -8,11 +8,16 @@
 // 700 + 511 tokens, 16 heads of 64, window 346, 64 sinks: 81 us, 17 TFLOP/s of a possible 74 (the first version, 64-row tiles with
 // transposed operands: 127 us).  Bound by the latency of shared-memory reads at 16 warps an SM (8 of 16 bytes for 32 packed
 // multiply-adds), and by the tiles' masked parts, half again of the work.
+#include <cooperative_groups.h>
 #include <math_constants.h>
+
+#include <algorithm>
 
 #include "sh_pairs.cuh"
 #include "sh_umma.cuh"
 #include "sh_window.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace {
 
@@ -43,13 +48,16 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
     __shared__ Tile tile_sh;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int kvh = blockIdx.y;
+    // (contexts and caches with masses) the CTAs of a cluster take the blocks of keys in turn
+    cg::cluster_group cluster = cg::this_cluster();
+    const int S = MODE == ATTEND_WINDOW ? 1 : cluster.num_blocks(), rank = MODE == ATTEND_WINDOW ? 0 : cluster.block_rank();
     if (tid < 32) {
-        const Tile t = find_tile<MODE>(p, blockIdx.x, BM);
+        const Tile t = find_tile<MODE>(p, MODE == ATTEND_WINDOW ? blockIdx.x : blockIdx.x / S, BM);
         if (tid == 0) tile_sh = t;
     }
     __syncthreads();
     const Tile t = tile_sh;
-    if (t.seq < 0) return;
+    if (t.seq < 0) return;                                           // (the whole cluster)
     const long long rows = (long long)t.count * p.g;
     const int qlo = (int)(t.row0 / p.g), qhi = (int)((min(t.row0 + BM, rows) - 1) / p.g);      // the tile's first and last token in the chunk
     const int oldest = t.cached + qlo - p.window + 1;                // the first row's window starts here
@@ -90,7 +98,13 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
         }
         shumma::cp_async_commit();
     };
+    auto next_of = [&](int b) {
+        b = seek(b + 1);
+        for (int i = 1; i < S && b < blocks; ++i) b = seek(b + 1);
+        return b;
+    };
     int b = seek(0), turn = 0;
+    for (int i = 0; i < rank && b < blocks; ++i) b = seek(b + 1);
     if (tid < BN) kpos[tid] = position(b, tid);
     for (int i = tid; i < BM * (D / 4); i += NT) {
         const int r = i / (D / 4), c = i % (D / 4);
@@ -99,7 +113,7 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
         cp16_or_zero(Qs + r * LDK + c * 4, take ? p.q.p + tok * p.q.ts + (kvh * p.g + (int)(row % p.g)) * p.q.hs + c * 16 : p.q.p, take);
     }
     __syncthreads();
-    if (MODE != ATTEND_CONTEXT || b < blocks) request(b, 0, false);      // (a context may have no rows)
+    if (MODE == ATTEND_WINDOW || b < blocks) request(b, 0, false);      // (a context may have no rows, a CTA no blocks)
     int qp[R];
     float m[R], l[R];
     uint64_t o[R][D / 32];                                           // pairs of columns
@@ -111,12 +125,12 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) o[a][c] = 0;
     }
-    if (MODE == ATTEND_CONTEXT && b >= blocks) shumma::cp_async_wait_all();
+    if (MODE != ATTEND_WINDOW && b >= blocks) shumma::cp_async_wait_all();
     while (b < blocks) {
         shumma::cp_async_wait_all();
         __syncthreads();                                             // the keys are there; the last block's P.V is done
         request(b, turn, true);
-        const int next = seek(b + 1);
+        const int next = MODE == ATTEND_WINDOW ? seek(b + 1) : next_of(b);
         if (next < blocks && tid < BN) kpos[(turn ^ 1) * BN + tid] = position(next, tid);
         uint64_t s2[R][NC] = {};                                     // even and odd elements of d
 #pragma unroll 2
@@ -213,10 +227,49 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
     }
 #pragma unroll
     for (int a = 0; a < R; ++a) {
-        float sum = l[a];
 #pragma unroll
-        for (int off = 8; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-        if (qp[a] < 0) continue;
+        for (int off = 8; off; off >>= 1) l[a] += __shfl_xor_sync(0xffffffffu, l[a], off);
+    }
+    // a cluster's CTAs merge: each finishes every S-th row from what the others have left in their shared memory
+    constexpr int LDO = D + 4;
+    if (MODE != ATTEND_WINDOW && S > 1) {
+        __syncthreads();                                             // (nobody reads tiles any more)
+#pragma unroll
+        for (int a = 0; a < R; ++a) {
+            float *row = sm + (ty * R + a) * LDO;
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) *reinterpret_cast<ulonglong2 *>(row + c * 64 + tx * 4) = make_ulonglong2(o[a][2 * c], o[a][2 * c + 1]);
+            if (tx == 0) { row[D] = m[a]; row[D + 1] = l[a]; }
+        }
+        cluster.sync();
+#pragma unroll
+        for (int a = 0; a < R; ++a) {
+            if ((ty * R + a) % S != rank) continue;
+            float M = -CUDART_INF_F;
+            for (int r = 0; r < S; ++r) M = fmaxf(M, cluster.map_shared_rank(sm + (ty * R + a) * LDO, r)[D]);
+            const float base = M == -CUDART_INF_F ? 0.f : M;
+            float L = 0.f;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) o[a][c] = 0;
+            for (int r = 0; r < S; ++r) {
+                const float *row = cluster.map_shared_rank(sm + (ty * R + a) * LDO, r);
+                const float f = shumma::ex2_approx(row[D] - base);
+                L += row[D + 1] * f;
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) {
+                    const ulonglong2 x = *reinterpret_cast<const ulonglong2 *>(row + c * 64 + tx * 4);
+                    o[a][2 * c] = fma2(x.x, f2(f, f), o[a][2 * c]);
+                    o[a][2 * c + 1] = fma2(x.y, f2(f, f), o[a][2 * c + 1]);
+                }
+            }
+            m[a] = M; l[a] = L;
+        }
+        cluster.sync();                                              // nobody's shared memory goes away while it is read
+    }
+#pragma unroll
+    for (int a = 0; a < R; ++a) {
+        const float sum = l[a];
+        if (qp[a] < 0 || (MODE != ATTEND_WINDOW && (ty * R + a) % S != rank)) continue;
         const long long row = t.row0 + ty * R + a, tok = t.first + row / p.g;
         const int h = kvh * p.g + (int)(row % p.g);
         Close end = {};
@@ -276,13 +329,33 @@ cudaError_t launch(const WindowParams &p, cudaStream_t s) {
     auto kern = sh_window_prefill_f32_kernel<D, MODE>;
     constexpr int bytes = Simt<D>::FLOATS * 4;
     static ShKernelSetup setup;
+    static_assert(BM * (D + 4) <= Simt<D>::FLOATS, "a CTA's result takes the place of its tiles");
     int sms = 0;
     const cudaError_t e = sh_setup_kernel(setup, kern, bytes, &sms);
     if (e != cudaSuccess) return e;
     const long long tiles = (long long)p.tokens * p.g / BM + p.sequences;      // each sequence adds at most one partial tile
     if (tiles > 0x7fffffffll) return cudaErrorInvalidValue;
-    kern<<<dim3((unsigned)tiles, p.hk), NT, bytes, s>>>(p);
-    return cudaGetLastError();
+    if constexpr (MODE == ATTEND_WINDOW) {
+        kern<<<dim3((unsigned)tiles, p.hk), NT, bytes, s>>>(p);
+        return cudaGetLastError();
+    } else {
+        // few row tiles: clusters share the keys of one, as long as all run at once (4 CTAs an SM) and have two blocks each (chunks of 64, 17
+        // and 200 tokens over 500, 0 and 31 rows, 12 heads of 64: 47 -> 32 us)
+        int S = 1;
+        while (S < 8 && tiles * p.hk * S * 2 <= 4ll * sms && p.slots >= 2 * S * 2 * Simt<D>::BN) S *= 2;
+        if (tiles * S > 0x7fffffffll) return cudaErrorInvalidValue;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(tiles * S), p.hk);
+        cfg.blockDim = dim3(NT);
+        cfg.dynamicSmemBytes = bytes;
+        cfg.stream = s;
+        cudaLaunchAttribute attr = {};
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = S; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, kern, p);
+    }
 }
 
 }  // namespace

@@ -1037,22 +1037,52 @@ __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __
     if (w.y < 0 || w.y > p.w.tokens || w.z > p.w.tokens - w.y) return;
     if (parts <= 1 || row0 / p.gb >= p.tpt || t * p.tpt + row0 / p.gb >= w.z) return;
     const bool live = row / p.gb < p.tpt && tok < w.z && h < p.w.g;
-    for (int i = c4; i < parts; i += D / 4) sums[i][r] = live ? part_sum<D>(p, id + i, t)[row] : make_float2(0.f, -1.f);
-    if (tid < ROWS) odd[tid] = 0;
-    __syncthreads();
-    float M = -CUDART_INF_F;
-    for (int i = 0; i < parts; ++i) M = fmaxf(M, sums[i][r].x);
-    float L = 0.f;
+    float M = -CUDART_INF_F, L = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     const float4 *at = part_o<D>(p, id, t) + c4 * TM + row;
+    if constexpr (MODE == ATTEND_WINDOW) {
+        for (int i = c4; i < parts; i += D / 4) sums[i][r] = live ? part_sum<D>(p, id + i, t)[row] : make_float2(0.f, -1.f);
+        if (tid < ROWS) odd[tid] = 0;
+        __syncthreads();
+        for (int i = 0; i < parts; ++i) M = fmaxf(M, sums[i][r].x);
 #pragma unroll 8
-    for (int i = 0; i < parts; ++i) {
-        const float2 s = sums[i][r];
-        if (s.y < 0.f) continue;                     // (nothing was written)
-        const float4 x = at[(long long)i * 2 * (D / 4) * TM];
-        const float f = s.x == -CUDART_INF_F ? 0.f : ex2_approx(s.x - M);      // (0 times NaN stays one)
-        L += s.y * f;
-        o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+        for (int i = 0; i < parts; ++i) {
+            const float2 s = sums[i][r];
+            if (s.y < 0.f) continue;                     // (nothing was written)
+            const float4 x = at[(long long)i * 2 * (D / 4) * TM];
+            const float f = s.x == -CUDART_INF_F ? 0.f : ex2_approx(s.x - M);      // (0 times NaN stays one)
+            L += s.y * f;
+            o.x = fmaf(x.x, f, o.x); o.y = fmaf(x.y, f, o.y); o.z = fmaf(x.z, f, o.z); o.w = fmaf(x.w, f, o.w);
+        }
+    } else {
+        // the parts' sums and outputs are asked for together, AHEAD parts at a time (256 rows of 18 parts: 3 us less)
+        constexpr int AHEAD = 8;
+        if (tid < ROWS) odd[tid] = 0;
+        for (int i0 = 0; i0 < parts; i0 += AHEAD) {
+            float2 s[AHEAD];
+            float4 x[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const bool there = live && i0 + k < parts;
+                s[k] = there ? part_sum<D>(p, id + i0 + k, t)[row] : make_float2(-CUDART_INF_F, -1.f);
+                x[k] = there ? at[(long long)(i0 + k) * 2 * (D / 4) * TM] : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            float top = M;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) top = s[k].y < 0.f ? top : fmaxf(top, s[k].x);
+            const float keep = M == -CUDART_INF_F ? 0.f : ex2_approx(M - top);
+            L *= keep;
+            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+            M = top;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (s[k].y < 0.f) continue;              // (nothing was written)
+                const float f = s[k].x == -CUDART_INF_F ? 0.f : ex2_approx(s[k].x - M);      // (0 times NaN stays one)
+                L += s[k].y * f;
+                o.x = fmaf(x[k].x, f, o.x); o.y = fmaf(x[k].y, f, o.y); o.z = fmaf(x[k].z, f, o.z); o.w = fmaf(x[k].w, f, o.w);
+            }
+        }
+        __syncthreads();
     }
     float inv = 1.f / L;                             // (as where there is nothing to merge)
     float4 prior = make_float4(0.f, 0.f, 0.f, 0.f);
