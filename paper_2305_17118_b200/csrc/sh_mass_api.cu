@@ -124,8 +124,9 @@ int sh_mass_prefill(const sh_attention *a, int tokens, int sequences, const sh_r
     p.lse = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + need - lse_bytes);
     fill_prior(p, prior, prior_dtype, prior_lse_dev, a, tokens);
     const cudaStream_t s = (cudaStream_t)stream;
-    cudaError_t e = a->dtype == SH_F32 ? sh_launch_window_prefill_f32(p, D, ATTEND_MASS, s) : sh_launch_window_prefill_umma(p, a->dtype, D, ATTEND_MASS, s);
-    if (e == cudaSuccess) e = sh_launch_window_append(p, es, D, ATTEND_MASS, s);
+    // the chunk goes into slots that the attention does not look at: the two run side by side
+    cudaError_t e = sh_launch_window_append(p, es, D, ATTEND_MASS, s);
+    if (e == cudaSuccess) e = a->dtype == SH_F32 ? sh_launch_window_prefill_f32(p, D, ATTEND_MASS, s) : sh_launch_window_prefill_umma(p, a->dtype, D, ATTEND_MASS, s);
     if (e == cudaSuccess) e = a->dtype == SH_F32 ? sh_launch_mass_columns_f32(p, D, s) : sh_launch_mass_columns_umma(p, a->dtype, D, s);
     return done(e);
 }

@@ -153,6 +153,7 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    sh_pdl_wait();                                 // (the rows' logs, the chunk in the cache)
     const uint32_t tbase = bars->tmem;
     if (tbase != 0) *(volatile int *)&bars->abort_flag = 0x631;          // (all 512 columns are this CTA's)
     bool ok = __all_sync(0xffffffffu, !aborted() && tbase == 0);
@@ -360,12 +361,15 @@ __global__ void __launch_bounds__(ADD) sh_mass_columns_add_kernel(const __grid_c
     p.mass[seq * p.rss + kvh * p.rhs + slot] += x;
 }
 
-// How many items share the row tiles of a key block.  The longest item has the rows of all tokens if they are one sequence's; then an SM has
-// about `load` tiles in all (half of them are behind the diagonal), and an item should be a quarter of that.  Four tiles an item at least.
+// How many items share the row tiles of a key block.  The longest sequence is taken to have twice the average's tokens: its first key blocks see
+// `tiles` row tiles, an SM has about `load` in all (half of them lie behind the diagonal), and an item should be half of that.  Four tiles an
+// item at least.  2048 tokens in one part 97 us, five 83, eight 86 (with the attention); 4096 tokens of one key head 173 in two, 112 in eight;
+// 1 to 2048 tokens of six sequences 130 in two and three, 140 in eight.
 int parts_of(int tokens, int sequences, int hk, int g, int slots) {
-    const double tiles = (double)tokens * g / ROWS, load = tiles * hk * ((double)tokens / KEYS + 1) / 2 / 148;
+    const double longest = std::min((double)tokens, 2.0 * tokens / sequences), tiles = longest * g / ROWS;
+    const double load = hk * std::ceil((double)tokens / KEYS) * tiles / 2 / 148;
     const double most = std::min(std::min(8.0, tiles / 4), (double)(64 << 20) / (4.0 * sequences * hk * slots));      // (64 MB of sums)
-    return (int)std::max(1.0, std::min(most, std::ceil(4 * tiles / std::max(load, 1.0))));
+    return (int)std::max(1.0, std::min(most, std::ceil(2 * tiles / std::max(load, 1.0))));
 }
 
 template <int FMT, int D>
@@ -389,20 +393,23 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     p.parts = parts_of(w.tokens, w.sequences, w.hk, w.g, w.slots);
     const long long items = (long long)std::min(w.sequences, w.tokens) * ((w.slots + KEYS - 1) / KEYS) * w.hk * p.parts;      // at most
-    kern<<<(unsigned)std::min<long long>(items, sms), NTH, ColCfg<D>::SMEM, s>>>(p, mq, mk);
-    const cudaError_t e2 = cudaGetLastError();
-    if (e2 != cudaSuccess || p.parts == 1) return e2;
     const long long blocks = (w.slots + ADD - 1) / ADD;
     if (blocks * w.sequences * w.hk > 0x7fffffffll) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(blocks * w.sequences * w.hk));
-    cfg.blockDim = dim3(ADD);
+    cfg.gridDim = dim3((unsigned)std::min<long long>(items, sms));
+    cfg.blockDim = dim3(NTH);
+    cfg.dynamicSmemBytes = ColCfg<D>::SMEM;
     cfg.stream = s;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
+    const cudaError_t e2 = cudaLaunchKernelEx(&cfg, kern, p, mq, mk);
+    if (e2 != cudaSuccess || p.parts == 1) return e2;
+    cfg.gridDim = dim3((unsigned)(blocks * w.sequences * w.hk));
+    cfg.blockDim = dim3(ADD);
+    cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, sh_mass_columns_add_kernel, w, (int)blocks, p.parts);
 }
 

@@ -57,7 +57,10 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
     }
     __syncthreads();
     const Tile t = tile_sh;
-    if (t.seq < 0) return;                                           // (the whole cluster)
+    if (t.seq < 0) {                                                 // (the whole cluster)
+        if (MODE == ATTEND_MASS) sh_pdl_wait();
+        return;
+    }
     const long long rows = (long long)t.count * p.g;
     const int qlo = (int)(t.row0 / p.g), qhi = (int)((min(t.row0 + BM, rows) - 1) / p.g);      // the tile's first and last token in the chunk
     const int oldest = t.cached + qlo - p.window + 1;                // the first row's window starts here
@@ -295,12 +298,14 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
             store_row<float, MODE>(p, tok, h, c * 64 + tx * 4, x);
         }
     }
+    if (MODE == ATTEND_MASS) sh_pdl_wait();                          // who comes after this launch also comes after the one that stores the chunk
 }
 
 // Copy the rows that a later token can see into their slots: PIECES lanes move one token's key and value row of one head.
 // A warp's rows are neighbouring heads of the same token.
 template <int MODE>
 __global__ void __launch_bounds__(256) sh_window_append_kernel(const WindowParams p, int pieces) {
+    if (MODE == ATTEND_MASS) sh_pdl_launch_dependents();      // (the attention needs nothing of this)
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
     const int c = (int)(id % pieces);
     const long long rh = id / pieces;
@@ -349,11 +354,13 @@ cudaError_t launch(const WindowParams &p, cudaStream_t s) {
         cfg.blockDim = dim3(NT);
         cfg.dynamicSmemBytes = bytes;
         cfg.stream = s;
-        cudaLaunchAttribute attr = {};
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = S; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
+        cudaLaunchAttribute attr[2] = {};
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = S; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = MODE == ATTEND_MASS ? 2 : 1;                  // (beside the launch that stores the chunk)
         return cudaLaunchKernelEx(&cfg, kern, p);
     }
 }

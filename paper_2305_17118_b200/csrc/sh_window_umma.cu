@@ -1013,6 +1013,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     tc_fence_before();
     __syncthreads();
     if (tid == 0 && bars->abort_flag) atomicCAS(&g_window_error, 0, bars->abort_flag);
+    if (MODE == ATTEND_MASS) sh_pdl_wait();            // who comes after this launch also comes after the one that stores the chunk
     if (warp == 0) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512) : "memory");
@@ -1170,18 +1171,21 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     share_out(items, w.tokens, MODE == ATTEND_CONTEXT ? w.slots : w.window, w.sinks, w.g, w.kc != nullptr, sms, p.share, p.parts);
     if (!w.part) p.parts = 1;
     if (items > 0x7fffffffll) return cudaErrorInvalidValue;
-    kern<<<(unsigned)(items * p.parts), NTH, Cfg<D>::SMEM, s>>>(p, mq, mk, mv, mkc, mvc, mo);
-    if (p.parts == 1) return cudaGetLastError();
-    const cudaError_t e2 = cudaGetLastError();
-    if (e2 != cudaSuccess) return e2;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(items * (2 * TM / 8)));
-    cfg.blockDim = dim3(2 * D);
+    cfg.gridDim = dim3((unsigned)(items * p.parts));
+    cfg.blockDim = dim3(NTH);
+    cfg.dynamicSmemBytes = Cfg<D>::SMEM;
     cfg.stream = s;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
+    cfg.numAttrs = MODE == ATTEND_MASS;                // (beside the launch that stores the chunk)
+    const cudaError_t e2 = cudaLaunchKernelEx(&cfg, kern, p, mq, mk, mv, mkc, mvc, mo);
+    if (e2 != cudaSuccess || p.parts == 1) return e2;
+    cfg.gridDim = dim3((unsigned)(items * (2 * TM / 8)));
+    cfg.blockDim = dim3(2 * D);
+    cfg.dynamicSmemBytes = 0;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, sh_window_prefill_merge_kernel<T, D, MODE>, p);
 }
