@@ -908,3 +908,116 @@ def mass_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, mass: torch.Tensor,
     _launch("mass_evict", lib.sh_mass_evict, device, stream, at, n, lp, cache, rec, keep, recent, to, to_rec, room, _ints(left, "left", n, device),
             work.data_ptr(), bytes_)
     return left
+
+
+class MassCache:
+    """Key/value cache of a batch under the policy "the ``recent`` newest tokens and those that have received most attention", at most ``budget``
+    rows per (sequence, key head) after an eviction and ``spare`` more in between: the sibling of ``Handle`` and ``WindowCache`` that goes by
+    accumulated attention weights.
+
+    Owns ``k``, ``v`` [sequences, kv_heads, budget + spare, head_dim], ``mass``, ``positions`` [sequences, kv_heads, budget + spare], ``lengths`` (rows
+    held; -1 marks an idle slot of the batch) and ``seen`` (tokens so far: the position of the next one), int32 on the device.  To begin a
+    new sequence in slot i set ``lengths[i] = 0`` and ``seen[i]`` to ``first``.
+
+    ``rope`` prepares the queries and keys of every call (positions default to the tokens' places).  ``prefix`` = (k, v) [1, kv_heads, rows,
+    head_dim]: keys (prepared) and values that every sequence begins with; it is kept once, attended to for the whole batch at once, never
+    evicted, and ``first`` is the number of its rows (else 0).
+
+    How full the sequences are is not known on the host: it counts the tokens that have come since the last eviction, one per ``decode`` and
+    ``longest`` per ``prefill``, and evicts when there may be no room.  (In a captured graph call ``evict`` where it belongs.)"""
+
+    def __init__(self, sequences: int, q_heads: int, kv_heads: int, head_dim: int, budget: int, recent: int, spare: int = 64, dtype="bf16",
+                 device="cuda:0", rope: Optional[Rope] = None, scale: Optional[float] = None, prefix=None):
+        dt = INPUT_TORCH_DTYPE[DTYPE_CODE[dtype]] if isinstance(dtype, str) else dtype
+        if dt not in _CODE_OF or dtype == "int4" or head_dim not in (64, 128) or sequences < 1:
+            raise ValueError(f"{sequences} sequences of dtype {dtype}, head_dim {head_dim}: need one or more, f32, f16 or bf16, 64 or 128")
+        if not (1 <= budget and 0 <= recent <= budget and 1 <= spare):
+            raise ValueError(f"budget {budget}, recent {recent}, spare {spare}: need 1 <= budget, 0 <= recent <= budget, 1 <= spare")
+        _attention_packed(dt, head_dim, q_heads, kv_heads, budget + spare, scale)
+        self.q_heads, self.budget, self.recent, self.spare, self.rope, self.scale, self.prefix = q_heads, budget, recent, spare, rope, scale, prefix
+        self.first = 0
+        if prefix is not None:
+            s = _slots_of(prefix[0], "prefix", 1, kv_heads, head_dim, dt, torch.device(device).index or 0)
+            _cache_packed(prefix[0], prefix[1], s, dt, prefix[0].get_device())
+            self.first = s[2]
+        self.k, self.v, self.mass, self.positions = self._rows(sequences, kv_heads, budget + spare, head_dim, dt, device)
+        self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
+        self.seen = torch.full((sequences,), self.first, dtype=torch.int32, device=device)
+        self._room, self._empty = budget + spare, True
+
+    @staticmethod
+    def _rows(sequences, kv_heads, slots, head_dim, dt, device):
+        shape = (sequences, kv_heads, slots)
+        return (torch.zeros((*shape, head_dim), dtype=dt, device=device), torch.zeros((*shape, head_dim), dtype=dt, device=device),
+                torch.zeros(shape, device=device), torch.zeros(shape, dtype=torch.int32, device=device))
+
+    def _prepare(self, q, k, positions, default):
+        if q.dim() != 3 or q.shape[1] != self.q_heads:
+            _fail("q", f"[tokens, {self.q_heads}, {self.k.shape[3]}]", q)
+        if self.rope is not None:
+            if positions is None:
+                if self.rope.axes != 1:
+                    raise ValueError("a rope of several axes needs positions")
+                positions = default()
+            q, k = qk_norm_rope(q, k, positions, self.rope)
+        elif positions is not None:
+            raise ValueError("positions without rope")
+        prior = None if self.prefix is None else context_attention(q, *self.prefix, scale=self.scale, partial=True)
+        return q, k, prior
+
+    def prefill(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                longest: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Chunks of prompts (``mass_prefill``), stored and counted.  ``longest``: the most tokens that a sequence has here (default: all of them).
+        A chunk that the spare slots do not hold is read in full in a cache of its own size and then evicted into this one."""
+        tokens = q.shape[0]
+        longest = tokens if longest is None else int(longest)
+        if not 0 <= longest <= tokens:
+            raise ValueError(f"longest {longest}: need 0 .. {tokens}")
+        if tokens == 0 or longest == 0:
+            return _new(q, q.shape, None, True) if out is None else out
+
+        def places():
+            row = torch.arange(tokens, dtype=torch.int32, device=self.k.device)
+            seq = (torch.searchsorted(starts, row, right=True) - 1).clamp(0, starts.numel() - 2)
+            return self.seen[seq] + (row - starts[seq]).clamp(min=0)
+
+        q, k, prior = self._prepare(q, k, positions, places)
+        count = torch.where(self.lengths < 0, 0, starts[1:] - starts[:-1])
+        if longest > self._room and longest <= self.spare:
+            self.evict()
+        if longest <= self._room:
+            out = mass_prefill(q, k, v, starts, self.lengths, self.k, self.v, self.mass, self.positions, self.seen, prior=prior, scale=self.scale, out=out)
+            self.lengths += count
+            self._room -= longest
+        else:
+            n, hk, _, d = self.k.shape
+            whole = self._rows(n, hk, self.budget + longest, d, self.k.dtype, self.k.device)
+            held = self.lengths
+            if not self._empty:
+                held = mass_evict(self.k, self.v, self.mass, self.positions, held, keep=self.budget, recent=self.recent, into=whole)
+            out = mass_prefill(q, k, v, starts, held, *whole, self.seen, prior=prior, scale=self.scale, out=out)
+            mass_evict(*whole, held + count, keep=self.budget, recent=self.recent, into=(self.k, self.v, self.mass, self.positions), left=self.lengths)
+            self._room = self.spare
+        self.seen += count
+        self._empty = False
+        return out
+
+    def decode(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """One token per sequence (``mass_decode``), stored and counted; before it the eviction, if some sequence may be full.  On the current
+        stream."""
+        q, k, prior = self._prepare(q, k, positions, lambda: self.seen)
+        if self._room == 0:
+            self.evict()
+        out = mass_decode(q, k, v, self.lengths, self.k, self.v, self.mass, self.positions, self.seen, prior=prior, scale=self.scale, out=out)
+        active = (self.lengths >= 0).to(torch.int32)
+        self.lengths += active
+        self.seen += active
+        self._room -= 1
+        self._empty = False
+        return out
+
+    def evict(self) -> None:
+        """Bring every sequence down to ``budget`` rows (``mass_evict``, in place).  On the current stream."""
+        mass_evict(self.k, self.v, self.mass, self.positions, self.lengths, keep=self.budget, recent=self.recent, left=self.lengths)
+        self._room = self.spare
