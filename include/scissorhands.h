@@ -507,7 +507,7 @@ typedef struct {
  * starts[i] .. starts[i+1] - 1 see the rows [0, lengths[i]) of context i, all of them.  starts_dev: int32 [contexts + 1], or NULL: one context that
  * all tokens share, or (contexts == tokens) one of its own for each token.  lengths_dev: int32 [contexts], or NULL: `slots` rows each;
  * lengths outside of 0 .. slots are clamped.  Outputs: out, and lse_dev [tokens][q_heads], the natural logs of the sums of exponentials.  A
- * context of length 0 gives zeros and -infinity; rows that belong to no context are left as they were.  starts that decrease or leave 0 .. tokens are clamped, outputs are then meaningless.
+ * context of length 0 gives zeros and -infinity; rows that belong to no context are left as they were, or (clear_rest = 1) get the same.  starts that decrease or leave 0 .. tokens are clamped, outputs are then meaningless.
  * 16-bit types: the weights are rounded once to the type (one token of each context: held in two parts).  out_dtype: a->dtype, or SH_F32
  * for a result that something continues from (it is then not rounded before it joins the rest).
  * workspace_dev: sh_context_attention_workspace_bytes(a, tokens, contexts, starts_dev != NULL) bytes of device memory, 16-byte aligned, or NULL; used
@@ -516,7 +516,8 @@ typedef struct {
  */
 size_t sh_context_attention_workspace_bytes(const sh_attention *a, int tokens, int contexts, int with_starts);
 int sh_context_attention(const sh_attention *a, int tokens, int contexts, const sh_rows *q, const sh_window_cache *context, const int32_t *starts_dev,
-                         const int32_t *lengths_dev, const sh_rows *out, int out_dtype, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+                         const int32_t *lengths_dev, const sh_rows *out, int out_dtype, float *lse_dev, int clear_rest, void *workspace_dev, size_t workspace_bytes,
+                         void *stream);
 
 /*
  * Prompt chunks: the tokens starts[i] .. starts[i+1] - 1 continue sequence i, which holds lengths[i] rows and has seen seen[i] tokens.  They are

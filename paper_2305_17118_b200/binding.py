@@ -127,7 +127,7 @@ def declare(lib: C.CDLL) -> C.CDLL:
     lib.sh_window_decode_workspace_bytes.argtypes = [window, C.c_int]
     lib.sh_window_decode_workspace_bytes.restype = C.c_size_t
     attention = records = vp
-    lib.sh_context_attention.argtypes = [attention, C.c_int, C.c_int, rows, cache, vp, vp, rows, C.c_int, vp, vp, C.c_size_t, vp]
+    lib.sh_context_attention.argtypes = [attention, C.c_int, C.c_int, rows, cache, vp, vp, rows, C.c_int, vp, C.c_int, vp, C.c_size_t, vp]
     lib.sh_context_attention_workspace_bytes.argtypes = [attention, C.c_int, C.c_int, C.c_int]
     lib.sh_mass_prefill.argtypes = [attention, C.c_int, C.c_int, rows, rows, rows, vp, vp, vp, cache, records, rows, C.c_int, vp, rows, vp, C.c_size_t, vp]
     lib.sh_mass_prefill_workspace_bytes.argtypes = [attention, C.c_int, C.c_int]
@@ -811,18 +811,17 @@ def context_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts:
         raise ValueError(f"{n} contexts for {tokens} tokens: without starts there must be one, or one for each token")
     lp = None if lengths is None else _ints(lengths, "lengths", n, device)
     odt = torch.float32 if partial else dtype
-    out = _new(q, shape, stream, sp is not None, odt) if out is None else out
+    if (out is None) != (lse is None):
+        raise ValueError("out and lse: give both or neither")
+    fresh = out is None
+    if fresh:
+        out, lse = _new(q, shape, stream, False, odt), _new(q, shape[:2], stream, False, torch.float32)
     outr = _more_rows(out, "out", shape, odt, device)
-    if lse is None:
-        lse = _new(q, shape[:2], stream, False, torch.float32)
-        if sp is not None:
-            with torch.cuda.stream(stream):
-                lse.fill_(float("-inf"))
     wp, bytes_ = None, lib.sh_context_attention_workspace_bytes(at, tokens, n, sp is not None)
     if bytes_:
         work = _new(q, bytes_, stream, False, torch.uint8)
         wp = work.data_ptr()
-    _launch("context_attention", lib.sh_context_attention, device, stream, at, tokens, n, qr, cache, sp, lp, outr, _CODE_OF[odt], _logs(lse, "lse", shape, device), wp, bytes_)
+    _launch("context_attention", lib.sh_context_attention, device, stream, at, tokens, n, qr, cache, sp, lp, outr, _CODE_OF[odt], _logs(lse, "lse", shape, device), int(fresh), wp, bytes_)
     return out, lse
 
 

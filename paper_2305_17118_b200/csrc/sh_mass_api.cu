@@ -42,6 +42,11 @@ void fill_prior(WindowParams &p, const sh_rows *r, int dtype, const float *lse, 
     p.prior_f32 = dtype == SH_F32;
 }
 size_t up(size_t x, size_t to) { return (x + to - 1) / to * to; }
+// Scratch of the single-token kernels' parts.  They cost a second launch and are never chosen for units of less than 432 KB: a cluster of 8 is
+// done with those first (best_split).  So nothing is asked for there.
+size_t step_scratch(const sh_attention *a, int sequences) {
+    return (long long)a->slots * 4 * a->head_dim < 432000 ? 0 : sh_window_decode_scratch(sequences, a->kv_heads, a->q_heads / a->kv_heads, a->dtype, a->head_dim);
+}
 long long score_stride(const sh_attention *a) { return ((long long)a->slots + 15) / 16 * 16; }
 
 }  // namespace
@@ -51,13 +56,14 @@ extern "C" {
 size_t sh_context_attention_workspace_bytes(const sh_attention *a, int tokens, int contexts, int with_starts) {
     if (!good_attention(a) || tokens < 1 || tokens >= MAX_POS || contexts < 1) return 0;
     const int g = a->q_heads / a->kv_heads;
-    if (!with_starts && tokens == contexts) return sh_window_decode_scratch(contexts, a->kv_heads, g, a->dtype, a->head_dim);
+    if (!with_starts && tokens == contexts) return step_scratch(a, contexts);
     return sh_window_prefill_scratch(tokens, contexts, a->kv_heads, g, a->slots, 0, true, a->dtype, a->head_dim);
 }
 
 int sh_context_attention(const sh_attention *a, int tokens, int contexts, const sh_rows *q, const sh_window_cache *context, const int32_t *starts_dev,
-                         const int32_t *lengths_dev, const sh_rows *out, int out_dtype, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream) {
-    if (!good_attention(a) || (out_dtype != SH_F32 && out_dtype != a->dtype) || tokens < 0 || tokens >= MAX_POS || contexts < 0) return SH_EINVAL;
+                         const int32_t *lengths_dev, const sh_rows *out, int out_dtype, float *lse_dev, int clear_rest, void *workspace_dev, size_t workspace_bytes,
+                         void *stream) {
+    if (!good_attention(a) || (out_dtype != SH_F32 && out_dtype != a->dtype) || (clear_rest & ~1) || tokens < 0 || tokens >= MAX_POS || contexts < 0) return SH_EINVAL;
     if (!starts_dev && contexts != 1 && contexts != tokens) return SH_EINVAL;
     if (tokens == 0 || contexts == 0) return SH_OK;
     const int D = a->head_dim, es = elem_size(a->dtype);
@@ -81,6 +87,11 @@ int sh_context_attention(const sh_attention *a, int tokens, int contexts, const 
     }
     if (!starts_dev && tokens == contexts) return done(sh_launch_window_decode(p, a->dtype, D, ATTEND_CONTEXT, (cudaStream_t)stream));
     p.window = MAX_POS;                          // every row of the context is in sight of every token
+    if (clear_rest && starts_dev) {
+        p.clear_rest = true;
+        const cudaError_t e = sh_launch_clear_rest(p, D * elem_size(out_dtype), (cudaStream_t)stream);
+        if (e != cudaSuccess) return done(e);
+    }
     return done(a->dtype == SH_F32 ? sh_launch_window_prefill_f32(p, D, ATTEND_CONTEXT, (cudaStream_t)stream)
                                    : sh_launch_window_prefill_umma(p, a->dtype, D, ATTEND_CONTEXT, (cudaStream_t)stream));
 }
@@ -133,7 +144,7 @@ int sh_mass_prefill(const sh_attention *a, int tokens, int sequences, const sh_r
 
 size_t sh_mass_decode_workspace_bytes(const sh_attention *a, int sequences) {
     if (!good_attention(a) || sequences < 1) return 0;
-    return up(sh_window_decode_scratch(sequences, a->kv_heads, a->q_heads / a->kv_heads, a->dtype, a->head_dim), 256) +
+    return up(step_scratch(a, sequences), 256) +
            sizeof(float) * (size_t)sequences * a->q_heads * (score_stride(a) + 1);
 }
 
@@ -159,7 +170,7 @@ int sh_mass_decode(const sh_attention *a, int sequences, const sh_rows *q, const
     p.v = rows(v, sequences, a->kv_heads, D, es);
     p.out = rows(out, sequences, a->q_heads, D, es);
     p.lengths = lengths_dev; p.seen = seen_dev;
-    const size_t part = up(sh_window_decode_scratch(sequences, p.hk, p.g, a->dtype, D), 256);
+    const size_t part = up(step_scratch(a, sequences), 256);
     if (part) p.part = static_cast<float *>(workspace_dev);
     p.score_stride = score_stride(a);
     p.scores = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + part);

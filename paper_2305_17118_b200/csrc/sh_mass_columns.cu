@@ -153,6 +153,7 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    sh_pdl_launch_dependents();
     sh_pdl_wait();                                 // (the rows' logs, the chunk in the cache)
     const uint32_t tbase = bars->tmem;
     if (tbase != 0) *(volatile int *)&bars->abort_flag = 0x631;          // (all 512 columns are this CTA's)

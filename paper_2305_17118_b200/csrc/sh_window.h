@@ -44,6 +44,7 @@ struct WindowParams {
     float *lse;                   // [tokens][hq]: log of each row's sum of exponentials, or NULL
     WinRows prior;                // rows to continue from, with prior_lse [tokens][hq], or NULL
     const float *prior_lse;
+    bool clear_rest;              // contexts: rows that belong to none become zeros, and -infinity
     bool out_f32, prior_f32;      // the rows of out (contexts), of the prior are fp32 whatever the type is
     float *scores, *total;        // single tokens: [sequences][hq][score_stride] logits, [sequences][hq] logs of their sums (base 2)
     long long score_stride;
@@ -82,6 +83,8 @@ cudaError_t sh_launch_window_prefill_umma(const WindowParams &p, int dtype, int 
 size_t sh_window_prefill_scratch(int tokens, int sequences, int hk, int g, int window, int sinks, bool with_cache, int dtype, int D);
 // code of the first bounded wait that gave up in a window kernel of the current device since the last call (0: none); synchronises
 cudaError_t sh_window_error_take(int *code, cudaStream_t s);
+// rows of out and lse that belong to no context, for calls with starts
+cudaError_t sh_launch_clear_rest(const WindowParams &p, int row_bytes, cudaStream_t s);
 cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, int mode, cudaStream_t s);      // (ATTEND_MASS: and the new rows' records)
 size_t sh_window_decode_scratch(int sequences, int hk, int g, int dtype, int D);
 cudaError_t sh_launch_window_decode(const WindowParams &p, int dtype, int D, int mode, cudaStream_t s);

@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
     __syncthreads();
     const Tile t = tile_sh;
     if (t.seq < 0) {                                                 // (the whole cluster)
-        if (MODE == ATTEND_MASS) sh_pdl_wait();
+        if (MODE != ATTEND_WINDOW) sh_pdl_wait();
         return;
     }
     const long long rows = (long long)t.count * p.g;
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
             store_row<float, MODE>(p, tok, h, c * 64 + tx * 4, x);
         }
     }
-    if (MODE == ATTEND_MASS) sh_pdl_wait();                          // who comes after this launch also comes after the one that stores the chunk
+    if (MODE != ATTEND_WINDOW) sh_pdl_wait();                        // who comes after this launch also comes after the one beside it
 }
 
 // Copy the rows that a later token can see into their slots: PIECES lanes move one token's key and value row of one head.
@@ -326,6 +326,20 @@ __global__ void __launch_bounds__(256) sh_window_append_kernel(const WindowParam
         const long long r = lo * p.rss + h * p.rhs + slot;
         p.mass[r] = 0.f;
         p.held[r] = p.seen[lo] + (int)(tok - first);
+    }
+}
+
+// Zeros, and -infinity, in the rows before the first context's and behind the last one's.
+__global__ void __launch_bounds__(256) sh_clear_rest_kernel(const WindowParams p, int pieces) {
+    sh_pdl_launch_dependents();      // (the attention writes other rows)
+    const int first = min(max(p.starts[0], 0), p.tokens), end = min(max(p.starts[p.sequences], first), p.tokens);
+    const long long rows = (long long)(p.tokens - (end - first)) * p.hq;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * pieces; i += gridDim.x * 256ll) {
+        const int c = (int)(i % pieces), h = (int)(i / pieces % p.hq);
+        long long tok = i / pieces / p.hq;
+        if (tok >= first) tok += end - first;
+        *reinterpret_cast<uint4 *>(p.out.p + tok * p.out.ts + h * p.out.hs + c * 16) = make_uint4(0, 0, 0, 0);
+        if (c == 0) p.lse[tok * p.hq + h] = -CUDART_INF_F;
     }
 }
 
@@ -360,7 +374,7 @@ cudaError_t launch(const WindowParams &p, cudaStream_t s) {
         attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
-        cfg.numAttrs = MODE == ATTEND_MASS ? 2 : 1;                  // (beside the launch that stores the chunk)
+        cfg.numAttrs = MODE == ATTEND_MASS || p.clear_rest ? 2 : 1;  // (beside the launch that stores the chunk, or clears what belongs to no context)
         return cudaLaunchKernelEx(&cfg, kern, p);
     }
 }
@@ -379,5 +393,10 @@ cudaError_t sh_launch_window_append(const WindowParams &p, int es, int D, int mo
     if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
     if (mode == ATTEND_MASS) sh_window_append_kernel<ATTEND_MASS><<<(unsigned)blocks, 256, 0, s>>>(p, pieces);
     else sh_window_append_kernel<ATTEND_WINDOW><<<(unsigned)blocks, 256, 0, s>>>(p, pieces);
+    return cudaGetLastError();
+}
+
+cudaError_t sh_launch_clear_rest(const WindowParams &p, int row_bytes, cudaStream_t s) {
+    sh_clear_rest_kernel<<<32, 256, 0, s>>>(p, row_bytes / 16);
     return cudaGetLastError();
 }

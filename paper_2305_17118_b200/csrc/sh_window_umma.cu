@@ -459,6 +459,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     Bars *bars = reinterpret_cast<Bars *>(sm + C::OFF_BAR);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     auto aborted = [&]() { return *(volatile int *)&bars->abort_flag != 0; };
+    if (MODE != ATTEND_WINDOW) sh_pdl_launch_dependents();      // (what follows waits; its CTAs take the places that these leave)
 
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem)), "r"(512) : "memory");
@@ -1013,7 +1014,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
     tc_fence_before();
     __syncthreads();
     if (tid == 0 && bars->abort_flag) atomicCAS(&g_window_error, 0, bars->abort_flag);
-    if (MODE == ATTEND_MASS) sh_pdl_wait();            // who comes after this launch also comes after the one that stores the chunk
+    if (MODE != ATTEND_WINDOW) sh_pdl_wait();          // who comes after this launch also comes after the one beside it
     if (warp == 0) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tbase), "r"(512) : "memory");
@@ -1031,6 +1032,7 @@ __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __
     const int item = blockIdx.x / (2 * TM / ROWS), id = item * p.parts;      // id: of its first part
     const int in = item % (p.w.hk * p.hblocks), kvh = in / p.hblocks, hb = in % p.hblocks;
     const int tok = t * p.tpt + row / p.gb, h = hb * p.gb + row % p.gb;      // of the item
+    if (MODE != ATTEND_WINDOW) sh_pdl_launch_dependents();
     sh_pdl_wait();
     const int4 w = part_item<D>(p)[item];
     const int parts = min(w.x, p.parts);
@@ -1057,7 +1059,7 @@ __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __
         }
     } else {
         // the parts' sums and outputs are asked for together, AHEAD parts at a time (256 rows of 18 parts: 3 us less)
-        constexpr int AHEAD = 8;
+        constexpr int AHEAD = 4;
         if (tid < ROWS) odd[tid] = 0;
         for (int i0 = 0; i0 < parts; i0 += AHEAD) {
             float2 s[AHEAD];
@@ -1180,7 +1182,7 @@ cudaError_t launch(const WindowParams &w, cudaStream_t s) {
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
-    cfg.numAttrs = MODE == ATTEND_MASS;                // (beside the launch that stores the chunk)
+    cfg.numAttrs = MODE == ATTEND_MASS || w.clear_rest;      // (beside the launch that stores the chunk, or clears what belongs to no context)
     const cudaError_t e2 = cudaLaunchKernelEx(&cfg, kern, p, mq, mk, mv, mkc, mvc, mo);
     if (e2 != cudaSuccess || p.parts == 1) return e2;
     cfg.gridDim = dim3((unsigned)(items * (2 * TM / 8)));

@@ -19,7 +19,7 @@ def _args(sh):
     cache = lambda at, slots: sh._WindowCache(at, at, 2 * slots * 64, slots * 64, 64)
     return dict(a=sh._Attention(sh.SH_F16, 64, 4, 2, 10, 0.0), q=rows(4), k=rows(2), v=rows(2), out=rows(4), starts=FAKE, lengths=FAKE, seen=FAKE,
                 cache=cache(FAKE, 10), rec=sh._Records(FAKE, FAKE, 20, 10), prior=None, prior_dtype=sh.SH_F16, prior_lse=None, out_dtype=sh.SH_F16,
-                lse=FAKE, tokens=4, n=3, keep=6, recent=2, into=None, into_rec=None, into_slots=0, left=FAKE + 4096, work=FAKE, work_bytes=HUGE)
+                lse=FAKE, clear=0, tokens=4, n=3, keep=6, recent=2, into=None, into_rec=None, into_slots=0, left=FAKE + 4096, work=FAKE, work_bytes=HUGE)
 
 
 def _calls(sh, x):
@@ -27,7 +27,7 @@ def _calls(sh, x):
     lib = sh.lib
     return dict(
         context=lambda: lib.sh_context_attention(ref(x["a"]), x["tokens"], x["n"], ref(x["q"]), ref(x["cache"]), x["starts"], x["lengths"], ref(x["out"]),
-                                                 x["out_dtype"], x["lse"], x["work"], x["work_bytes"], None),
+                                                 x["out_dtype"], x["lse"], x["clear"], x["work"], x["work_bytes"], None),
         prefill=lambda: lib.sh_mass_prefill(ref(x["a"]), x["tokens"], x["n"], ref(x["q"]), ref(x["k"]), ref(x["v"]), x["starts"], x["lengths"], x["seen"],
                                             ref(x["cache"]), ref(x["rec"]), ref(x["prior"]), x["prior_dtype"], x["prior_lse"], ref(x["out"]), x["work"],
                                             x["work_bytes"], None),
@@ -51,7 +51,7 @@ ALL, MASS, STEPS, TOKENS = ("context", "prefill", "decode", "evict"), ("prefill"
     (STEPS, dict(v__data=None)), (ALL[:3], dict(q=None)), (ALL[:3], dict(out=None)), (ALL[:3], dict(q__data=FAKE + 8)),
     (ALL[:3], dict(q__token_stride=68)), (ALL[:3], dict(out__token_stride=128)), (ALL, dict(cache__k=FAKE + 4)), (ALL, dict(cache__slot_stride=32)),
     (MASS, dict(cache__head_stride=64)), (MASS, dict(cache__sequence_stride=640)), (ALL, dict(cache__sequence_stride=0)),
-    (("context",), dict(out_dtype=2)), (("context",), dict(lse=None)), (("context",), dict(lse=FAKE + 2)), (("context",), dict(out_dtype=0, out__head_stride=66)),
+    (("context",), dict(out_dtype=2)), (("context",), dict(clear=2)), (("context",), dict(lse=None)), (("context",), dict(lse=FAKE + 2)), (("context",), dict(out_dtype=0, out__head_stride=66)),
     (STEPS, dict(prior_lse=FAKE)), (MASS, dict(work=None)), (ALL, dict(work=FAKE + 8)),
     (("evict",), dict(keep=0)), (("evict",), dict(keep=11)), (("evict",), dict(recent=-1)), (("evict",), dict(recent=7)), (("evict",), dict(left=None)),
     (("evict",), dict(left=FAKE + 4)), (("evict",), dict(into_rec="rec")), (("evict",), dict(into="cache")),
@@ -91,6 +91,9 @@ def test_workspaces():
     sh = _sh()
     x = _args(sh)
     a, lib = C.byref(x["a"]), sh.lib
+    x["a"].slots = 9000
+    x["cache"] = sh._WindowCache(FAKE, FAKE, 2 * 9000 * 64, 9000 * 64, 64)
+    x["rec"] = sh._Records(FAKE, FAKE, 18000, 9000)
     sizes = dict(prefill=lib.sh_mass_prefill_workspace_bytes(a, 4, 3), decode=lib.sh_mass_decode_workspace_bytes(a, 3),
                  evict=lib.sh_mass_evict_workspace_bytes(a, 3, 6, 1), context=lib.sh_context_attention_workspace_bytes(a, 3, 3, 0))
     x["tokens"] = 4
@@ -102,8 +105,10 @@ def test_workspaces():
         assert _calls(sh, x)[name]() == sh.SH_ENOMEM, name
     assert lib.sh_mass_prefill_workspace_bytes(a, 0, 3) == 0 and lib.sh_mass_prefill_workspace_bytes(None, 4, 3) == 0
     assert lib.sh_mass_decode_workspace_bytes(a, 0) == 0 and lib.sh_mass_decode_workspace_bytes(None, 3) == 0
-    assert lib.sh_mass_evict_workspace_bytes(a, 3, 0, 1) == 0 and lib.sh_mass_evict_workspace_bytes(a, 3, 11, 1) == 0
+    assert lib.sh_mass_evict_workspace_bytes(a, 3, 0, 1) == 0 and lib.sh_mass_evict_workspace_bytes(a, 3, 9001, 1) == 0
     assert lib.sh_mass_evict_workspace_bytes(a, 3, 11, 0) > 0
+    x["a"].slots = 9
+    assert lib.sh_context_attention_workspace_bytes(a, 3, 3, 0) == 0          # little to read: nothing is dealt out
     assert lib.sh_context_attention_workspace_bytes(a, 0, 3, 1) == 0 and lib.sh_context_attention_workspace_bytes(None, 4, 3, 1) == 0
 
 
