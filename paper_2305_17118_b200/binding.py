@@ -815,7 +815,8 @@ def context_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts:
         raise ValueError("out and lse: give both or neither")
     fresh = out is None
     if fresh:
-        out, lse = _new(q, shape, stream, False, odt), _new(q, shape[:2], stream, False, torch.float32)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format) if stream is None and odt is dtype else _new(q, shape, stream, False, odt)
+        lse = _new(q, shape[:2], stream, False, torch.float32)
     outr = _more_rows(out, "out", shape, odt, device)
     wp, bytes_ = None, lib.sh_context_attention_workspace_bytes(at, tokens, n, sp is not None)
     if bytes_:

@@ -103,7 +103,7 @@ size_t sh_mass_prefill_workspace_bytes(const sh_attention *a, int tokens, int se
     // (the columns kernel comes after the attention: they share a place)
     return up(std::max(sh_window_prefill_scratch(tokens, sequences, a->kv_heads, g, a->slots, 0, true, a->dtype, a->head_dim),
                        a->dtype == SH_F32 ? 0 : sh_mass_columns_scratch(tokens, sequences, a->kv_heads, g, a->slots)), 256) +
-           up(sizeof(float) * (size_t)tokens * a->q_heads, 256);
+           up(sizeof(float) * (size_t)tokens * a->q_heads + sizeof(int), 256);
 }
 
 int sh_mass_prefill(const sh_attention *a, int tokens, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *starts_dev,
@@ -130,9 +130,10 @@ int sh_mass_prefill(const sh_attention *a, int tokens, int sequences, const sh_r
     p.out = rows(out, tokens, a->q_heads, D, es);
     p.starts = starts_dev; p.lengths = lengths_dev; p.seen = seen_dev;
     p.fit = a->slots;
-    const size_t lse_bytes = up(sizeof(float) * (size_t)tokens * a->q_heads, 256);
+    const size_t lse_bytes = up(sizeof(float) * (size_t)tokens * a->q_heads + sizeof(int), 256);
     if (need > lse_bytes) p.part = static_cast<float *>(workspace_dev);
     p.lse = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + need - lse_bytes);
+    p.taken = reinterpret_cast<int *>(p.lse + (size_t)tokens * a->q_heads);
     fill_prior(p, prior, prior_dtype, prior_lse_dev, a, tokens);
     const cudaStream_t s = (cudaStream_t)stream;
     // the chunk goes into slots that the attention does not look at: the two run side by side

@@ -10,9 +10,9 @@
 //   warp 17          finds the items (128 keys of a key head), publishes them in a ring and requests the tiles (TMA, 128-byte swizzle)
 //
 // Four buffers of S fill tensor memory.  The rows' logs are read from global memory two tiles ahead by the group that needs them, a thread
-// a row, and handed around in shared memory.  A CTA walks over items in a fixed order, from the ends of the list in turn (the first
-// key blocks of a sequence are seen by all its rows, the last by few).  Where an item would be long against what an SM has to do in all, its
-// row tiles are dealt out to several items, whose sums a second launch adds up in their order: no atomics, the same result every time.
+// a row, and handed around in shared memory.  A CTA takes the next item when it has requested the last tile of the one before (the first
+// key blocks of a sequence are seen by all its rows, the last by few: long ones come first).  Where an item would be long against what an SM has to do in all, its
+// row tiles are dealt out to several items, whose sums a second launch adds up in their order: whoever takes them, the result is the same.
 //
 // Bound by the exponentials: a tile has 16384, at 16 a cycle on an SM, while its MMAs take 256 cycles (D = 128).
 #include <math_constants.h>
@@ -75,9 +75,6 @@ __device__ __forceinline__ bool wait_for(ColBars *bars, uint64_t *bar, uint32_t 
     *(volatile int *)&bars->abort_flag = code;
     return false;
 }
-// The n-th item of this CTA among all CTAs of the launch.
-__device__ __forceinline__ long long item_of(long long n, int cta, int ctas) { return n * ctas + (n & 1 ? ctas - 1 - cta : cta); }
-
 __device__ __forceinline__ ColItem find_item(const ColParams &p, long long id) {
     ColItem r = {};
     const int lane = threadIdx.x & 31;
@@ -201,7 +198,9 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
         uint32_t it = 0, tiles = 0, loads = 0;
         bool more = true;
         while (ok && more) {
-            const ColItem w = find_item(p, item_of(it, blockIdx.x, gridDim.x));
+            int id = 0;
+            if (lane == 0) id = atomicAdd(p.w.taken, 1);
+            const ColItem w = find_item(p, __shfl_sync(0xffffffffu, id, 0));
             more = w.seq >= 0;
             ok = __all_sync(0xffffffffu, it < RING || wait_for(bars, &bars->item_free[it % RING], (it / RING - 1) & 1, 0x636));
             if (!ok) break;
@@ -324,6 +323,7 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
                 }
             }
             if (__any_sync(0xffffffffu, !ok)) break;
+            const uint32_t lead = tiles % GROUPS;                        // the group that has taken the item's first tile
             tiles += w.tiles;
             float a, b;
             un2(add2(sum0, sum1), a, b);
@@ -333,7 +333,9 @@ sh_mass_columns_umma_kernel(const __grid_constant__ ColParams p, const __grid_co
             ok = wait_for(bars, &bars->part_full, turn, 0x63e);
             if (__any_sync(0xffffffffu, !ok)) break;
             if (grp == (int)(it % GROUPS) && slot < n_keys) {
-                const float x = (bars->part[turn][0][key] + bars->part[turn][1][key]) + (bars->part[turn][2][key] + bars->part[turn][3][key]);
+                // in the order of the tiles, whatever the CTA has done before
+                auto part = [&](uint32_t i) { return bars->part[turn][(lead + i) % GROUPS][key]; };
+                const float x = (part(0) + part(1)) + (part(2) + part(3));
                 if (p.parts == 1) p.w.mass[w.seq * p.w.rss + w.kvh * p.w.rhs + slot] += x;
                 else p.w.part[(((long long)w.part * p.w.sequences + w.seq) * p.w.hk + w.kvh) * p.w.slots + slot] = x;
             }

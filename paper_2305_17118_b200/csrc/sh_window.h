@@ -44,6 +44,7 @@ struct WindowParams {
     float *lse;                   // [tokens][hq]: log of each row's sum of exponentials, or NULL
     WinRows prior;                // rows to continue from, with prior_lse [tokens][hq], or NULL
     const float *prior_lse;
+    int *taken;                   // prompts over a cache with masses: items of the columns kernel that a CTA has taken (zeroed with the append)
     bool clear_rest;              // contexts: rows that belong to none become zeros, and -infinity
     bool out_f32, prior_f32;      // the rows of out (contexts), of the prior are fp32 whatever the type is
     float *scores, *total;        // single tokens: [sequences][hq][score_stride] logits, [sequences][hq] logs of their sums (base 2)

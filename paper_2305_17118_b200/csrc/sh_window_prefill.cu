@@ -305,7 +305,10 @@ __global__ void __launch_bounds__(NT, 4) sh_window_prefill_f32_kernel(const Wind
 // A warp's rows are neighbouring heads of the same token.
 template <int MODE>
 __global__ void __launch_bounds__(256) sh_window_append_kernel(const WindowParams p, int pieces) {
-    if (MODE == ATTEND_MASS) sh_pdl_launch_dependents();      // (the attention needs nothing of this)
+    if (MODE == ATTEND_MASS) {
+        sh_pdl_launch_dependents();      // (the attention needs nothing of this)
+        if (blockIdx.x == 0 && threadIdx.x == 0 && p.taken) *p.taken = 0;
+    }
     const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
     const int c = (int)(id % pieces);
     const long long rh = id / pieces;
