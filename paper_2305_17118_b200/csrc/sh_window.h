@@ -49,7 +49,7 @@ struct WindowParams {
     bool out_f32, prior_f32;      // the rows of out (contexts), of the prior are fp32 whatever the type is
     float *scores, *total;        // single tokens: [sequences][hq][score_stride] logits, [sequences][hq] logs of their sums (base 2)
     long long score_stride;
-    bool add_here;                // the single-token kernel adds the weights to the masses itself
+    int add;                      // how the weights get to the masses (ADD_*)
     const int32_t *seen;          // [sequences]: position of a sequence's next token
     float *mass;                  // [sequences][hk][slots] with the strides below, in elements; positions alike
     int32_t *held;
@@ -59,6 +59,8 @@ struct WindowParams {
 // What a kernel attends to and leaves: the window's calls; the same over a cache with accumulated weights (every live slot is in sight,
 // the logs of the rows' sums are kept); a context that all its tokens see in full.
 enum { ATTEND_WINDOW = 0, ATTEND_MASS = 1, ATTEND_CONTEXT = 2 };
+// Single tokens: by a launch of its own, by the attention's CTAs from the scores in global memory, or from scores that they keep in shared memory.
+enum { ADD_LATER = 0, ADD_IN_PLACE = 1, ADD_FROM_SHARED = 2 };
 
 // SMs of the current device, and that a kernel may use `smem` bytes of shared memory there.  Both are facts of the device, asked once
 // (two threads that come first together both ask, and write the same).

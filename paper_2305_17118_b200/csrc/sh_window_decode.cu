@@ -104,15 +104,16 @@ __device__ __forceinline__ int rows_before(const WindowParams &p, int seq) {
 }
 
 // The last step for N elements of a row, from d on: `base` + log2(L) is the log of its sum, x its unnormalised output.  Over a cache with
-// accumulated weights the row continues from the prior's, if there is one, and leaves that log for the masses; a context's goes to the caller.
+// accumulated weights the row continues from the prior's, if there is one, and leaves that log for the masses in `total`; a context's goes to
+// the caller.
 template <typename T, int MODE, int N>
-__device__ __forceinline__ void finish(const WindowParams &p, int seq, int h, int d, float base, float L, bool empty, float (&x)[N]) {
+__device__ __forceinline__ void finish(const WindowParams &p, int seq, int h, int d, float base, float L, bool empty, float *total, float (&x)[N]) {
     if constexpr (MODE == ATTEND_WINDOW) {
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] /= L;
     } else {
         const Close c = close_row<MODE>(p, seq, h, base, L);
-        if (MODE == ATTEND_MASS && d == 0) p.total[(long long)seq * p.hq + h] = c.total;
+        if (MODE == ATTEND_MASS && d == 0) *total = c.total;
         if (MODE == ATTEND_CONTEXT && d == 0) p.lse[(long long)seq * p.hq + h] = empty ? -CUDART_INF_F : 0.69314718055994531f * c.total;
         float y[N] = {};
         if (c.other != 0.f) prior_row<T>(p, seq, h, d, y);
@@ -121,12 +122,15 @@ __device__ __forceinline__ void finish(const WindowParams &p, int seq, int h, in
     }
 }
 
+__device__ __forceinline__ float *scores_of(const WindowParams &p, int seq, int h) { return p.scores + ((long long)seq * p.hq + h) * p.score_stride; }
+__device__ __forceinline__ float *total_of(const WindowParams &p, int seq, int h) { return p.total + (long long)seq * p.hq + h; }
+
 // The step's weights into the masses, once the unit's scores and totals are there for the whole cluster: a CTA takes the chunks of ROWS slots that
 // it attended to, a thread a slot, the heads in their order (as sh_mass_fold_kernel, which does it where a key head has several units or
 // its rows were dealt out).
 template <int ROWS>
 __device__ __forceinline__ void add_weights(const WindowParams &p, int seq, int kvh, int t, int rank, int S) {
-    const float *score = p.scores + ((long long)seq * p.hq + kvh * p.g) * p.score_stride, *total = p.total + (long long)seq * p.hq + kvh * p.g;
+    const float *score = scores_of(p, seq, kvh * p.g), *total = total_of(p, seq, kvh * p.g);
     const long long at = seq * p.rss + kvh * p.rhs;
     for (int i = threadIdx.x; ; i += blockDim.x) {
         const int first = (rank + i / ROWS * S) * ROWS, j = first + i % ROWS;
@@ -189,7 +193,7 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
                 s[r] += __shfl_xor_sync(0xffffffffu, s[r], 2);
                 s[r] += __shfl_xor_sync(0xffffffffu, s[r], 4);
                 if (valid[r]) mn = fmaxf(mn, s[r]);
-                if (MODE == ATTEND_MASS && valid[r] && l8 == 0 && q < nq) p.scores[((long long)seq * p.hq + h0 + q) * p.score_stride + first + 4 * r] = s[r];
+                if (MODE == ATTEND_MASS && valid[r] && l8 == 0 && q < nq) scores_of(p, seq, h0 + q)[first + 4 * r] = s[r];
             }
             const float base = mn == -CUDART_INF_F ? 0.f : mn, keep = ex2_approx(m[q] - base);
             m[q] = mn;
@@ -302,11 +306,11 @@ __global__ void __launch_bounds__(NT) sh_window_decode_simt_kernel(const WindowP
 #pragma unroll
             for (int e = 0; e < N; ++e) x[e] = fmaf(c[2 + d + e], f, x[e]);
         }
-        finish<T, MODE>(p, seq, h0 + q, d, M, L, live == 0, x);
+        finish<T, MODE>(p, seq, h0 + q, d, M, L, live == 0, total_of(p, seq, h0 + q), x);
         store_row<T, MODE>(p, seq, h0 + q, d, x);
     }
     cluster.sync();      // nobody's shared memory goes away while it is read
-    if (MODE == ATTEND_MASS && p.add_here) add_weights<WARPS * BLOCK>(p, seq, kvh, t, rank, S);
+    if (MODE == ATTEND_MASS && p.add == ADD_IN_PLACE) add_weights<WARPS * BLOCK>(p, seq, kvh, t, rank, S);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -341,6 +345,7 @@ template <int D, int MW> struct Mma {      // MW: warps of a CTA
     static constexpr int OFF_F32 = OFF_NEW + 2 * ROW;                         // [MQ + 2][D] fp32: the same rows before the rounding
     static constexpr int OFF_PART = OFF_F32;                                  // (later) this CTA's maximum, sum, output: [MQ][D + 2]
     static constexpr int SMEM = OFF_F32 + (MQ + 2) * D * 4;
+    static constexpr int SHARED_SCORES = (MQ + 2) * D - (D + 2) - 1;           // scores of one query that have a place besides its result
     static_assert(MQ * (D + 2) <= (MQ + 2) * D, "");
     static_assert(STAGES * STAGE >= MQ * (D + 2) * 4, "a warp's result takes the place of its ring");
 };
@@ -381,7 +386,8 @@ template <typename T> __device__ __forceinline__ void split2(float x, float y, u
 // One query by the D / 8 lanes that finish it: every live row once, in fp32.  x: this lane's 8 elements of the prepared query; fresh: key and
 // value rows that stand for those of slot snew (NULL: they are in the cache already).
 template <typename T, int D, int MODE>
-__device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, int h, int live, int snew, const unsigned char *fresh, const float4 x0, const float4 x1) {
+__device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, int h, int live, int snew, const unsigned char *fresh, const float4 x0, const float4 x1,
+                                       float *scores, float *total) {
     constexpr int CHUNKS = D / 8;
     const int c = threadIdx.x % CHUNKS;
     const unsigned group = ((1u << CHUNKS) - 1u) << ((threadIdx.x & 31) & ~(CHUNKS - 1));
@@ -399,14 +405,14 @@ __device__ __noinline__ void plain_row(const WindowParams &p, int seq, int kvh, 
 #pragma unroll
         for (int i = CHUNKS / 2; i; i >>= 1) s += __shfl_xor_sync(group, s, i);
         s *= p.scale_log2e;
-        if (MODE == ATTEND_MASS && c == 0) p.scores[((long long)seq * p.hq + h) * p.score_stride + j] = s;
+        if (MODE == ATTEND_MASS && c == 0) scores[j] = s;
         const float mn = fmaxf(m, s), b = mn == -CUDART_INF_F ? 0.f : mn, keep = ex2_approx(m - b), w = ex2_approx(s - b);
         m = mn;
         l = l * keep + w;
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = fmaf(w, v[e], o[e] * keep);
     }
-    finish<T, MODE>(p, seq, h, c * 8, m, l, false, o);
+    finish<T, MODE>(p, seq, h, c * 8, m, l, false, total, o);
     store_row<T, MODE>(p, seq, h, c * 8, o);
 }
 
@@ -476,6 +482,13 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) ldsm4(shasync::smem_u32(sm) + C::OFF_Q + mrow * C::ROW + (((2 * k + mcol) ^ (mrow & 7)) << 4), qf[k]);
 
+    // scores and logs of the unit's rows: for small caches in the place of the staged rows, behind what the merge puts there
+    float *scores = nullptr, *total = nullptr;
+    if (MODE == ATTEND_MASS) {
+        const bool shared = p.add == ADD_FROM_SHARED;
+        scores = shared ? rows + nq * (D + 2) : scores_of(p, seq, h0);
+        total = shared ? scores + nq * p.score_stride : total_of(p, seq, h0);
+    }
     float o[D / 16][4];
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.f;
@@ -521,7 +534,7 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
 #pragma unroll
             for (int e = 0; e < 2; ++e) x[2 * n + e] = j + 8 * n + e < live ? (s[n][e] + s[n][2 + e]) * p.scale_log2e : -CUDART_INF_F;
         if (MODE == ATTEND_MASS && (lane >> 2) < nq) {      // (a row of scores has a place for every row of the last block)
-            float *to = p.scores + ((long long)seq * p.hq + h0 + (lane >> 2)) * p.score_stride + j;
+            float *to = scores + (lane >> 2) * p.score_stride + j;
             *reinterpret_cast<float2 *>(to) = make_float2(x[0], x[1]);
             *reinterpret_cast<float2 *>(to + 8) = make_float2(x[2], x[3]);
         }
@@ -554,6 +567,13 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
         st = st == C::STAGES - 1 ? 0 : st + 1;
     }
     cp_wait<0>();
+    constexpr int OLD = C::SHARED_SCORES / (MW * 32) + 1;
+    float old[OLD];                                   // masses that the step's weights are added to: asked for before the results are merged
+    const long long records = seq * p.rss + kvh * p.rhs;
+    if (MODE == ATTEND_MASS && p.add == ADD_FROM_SHARED) {
+#pragma unroll
+        for (int i = 0; i < OLD; ++i) old[i] = tid + i * MW * 32 < t ? p.mass[records + tid + i * MW * 32] : 0.f;
+    }
     l += __shfl_xor_sync(0xffffffffu, l, 1);
     l += __shfl_xor_sync(0xffffffffu, l, 2);
     __syncwarp();
@@ -610,7 +630,7 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
             for (int e = 0; e < 8; ++e) acc[e] = fmaf(c[2 + d + e], f, acc[e]);
         }
         bool odd = false;
-        finish<T, MODE>(p, seq, h0 + q, d, M - Weights<T>::LIFT, L, live == 0, acc);
+        finish<T, MODE>(p, seq, h0 + q, d, M - Weights<T>::LIFT, L, live == 0, total + q, acc);
 #pragma unroll
         for (int e = 0; e < 8; ++e) odd |= !isfinite(acc[e]);
         // the low part of a weight or of a query may be zero and meet an infinity: such rows are computed again in plain fp32
@@ -622,12 +642,23 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
         const float4 x0 = make_float4(hi[0], hi[1], hi[2], hi[3]), x1 = make_float4(hi[4], hi[5], hi[6], hi[7]);
         const unsigned group = ((1u << CHUNKS) - 1u) << (lane & ~(CHUNKS - 1));
         if (__any_sync(group, odd))
-            plain_row<T, D, MODE>(p, seq, kvh, h0 + q, live, snew, MODE == ATTEND_CONTEXT ? nullptr : sm + C::OFF_NEW, x0, x1);
+            plain_row<T, D, MODE>(p, seq, kvh, h0 + q, live, snew, MODE == ATTEND_CONTEXT ? nullptr : sm + C::OFF_NEW, x0, x1, scores + q * p.score_stride, total + q);
         else
             store_row<T, MODE>(p, seq, h0 + q, d, acc);
     }
     cluster.sync();                                   // nobody's shared memory goes away while it is read
-    if (MODE == ATTEND_MASS && p.add_here) add_weights<MW * MB>(p, seq, kvh, t, rank, S);
+    if (MODE == ATTEND_MASS && p.add == ADD_IN_PLACE) add_weights<MW * MB>(p, seq, kvh, t, rank, S);
+    if (MODE == ATTEND_MASS && p.add == ADD_FROM_SHARED) {
+#pragma unroll
+        for (int i = 0; i < OLD; ++i) {
+            const int j = tid + i * MW * 32;
+            if (j > t) break;
+            float sum = 0.f;
+            for (int q = 0; q < nq; ++q) sum += ex2_approx(scores[q * p.score_stride + j] - total[q]);
+            p.mass[records + j] = old[i] + sum;
+            if (j == t) p.held[records + j] = p.seen[seq];
+        }
+    }
 }
 
 // Merge the `parts` results of each unit: a CTA per (unit, query), SLICES groups of D / 8 lanes that take every SLICES-th part each.
@@ -681,12 +712,12 @@ __global__ void __launch_bounds__(SLICES * D / 8) sh_window_decode_merge_kernel(
         acc[e] = x;
     }
     const int h = kvh * p.g + qb * MQ + q;
-    finish<T, MODE>(p, seq, h, c * 8, M - Weights<T>::LIFT, L, t == 0, acc);
+    finish<T, MODE>(p, seq, h, c * 8, M - Weights<T>::LIFT, L, t == 0, total_of(p, seq, h), acc);
 #pragma unroll
     for (int e = 0; e < 8; ++e) odd |= !isfinite(acc[e]);
     if (__any_sync((1u << CHUNKS) - 1u, odd)) {
         const float4 *x = reinterpret_cast<const float4 *>(p.part + units * parts * REC + unit * (MQ * D) + q * D + c * 8);
-        plain_row<T, D, MODE>(p, seq, kvh, h, MODE == ATTEND_CONTEXT ? t : min(t + 1, p.sinks + p.window), 0, nullptr, x[0], x[1]);
+        plain_row<T, D, MODE>(p, seq, kvh, h, MODE == ATTEND_CONTEXT ? t : min(t + 1, p.sinks + p.window), 0, nullptr, x[0], x[1], scores_of(p, seq, h), total_of(p, seq, h));
     } else {
         store_row<T, MODE>(p, seq, h, c * 8, acc);
     }
@@ -747,16 +778,21 @@ cudaError_t launch_units(const WindowParams &p, int qblocks, int threads, size_t
     return cudaLaunchKernelEx(&cfg, kern, p, qblocks, parts);
 }
 
-// A launch of clusters and, for the masses, the weights' addition: by the CTAs themselves where a key head is one unit and all of them run
-// at once, as it saves a launch (5 sequences, 12 heads of 64, fp32: 8.3 -> 7.3 us); else by a launch of its own, as the CTAs that wait for a
-// place wait for it too (9216 units of 442 rows: 356 against 396 us).
+// A launch of clusters and, for the masses, the weights' addition: by the CTAs themselves from scores in shared memory where a unit is one
+// CTA and they fit (`places`: floats for them; 9216 units of 442 rows: 350 against 356 us), or from scores in global memory where a key
+// head is one unit and all of them run at once, as it saves a launch (5 sequences, 12 heads of 64, fp32: 8.3 -> 7.3 us); else by a launch of
+// its own, as the CTAs that wait for a place wait for the scores' way too (the same 9216 units: 396 us).
 template <auto kern, int MODE>
-cudaError_t launch_step(WindowParams p, int qblocks, int threads, size_t smem, int S, const int (&slots)[4], cudaStream_t s) {
+cudaError_t launch_step(WindowParams p, int D, int qblocks, int threads, size_t smem, int S, const int (&slots)[4], int places, cudaStream_t s) {
     int i = 0;
     while (1 << i < S) ++i;
-    p.add_here = MODE == ATTEND_MASS && qblocks == 1 && (long long)p.sequences * p.hk * S <= slots[i];
+    p.add = ADD_LATER;
+    if (MODE == ATTEND_MASS && qblocks == 1) {
+        if (S == 1 && p.g * (D + 2 + p.score_stride + 1) <= places) p.add = ADD_FROM_SHARED;
+        else if ((long long)p.sequences * p.hk * S <= slots[i]) p.add = ADD_IN_PLACE;
+    }
     const cudaError_t e = launch_units<kern>(p, qblocks, threads, smem, S, 0, s);
-    return MODE == ATTEND_MASS && e == cudaSuccess && !p.add_here ? sh_launch_mass_fold(p, s) : e;
+    return MODE == ATTEND_MASS && e == cudaSuccess && p.add == ADD_LATER ? sh_launch_mass_fold(p, s) : e;
 }
 
 template <int D, int GQ, int MODE>
@@ -767,7 +803,7 @@ cudaError_t launch_simt(const WindowParams &p, cudaStream_t s) {
     const cudaError_t e = cluster_slots<kern>(NT, 0, slots);
     if (e != cudaSuccess) return e;
     const Shape a = best_split((long long)p.sequences * p.hk * qblocks, (long long)p.window + p.sinks, 8 * D, slots, 3.0e4);
-    return launch_step<kern, MODE>(p, qblocks, NT, 0, a.S, slots, s);
+    return launch_step<kern, MODE>(p, D, qblocks, NT, 0, a.S, slots, 0, s);
 }
 template <int D, int MODE>
 cudaError_t launch_f32(const WindowParams &p, cudaStream_t s) {
@@ -809,8 +845,9 @@ cudaError_t launch_mma(const WindowParams &p, cudaStream_t s) {
             return MODE == ATTEND_MASS && e == cudaSuccess ? sh_launch_mass_fold(p, s) : e;
         }
     }
-    return a.us <= b.us ? launch_step<small, MODE>(p, qblocks, 128, Small::SMEM, a.S, slots_a, s)
-                        : launch_step<large, MODE>(p, qblocks, 256, Large::SMEM, b.S, slots_b, s);
+    constexpr int places = (MQ + 2) * D;
+    return a.us <= b.us ? launch_step<small, MODE>(p, D, qblocks, 128, Small::SMEM, a.S, slots_a, places, s)
+                        : launch_step<large, MODE>(p, D, qblocks, 256, Large::SMEM, b.S, slots_b, places, s);
 }
 
 }  // namespace
