@@ -121,20 +121,40 @@ __global__ void __launch_bounds__(CNT) sh_mass_columns_f32_kernel(const __grid_c
             *reinterpret_cast<uint4 *>(Ks + r * LD + c * 4) = x;
         }
         float acc[4] = {};
-        for (int base = max(0, w.slot0 - w.cached) * p.g + rank * BQ; base < rows; base += S * BQ) {
+        // a row tile's queries and logs are asked for while the tile before is worked on
+        constexpr int EACH_Q = BQ * CH / CNT;
+        uint4 ahead[EACH_Q];
+        float log_ahead = 0.f;
+        int last_ahead = -1;
+        auto ask = [&](int base) {
+#pragma unroll
+            for (int k = 0; k < EACH_Q; ++k) {
+                const int i = tid + k * CNT, row = base + i / CH;
+                ahead[k] = make_uint4(0, 0, 0, 0);
+                if (row < rows) ahead[k] = *reinterpret_cast<const uint4 *>(p.q.p + (long long)(w.first + row / p.g) * p.q.ts + (kvh * p.g + row % p.g) * p.q.hs + i % CH * 16);
+            }
+            const int row = base + tid;
+            last_ahead = -1;
+            if (tid < BQ && row < rows) {
+                last_ahead = w.cached + row / p.g;
+                log_ahead = p.lse[(long long)(w.first + row / p.g) * p.hq + kvh * p.g + row % p.g] * LOG2E;
+            }
+        };
+        int base = max(0, w.slot0 - w.cached) * p.g + rank * BQ;
+        if (base < rows) ask(base);
+        for (; base < rows; base += S * BQ) {
             __syncthreads();
-            for (int i = tid; i < BQ * CH; i += CNT) {
-                const int r = i / CH, c = i % CH, row = base + r;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (row < rows) x = *reinterpret_cast<const uint4 *>(p.q.p + (long long)(w.first + row / p.g) * p.q.ts + (kvh * p.g + row % p.g) * p.q.hs + c * 16);
-                *reinterpret_cast<uint4 *>(Qs + r * LD + c * 4) = x;
+#pragma unroll
+            for (int k = 0; k < EACH_Q; ++k) {
+                const int i = tid + k * CNT;
+                *reinterpret_cast<uint4 *>(Qs + i / CH * LD + i % CH * 4) = ahead[k];
             }
             if (tid < BQ) {
-                const int row = base + tid;
-                last_of[tid] = row < rows ? w.cached + row / p.g : -1;
-                log_of[tid] = row < rows ? p.lse[(long long)(w.first + row / p.g) * p.hq + kvh * p.g + row % p.g] * LOG2E : 0.f;
+                last_of[tid] = last_ahead;
+                log_of[tid] = log_ahead;
             }
             __syncthreads();
+            if (base + S * BQ < rows) ask(base + S * BQ);
             uint64_t s2[4][4] = {};
 #pragma unroll 4
             for (int d = 0; d < D; d += 4) {
@@ -187,10 +207,15 @@ cudaError_t launch_columns(const WindowParams &p, cudaStream_t s) {
     int sms = 0;
     const cudaError_t e = sh_setup_kernel(setup, kern, Cols<D>::BYTES, &sms);
     if (e != cudaSuccess) return e;
-    // as many key blocks as there can be, each a cluster whose CTAs share its rows when there are fewer than the device has places for
+    // As many key blocks as there can be; CTAs of a cluster share a block's row tiles.  A tile takes about 3 us, a block 6 to begin and end, 4
+    // more in a cluster; the longest block has the rows of all tokens.  (690 tokens of one key head: 72 us alone, 34 by 8; 592 short blocks of 8
+    // heads: 119 alone, 188 by 2.)
     const long long blocks = std::min((long long)std::min(p.sequences, p.tokens) * ((p.slots + BK - 1) / BK), (1ll << 31) / p.hk) * p.hk, places = 2ll * sms;
+    const double tiles = (double)p.tokens * p.g / BQ;
+    auto us = [&](int n) { return (double)((blocks * n + places - 1) / places) * (n > 1 ? 10 : 6) + tiles / n * 3; };
     int S = 1;
-    while (S < 8 && blocks * S * 2 <= places && (long long)p.tokens * p.g >= 2ll * S * BQ) S *= 2;
+    for (int n = 2; n <= 8; n *= 2)
+        if (us(n) < us(S)) S = n;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(std::min(blocks, std::max(1ll, places / S)) * S));
     cfg.blockDim = dim3(CNT);

@@ -364,7 +364,7 @@ cudaError_t launch(const WindowParams &p, cudaStream_t s) {
         // few row tiles: clusters share the keys of one, as long as all run at once (4 CTAs an SM) and have two blocks each (chunks of 64, 17
         // and 200 tokens over 500, 0 and 31 rows, 12 heads of 64: 47 -> 32 us)
         int S = 1;
-        while (S < 8 && tiles * p.hk * S * 2 <= 4ll * sms && p.slots >= 2 * S * 2 * Simt<D>::BN) S *= 2;
+        while (S < 8 && tiles * p.hk * S * 2 <= 16ll * sms && p.slots >= 2 * S * 2 * Simt<D>::BN) S *= 2;
         if (tiles * S > 0x7fffffffll) return cudaErrorInvalidValue;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(tiles * S), p.hk);
