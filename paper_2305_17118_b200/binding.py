@@ -924,7 +924,8 @@ class MassCache:
     evicted, and ``first`` is the number of its rows (else 0).
 
     How full the sequences are is not known on the host: it counts the tokens that have come since the last eviction, one per ``decode`` and
-    ``longest`` per ``prefill``, and evicts when there may be no room.  (In a captured graph call ``evict`` where it belongs.)"""
+    ``longest`` per ``prefill``, and evicts when there may be no room.  (In a captured graph, and after its tensors have been given other
+    contents, call ``evict`` where it belongs.)"""
 
     def __init__(self, sequences: int, q_heads: int, kv_heads: int, head_dim: int, budget: int, recent: int, spare: int = 64, dtype="bf16",
                  device="cuda:0", rope: Optional[Rope] = None, scale: Optional[float] = None, prefix=None):
@@ -943,7 +944,7 @@ class MassCache:
         self.k, self.v, self.mass, self.positions = self._rows(sequences, kv_heads, budget + spare, head_dim, dt, device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
         self.seen = torch.full((sequences,), self.first, dtype=torch.int32, device=device)
-        self._room, self._empty = budget + spare, True
+        self._room = budget + spare
 
     @staticmethod
     def _rows(sequences, kv_heads, slots, head_dim, dt, device):
@@ -967,8 +968,8 @@ class MassCache:
 
     def prefill(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, positions: Optional[torch.Tensor] = None,
                 longest: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Chunks of prompts (``mass_prefill``), stored and counted.  ``longest``: the most tokens that a sequence has here (default: all of them).
-        A chunk that the spare slots do not hold is read in full in a cache of its own size and then evicted into this one."""
+        """Chunks of prompts (``mass_prefill``), stored and counted.  ``longest``: the most tokens that a sequence has here, or more (default: all of
+        them).  A chunk that the spare slots do not hold is read in full in a cache of its own size and then evicted into this one."""
         tokens = q.shape[0]
         longest = tokens if longest is None else int(longest)
         if not 0 <= longest <= tokens:
@@ -992,14 +993,11 @@ class MassCache:
         else:
             n, hk, _, d = self.k.shape
             whole = self._rows(n, hk, self.budget + longest, d, self.k.dtype, self.k.device)
-            held = self.lengths
-            if not self._empty:
-                held = mass_evict(self.k, self.v, self.mass, self.positions, held, keep=self.budget, recent=self.recent, into=whole)
+            held = mass_evict(self.k, self.v, self.mass, self.positions, self.lengths, keep=self.budget, recent=self.recent, into=whole)
             out = mass_prefill(q, k, v, starts, held, *whole, self.seen, prior=prior, scale=self.scale, out=out)
             mass_evict(*whole, held + count, keep=self.budget, recent=self.recent, into=(self.k, self.v, self.mass, self.positions), left=self.lengths)
             self._room = self.spare
         self.seen += count
-        self._empty = False
         return out
 
     def decode(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor] = None,
@@ -1014,7 +1012,6 @@ class MassCache:
         self.lengths += active
         self.seen += active
         self._room -= 1
-        self._empty = False
         return out
 
     def evict(self) -> None:

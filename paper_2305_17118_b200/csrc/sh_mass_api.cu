@@ -205,7 +205,8 @@ int sh_mass_evict(const sh_attention *a, int sequences, const int32_t *lengths_d
     if (into) {
         sh_window w2 = w;
         w2.window = into_slots;
-        if (!good_cache(into, &w2, sequences) || !good_records(into_rec, into_slots, a->kv_heads, sequences) || into->k == cache->k || into->v == cache->v)
+        if (!good_cache(into, &w2, sequences) || !good_records(into_rec, into_slots, a->kv_heads, sequences) || into->k == cache->k || into->v == cache->v ||
+            into_rec->mass == rec->mass || into_rec->positions == rec->positions)
             return SH_EINVAL;
         fill_window(to, &w2, into, sequences);
         p.out = records(into_rec, a->kv_heads, sequences);

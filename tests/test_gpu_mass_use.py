@@ -375,3 +375,40 @@ def test_wrappers_refuse():
     with pytest.raises(sh.ShError):                              # a stride that is no multiple of 16 bytes
         odd = torch.zeros(2 * 2 * 5 * 68, dtype=dt, device="cuda").as_strided((2, 2, 5, 64), (2 * 5 * 68, 5 * 68, 68, 1))
         sh.context_attention(q, odd, odd)
+
+
+@pytest.mark.parametrize("n,hk,d,slots,keep,recent", [(40, 32, 64, 100, 70, 10), (5, 1, 128, 200, 150, 60), (76, 1, 64, 47000, 500, 100), (3, 1, 64, 380000, 9000, 50)])
+def test_eviction_of_other_shapes(n, hk, d, slots, keep, recent):
+    """Many short caches, which move their own rows; long ones whose keys do not fit into shared memory."""
+    sh, rnd, dt = _sh(), _rnd(slots), torch.float16
+    state = [rnd(n, hk, slots, d, dtype=dt), rnd(n, hk, slots, d, dtype=dt), (rnd(n, hk, slots, dtype=torch.float32) * 8).round() / 8,
+             torch.rand(n, hk, slots, device="cuda").argsort(-1).to(torch.int32)]
+    held = [slots - (i * 37) % (slots // 2) for i in range(n)]
+    old = [x.clone() for x in state]
+    lengths = _i32(held)
+    left = sh.mass_evict(*state, lengths, keep=keep, recent=recent)
+    assert left.tolist() == [min(c, keep) for c in held]
+    assert sh.mass_evict(*[x.clone() for x in old], lengths, keep=keep, recent=recent, left=lengths).tolist() == left.tolist()
+    for i in sorted({0, n // 2, n - 1}):
+        for h in sorted({0, hk - 1}):
+            _, holes, moved = mr.evict(old[2][i, h, :held[i]].tolist(), old[3][i, h, :held[i]].tolist(), keep, recent)
+            for x, y in zip(old, state):
+                want = x[i, h].clone()
+                want[holes] = x[i, h][moved]
+                assert torch.equal(y[i, h], want)
+
+
+@pytest.mark.parametrize("dtype,g", [("f16", 4), ("bf16", 9), ("f32", 3)])
+def test_steps_of_many_sequences(dtype, g):
+    """More units than run at once: the weights are added by a launch of their own."""
+    sh, rnd, dt, n, hk, d, slots = _sh(), _rnd(g), DT[dtype], 900, 2, 64, 600
+    q, k, v = (rnd(n, x, d, dtype=dt) for x in (hk * g, hk, hk))
+    held = [(i * 71) % slots if i % 10 else -1 for i in range(n)]
+    old = [rnd(n, hk, slots, d, dtype=dt), rnd(n, hk, slots, d, dtype=dt), torch.ones(n, hk, slots, device="cuda"), torch.zeros(n, hk, slots, dtype=torch.int32, device="cuda")]
+    new = [x.clone() for x in old]
+    out = sh.mass_decode(q, k, v, _i32(held), *new, _i32([max(c, 0) for c in held]))
+    for i in (0, 1, 2, 333, 511, 899):
+        if held[i] < 0:
+            assert (out[i] == 0).all() and all(torch.equal(x[i], y[i]) for x, y in zip(new, old))
+        else:
+            _check_sequence(old, new, i, held[i], 1, q[i:i + 1], k[i:i + 1], v[i:i + 1], out[i:i + 1], held[i], g, dt, STEP)

@@ -55,12 +55,14 @@ ALL, MASS, STEPS, TOKENS = ("context", "prefill", "decode", "evict"), ("prefill"
     (STEPS, dict(prior_lse=FAKE)), (MASS, dict(work=None)), (ALL, dict(work=FAKE + 8)),
     (("evict",), dict(keep=0)), (("evict",), dict(keep=11)), (("evict",), dict(recent=-1)), (("evict",), dict(recent=7)), (("evict",), dict(left=None)),
     (("evict",), dict(left=FAKE + 4)), (("evict",), dict(into_rec="rec")), (("evict",), dict(into="cache")),
-    (("evict",), dict(into="cache", into_rec="rec", into_slots=10)), (("evict",), dict(into="other", into_rec="rec", into_slots=5)),
-    (("evict",), dict(into="other", into_rec="rec", into_slots=1 << 30)),
+    (("evict",), dict(into="cache", into_rec="spare", into_slots=10)), (("evict",), dict(into="other", into_rec="spare", into_slots=5)),
+    (("evict",), dict(into="other", into_rec="rec", into_slots=10)),
+    (("evict",), dict(into="other", into_rec="spare", into_slots=1 << 30)),
 ])
 def test_calls_refuse(which, change):
     sh = _sh()
     x = _args(sh)
+    x["spare"] = sh._Records(FAKE * 6, FAKE * 7, 20, 10)
     x["other"] = sh._WindowCache(FAKE * 4, FAKE * 4, 2 * 10 * 64, 10 * 64, 64)
     for name, value in change.items():
         if "__" in name:
