@@ -936,12 +936,14 @@ class MassCache:
             raise ValueError(f"budget {budget}, recent {recent}, spare {spare}: need 1 <= budget, 0 <= recent <= budget, 1 <= spare")
         _attention_packed(dt, head_dim, q_heads, kv_heads, budget + spare, scale)
         self.q_heads, self.budget, self.recent, self.spare, self.rope, self.scale, self.prefix = q_heads, budget, recent, spare, rope, scale, prefix
+        self.k, self.v, self.mass, self.positions = self._rows(sequences, kv_heads, budget + spare, head_dim, dt, device)
         self.first = 0
         if prefix is not None:
-            s = _slots_of(prefix[0], "prefix", 1, kv_heads, head_dim, dt, torch.device(device).index or 0)
-            _cache_packed(prefix[0], prefix[1], s, dt, prefix[0].get_device())
+            if not (isinstance(prefix, (tuple, list)) and len(prefix) == 2):
+                _fail("prefix", "a pair (k, v)", prefix)
+            s = _slots_of(prefix[0], "prefix", 1, kv_heads, head_dim, dt, self.k.get_device())
+            _cache_packed(*prefix, s, dt, self.k.get_device())
             self.first = s[2]
-        self.k, self.v, self.mass, self.positions = self._rows(sequences, kv_heads, budget + spare, head_dim, dt, device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
         self.seen = torch.full((sequences,), self.first, dtype=torch.int32, device=device)
         self._room = budget + spare

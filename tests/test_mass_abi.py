@@ -142,3 +142,16 @@ def test_mass_cache_refuses(change):
     args = dict(sequences=2, q_heads=4, kv_heads=2, head_dim=64, budget=10, recent=2, spare=4, dtype="f16", device="cpu")
     with pytest.raises(ValueError):
         sh.MassCache(**{**args, **change})
+
+
+def test_mass_cache_checks_its_prefix():
+    sh = _sh()
+    args = dict(sequences=2, q_heads=4, kv_heads=2, head_dim=64, budget=10, recent=2, spare=4, dtype="f16", device="cpu")
+    t = lambda *shape, dtype=torch.float16: torch.zeros(shape, dtype=dtype)
+    good = t(1, 2, 7, 64)
+    cache = sh.MassCache(**args, prefix=(good, good))
+    assert cache.first == 7 and cache.seen.tolist() == [7, 7] and cache.lengths.tolist() == [0, 0]
+    for prefix in (good, (good,), (good, good, good), (good, None), (t(2, 2, 7, 64),) * 2, (t(1, 4, 7, 64),) * 2, (t(1, 2, 7, 128),) * 2,
+                   (good, t(1, 2, 6, 64)), (t(1, 2, 7, 64, dtype=torch.bfloat16),) * 2, (good.transpose(2, 3).contiguous().transpose(2, 3),) * 2):
+        with pytest.raises(ValueError):
+            sh.MassCache(**args, prefix=prefix)
