@@ -507,7 +507,8 @@ typedef struct {
  * starts[i] .. starts[i+1] - 1 see the rows [0, lengths[i]) of context i, all of them.  starts_dev: int32 [contexts + 1], or NULL: one context that
  * all tokens share, or (contexts == tokens) one of its own for each token.  lengths_dev: int32 [contexts], or NULL: `slots` rows each;
  * lengths outside of 0 .. slots are clamped.  Outputs: out, and lse_dev [tokens][q_heads], the natural logs of the sums of exponentials.  A
- * context of length 0 gives zeros and -infinity; rows that belong to no context are left as they were, or (clear_rest = 1) get the same.  starts that decrease or leave 0 .. tokens are clamped, outputs are then meaningless.
+ * context of length 0 gives zeros and -infinity; rows that belong to no context (all of them where there are no contexts) are left as they
+ * were, or (clear_rest = 1) get the same.  starts that decrease or leave 0 .. tokens are clamped, outputs are then meaningless.
  * 16-bit types: the weights are rounded once to the type (one token of each context: held in two parts).  out_dtype: a->dtype, or SH_F32
  * for a result that something continues from (it is then not rounded before it joins the rest).
  * workspace_dev: sh_context_attention_workspace_bytes(a, tokens, contexts, starts_dev != NULL) bytes of device memory, 16-byte aligned, or NULL; used

@@ -65,10 +65,11 @@ int sh_context_attention(const sh_attention *a, int tokens, int contexts, const 
                          void *stream) {
     if (!good_attention(a) || (out_dtype != SH_F32 && out_dtype != a->dtype) || (clear_rest & ~1) || tokens < 0 || tokens >= MAX_POS || contexts < 0) return SH_EINVAL;
     if (!starts_dev && contexts != 1 && contexts != tokens) return SH_EINVAL;
-    if (tokens == 0 || contexts == 0) return SH_OK;
+    if (tokens == 0 || (contexts == 0 && !clear_rest)) return SH_OK;      // (without contexts every row belongs to none)
     const int D = a->head_dim, es = elem_size(a->dtype);
-    if (!rows_in(q, tokens, a->q_heads, D, es) || !rows_out(out, tokens, a->q_heads, D, elem_size(out_dtype)) || !cache_in(context, a->kv_heads, D, es, a->slots, contexts) ||
-        (starts_dev && !good_ints(starts_dev)) || (lengths_dev && !good_ints(lengths_dev)) || !lse_dev || ((uintptr_t)lse_dev & 3))
+    if (!rows_in(q, tokens, a->q_heads, D, es) || !rows_out(out, tokens, a->q_heads, D, elem_size(out_dtype)) ||
+        (contexts > 0 && !cache_in(context, a->kv_heads, D, es, a->slots, contexts)) || (starts_dev && !good_ints(starts_dev)) ||
+        (lengths_dev && !good_ints(lengths_dev)) || !lse_dev || ((uintptr_t)lse_dev & 3))
         return SH_EINVAL;
     const sh_window w = as_window(a);
     WindowParams p = {};
@@ -90,7 +91,7 @@ int sh_context_attention(const sh_attention *a, int tokens, int contexts, const 
     if (clear_rest && starts_dev) {
         p.clear_rest = true;
         const cudaError_t e = sh_launch_clear_rest(p, D * elem_size(out_dtype), (cudaStream_t)stream);
-        if (e != cudaSuccess) return done(e);
+        if (e != cudaSuccess || contexts == 0) return done(e);
     }
     return done(a->dtype == SH_F32 ? sh_launch_window_prefill_f32(p, D, ATTEND_CONTEXT, (cudaStream_t)stream)
                                    : sh_launch_window_prefill_umma(p, a->dtype, D, ATTEND_CONTEXT, (cudaStream_t)stream));
