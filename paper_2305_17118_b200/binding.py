@@ -954,6 +954,13 @@ class MassCache:
         return (torch.zeros((*shape, head_dim), dtype=dt, device=device), torch.zeros((*shape, head_dim), dtype=dt, device=device),
                 torch.zeros(shape, device=device), torch.zeros(shape, dtype=torch.int32, device=device))
 
+    @staticmethod
+    def _stored(starts, tokens: int, lengths, slots: int) -> torch.Tensor:
+        """Rows of each sequence that ``mass_prefill`` stores in caches of that many slots: none where it is idle or has no room."""
+        at = starts.clamp(0, tokens)
+        count = (at[1:] - at[:-1]).clamp(min=0)
+        return torch.where((lengths >= 0) & (count <= slots - lengths), count, 0)
+
     def _prepare(self, q, k, positions, default):
         if q.dim() != 3 or q.shape[1] != self.q_heads:
             _fail("q", f"[tokens, {self.q_heads}, {self.k.shape[3]}]", q)
@@ -971,7 +978,8 @@ class MassCache:
     def prefill(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, positions: Optional[torch.Tensor] = None,
                 longest: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Chunks of prompts (``mass_prefill``), stored and counted.  ``longest``: the most tokens that a sequence has here, or more (default: all of
-        them).  A chunk that the spare slots do not hold is read in full in a cache of its own size and then evicted into this one."""
+        them).  A chunk that the spare slots do not hold is read in full in a cache of its own size and then evicted into this one.
+        (If a sequence has more than ``longest`` tokens and there is no room for them, it takes no part: its ``lengths`` and ``seen`` stay.)"""
         tokens = q.shape[0]
         longest = tokens if longest is None else int(longest)
         if not 0 <= longest <= tokens:
@@ -985,10 +993,10 @@ class MassCache:
             return self.seen[seq] + (row - starts[seq]).clamp(min=0)
 
         q, k, prior = self._prepare(q, k, positions, places)
-        count = torch.where(self.lengths < 0, 0, starts[1:] - starts[:-1])
         if longest > self._room and longest <= self.spare:
             self.evict()
         if longest <= self._room:
+            count = self._stored(starts, tokens, self.lengths, self.k.shape[2])
             out = mass_prefill(q, k, v, starts, self.lengths, self.k, self.v, self.mass, self.positions, self.seen, prior=prior, scale=self.scale, out=out)
             self.lengths += count
             self._room -= longest
@@ -996,6 +1004,7 @@ class MassCache:
             n, hk, _, d = self.k.shape
             whole = self._rows(n, hk, self.budget + longest, d, self.k.dtype, self.k.device)
             held = mass_evict(self.k, self.v, self.mass, self.positions, self.lengths, keep=self.budget, recent=self.recent, into=whole)
+            count = self._stored(starts, tokens, held, self.budget + longest)
             out = mass_prefill(q, k, v, starts, held, *whole, self.seen, prior=prior, scale=self.scale, out=out)
             mass_evict(*whole, held + count, keep=self.budget, recent=self.recent, into=(self.k, self.v, self.mass, self.positions), left=self.lengths)
             self._room = self.spare
@@ -1004,13 +1013,13 @@ class MassCache:
 
     def decode(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: Optional[torch.Tensor] = None,
                out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """One token per sequence (``mass_decode``), stored and counted; before it the eviction, if some sequence may be full.  On the current
-        stream."""
+        """One token per sequence (``mass_decode``), stored and counted; before it the eviction, if some sequence may be full.  (One that is full
+        all the same, after replays of a captured step, takes no part: its ``lengths`` and ``seen`` stay.)  On the current stream."""
         q, k, prior = self._prepare(q, k, positions, lambda: self.seen)
         if self._room == 0:
             self.evict()
         out = mass_decode(q, k, v, self.lengths, self.k, self.v, self.mass, self.positions, self.seen, prior=prior, scale=self.scale, out=out)
-        active = (self.lengths >= 0).to(torch.int32)
+        active = self.lengths == self.lengths.clamp(0, self.k.shape[2] - 1)      # (neither idle nor full, as the kernel has it)
         self.lengths += active
         self.seen += active
         self._room -= 1
