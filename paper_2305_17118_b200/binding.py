@@ -977,14 +977,20 @@ class MassCache:
 
     def prefill(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, positions: Optional[torch.Tensor] = None,
                 longest: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Chunks of prompts (``mass_prefill``), stored and counted.  ``longest``: the most tokens that a sequence has here, or more (default: all of
-        them).  A chunk that the spare slots do not hold is read in full in a cache of its own size and then evicted into this one.
+        """Chunks of prompts (``mass_prefill``), stored and counted.  ``longest``: the most tokens that a sequence has here, or more.  Default: what
+        ``starts`` says, for which the call waits for the stream (one sequence, and under capture: all tokens).  A chunk that the spare
+        slots do not hold is read in full in a cache of its own size and then evicted into this one.
         (If a sequence has more than ``longest`` tokens and there is no room for them, it takes no part: its ``lengths`` and ``seen`` stay.)"""
-        tokens = q.shape[0]
-        longest = tokens if longest is None else int(longest)
-        if not 0 <= longest <= tokens:
+        tokens, n = q.shape[0], self.k.shape[0]
+        if longest is not None and not 0 <= int(longest) <= tokens:
             raise ValueError(f"longest {longest}: need 0 .. {tokens}")
-        if tokens == 0 or longest == 0:
+        if tokens > 0:
+            _ints(starts, "starts", n + 1, self.k.get_device())
+        if longest is None:
+            bound = tokens == 0 or n == 1 or (starts.is_cuda and torch.cuda.is_current_stream_capturing())
+            longest = tokens if bound else self._stored(starts, tokens, self.lengths, 1 << 30).max()
+        longest = int(longest)
+        if longest == 0:
             return _new(q, q.shape, None, True) if out is None else out
 
         def places():
@@ -1001,7 +1007,7 @@ class MassCache:
             self.lengths += count
             self._room -= longest
         else:
-            n, hk, _, d = self.k.shape
+            hk, d = self.k.shape[1], self.k.shape[3]
             whole = self._rows(n, hk, self.budget + longest, d, self.k.dtype, self.k.device)
             held = mass_evict(self.k, self.v, self.mass, self.positions, self.lengths, keep=self.budget, recent=self.recent, into=whole)
             count = self._stored(starts, tokens, held, self.budget + longest)

@@ -78,3 +78,25 @@ def test_replayed_steps_stop_at_the_last_slot():
     assert all(torch.equal(a, b[1]) for a, b in zip(full, (cache.k, cache.v, cache.mass, cache.positions)))
     cache.evict()
     assert cache.lengths.tolist() == [18, 24] and sorted(cache.positions[1, 0, :24].tolist())[-6:] == list(range(76, 82))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_longest_chunk_is_looked_up(dtype):
+    """Without `longest` a batch is treated as with it: what stays does not depend on how many sequences share a call."""
+    sh, dt, n, hk, g, d = _sh(), DT[dtype], 6, 2, 2, 64
+    sides = []
+    for given in (True, False):
+        rnd = _rnd(7)
+        cache = sh.MassCache(n, hk * g, hk, d, 24, 6, 16, dtype=dtype)
+        cache.lengths[4] = -1
+        got = []
+        for counts in ([9, 10, 0, 3, 5, 1], [10, 10, 10, 10, 0, 10], [10, 1, 0, 0, 0, 10], [9, 9, 9, 0, 0, 0], [41, 3, 0, 0, 0, 0], [4, 4, 4, 4, 4, 4]):
+            starts = [1]
+            for x in counts:
+                starts.append(starts[-1] + x)
+            q, k, v = (rnd(starts[-1] + 2, x, d, dtype=dt) for x in (hk * g, hk, hk))
+            options = dict(longest=max(counts)) if given else {}
+            got.append(cache.prefill(q, k, v, _i32(starts), **options))
+        sides.append(got + [cache.lengths, cache.seen, cache.k, cache.v, cache.mass, cache.positions])
+    for a, b in zip(*sides):
+        assert torch.equal(a, b)

@@ -75,3 +75,32 @@ def test_a_token_without_room_is_not_counted(made):
     for lengths, seen in (([32, 32, -1, 1], [50, 61, 0, 1]), ([32, 32, -1, 2], [50, 61, 0, 2])):
         cache.decode(*_rows(4))
         assert cache.lengths.tolist() == lengths and cache.seen.tolist() == seen
+
+
+def test_the_longest_chunk_is_looked_up(made):
+    """How many sequences share a call does not matter for when it evicts."""
+    cache = _cache(made, 8, 100, 64)
+    cache.lengths[5] = -1
+    starts = _i32([3, 13, 13, 23, 33, 42, 92, 102, 105])                  # ten rows at most (fifty are an idle sequence's), some of nobody
+    for _ in range(16):
+        cache.prefill(*_rows(110), starts)
+    assert [c[:2] for c in made.calls] == [("prefill", 164)] * 16
+    cache.prefill(*_rows(110), starts)
+    assert [c[:2] for c in made.calls[16:]] == [("evict", 164), ("prefill", 164)]
+
+
+def test_a_call_without_rows_of_any_sequence_does_nothing(made):
+    cache = _cache(made, 2, 10, 4)
+    assert cache.prefill(*_rows(7), _i32([3, 3, 3])).shape == (7, 4, 64)
+    assert made.calls == [] and cache.lengths.tolist() == [0, 0] and cache.seen.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("starts", [[0, 7], [0, 3, 5, 7], [7]])
+def test_prefill_refuses_starts_of_another_batch(made, starts):
+    cache = _cache(made, 2, 10, 4)
+    for longest in (None, 5):
+        with pytest.raises(ValueError):
+            cache.prefill(*_rows(7), _i32(starts), longest=longest)
+    with pytest.raises(ValueError):
+        cache.prefill(*_rows(7), torch.tensor([0, 3, 7]))                 # (not int32)
+    assert made.calls == []
