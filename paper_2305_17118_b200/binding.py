@@ -949,10 +949,10 @@ class MassCache:
         self._room = budget + spare
 
     @staticmethod
-    def _rows(sequences, kv_heads, slots, head_dim, dt, device):
+    def _rows(sequences, kv_heads, slots, head_dim, dt, device, new=torch.zeros):
         shape = (sequences, kv_heads, slots)
-        return (torch.zeros((*shape, head_dim), dtype=dt, device=device), torch.zeros((*shape, head_dim), dtype=dt, device=device),
-                torch.zeros(shape, device=device), torch.zeros(shape, dtype=torch.int32, device=device))
+        return (new((*shape, head_dim), dtype=dt, device=device), new((*shape, head_dim), dtype=dt, device=device),
+                new(shape, dtype=torch.float32, device=device), new(shape, dtype=torch.int32, device=device))
 
     @staticmethod
     def _stored(starts, tokens: int, lengths, slots: int) -> torch.Tensor:
@@ -1008,7 +1008,8 @@ class MassCache:
             self._room -= longest
         else:
             hk, d = self.k.shape[1], self.k.shape[3]
-            whole = self._rows(n, hk, self.budget + longest, d, self.k.dtype, self.k.device)
+            # (every row of it that anybody looks at is written by the eviction into it or stored with the chunk)
+            whole = self._rows(n, hk, self.budget + longest, d, self.k.dtype, self.k.device, new=torch.empty)
             held = mass_evict(self.k, self.v, self.mass, self.positions, self.lengths, keep=self.budget, recent=self.recent, into=whole)
             count = self._stored(starts, tokens, held, self.budget + longest)
             out = mass_prefill(q, k, v, starts, held, *whole, self.seen, prior=prior, scale=self.scale, out=out)

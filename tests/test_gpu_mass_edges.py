@@ -100,3 +100,27 @@ def test_the_longest_chunk_is_looked_up(dtype):
         sides.append(got + [cache.lengths, cache.seen, cache.k, cache.v, cache.mass, cache.positions])
     for a, b in zip(*sides):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_a_cache_of_the_chunks_own_size_holds_anything_at_first(dtype):
+    """New memory is filled with NaN (and the largest integers): nothing of the cache in which a long chunk is read counts before it is written."""
+    sh, dt, n, hk, g, d = _sh(), DT[dtype], 4, 2, 3, 64
+    sides = []
+    for poisoned in (False, True):
+        rnd = _rnd(11)
+        cache = sh.MassCache(n, hk * g, hk, d, 24, 6, 16, dtype=dtype)
+        got = []
+        torch.use_deterministic_algorithms(poisoned, warn_only=True)      # (with it, torch fills what it allocates)
+        try:
+            for counts in ([70, 1, 0, 33], [2, 0, 0, 90], [200, 200, 200, 1]):
+                starts = [0]
+                for x in counts:
+                    starts.append(starts[-1] + x)
+                q, k, v = (rnd(starts[-1], x, d, dtype=dt) for x in (hk * g, hk, hk))
+                got.append(cache.prefill(q, k, v, _i32(starts), longest=max(counts)))
+        finally:
+            torch.use_deterministic_algorithms(False)
+        sides.append(got + [cache.lengths, cache.seen, cache.k, cache.v, cache.mass, cache.positions])
+    for a, b in zip(*sides):
+        assert a.isfinite().all() and torch.equal(a, b)
