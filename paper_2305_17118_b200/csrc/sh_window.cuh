@@ -108,14 +108,16 @@ struct Ring {
 };
 
 // The end of a row: its unnormalised output times `own`, plus the prior's row times `other` (0: there is none, or it has seen nothing, and
-// its row does not matter).  `total`: the log (base 2) of the sum of exponentials that this is divided by.
+// its row does not matter).  `total`: the log (base 2) of the sum of exponentials that this is divided by.  `lost`: the prior's log is NaN or
+// infinite, and with it the whole row NaN.
 struct Close {
     float own, other, total;
+    bool lost;
 };
 // `base` + log2(L) is the log of the row's own sum.
 template <int MODE>
 __device__ __forceinline__ Close close_row(const WindowParams &p, long long token, int h, float base, float L) {
-    Close r = {1.f / L, 0.f, 0.f};
+    Close r = {1.f / L, 0.f, 0.f, false};
     if (MODE == ATTEND_MASS && p.prior_lse) {
         const float pl = p.prior_lse[token * p.hq + h] * 1.4426950408889634f;
         if (pl != -CUDART_INF_F) {
@@ -123,6 +125,7 @@ __device__ __forceinline__ Close close_row(const WindowParams &p, long long toke
             L = fmaf(L, f, g);
             r.own = f / L;
             r.other = g / L;
+            r.lost = !(pl < CUDART_INF_F);
             base = top;
         }
     }

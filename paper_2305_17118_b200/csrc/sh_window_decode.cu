@@ -105,12 +105,16 @@ __device__ __forceinline__ int rows_before(const WindowParams &p, int seq) {
 
 // The last step for N elements of a row, from d on: `base` + log2(L) is the log of its sum, x its unnormalised output.  Over a cache with
 // accumulated weights the row continues from the prior's, if there is one, and leaves that log for the masses in `total`; a context's goes to
-// the caller.
+// the caller.  Is what the row itself brings not finite?  (Whatever the prior holds, it asks for no second look at the keys.)
 template <typename T, int MODE, int N>
-__device__ __forceinline__ void finish(const WindowParams &p, int seq, int h, int d, float base, float L, bool empty, float *total, float (&x)[N]) {
+__device__ __forceinline__ bool finish(const WindowParams &p, int seq, int h, int d, float base, float L, bool empty, float *total, float (&x)[N]) {
+    bool odd = false;
     if constexpr (MODE == ATTEND_WINDOW) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] /= L;
+        for (int e = 0; e < N; ++e) {
+            x[e] /= L;
+            odd |= !isfinite(x[e]);
+        }
     } else {
         const Close c = close_row<MODE>(p, seq, h, base, L);
         if (MODE == ATTEND_MASS && d == 0) *total = c.total;
@@ -118,8 +122,13 @@ __device__ __forceinline__ void finish(const WindowParams &p, int seq, int h, in
         float y[N] = {};
         if (c.other != 0.f) prior_row<T>(p, seq, h, d, y);
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = MODE == ATTEND_CONTEXT && empty ? 0.f : fmaf(y[e], c.other, x[e] * c.own);
+        for (int e = 0; e < N; ++e) {
+            const float own = MODE == ATTEND_CONTEXT && empty ? 0.f : x[e] * c.own;
+            odd |= !isfinite(own) && !c.lost;
+            x[e] = fmaf(y[e], c.other, own);
+        }
     }
+    return odd;
 }
 
 __device__ __forceinline__ float *scores_of(const WindowParams &p, int seq, int h) { return p.scores + ((long long)seq * p.hq + h) * p.score_stride; }
@@ -629,10 +638,7 @@ __global__ void __launch_bounds__(MW * 32) sh_window_decode_mma_kernel(const __g
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[e] = fmaf(c[2 + d + e], f, acc[e]);
         }
-        bool odd = false;
-        finish<T, MODE>(p, seq, h0 + q, d, M - Weights<T>::LIFT, L, live == 0, total + q, acc);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) odd |= !isfinite(acc[e]);
+        const bool odd = finish<T, MODE>(p, seq, h0 + q, d, M - Weights<T>::LIFT, L, live == 0, total + q, acc);
         // the low part of a weight or of a query may be zero and meet an infinity: such rows are computed again in plain fp32
         float hi[8], lo[8];
         Vec<T>::unpack(*reinterpret_cast<const uint4 *>(sm + C::OFF_Q + q * C::ROW + (((d / 8) ^ (q & 7)) << 4)), hi);
@@ -703,7 +709,6 @@ __global__ void __launch_bounds__(SLICES * D / 8) sh_window_decode_merge_kernel(
     L = 0.f;
 #pragma unroll
     for (int i = 0; i < SLICES; ++i) L += sum[i];
-    bool odd = false;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         float x = 0.f;
@@ -712,9 +717,7 @@ __global__ void __launch_bounds__(SLICES * D / 8) sh_window_decode_merge_kernel(
         acc[e] = x;
     }
     const int h = kvh * p.g + qb * MQ + q;
-    finish<T, MODE>(p, seq, h, c * 8, M - Weights<T>::LIFT, L, t == 0, total_of(p, seq, h), acc);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) odd |= !isfinite(acc[e]);
+    const bool odd = finish<T, MODE>(p, seq, h, c * 8, M - Weights<T>::LIFT, L, t == 0, total_of(p, seq, h), acc);
     if (__any_sync((1u << CHUNKS) - 1u, odd)) {
         const float4 *x = reinterpret_cast<const float4 *>(p.part + units * parts * REC + unit * (MQ * D) + q * D + c * 8);
         plain_row<T, D, MODE>(p, seq, kvh, h, MODE == ATTEND_CONTEXT ? t : min(t + 1, p.sinks + p.window), 0, nullptr, x[0], x[1], scores_of(p, seq, h), total_of(p, seq, h));

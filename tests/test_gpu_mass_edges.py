@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_mass import DT, INF, NAN, STEP, _check_sequence, _i32, _rnd, _sh
+from test_gpu_mass import DT, INF, NAN, STEP, _check_sequence, _i32, _rnd, _same, _sh
 
 pytestmark = pytest.mark.gpu
 
@@ -124,3 +124,53 @@ def test_a_cache_of_the_chunks_own_size_holds_anything_at_first(dtype):
         sides.append(got + [cache.lengths, cache.seen, cache.k, cache.v, cache.mass, cache.positions])
     for a, b in zip(*sides):
         assert a.isfinite().all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n,hk,g,slots,held", [(3, 2, 4, 300, [299, 100, 64]), (1, 1, 4, 12000, [11990]), (40, 8, 2, 500, [480] * 40), (5, 3, 1, 100, [99, 0, 50, 7, 98])])
+def test_a_prior_that_is_not_finite(dtype, n, hk, g, slots, held):
+    """It shows in its own elements.  All others, and the masses, are the same bits: the keys are not gone over again for it.  (One CTA or a cluster a
+    unit, a unit dealt out and merged; weights added by a launch of their own, by the unit, from shared memory.)"""
+    sh, rnd, dt, d = _sh(), _rnd(slots), DT[dtype], 64
+    q, k, v = (rnd(n, x, d, dtype=dt) for x in (hk * g, hk, hk))
+    state = [rnd(n, hk, slots, d, dtype=dt), rnd(n, hk, slots, d, dtype=dt), torch.ones(n, hk, slots, device="cuda"), torch.zeros(n, hk, slots, dtype=torch.int32, device="cuda")]
+    for odt in (torch.float32, dt):
+        prior, lse = rnd(n, hk * g, d, dtype=odt), torch.full((n, hk * g), 5.0, device="cuda")
+        bad = prior.clone()
+        bad[0, 1, 3], bad[0, 2, 63], bad[n - 1, 0, 0] = NAN, INF, -INF
+        runs = []
+        for p in (prior, bad):
+            now = [x.clone() for x in state]
+            runs.append([sh.mass_decode(q, k, v, _i32(held), *now, _i32(held), prior=(p, lse))] + now)
+        odd = ~bad.isfinite()
+        assert torch.equal(runs[0][0][~odd], runs[1][0][~odd])
+        assert _same(runs[1][0][odd], bad[odd].to(dt))
+        for a, b in zip(runs[0][1:], runs[1][1:]):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("log", [NAN, INF, -INF])
+def test_a_prior_whose_log_is_not_finite(dtype, log):
+    """NaN and infinity take their row with them, and the masses of its key head; minus infinity is a prior that has seen nothing."""
+    sh, rnd, dt, n, hk, g, d, slots = _sh(), _rnd(8), DT[dtype], 2, 2, 2, 128, 400
+    q, k, v = (rnd(n, x, d, dtype=dt) for x in (hk * g, hk, hk))
+    state = [rnd(n, hk, slots, d, dtype=dt), rnd(n, hk, slots, d, dtype=dt), torch.ones(n, hk, slots, device="cuda"), torch.zeros(n, hk, slots, dtype=torch.int32, device="cuda")]
+    held, prior, lse = [399, 20], rnd(n, hk * g, d, dtype=torch.float32), torch.full((n, hk * g), 4.0, device="cuda")
+    odd = lse.clone()
+    odd[0, 1] = log
+    if log == -INF:
+        prior[0, 1] = NAN
+    runs = []
+    for x in (None, lse, odd):
+        now = [t.clone() for t in state]
+        runs.append([sh.mass_decode(q, k, v, _i32(held), *now, _i32(held), prior=None if x is None else (prior, x))] + now)
+    (alone, _, _, _, _), (clean, _, _, mass, _), (out, _, _, got, _) = runs
+    others = torch.ones(n, hk * g, dtype=torch.bool, device="cuda")
+    others[0, 1] = False
+    assert torch.equal(out[others], clean[others])
+    assert torch.equal(got[1], mass[1]) and torch.equal(got[0, 1], mass[0, 1])
+    if log == -INF:
+        assert torch.equal(out[0, 1], alone[0, 1])
+    else:
+        assert out[0, 1].isnan().all() and got[0, 0, :400].isnan().all()
