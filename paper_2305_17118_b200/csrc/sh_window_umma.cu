@@ -921,11 +921,13 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             if (__any_sync(0xffffffffu, !ok)) break;
             tc_fence_after();
             float inv = 1.f / l, other = 0.f;         // (of the row's own output, of the prior's)
+            bool lost = false;
             if (MODE != ATTEND_WINDOW && live) {
                 const Close end = close_row<MODE>(p.w, row0 + qi, kvh * p.w.g + h, m * c - Fmt<T>::LIFT, l);
                 *lse_of(p.w, row0 + qi, kvh * p.w.g + h) = LN2 * end.total;
                 inv = end.own;
                 other = end.other;
+                lost = end.lost;
             }
             if (MODE == ATTEND_CONTEXT && p.w.out_f32) {      // fp32 rows leave by their threads
                 float zero = 0.f;
@@ -981,7 +983,7 @@ sh_window_prefill_umma_kernel(const __grid_constant__ UmmaParams p, const __grid
             }
             float z0, z1;
             un2(zero, z0, z1);
-            const bool odd = !(z0 + z1 == 0.f);
+            const bool odd = !(z0 + z1 == 0.f) && !lost;
             tc_fence_before();      // O has been read before the arrivals that let the next item overwrite it
             fence_async_shared();   // (for the copy, and for the queries that arrive here next)
             __syncwarp();
@@ -1088,11 +1090,13 @@ __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __
         __syncthreads();
     }
     float inv = 1.f / L;                             // (as where there is nothing to merge)
+    bool lost = false;
     float4 prior = make_float4(0.f, 0.f, 0.f, 0.f);
     if (MODE != ATTEND_WINDOW && live) {
         const Close end = close_row<MODE>(p.w, w.y + tok, kvh * p.w.g + h, M, L);
         if (c4 == 0) *lse_of(p.w, w.y + tok, kvh * p.w.g + h) = LN2 * end.total;
         inv = end.own;
+        lost = end.lost;
         if (end.other != 0.f) {
             const char *row = p.w.prior.p + (long long)(w.y + tok) * p.w.prior.ts + (kvh * p.w.g + h) * p.w.prior.hs;
             float *y = &prior.x;
@@ -1101,7 +1105,7 @@ __global__ void __launch_bounds__(2 * D) sh_window_prefill_merge_kernel(const __
         }
     }
     o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
-    if (live && !(isfinite(o.x) && isfinite(o.y) && isfinite(o.z) && isfinite(o.w))) odd[r] = 1;
+    if (live && !lost && !(isfinite(o.x) && isfinite(o.y) && isfinite(o.z) && isfinite(o.w))) odd[r] = 1;
     __syncthreads();
     o.x += prior.x; o.y += prior.y; o.z += prior.z; o.w += prior.w;
     if (live && !odd[r]) {

@@ -174,3 +174,29 @@ def test_a_prior_whose_log_is_not_finite(dtype, log):
         assert torch.equal(out[0, 1], alone[0, 1])
     else:
         assert out[0, 1].isnan().all() and got[0, 0, :400].isnan().all()
+
+
+@pytest.mark.parametrize("dtype,tokens,held", [("bf16", 1024, 1000), ("f16", 64, 3000)])
+def test_rows_that_a_prior_spoils_are_not_computed_again(dtype, tokens, held):
+    """A log that is NaN makes its row NaN, whatever the keys are: going over them again, a row by a warp (30 to 100 times the whole call's time
+    here), could change nothing.  (One CTA an item; items dealt out and merged.)"""
+    sh, rnd, dt, hk, g, d = _sh(), _rnd(tokens), DT[dtype], 8, 4, 128
+    q, k, v = (rnd(tokens, x, d, dtype=dt) for x in (hk * g, hk, hk))
+    slots = held + tokens
+    state = [rnd(1, hk, slots, d, dtype=dt), rnd(1, hk, slots, d, dtype=dt), torch.ones(1, hk, slots, device="cuda"), torch.zeros(1, hk, slots, dtype=torch.int32, device="cuda")]
+    prior, lse = rnd(tokens, hk * g, d, dtype=torch.float32), torch.full((tokens, hk * g), 3.0, device="cuda")
+    odd = lse.clone()
+    odd[:, 5] = NAN
+    outs, times = [], []
+    for x in (lse, odd):
+        call = lambda: sh.mass_prefill(q, k, v, _i32([0, tokens]), _i32([held]), *state, _i32([held]), prior=(prior, x), out=out)
+        out, us = torch.empty_like(q), []
+        for _ in range(6):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record(), call(), b.record()
+            torch.cuda.synchronize()
+            us.append(a.elapsed_time(b) * 1000)
+        outs.append(out), times.append(min(us))
+    others = [h for h in range(hk * g) if h != 5]
+    assert torch.equal(outs[0][:, others], outs[1][:, others]) and outs[1][:, 5].isnan().all()
+    assert times[1] < 4 * times[0] + 100, times
