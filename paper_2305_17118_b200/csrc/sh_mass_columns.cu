@@ -370,7 +370,8 @@ __global__ void __launch_bounds__(ADD) sh_mass_columns_add_kernel(const __grid_c
 // How many items share the row tiles of a key block.  The longest sequence is taken to have twice the average's tokens: its first key blocks see
 // `tiles` row tiles, an SM has about `load` in all (half of them lie behind the diagonal), and an item should be half of that.  Four tiles an
 // item at least.  2048 tokens in one part 97 us, five 83, eight 86 (with the attention); 4096 tokens of one key head 173 in two, 112 in eight;
-// 1 to 2048 tokens of six sequences 130 in two and three, 140 in eight.
+// 1 to 2048 tokens of six sequences 130 in two and three, 140 in eight.  (148: the SMs of a B200.  The size of the workspace follows from this too,
+// and is asked for where there is no device to look at.)
 int parts_of(int tokens, int sequences, int hk, int g, int slots) {
     const double longest = std::min((double)tokens, 2.0 * tokens / sequences), tiles = longest * g / ROWS;
     const double load = hk * std::ceil((double)tokens / KEYS) * tiles / 2 / 148;

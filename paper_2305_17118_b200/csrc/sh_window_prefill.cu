@@ -361,8 +361,11 @@ cudaError_t launch(const WindowParams &p, cudaStream_t s) {
         kern<<<dim3((unsigned)tiles, p.hk), NT, bytes, s>>>(p);
         return cudaGetLastError();
     } else {
-        // few row tiles: clusters share the keys of one, as long as all run at once (4 CTAs an SM) and have two blocks each (chunks of 64, 17
-        // and 200 tokens over 500, 0 and 31 rows, 12 heads of 64: 47 -> 32 us)
+        // few row tiles: clusters share the keys of one, up to 16 CTAs an SM (4 run at once, so in up to four waves) with two blocks each.
+        // Chunks of 64, 17 and 200 tokens over 500, 0 and 31 rows, 12 heads of 64: 47 -> 32 us.  Up to 16 an SM against up to 4, us of attention
+        // to contexts: 128 tokens over 3000 rows, 40 heads of 64: 173, 198; 256 tokens: 313, 373; chunks
+        // of 64, 17 and 200 over 7900, 4000 and 7000, 12 heads: 288, 310; 512 over 3000, 8 heads: 138, 130; 4 x 64 over 3900, 16 heads over 2
+        // of 128: 327, 315.  Where the caches hold little of what they have room for (4 x 64 over 390 of 4000), it costs more: 58, 50.
         int S = 1;
         while (S < 8 && tiles * p.hk * S * 2 <= 16ll * sms && p.slots >= 2 * S * 2 * Simt<D>::BN) S *= 2;
         if (tiles * S > 0x7fffffffll) return cudaErrorInvalidValue;
