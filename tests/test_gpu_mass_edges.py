@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_mass import DT, INF, NAN, STEP, _check_sequence, _i32, _rnd, _same, _sh
+from test_gpu_mass import DT, INF, NAN, PROMPT, STEP, _check_sequence, _i32, _rnd, _same, _sh
 
 pytestmark = pytest.mark.gpu
 
@@ -200,3 +200,27 @@ def test_rows_that_a_prior_spoils_are_not_computed_again(dtype, tokens, held):
     others = [h for h in range(hk * g) if h != 5]
     assert torch.equal(outs[0][:, others], outs[1][:, others]) and outs[1][:, 5].isnan().all()
     assert times[1] < 4 * times[0] + 100, times
+
+
+def test_captured_chunks_without_longest():
+    """Under capture nothing can be looked up: all tokens are the bound.  Replays read starts and lengths as they are then."""
+    sh, rnd, dt, n, hk, g, d = _sh(), _rnd(3), torch.float16, 3, 2, 2, 64
+    cache = sh.MassCache(n, hk * g, hk, d, 40, 6, 16, dtype="f16")
+    q, k, v = (rnd(12, x, d, dtype=dt) for x in (hk * g, hk, hk))
+    starts = _i32([0, 4, 8, 12])
+    cache.prefill(q, k, v, starts)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = cache.prefill(q, k, v, starts)
+    want = [4, 4, 4]
+    for at in ([0, 12, 12, 12], [1, 3, 9, 11], [0, 0, 5, 12]):
+        starts.copy_(_i32(at))
+        old = [x.clone() for x in (cache.k, cache.v, cache.mass, cache.positions)]
+        graph.replay()
+        for i in range(n):
+            a, b = at[i], at[i + 1]
+            if a < b:
+                _check_sequence(old, (cache.k, cache.v, cache.mass, cache.positions), i, want[i], b - a, q[a:b], k[a:b], v[a:b], out[a:b], want[i], g, dt, PROMPT)
+            want[i] += b - a
+        assert cache.lengths.tolist() == want and cache.seen.tolist() == want
