@@ -526,7 +526,7 @@ int sh_context_attention(const sh_attention *a, int tokens, int contexts, const 
  * slot's mass grows by the weights it gets from them (new slots start at 0).  The caller advances lengths and seen.  A sequence of
  * negative length is idle, and one whose chunk has no room (lengths[i] + tokens > slots) takes no part either: nothing of it is read or written.
  * prior (rows of prior_dtype: a->dtype or SH_F32), prior_lse_dev [tokens][q_heads]: what the tokens have seen elsewhere (out and lse of
- * sh_context_attention), or both NULL.
+ * sh_context_attention), or both NULL.  A log of minus infinity: nothing was seen, and the row does not matter; NaN or infinity makes the row NaN.
  * workspace_dev: sh_mass_prefill_workspace_bytes(a, tokens, sequences) bytes of device memory, 16-byte aligned; in use until `stream` has passed
  * the call, so calls that may run at once need one each.
  * Errors: SH_EINVAL, SH_ENOMEM, SH_ECUDA (a call that fails midway may have stored the chunk); bounded waits as in sh_window_status.
@@ -539,7 +539,8 @@ int sh_mass_prefill(const sh_attention *a, int tokens, int sequences, const sh_r
 /*
  * One token per sequence, as above: token i goes to slot lengths[i] of sequence i with position seen[i].  A sequence of negative length, or
  * whose cache is full (lengths[i] >= slots), takes no part.
- * workspace_dev: sh_mass_decode_workspace_bytes(a, sequences) bytes, 16-byte aligned; used as sh_mass_prefill's.
+ * workspace_dev: sh_mass_decode_workspace_bytes(a, sequences) bytes (4 for each sequence, query head and slot, and a little more), 16-byte
+ * aligned; used as sh_mass_prefill's.
  */
 size_t sh_mass_decode_workspace_bytes(const sh_attention *a, int sequences);
 int sh_mass_decode(const sh_attention *a, int sequences, const sh_rows *q, const sh_rows *k, const sh_rows *v, const int32_t *lengths_dev,
